@@ -15,6 +15,12 @@
  *      infllmv2_dense_attn_fwd  causal GQA attention                                  (Eq. 1, Appendix Alg. 3)
  *      infllmv2_sparse_decode   stages 2-4 for the one newest token of each sequence
  *                               against K/V and K^{C1} caches
+ * Around it, for serving from a cache in pages (data's type or 8 bits) and for rotary positions:
+ *   infllmv2_rotary_fwd / _bwd  rotary positions of Q or K, and the gradient
+ *   infllmv2_cache_append       new K (rotated on the way) and V into the pages of each sequence
+ *   infllmv2_cache_compress_k   stage 1 for the rows that a growing paged cache has just completed
+ *   infllmv2_decode_blocks      stages 2-3 of the decode step: the block lists alone
+ *   infllmv2_cache_attn         stage 4 (or dense attention) of the newest tokens over the pages
  *
  * General rules
  *   - Every pointer named *_d or documented "device" is GPU memory on the current
@@ -43,7 +49,8 @@
  *     [T, hkv, d] and head-major [hkv, T, d] work; head-major keeps a 64-token
  *     block in one contiguous 16 KB run and is the fast layout.
  *   - dtype selects the element type of Q, K, V, O only.  K^{C1}, scores and lse
- *     are always float32; block indices are int32.
+ *     are always float32; block indices are int32.  (The pages of a cache hold dtype
+ *     or 8-bit elements, see infllmv2_cache.)
  *   - A call with zero total tokens (or batch 0) is a no-op that returns INFLLMV2_OK; data pointers may
  *     then be NULL.
  *   - Return value: INFLLMV2_OK (0) or a negative infllmv2_status.  Arguments are
@@ -119,7 +126,9 @@ typedef enum infllmv2_op {
     INFLLMV2_OP_TOPK_POOLED = 7,
     INFLLMV2_OP_SPARSE_ATTN_BWD = 8,        /* including the selection bitmap (see infllmv2_sparse_attn_bwd) */
     INFLLMV2_OP_SPARSE_ATTN_BWD_MIN = 9,    /* without it */
-    INFLLMV2_OP_COMPRESS_K_APPEND = 10
+    INFLLMV2_OP_COMPRESS_K_APPEND = 10,
+    INFLLMV2_OP_CACHE_ATTN = 11,            /* total_tokens: query tokens; max_seqlen: longest context */
+    INFLLMV2_OP_DECODE_BLOCKS = 12          /* as INFLLMV2_OP_SPARSE_DECODE */
 } infllmv2_op;
 
 /*
@@ -318,6 +327,135 @@ int infllmv2_sparse_decode_static(const infllmv2_params *p, const void *q_d, con
                                   const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
                                   int32_t *block_idx_out_d, void *out_d, float *lse_d, void *stream);
 size_t infllmv2_sparse_decode_static_capacity(void);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Rotary positions.  Pair i of a head (i < rot_dim / 2) is turned by the angle position * frequency_i:
+ *     (x1, x2) -> magnitude * (x1 cos - x2 sin, x1 sin + x2 cos),
+ * the channels from rot_dim on are left as they are.  A frequency is given in turns per position as a 64-bit binary
+ * fraction, turns[i] = frequency_i / (2 pi) * 2^64 rounded: position * turns[i] modulo 2^64 is the angle modulo a full
+ * turn without rounding, at any int32 position (negative ones too).
+ */
+#define INFLLMV2_ROTARY_HALF 0          /* pair i = channels i and i + rot_dim / 2 */
+#define INFLLMV2_ROTARY_INTERLEAVED 1   /* pair i = channels 2 i and 2 i + 1 */
+
+typedef struct infllmv2_rotary {
+    int32_t rot_dim;          /* channels that are turned: even, 2 <= rot_dim <= head_dim                       */
+    int32_t layout;           /* INFLLMV2_ROTARY_HALF or INFLLMV2_ROTARY_INTERLEAVED                            */
+    float   magnitude;        /* finite, > 0; 1 unless a scaling for long contexts asks for another             */
+    int32_t reserved;         /* 0                                                                              */
+    const uint64_t *turns_d;  /* device [rot_dim / 2], 8-byte aligned                                           */
+} infllmv2_rotary;
+
+#define INFLLMV2_SCALING_NONE 0     /* frequency_i = base^(-2 i / rot_dim)                                             */
+#define INFLLMV2_SCALING_LINEAR 1   /* divided by factor                                                               */
+#define INFLLMV2_SCALING_BASE 2     /* base * factor^(rot_dim / (rot_dim - 2)): the slowest pair is stretched by factor,
+                                       the fastest not at all (rot_dim > 2)                                            */
+#define INFLLMV2_SCALING_PARTS 3    /* pairs that turn more than beta_fast times over original_len positions keep their
+                                       frequency, those that turn less than beta_slow times are divided by factor, in
+                                       between the two are mixed linearly in the number of turns                       */
+/* Fills turns_h (host, [rot_dim / 2]) for the frequencies above.  base > 1, factor >= 1; original_len > 0 and
+ * beta_fast > beta_slow > 0 are read for INFLLMV2_SCALING_PARTS only.  Host helper, no GPU needed.  Other frequency
+ * tables can be given as well: infllmv2_rotary only holds the result. */
+int infllmv2_rotary_turns(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len,
+                          double beta_fast, double beta_slow, uint64_t *turns_h);
+
+/*
+ * Rotary positions of Q or K, and their gradient (the same with the angle negated).
+ *   x_d / y_d, dy_d / dx_d   device, dtype; channel c of head h of token t at base + t * tok_stride + h * head_stride + c
+ *                 (strides in elements, >= 0 for the input; rows of the output must not overlap).  Input and output may
+ *                 be the same memory with the same strides, else they must not overlap.
+ *   pos_d         device int32 [tokens]: the token's position
+ *   heads         rows per token (num_q_heads, num_kv_heads or any other number; of p only dtype and head_dim are used)
+ */
+int infllmv2_rotary_fwd(const infllmv2_params *p, const infllmv2_rotary *r, const void *x_d, int64_t x_tok_stride,
+                        int64_t x_head_stride, void *y_d, int64_t y_tok_stride, int64_t y_head_stride,
+                        const int32_t *pos_d, int64_t tokens, int32_t heads, void *stream);
+int infllmv2_rotary_bwd(const infllmv2_params *p, const infllmv2_rotary *r, const void *dy_d, int64_t dy_tok_stride,
+                        int64_t dy_head_stride, void *dx_d, int64_t dx_tok_stride, int64_t dx_head_stride,
+                        const int32_t *pos_d, int64_t tokens, int32_t heads, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * A K/V cache in pages.  A page holds block_size (64) consecutive tokens of one sequence, i.e. one selection block, for
+ * every KV head; block j of sequence b is in page page_table[b * table_stride + j].  An entry outside [0, num_pages) is
+ * a page that is not there: its tokens are not written by infllmv2_cache_append and take no part in attention (in
+ * infllmv2_cache_compress_k they count as 0).  Sequences may share pages that nobody writes to.
+ *   INFLLMV2_CACHE_NATIVE  elements of dtype
+ *   INFLLMV2_CACHE_E4M3    8 bits (OCP e4m3: 4 exponent, 3 mantissa bits, largest 448) and one float32 scale per page
+ *                          and KV head, for K and V each: value = code * scale.  Scales are powers of two in
+ *                          [2^-100, 2^119]: the smallest with which the largest finite magnitude written to that page
+ *                          fits (larger magnitudes than 448 * 2^119 saturate), so an element is rounded as in a
+ *                          3-bit-mantissa float (relative error at most 2^-4) unless it is over 2^13 times smaller than
+ *                          the largest of its page.  A page that is continued keeps its scale or gets a larger one, and the
+ *                          codes that it holds are then rounded again (exact unless they become subnormal).  NaN and
+ *                          infinities are stored as NaN.
+ */
+#define INFLLMV2_CACHE_NATIVE 0
+#define INFLLMV2_CACHE_E4M3 1
+
+typedef struct infllmv2_cache {
+    int32_t kv_type;              /* INFLLMV2_CACHE_NATIVE or INFLLMV2_CACHE_E4M3                                */
+    int32_t num_pages;            /* >= 1                                                                        */
+    void *k_d, *v_d;              /* device, 16-byte aligned; row r of head h of page g at
+                                     base + g * page_stride + h * head_stride + r * tok_stride, head_dim contiguous */
+    int64_t page_stride, head_stride, tok_stride;   /* elements, >= head_dim, multiples of 16 bytes               */
+    float *k_scale_d, *v_scale_d; /* INFLLMV2_CACHE_E4M3: device [num_pages, num_kv_heads]; else ignored          */
+    const int32_t *page_table_d;  /* device [batch, table_stride]                                                */
+    int32_t table_stride;         /* >= ceil(longest context / 64), else INVALID_ARGUMENT                        */
+    int32_t reserved;             /* 0                                                                           */
+} infllmv2_cache;
+
+/*
+ * Writes new tokens behind those that the cache holds.  Sequence b had prev_lens[b] tokens and gets
+ * cu_new[b + 1] - cu_new[b] more; the new rows stand packed in k_d and v_d (K/V strides of the general rules).
+ *   r             NULL: keys are stored as they are; else they are turned by their positions first (in float32, rounded
+ *                 once, to the cache's type)
+ *   pos_d         device int32 [total new tokens] or NULL: token i of sequence b is at position prev_lens[b] + i
+ *   cu_new_h/d    host / device int32 [batch + 1]; prev_lens_h/d host / device int32 [batch]
+ * A page is written by one sequence at a time: the pages that new tokens fall into must not be listed twice.  Rows that
+ * do not belong to the new tokens stay as they are, up to the larger scale of a page that is continued.
+ */
+int infllmv2_cache_append(const infllmv2_params *p, const infllmv2_cache *c, const infllmv2_rotary *r, const void *k_d,
+                          const void *v_d, int64_t kv_tok_stride, int64_t kv_head_stride, const int32_t *cu_new_h,
+                          const int32_t *cu_new_d, const int32_t *prev_lens_h, const int32_t *prev_lens_d,
+                          const int32_t *pos_d, int32_t batch, void *stream);
+
+/*
+ * infllmv2_compress_k_append for a paged cache: rows nc(prev_lens[b]) .. nc(ctx_lens[b]) - 1 of every KV head's plane of
+ * kc_cache_d from the keys as the cache holds them (of c, the V members are not used).  Other arguments as there.
+ */
+int infllmv2_cache_compress_k(const infllmv2_params *p, const infllmv2_cache *c, float *kc_cache_d, int64_t kc_head_stride,
+                              const int32_t *prev_lens_h, const int32_t *prev_lens_d, const int32_t *ctx_lens_h,
+                              const int32_t *ctx_lens_d, int32_t batch, void *stream);
+
+/*
+ * Stages 2 and 3 for the newest token of every sequence, as in infllmv2_sparse_decode: the block lists alone, for a step
+ * whose attention is infllmv2_cache_attn.
+ *   q_d, kc_cache_d, ctx_lens as there; block_idx_d device out int32 [batch, num_kv_heads, topk_total].  Lists of
+ *   sequences shorter than dense_threshold are -1.
+ *   workspace_d   device scratch (INFLLMV2_OP_DECODE_BLOCKS: infllmv2_decode_workspace_bytes)
+ */
+int infllmv2_decode_blocks(const infllmv2_params *p, const void *q_d, const float *kc_cache_d, int64_t kc_head_stride,
+                           const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch, int32_t *block_idx_d,
+                           void *workspace_d, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention of the newest tokens of each sequence over its pages.  Sequence b has ctx_lens[b] cached tokens, of which the
+ * last n = cu_q[b + 1] - cu_q[b] <= ctx_lens[b] are the queries (already appended): query i is at position
+ * ctx_lens[b] - n + i and attends to the keys at positions up to its own.  n = 1 is a decode step, larger ones a chunk of a
+ * prompt or proposed tokens; sequences of both kinds may share a call, and n = 0 skips one.
+ *   q_d, out_d     device, dtype [total, num_q_heads, head_dim]
+ *   cu_q_h/d       host / device int32 [batch + 1]; ctx_lens_h/d host / device int32 [batch]
+ *   block_idx_d    device int32 [total, num_kv_heads, topk_total]: the blocks that a token attends to, each listed once, in
+ *                  any order (entries outside 0 .. the token's own block are skipped); sequences with
+ *                  ctx_lens[b] < dense_threshold attend to every key.  NULL: all sequences do.
+ *   lse_d          device float32 [total, num_q_heads] or NULL
+ *   A token that has no key at all (empty list, or no page) gets zeros and lse = -infinity.
+ *   workspace_d    device scratch (INFLLMV2_OP_CACHE_ATTN)
+ */
+int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h,
+                        const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
+                        const int32_t *block_idx_d, void *out_d, float *lse_d, void *workspace_d, size_t workspace_bytes,
+                        void *stream);
 
 #ifdef __cplusplus
 }

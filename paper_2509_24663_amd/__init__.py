@@ -12,16 +12,25 @@ from .binding import (  # noqa: F401
     DecodeInfo,
     FP32,
     InfllmV2Error,
+    PagedCache,
     Params,
+    Rotary,
     SeqInfo,
     block_scores,
     block_scores_pooled,
+    cache_append,
+    cache_attn,
+    cache_compress_k,
     compress_k,
     compress_k_append,
+    decode_blocks,
     decode_workspace_bytes,
     dense_attn_fwd,
     lib,
     num_cmp,
+    rotary_bwd,
+    rotary_fwd,
+    rotary_turns,
     sparse_attn_bwd,
     sparse_attn_fwd,
     sparse_decode,
@@ -37,7 +46,9 @@ from .binding import (  # noqa: F401
 
 # `op` codes of infllmv2_workspace_bytes
 (OP_COMPRESS_K, OP_BLOCK_SCORES, OP_TOPK_BLOCKS, OP_SPARSE_ATTN_FWD, OP_DENSE_ATTN_FWD, OP_SPARSE_DECODE,
- OP_BLOCK_SCORES_POOLED, OP_TOPK_POOLED, OP_SPARSE_ATTN_BWD, OP_SPARSE_ATTN_BWD_MIN, OP_COMPRESS_K_APPEND) = (
+ OP_BLOCK_SCORES_POOLED, OP_TOPK_POOLED, OP_SPARSE_ATTN_BWD, OP_SPARSE_ATTN_BWD_MIN, OP_COMPRESS_K_APPEND,
+ OP_CACHE_ATTN, OP_DECODE_BLOCKS) = (
     _binding.OP_COMPRESS_K, _binding.OP_BLOCK_SCORES, _binding.OP_TOPK_BLOCKS, _binding.OP_SPARSE_ATTN_FWD,
     _binding.OP_DENSE_ATTN_FWD, _binding.OP_SPARSE_DECODE, _binding.OP_BLOCK_SCORES_POOLED, _binding.OP_TOPK_POOLED,
-    _binding.OP_SPARSE_ATTN_BWD, _binding.OP_SPARSE_ATTN_BWD_MIN, _binding.OP_COMPRESS_K_APPEND)
+    _binding.OP_SPARSE_ATTN_BWD, _binding.OP_SPARSE_ATTN_BWD_MIN, _binding.OP_COMPRESS_K_APPEND,
+    _binding.OP_CACHE_ATTN, _binding.OP_DECODE_BLOCKS)

@@ -58,6 +58,26 @@ _lib = None
 _P = ctypes.c_void_p
 _I32, _I64, _SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 _PP = ctypes.POINTER(Params)
+_DBL = ctypes.c_double
+
+
+class _RotaryC(ctypes.Structure):
+    """Mirror of `infllmv2_rotary`."""
+
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("turns_d", ctypes.c_void_p)]
+
+
+class _CacheC(ctypes.Structure):
+    """Mirror of `infllmv2_cache`."""
+
+    _fields_ = [("kv_type", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("k_d", ctypes.c_void_p), ("v_d", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64),
+                ("k_scale_d", ctypes.c_void_p), ("v_scale_d", ctypes.c_void_p), ("page_table_d", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+_RP, _CP = ctypes.POINTER(_RotaryC), ctypes.POINTER(_CacheC)
 
 _SIGNATURES = {
     "infllmv2_num_cmp": (_I32, [_PP, _I32]),
@@ -80,6 +100,13 @@ _SIGNATURES = {
     "infllmv2_sparse_decode_static": (ctypes.c_int, [_PP, _P, _P, _P, _I64, _I64, _I64, _P, _I64, _P, _P, _I32, _P, _P, _P,
                                                      _P]),
     "infllmv2_sparse_decode_static_capacity": (_SZ, []),
+    "infllmv2_rotary_turns": (ctypes.c_int, [_I32, _DBL, _I32, _DBL, _DBL, _DBL, _DBL, _P]),
+    "infllmv2_rotary_fwd": (ctypes.c_int, [_PP, _RP, _P, _I64, _I64, _P, _I64, _I64, _P, _I64, _I32, _P]),
+    "infllmv2_rotary_bwd": (ctypes.c_int, [_PP, _RP, _P, _I64, _I64, _P, _I64, _I64, _P, _I64, _I32, _P]),
+    "infllmv2_cache_append": (ctypes.c_int, [_PP, _CP, _RP, _P, _P, _I64, _I64, _P, _P, _P, _P, _P, _I32, _P]),
+    "infllmv2_cache_compress_k": (ctypes.c_int, [_PP, _CP, _P, _I64, _P, _P, _P, _P, _I32, _P]),
+    "infllmv2_decode_blocks": (ctypes.c_int, [_PP, _P, _P, _I64, _P, _P, _I32, _P, _P, _SZ, _P]),
+    "infllmv2_cache_attn": (ctypes.c_int, [_PP, _CP, _P, _P, _P, _P, _P, _I32, _P, _P, _P, _P, _SZ, _P]),
 }
 
 
@@ -139,6 +166,7 @@ def _stream():
 # `op` of infllmv2_workspace_bytes (enum infllmv2_op)
 OP_COMPRESS_K, OP_BLOCK_SCORES, OP_TOPK_BLOCKS, OP_SPARSE_ATTN_FWD, OP_DENSE_ATTN_FWD, OP_SPARSE_DECODE = range(6)
 OP_BLOCK_SCORES_POOLED, OP_TOPK_POOLED, OP_SPARSE_ATTN_BWD, OP_SPARSE_ATTN_BWD_MIN, OP_COMPRESS_K_APPEND = range(6, 11)
+OP_CACHE_ATTN, OP_DECODE_BLOCKS = 11, 12
 
 
 def workspace_bytes(op: int, p: Params, batch: int, total_tokens: int, max_seqlen: int) -> int:
@@ -412,3 +440,151 @@ def sparse_prefill(p: Params, q, k, v, cu_seqlens, buffers: Optional[dict] = Non
     out, lse = sparse_attn_fwd(p, q, k, v, idx, si, out=b.get("out"), lse=b.get("lse"), workspace=ws_attn)
     return dict(out=out, lse=lse, block_idx=idx, kc=kc, cu_seqlens_c=cu_c, ws_attn=ws_attn, ws_scores=ws_scores,
                 **scores)
+
+
+# ---------------------------------------------------------------------------------- rotary positions
+SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+LAYOUTS = {"half": 0, "interleaved": 1}
+CACHE_NATIVE, CACHE_E4M3 = 0, 1
+
+
+def rotary_turns(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, *, original_len: float = 4096,
+                 beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda") -> torch.Tensor:
+    """Frequencies of rot_dim / 2 pairs of channels as 64-bit fractions of a turn per position (int64 bit patterns, device)."""
+    turns = torch.empty(max(int(rot_dim), 0) // 2, dtype=torch.int64)
+    st = lib().infllmv2_rotary_turns(int(rot_dim), float(base), SCALINGS[scaling], float(factor), float(original_len),
+                                     float(beta_fast), float(beta_slow), turns.data_ptr())
+    _check(st, "infllmv2_rotary_turns")
+    return turns.to(device)
+
+
+class Rotary:
+    """How keys and queries are turned by their positions: the frequency table (rotary_turns) and how channels are paired."""
+
+    def __init__(self, turns: torch.Tensor, rot_dim: int, layout: str = "half", magnitude: float = 1.0):
+        assert turns.dtype == torch.int64 and turns.is_contiguous() and turns.numel() == int(rot_dim) // 2
+        self.turns = turns
+        self.c = _RotaryC(int(rot_dim), LAYOUTS[layout], float(magnitude), 0, turns.data_ptr())
+
+
+def _rotary(name, p: Params, rot: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor]):
+    assert x.dim() == 3 and x.stride(2) == 1 and x.shape[2] == p.head_dim and x.dtype == p.torch_dtype
+    assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == x.shape[0]
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    assert out.shape == x.shape and out.stride(2) == 1 and out.dtype == x.dtype
+    st = getattr(lib(), name)(ctypes.byref(p), ctypes.byref(rot.c), _ptr(x), x.stride(0), x.stride(1), _ptr(out), out.stride(0),
+                              out.stride(1), _ptr(positions), x.shape[0], x.shape[1], _stream())
+    _check(st, name)
+    return out
+
+
+def rotary_fwd(p: Params, rot: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None):
+    """x [T, heads, d] (any strides, d contiguous) turned by positions (device int32 [T]).  out: optional buffer, x itself allowed."""
+    return _rotary("infllmv2_rotary_fwd", p, rot, x, positions, out)
+
+
+def rotary_bwd(p: Params, rot: Rotary, dy: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None):
+    """Gradient of rotary_fwd with respect to its input, from that of its output."""
+    return _rotary("infllmv2_rotary_bwd", p, rot, dy, positions, out)
+
+
+# ---------------------------------------------------------------------------------- the paged cache
+class PagedCache:
+    """A K/V cache in pages of 64 tokens: k, v [num_pages, hkv, 64, d] (any strides, d contiguous; the data's type, or
+    torch.float8_e4m3fn with float32 scales [num_pages, hkv]) and page_table [batch, blocks] (device int32)."""
+
+    def __init__(self, p: Params, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        coded = k.dtype == torch.float8_e4m3fn
+        assert k.shape == v.shape and k.dtype == v.dtype and k.stride() == v.stride() and k.stride(3) == 1
+        assert k.shape[1:] == (p.num_kv_heads, p.block_size, p.head_dim) and (coded or k.dtype == p.torch_dtype)
+        assert page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.stride(1) == 1
+        for s in (k_scale, v_scale) if coded else ():
+            assert s.dtype == torch.float32 and s.is_contiguous() and s.shape == k.shape[:2]
+        self.k, self.v, self.page_table, self.k_scale, self.v_scale = k, v, page_table, k_scale, v_scale
+        self.batch = page_table.shape[0]
+        self.c = _CacheC(CACHE_E4M3 if coded else CACHE_NATIVE, k.shape[0], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                         k.stride(2), _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(),
+                         page_table.stride(0) if self.batch > 1 else page_table.shape[1], 0)
+
+    @staticmethod
+    def empty(p: Params, num_pages: int, page_table: torch.Tensor, kv_type: str = "e4m3") -> "PagedCache":
+        """A cache with nothing in it."""
+        shape, dev = (num_pages, p.num_kv_heads, p.block_size, p.head_dim), page_table.device
+        dtype = {"e4m3": torch.float8_e4m3fn, "native": p.torch_dtype}[kv_type]
+        k, v = (torch.empty(shape, dtype=dtype, device=dev) for _ in range(2))
+        scales = [torch.ones(shape[:2], dtype=torch.float32, device=dev) for _ in range(2)] if kv_type == "e4m3" else [None, None]
+        return PagedCache(p, k, v, page_table, *scales)
+
+
+def _decode_info(lens) -> "DecodeInfo":
+    return lens if isinstance(lens, DecodeInfo) else DecodeInfo(lens)
+
+
+def cache_append(p: Params, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, cu_new, prev_lens, rotary: Optional[Rotary] = None,
+                 positions: Optional[torch.Tensor] = None):
+    """New keys and values k, v [hkv, T, d] (packed by cu_new) written behind the prev_lens[b] tokens that sequence b has; keys turned by
+    `rotary` (positions: device int32 [T], else a token's place in its sequence).  Returns the cache."""
+    si, pv = _seq_info(cu_new), _decode_info(prev_lens)
+    ts, hs = _kv_strides(k)
+    assert _kv_strides(v) == (ts, hs) and k.dtype == v.dtype == p.torch_dtype and k.shape == v.shape == (p.num_kv_heads, si.total, p.head_dim)
+    assert si.batch == pv.batch <= cache.batch
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == si.total)
+    st = lib().infllmv2_cache_append(ctypes.byref(p), ctypes.byref(cache.c), ctypes.byref(rotary.c) if rotary is not None else None,
+                                     _ptr(k), _ptr(v), ts, hs, _ptr(si.cu_h), _ptr(si.cu_d), _ptr(pv.ctx_h), _ptr(pv.ctx_d),
+                                     _ptr(positions), si.batch, _stream())
+    _check(st, "infllmv2_cache_append")
+    return cache
+
+
+def cache_compress_k(p: Params, cache: PagedCache, kc_cache: torch.Tensor, prev_lens, ctx_lens):
+    """compress_k_append from the pages: kc_cache [B, hkv, max_nc, d] fp32 brought up to date in place."""
+    pv, cx = _decode_info(prev_lens), _decode_info(ctx_lens)
+    assert kc_cache.dim() == 4 and kc_cache.is_contiguous() and kc_cache.dtype == torch.float32
+    assert kc_cache.shape[1] == p.num_kv_heads and kc_cache.shape[3] == p.head_dim
+    assert pv.batch == cx.batch <= min(cache.batch, kc_cache.shape[0])
+    st = lib().infllmv2_cache_compress_k(ctypes.byref(p), ctypes.byref(cache.c), _ptr(kc_cache), kc_cache.stride(1), _ptr(pv.ctx_h),
+                                         _ptr(pv.ctx_d), _ptr(cx.ctx_h), _ptr(cx.ctx_d), cx.batch, _stream())
+    _check(st, "infllmv2_cache_compress_k")
+    return kc_cache
+
+
+def decode_blocks(p: Params, q: torch.Tensor, kc_cache: torch.Tensor, ctx_lens, out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None):
+    """Stages 2 and 3 of a decode step: q [B, hq, d], kc_cache [B, hkv, max_nc, d] fp32 -> block_idx [B, hkv, topk_total] int32."""
+    di = _decode_info(ctx_lens)
+    assert q.is_contiguous() and q.dtype == p.torch_dtype and q.shape == (di.batch, p.num_q_heads, p.head_dim)
+    assert kc_cache.dim() == 4 and kc_cache.is_contiguous() and kc_cache.dtype == torch.float32 and kc_cache.shape[0] >= di.batch
+    if out is None:
+        out = torch.empty((di.batch, p.num_kv_heads, p.topk_total), dtype=torch.int32, device=q.device)
+    assert out.is_contiguous() and out.dtype == torch.int32
+    if workspace is None:
+        need = workspace_bytes(OP_DECODE_BLOCKS, p, di.batch, 0, di.max_ctx)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    st = lib().infllmv2_decode_blocks(ctypes.byref(p), _ptr(q), _ptr(kc_cache), kc_cache.stride(1), _ptr(di.ctx_h), _ptr(di.ctx_d),
+                                      di.batch, _ptr(out), *_ws_args(workspace), _stream())
+    _check(st, "infllmv2_decode_blocks")
+    return out
+
+
+def cache_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q, ctx_lens, block_idx: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Attention of the newest tokens of each sequence over its pages.  q [T, hq, d], packed by cu_seqlens_q; sequence b has ctx_lens[b]
+    cached tokens, its queries the last of them.  block_idx [T, hkv, topk_total] int32 or None (all keys).  Returns (out [T, hq, d],
+    lse [T, hq])."""
+    si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
+    assert q.is_contiguous() and q.dtype == p.torch_dtype and q.shape == (si.total, p.num_q_heads, p.head_dim)
+    assert si.batch == cx.batch <= cache.batch
+    assert block_idx is None or (block_idx.is_contiguous() and block_idx.dtype == torch.int32 and
+                                 block_idx.shape == (si.total, p.num_kv_heads, p.topk_total))
+    out = torch.empty_like(q) if out is None else out
+    lse = torch.empty((si.total, p.num_q_heads), dtype=torch.float32, device=q.device) if lse is None else lse
+    assert out.is_contiguous() and lse.is_contiguous()
+    if workspace is None:
+        need = workspace_bytes(OP_CACHE_ATTN, p, si.batch, si.total, cx.max_ctx)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    st = lib().infllmv2_cache_attn(ctypes.byref(p), ctypes.byref(cache.c), _ptr(q), _ptr(si.cu_h), _ptr(si.cu_d), _ptr(cx.ctx_h),
+                                   _ptr(cx.ctx_d), si.batch, _ptr(block_idx), _ptr(out), _ptr(lse), *_ws_args(workspace), _stream())
+    _check(st, "infllmv2_cache_attn")
+    return out, lse

@@ -36,6 +36,7 @@ EXTRA_FLAGS = {
     "attn_bwd.hip": _VGPR_FORM,
     "attn_staged.hip": _VGPR_FORM,
     "block_scores.hip": _VGPR_FORM,
+    "cache_attn.hip": _VGPR_FORM,
 }
 
 

@@ -17,9 +17,11 @@ int launch_decode_mfma(const infllmv2_params *p, const void *q, const void *k, c
                        int64_t kv_head_stride, int64_t kv_tok_stride, const float *kc, int64_t kc_head_stride,
                        const int32_t *ctx_h, const int32_t *ctx_d, int batch, int32_t *idx_out, void *out, float *lse,
                        void *ws, size_t ws_bytes, hipStream_t stream);
+size_t cache_attn_ws_bound(const infllmv2_params *p, int64_t tokens, int32_t max_ctx);
 }  // namespace ifv2
 
-static int check_params(const infllmv2_params *p) {
+namespace ifv2 {
+int check_params(const infllmv2_params *p) {
     if (p == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (p->dtype != INFLLMV2_FP32 && p->dtype != INFLLMV2_BF16) return INFLLMV2_ERR_UNSUPPORTED;
     if (p->num_q_heads <= 0 || p->num_kv_heads <= 0 || p->num_q_heads % p->num_kv_heads != 0)
@@ -41,7 +43,7 @@ static int check_params(const infllmv2_params *p) {
 }
 
 // cu_seqlens: [batch+1], starts at 0, non-decreasing.  Returns total tokens / longest sequence.
-static int check_cu(const int32_t *cu_h, const int32_t *cu_d, int32_t batch, int64_t *total, int32_t *max_len) {
+int check_cu(const int32_t *cu_h, const int32_t *cu_d, int32_t batch, int64_t *total, int32_t *max_len) {
     if (cu_h == nullptr || cu_d == nullptr || batch < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (cu_h[0] != 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
     int32_t mx = 0;
@@ -56,11 +58,12 @@ static int check_cu(const int32_t *cu_h, const int32_t *cu_d, int32_t batch, int
 }
 
 // workspace arguments: 256-byte aligned when present; need == 0 accepts anything (also NULL)
-static int check_ws(const void *ws, size_t ws_bytes, size_t need) {
+int check_ws(const void *ws, size_t ws_bytes, size_t need) {
     if (need == 0) return INFLLMV2_OK;
     if (ws == nullptr || ((uintptr_t)ws & 255) != 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
     return ws_bytes < need ? INFLLMV2_ERR_WORKSPACE_TOO_SMALL : INFLLMV2_OK;
 }
+}  // namespace ifv2
 
 static RowMap prefill_map(const infllmv2_params *p, const int32_t *cu_d, const int32_t *cu_c_d, int batch,
                           int64_t total, int64_t tok_stride, int64_t head_stride, int64_t kc_total_c) {
@@ -295,7 +298,7 @@ static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; 
 size_t infllmv2_workspace_bytes(int op, const infllmv2_params *p, int32_t batch, int64_t total_tokens,
                                 int32_t max_seqlen) {
     if (check_params(p) != INFLLMV2_OK || batch < 0 || total_tokens < 0 || max_seqlen < 0) return 0;
-    if (op == INFLLMV2_OP_SPARSE_DECODE) return infllmv2_decode_workspace_bytes(p, batch, max_seqlen);
+    if (op == INFLLMV2_OP_SPARSE_DECODE || op == INFLLMV2_OP_DECODE_BLOCKS) return infllmv2_decode_workspace_bytes(p, batch, max_seqlen);
     if (total_tokens >= (1ll << 31)) return 0;
     const BatchTotals t = bound_totals(p, batch, total_tokens, max_seqlen);
     switch (op) {
@@ -305,12 +308,42 @@ size_t infllmv2_workspace_bytes(int op, const infllmv2_params *p, int32_t batch,
         case INFLLMV2_OP_DENSE_ATTN_FWD: return attn_fwd_ws_bytes(p, t);
         case INFLLMV2_OP_SPARSE_ATTN_BWD: return attn_bwd_ws_bytes(p, t, true);
         case INFLLMV2_OP_SPARSE_ATTN_BWD_MIN: return attn_bwd_ws_bytes(p, t, false);
+        case INFLLMV2_OP_CACHE_ATTN: return cache_attn_ws_bound(p, total_tokens, max_seqlen);
         default: return 0;      // compress_k, compress_k_append, top-k: no scratch
     }
 }
 
 size_t infllmv2_decode_workspace_bytes(const infllmv2_params *p, int32_t batch, int32_t max_ctx_len) {
     return check_params(p) != INFLLMV2_OK || batch < 0 || max_ctx_len < 0 ? 0 : ifv2::decode_scratch_bytes(p, batch, max_ctx_len, true);
+}
+
+// a decode step's rows for the generic kernels
+static Launch decode_launch(const infllmv2_params *p, int64_t kv_tok_stride, int64_t kv_head_stride, int64_t kv_batch_stride,
+                            int64_t kc_head_stride, const int32_t *ctx_lens_d, int32_t batch, int32_t max_ctx, void *stream) {
+    RowMap m;
+    m.cu = nullptr;
+    m.cu_c = nullptr;
+    m.ctx = ctx_lens_d;
+    m.batch = batch;
+    m.total_rows = batch;
+    m.num_kv_heads = p->num_kv_heads;
+    m.kv_tok_stride = kv_tok_stride;
+    m.kv_head_stride = kv_head_stride;
+    m.kv_batch_stride = kv_batch_stride;
+    m.kc_total_c = 0;
+    m.kc_head_stride = kc_head_stride;
+    return Launch{p, m, (hipStream_t)stream, max_ctx, nullptr, 0};
+}
+
+// stages 2 and 3 of a decode step on the generic kernels; *idx: the caller's lists, or nullptr: into the workspace
+static int decode_blocks_generic(const Launch &L, const void *q_d, const float *kc_cache_d, int32_t **idx, void *workspace_d) {
+    const infllmv2_params *p = L.p;
+    const size_t rs = align_up((size_t)num_cmp(L.max_len, p->cmp_len, p->cmp_stride) + 4, 4);
+    const size_t rows = (size_t)L.map.batch * p->num_kv_heads;
+    float *scores = (float *)workspace_d;
+    if (*idx == nullptr) *idx = (int32_t *)((char *)workspace_d + align_up(rows * rs * sizeof(float), 256));
+    const int st = launch_block_scores(L, q_d, kc_cache_d, scores, (int64_t)rs, nullptr, false);
+    return st ? st : launch_topk(L, scores, (int64_t)rs, *idx, false);
 }
 
 int infllmv2_sparse_decode(const infllmv2_params *p, const void *q_d, const void *k_cache_d, const void *v_cache_d,
@@ -349,30 +382,37 @@ int infllmv2_sparse_decode(const infllmv2_params *p, const void *q_d, const void
         if (rc != INFLLMV2_ERR_UNSUPPORTED) return rc;
     }
 
-    const size_t rs = align_up((size_t)num_cmp(max_ctx, p->cmp_len, p->cmp_stride) + 4, 4);
-    const size_t rows = (size_t)batch * p->num_kv_heads;
-    float *scores = (float *)workspace_d;
-    int32_t *idx_ws = (int32_t *)((char *)workspace_d + align_up(rows * rs * sizeof(float), 256));
-    int32_t *idx = block_idx_out_d ? block_idx_out_d : idx_ws;
-
-    RowMap m;
-    m.cu = nullptr;
-    m.cu_c = nullptr;
-    m.ctx = ctx_lens_d;
-    m.batch = batch;
-    m.total_rows = batch;
-    m.num_kv_heads = p->num_kv_heads;
-    m.kv_tok_stride = kv_tok_stride;
-    m.kv_head_stride = kv_head_stride;
-    m.kv_batch_stride = kv_batch_stride;
-    m.kc_total_c = 0;
-    m.kc_head_stride = kc_head_stride;
-    Launch L{p, m, (hipStream_t)stream, max_ctx, nullptr, 0};
-    st = launch_block_scores(L, q_d, kc_cache_d, scores, (int64_t)rs, nullptr, false);
-    if (st) return st;
-    st = launch_topk(L, scores, (int64_t)rs, idx, false);
+    int32_t *idx = block_idx_out_d;
+    const Launch L = decode_launch(p, kv_tok_stride, kv_head_stride, kv_batch_stride, kc_head_stride, ctx_lens_d, batch, max_ctx, stream);
+    st = decode_blocks_generic(L, q_d, kc_cache_d, &idx, workspace_d);
     if (st) return st;
     return launch_attn_generic(L, q_d, k_cache_d, v_cache_d, idx, p->dense_threshold, out_d, lse_d, nullptr);
+}
+
+int infllmv2_decode_blocks(const infllmv2_params *p, const void *q_d, const float *kc_cache_d, int64_t kc_head_stride,
+                           const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch, int32_t *block_idx_d,
+                           void *workspace_d, size_t workspace_bytes, void *stream) {
+    int st = check_params(p);
+    if (st) return st;
+    if (batch < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (batch == 0) return INFLLMV2_OK;
+    if (q_d == nullptr || kc_cache_d == nullptr || ctx_lens_h == nullptr || ctx_lens_d == nullptr || block_idx_d == nullptr)
+        return INFLLMV2_ERR_INVALID_ARGUMENT;
+    int32_t max_ctx = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (ctx_lens_h[b] < 1) return INFLLMV2_ERR_INVALID_ARGUMENT;
+        if (ctx_lens_h[b] > max_ctx) max_ctx = ctx_lens_h[b];
+    }
+    if (kc_head_stride < (int64_t)num_cmp(max_ctx, p->cmp_len, p->cmp_stride) * p->head_dim) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    st = check_ws(workspace_d, workspace_bytes, ifv2::decode_scratch_bytes(p, batch, max_ctx, false));
+    if (st) return st;
+    if (decode_mfma_supported(p) && (((uintptr_t)q_d | (uintptr_t)kc_cache_d) & 15) == 0 && kc_head_stride % 4 == 0) {
+        const int rc = launch_decode_mfma(p, q_d, nullptr, nullptr, 0, 0, 0, kc_cache_d, kc_head_stride, ctx_lens_h, ctx_lens_d, batch,
+                                          block_idx_d, nullptr, nullptr, workspace_d, workspace_bytes, (hipStream_t)stream);
+        if (rc != INFLLMV2_ERR_UNSUPPORTED) return rc;
+    }
+    return decode_blocks_generic(decode_launch(p, 0, 0, 0, kc_head_stride, ctx_lens_d, batch, max_ctx, stream), q_d, kc_cache_d,
+                                 &block_idx_d, workspace_d);
 }
 
 }  // extern "C"

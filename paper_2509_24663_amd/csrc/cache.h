@@ -1,0 +1,89 @@
+// The paged K/V cache on the device: where a page's rows are, e4m3 codes and their scales, which sequence a work item belongs to.
+#pragma once
+#include "common.h"
+
+namespace ifv2 {
+namespace cache {
+
+struct Args {
+    char *k, *v;
+    int64_t page_stride, head_stride, tok_stride;      // bytes
+    float *ks, *vs;                                    // [num_pages, hkv], e4m3 only
+    const int32_t *table;
+    int32_t table_stride, num_pages, hkv;
+    // page of block j of sequence b, or -1
+    __device__ inline int page(int b, int j) const {
+        const int g = table[(int64_t)b * table_stride + j];
+        return g >= 0 && g < num_pages ? g : -1;
+    }
+    __device__ inline int64_t at(int page, int h) const { return page * page_stride + h * head_stride; }
+};
+
+int check(const infllmv2_params *p, const infllmv2_cache *c, int max_ctx, bool values);
+Args args(const infllmv2_params *p, const infllmv2_cache *c);
+
+constexpr float kTop = 448.f;                          // largest e4m3 magnitude
+constexpr int kMinExp = -100, kMaxExp = 119;           // of a scale
+
+// smallest power of two 2^e with top <= 448 * 2^e, e clamped
+__device__ inline float scale_for(float top) {
+    // top = 2^x * f, f in [1, 2): 448 = 1.75 * 2^8, so e = x - 8, one more if f > 1.75 (subnormal tops have x = -127 here: clamped anyway)
+    const uint32_t u = __float_as_uint(top);
+    int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = e < kMinExp ? kMinExp : e > kMaxExp ? kMaxExp : e;
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+__device__ inline float reciprocal_of_power(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
+
+// two values, in units of the scale, as two codes (nearest, ties to even; saturating; NaN and infinities as NaN)
+__device__ inline uint32_t code(float x) {
+    return fabsf(x) <= 3.4028234e38f ? (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fminf(fmaxf(x, -kTop), kTop), 0.f, 0, false) & 0xffu : 0x7fu;
+}
+// four values
+__device__ inline uint32_t codes4(float a, float b, float c, float d) {
+    const float top = fmaxf(fmaxf(fabsf(a), fabsf(b)), fmaxf(fabsf(c), fabsf(d)));
+    const bool odd = !(fabsf(a) <= 3.4028234e38f && fabsf(b) <= 3.4028234e38f && fabsf(c) <= 3.4028234e38f && fabsf(d) <= 3.4028234e38f);
+    if (odd || top > kTop) return code(a) | code(b) << 8 | code(c) << 16 | code(d) << 24;
+    int x = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, x, true);
+}
+
+// Which sequence the item-th of a batch's work items belongs to, when sequence s has count(s) of them; rem: which of the sequence's; before: the sum
+// of weight(s) over the sequences in front.  As find_seq_count (common.h), for counts that do not come from one list of offsets.  Called by every
+// thread of a workgroup; one barrier; returns >= batch past the last item.
+template <class Count, class Weight>
+__device__ inline int find_item(int batch, int64_t item, int &rem, int64_t &before, int64_t *s_out, Count count, Weight weight) {
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
+        int64_t items = 0, sum = 0, bef = 0;
+        int seq = batch, r = 0;
+        for (int s0 = 0; s0 < batch; s0 += 64) {
+            const int s = s0 + lane;
+            const int64_t n = s < batch ? count(s) : 0, wt = s < batch ? weight(s) : 0;
+            int64_t incl = n, wincl = wt;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int64_t up = __shfl_up(incl, o), wup = __shfl_up(wincl, o);
+                if (lane >= o) { incl += up; wincl += wup; }
+            }
+            const uint64_t hit = __ballot(items + incl > item);
+            if (hit) {
+                const int l = __ffsll((long long)hit) - 1;
+                seq = s0 + l;
+                r = (int)(item - items - __shfl(incl - n, l));
+                bef = sum + __shfl(wincl - wt, l);
+                break;
+            }
+            items += __shfl(incl, 63);
+            sum += __shfl(wincl, 63);
+        }
+        if (lane == 0) { s_out[0] = seq; s_out[1] = r; s_out[2] = bef; }
+    }
+    __syncthreads();
+    rem = (int)s_out[1];
+    before = s_out[2];
+    return (int)s_out[0];
+}
+
+}  // namespace cache
+}  // namespace ifv2

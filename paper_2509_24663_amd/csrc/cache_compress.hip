@@ -1,0 +1,132 @@
+// Stage 1 for a growing paged cache: K^{C1}_i = Mean(K[i*s : i*s + l]) (Sec. 3.3, Eq. 3) for the rows that became complete while sequence b grew
+// from prev[b] to ctx[b] tokens, from the keys as the pages hold them.  As the append of compress_k.hip, with a page looked up for every 64
+// tokens of a window; the additions are in the order of the window, in 32 bits.
+#include "cache.h"
+#include "gen_unit.h"
+
+namespace ifv2 {
+
+namespace {
+
+constexpr int VEC = 8;            // channels per thread
+constexpr int U = 16;             // rows requested at once
+
+struct CompressArgs {
+    cache::Args c;
+    float *kc;
+    int64_t kc_head_stride;
+    const int32_t *prev, *ctx;
+    int pairs, lc, sc, rows;
+};
+
+template <typename T, int D, bool CODES>
+__global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
+    constexpr int VPR = D / VEC;
+    const int slot = threadIdx.x / VPR, pair = (int)((blockIdx.y * (64u / VPR) + slot) / a.rows);
+    if (pair >= a.pairs) return;
+    const int b = pair / a.c.hkv, h = pair - b * a.c.hkv;
+    const int i = num_cmp(a.prev[b], a.lc, a.sc) + (int)blockIdx.x * a.rows + (slot & (a.rows - 1));
+    if (i >= num_cmp(a.ctx[b], a.lc, a.sc)) return;
+    const int c0 = (threadIdx.x % VPR) * VEC;
+    float acc[VEC];
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) acc[c] = 0.f;
+    const int end = i * a.sc + a.lc;
+    for (int t = i * a.sc; t < end;) {
+        const int block = t / kBlock, stop = min(end, (block + 1) * kBlock);
+        const int page = a.c.page(b, block);
+        if (page >= 0) {
+            const char *base = a.c.k + a.c.at(page, h) - (int64_t)block * kBlock * a.c.tok_stride;
+            const float scale = CODES ? a.c.ks[(int64_t)page * a.c.hkv + h] : 1.f;
+            for (int u0 = t; u0 < stop; u0 += U) {
+                if constexpr (CODES) {
+                    uint2 x[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const uint2 *>(base + (int64_t)min(u0 + u, stop - 1) * a.c.tok_stride + c0);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const bool in = u0 + u < stop;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int w = (int)(j ? x[u].y : x[u].x);
+                            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                            acc[4 * j] += in ? lo[0] * scale : 0.f, acc[4 * j + 1] += in ? lo[1] * scale : 0.f;
+                            acc[4 * j + 2] += in ? hi[0] * scale : 0.f, acc[4 * j + 3] += in ? hi[1] * scale : 0.f;
+                        }
+                    }
+                } else {
+                    typedef typename std::conditional<sizeof(T) == 2, gen::u16x8_u, gen::f32x8_u>::type Vec;
+                    Vec x[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        x[u] = *reinterpret_cast<const Vec *>(base + (int64_t)min(u0 + u, stop - 1) * a.c.tok_stride + c0 * sizeof(T));
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const bool in = u0 + u < stop;
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) {
+                            if constexpr (sizeof(T) == 2) acc[c] += in ? bf16_to_float(x[u][c]) : 0.f;
+                            else acc[c] += in ? x[u][c] : 0.f;
+                        }
+                    }
+                }
+            }
+        }
+        t = stop;
+    }
+    const float inv = 1.0f / (float)a.lc;
+#pragma unroll
+    for (int c = 0; c < VEC; ++c) acc[c] *= inv;
+    gen::store_row<float, VEC>(a.kc + (int64_t)pair * a.kc_head_stride + (int64_t)i * D + c0, acc);
+}
+
+template <typename T, int D>
+int launch_t(CompressArgs a, bool codes, int max_new, hipStream_t stream) {
+    // consecutive new rows of a pair share a workgroup
+    const int per = 64 / (D / VEC);
+    a.rows = 1;
+    while (a.rows < per && a.rows < max_new) a.rows *= 2;
+    const int64_t y = ((int64_t)a.pairs * a.rows + per - 1) / per;
+    if (y > 65535) return INFLLMV2_ERR_UNSUPPORTED;
+    const dim3 grid((max_new + a.rows - 1) / a.rows, (unsigned)y);
+    if (codes) hipLaunchKernelGGL((cache_compress_kernel<T, D, true>), grid, dim3(64), 0, stream, a);
+    else hipLaunchKernelGGL((cache_compress_kernel<T, D, false>), grid, dim3(64), 0, stream, a);
+    return hip_status(hipGetLastError());
+}
+
+}  // namespace
+
+}  // namespace ifv2
+
+extern "C" int infllmv2_cache_compress_k(const infllmv2_params *p, const infllmv2_cache *c, float *kc_cache_d, int64_t kc_head_stride,
+                                         const int32_t *prev_lens_h, const int32_t *prev_lens_d, const int32_t *ctx_lens_h,
+                                         const int32_t *ctx_lens_d, int32_t batch, void *stream) {
+    using namespace ifv2;
+    int st = check_params(p);
+    if (st) return st;
+    if (batch < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (batch == 0) return INFLLMV2_OK;
+    if (prev_lens_h == nullptr || prev_lens_d == nullptr || ctx_lens_h == nullptr || ctx_lens_d == nullptr)
+        return INFLLMV2_ERR_INVALID_ARGUMENT;
+    int max_new = 0, max_nc = 0, max_ctx = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (prev_lens_h[b] < 0 || ctx_lens_h[b] < prev_lens_h[b] || ctx_lens_h[b] > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
+        const int n1 = num_cmp(ctx_lens_h[b], p->cmp_len, p->cmp_stride);
+        const int grown = n1 - num_cmp(prev_lens_h[b], p->cmp_len, p->cmp_stride);
+        if (grown > max_new) max_new = grown;
+        if (n1 > max_nc) max_nc = n1;
+        if (ctx_lens_h[b] > max_ctx) max_ctx = ctx_lens_h[b];
+    }
+    if (max_new == 0) return INFLLMV2_OK;
+    if (kc_cache_d == nullptr || kc_head_stride < (int64_t)max_nc * p->head_dim) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    st = cache::check(p, c, max_ctx, false);
+    if (st) return st;
+    CompressArgs a{cache::args(p, c), kc_cache_d, kc_head_stride, prev_lens_d, ctx_lens_d, batch * p->num_kv_heads, p->cmp_len, p->cmp_stride, 1};
+    const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
+    const hipStream_t s = (hipStream_t)stream;
+    if (p->head_dim == 128)
+        return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 128>(a, codes, max_new, s) : launch_t<float, 128>(a, codes, max_new, s);
+    return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 64>(a, codes, max_new, s) : launch_t<float, 64>(a, codes, max_new, s);
+}

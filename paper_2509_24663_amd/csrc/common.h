@@ -201,6 +201,13 @@ int launch_attn_bwd(const Launch &L, const void *q, const void *k, const void *v
                     const void *out, const float *lse, const void *dout, void *dq, float *dk, float *dv,
                     const int32_t *cu_h);
 
+// ---------------------------------------------------------------- argument checks shared by the entry points (api.hip)
+int check_params(const infllmv2_params *p);
+// cu_seqlens: [batch+1], starts at 0, non-decreasing; total tokens / longest sequence
+int check_cu(const int32_t *cu_h, const int32_t *cu_d, int32_t batch, int64_t *total, int32_t *max_len);
+// 256-byte aligned when present; need == 0 accepts anything (also NULL)
+int check_ws(const void *ws, size_t ws_bytes, size_t need);
+
 inline int hip_status(hipError_t e) { return e == hipSuccess ? INFLLMV2_OK : INFLLMV2_ERR_HIP; }
 
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }

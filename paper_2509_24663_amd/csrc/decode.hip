@@ -1215,6 +1215,7 @@ size_t decode_mfma_workspace(const infllmv2_params *p, int batch, int max_ctx, b
     return dec_layout(p, batch, max_ctx, (dense_tokens + kBlock - 1) / kBlock, fine).total;
 }
 
+// out == nullptr: the block lists alone (idx_out; k, v and lse are not used)
 int launch_decode_mfma(const infllmv2_params *p, const void *q, const void *k, const void *v, int64_t kv_batch_stride,
                        int64_t kv_head_stride, int64_t kv_tok_stride, const float *kc, int64_t kc_head_stride,
                        const int32_t *ctx_h, const int32_t *ctx_d, int batch, int32_t *idx_out, void *out, float *lse,
@@ -1264,6 +1265,19 @@ int launch_decode_mfma(const infllmv2_params *p, const void *q, const void *k, c
     a.nslot = d.nslot;
     a.bpw = d.bpw;
     const size_t attn_lds = (size_t)AW * TILE_ELEMS * sizeof(uint16_t);
+    if (d.staged && out == nullptr) {
+        const int max_nc = num_cmp(max_ctx, p->cmp_len, p->cmp_stride), max_nb = (max_ctx + kBlock - 1) / kBlock;
+        const bool row = max_nc <= kRowKeys && max_nb <= kRowBlocks && pairs <= 512;        // (as below)
+        a.fsplit = 0;
+        hipLaunchKernelGGL(dec_front_kernel, dim3(d.nchunk, pairs), dim3(256), (size_t)FW * TILE_ELEMS * sizeof(uint16_t), stream, a);
+        if (row) {
+            hipLaunchKernelGGL((dec_pick_kernel<2 * AW, true>), dim3(pairs), dim3(2 * AW * 64), 0, stream, a);
+        } else {
+            hipLaunchKernelGGL(dec_pool_kernel, dim3((max_nb + PB - 1) / PB, pairs), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((dec_pick_kernel<AW, false>), dim3(pairs), dim3(AW * 64), 0, stream, a);
+        }
+        return hip_status(hipGetLastError());
+    }
     if (d.staged) {
         // Larger-than-default dynamic LDS has to be enabled per kernel; the same fixed limit is set on every call,
         // so nothing has to be remembered between calls.
@@ -1308,6 +1322,7 @@ int launch_decode_mfma(const infllmv2_params *p, const void *q, const void *k, c
         return INFLLMV2_ERR_HIP;
     hipLaunchKernelGGL(dec_scores_kernel, dim3(d.nchunk, pairs), dim3(256), 0, stream, a);
     hipLaunchKernelGGL(dec_select_kernel, dim3(pairs), dim3(SEL_THREADS), sel_lds, stream, a, sh_cap);
+    if (out == nullptr) return hip_status(hipGetLastError());
     hipLaunchKernelGGL(dec_attn_kernel, dim3(d.nsplit, pairs), dim3(AW * 64), attn_lds, stream, a);
     hipLaunchKernelGGL(dec_merge_kernel, dim3(pairs), dim3(kMergeThreads), 0, stream, a);
     return hip_status(hipGetLastError());
