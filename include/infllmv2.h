@@ -397,7 +397,8 @@ typedef struct infllmv2_cache {
     int32_t num_pages;            /* >= 1                                                                        */
     void *k_d, *v_d;              /* device, 16-byte aligned; row r of head h of page g at
                                      base + g * page_stride + h * head_stride + r * tok_stride, head_dim contiguous */
-    int64_t page_stride, head_stride, tok_stride;   /* elements, >= head_dim, multiples of 16 bytes               */
+    int64_t page_stride, head_stride, tok_stride;   /* elements, >= head_dim, multiples of 16 bytes; tok_stride at most
+                                     2^24 in infllmv2_cache_attn (else UNSUPPORTED)                               */
     float *k_scale_d, *v_scale_d; /* INFLLMV2_CACHE_E4M3: device [num_pages, num_kv_heads]; else ignored          */
     const int32_t *page_table_d;  /* device [batch, table_stride]                                                */
     int32_t table_stride;         /* >= ceil(longest context / 64), else INVALID_ARGUMENT                        */

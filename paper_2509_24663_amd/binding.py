@@ -467,14 +467,20 @@ class Rotary:
         self.c = _RotaryC(int(rot_dim), LAYOUTS[layout], float(magnitude), 0, turns.data_ptr())
 
 
+# (The checks below take shapes and strides as whole tuples: each question to a tensor is 0.1 to 0.3 us, and these calls are short.)
 def _rotary(name, p: Params, rot: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor]):
-    assert x.dim() == 3 and x.stride(2) == 1 and x.shape[2] == p.head_dim and x.dtype == p.torch_dtype
-    assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == x.shape[0]
+    tokens, heads, d = x.shape
+    x_tok, x_head, one = x.stride()
+    assert one == 1 and d == p.head_dim and x.dtype is p.torch_dtype
+    assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (tokens,)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    assert out.shape == x.shape and out.stride(2) == 1 and out.dtype == x.dtype
-    st = getattr(lib(), name)(ctypes.byref(p), ctypes.byref(rot.c), _ptr(x), x.stride(0), x.stride(1), _ptr(out), out.stride(0),
-                              out.stride(1), _ptr(positions), x.shape[0], x.shape[1], _stream())
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        y_tok, y_head = heads * d, d
+    else:
+        y_tok, y_head, one = out.stride()
+        assert one == 1 and out.shape == x.shape and out.dtype is x.dtype
+    st = getattr(lib(), name)(ctypes.byref(p), ctypes.byref(rot.c), x.data_ptr(), x_tok, x_head, out.data_ptr(), y_tok, y_head,
+                              positions.data_ptr(), tokens, heads, _stream())
     _check(st, name)
     return out
 
@@ -527,13 +533,14 @@ def cache_append(p: Params, cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
     """New keys and values k, v [hkv, T, d] (packed by cu_new) written behind the prev_lens[b] tokens that sequence b has; keys turned by
     `rotary` (positions: device int32 [T], else a token's place in its sequence).  Returns the cache."""
     si, pv = _seq_info(cu_new), _decode_info(prev_lens)
-    ts, hs = _kv_strides(k)
-    assert _kv_strides(v) == (ts, hs) and k.dtype == v.dtype == p.torch_dtype and k.shape == v.shape == (p.num_kv_heads, si.total, p.head_dim)
-    assert si.batch == pv.batch <= cache.batch
+    hs, ts, one = stride = k.stride()
+    dtype, batch = p.torch_dtype, si.batch
+    assert one == 1 and v.stride() == stride and k.dtype is dtype and v.dtype is dtype
+    assert k.shape == v.shape == (p.num_kv_heads, si.total, p.head_dim) and batch == pv.batch <= cache.batch
     assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == si.total)
     st = lib().infllmv2_cache_append(ctypes.byref(p), ctypes.byref(cache.c), ctypes.byref(rotary.c) if rotary is not None else None,
-                                     _ptr(k), _ptr(v), ts, hs, _ptr(si.cu_h), _ptr(si.cu_d), _ptr(pv.ctx_h), _ptr(pv.ctx_d),
-                                     _ptr(positions), si.batch, _stream())
+                                     k.data_ptr(), v.data_ptr(), ts, hs, si.cu_h.data_ptr(), si.cu_d.data_ptr(), pv.ctx_h.data_ptr(),
+                                     pv.ctx_d.data_ptr(), _ptr(positions), batch, _stream())
     _check(st, "infllmv2_cache_append")
     return cache
 
@@ -541,11 +548,11 @@ def cache_append(p: Params, cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
 def cache_compress_k(p: Params, cache: PagedCache, kc_cache: torch.Tensor, prev_lens, ctx_lens):
     """compress_k_append from the pages: kc_cache [B, hkv, max_nc, d] fp32 brought up to date in place."""
     pv, cx = _decode_info(prev_lens), _decode_info(ctx_lens)
-    assert kc_cache.dim() == 4 and kc_cache.is_contiguous() and kc_cache.dtype == torch.float32
-    assert kc_cache.shape[1] == p.num_kv_heads and kc_cache.shape[3] == p.head_dim
-    assert pv.batch == cx.batch <= min(cache.batch, kc_cache.shape[0])
-    st = lib().infllmv2_cache_compress_k(ctypes.byref(p), ctypes.byref(cache.c), _ptr(kc_cache), kc_cache.stride(1), _ptr(pv.ctx_h),
-                                         _ptr(pv.ctx_d), _ptr(cx.ctx_h), _ptr(cx.ctx_d), cx.batch, _stream())
+    planes, hkv, rows, d = kc_cache.shape
+    assert kc_cache.is_contiguous() and kc_cache.dtype is torch.float32 and hkv == p.num_kv_heads and d == p.head_dim
+    assert pv.batch == cx.batch <= cache.batch and cx.batch <= planes
+    st = lib().infllmv2_cache_compress_k(ctypes.byref(p), ctypes.byref(cache.c), kc_cache.data_ptr(), rows * d, pv.ctx_h.data_ptr(),
+                                         pv.ctx_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), cx.batch, _stream())
     _check(st, "infllmv2_cache_compress_k")
     return kc_cache
 
@@ -574,17 +581,24 @@ def cache_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q, ctx_
     cached tokens, its queries the last of them.  block_idx [T, hkv, topk_total] int32 or None (all keys).  Returns (out [T, hq, d],
     lse [T, hq])."""
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
-    assert q.is_contiguous() and q.dtype == p.torch_dtype and q.shape == (si.total, p.num_q_heads, p.head_dim)
+    tokens, hq, _ = shape = q.shape
+    assert q.is_contiguous() and q.dtype is p.torch_dtype and shape == (si.total, p.num_q_heads, p.head_dim)
     assert si.batch == cx.batch <= cache.batch
-    assert block_idx is None or (block_idx.is_contiguous() and block_idx.dtype == torch.int32 and
-                                 block_idx.shape == (si.total, p.num_kv_heads, p.topk_total))
-    out = torch.empty_like(q) if out is None else out
-    lse = torch.empty((si.total, p.num_q_heads), dtype=torch.float32, device=q.device) if lse is None else lse
-    assert out.is_contiguous() and lse.is_contiguous()
+    if block_idx is not None:
+        assert block_idx.is_contiguous() and block_idx.dtype is torch.int32 and block_idx.shape == (tokens, p.num_kv_heads, p.topk_total)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        assert out.is_contiguous() and out.shape == shape and out.dtype is q.dtype
+    if lse is None:
+        lse = q.new_empty((tokens, hq), dtype=torch.float32)
+    else:
+        assert lse.is_contiguous() and lse.shape == (tokens, hq) and lse.dtype is torch.float32
     if workspace is None:
         need = workspace_bytes(OP_CACHE_ATTN, p, si.batch, si.total, cx.max_ctx)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    st = lib().infllmv2_cache_attn(ctypes.byref(p), ctypes.byref(cache.c), _ptr(q), _ptr(si.cu_h), _ptr(si.cu_d), _ptr(cx.ctx_h),
-                                   _ptr(cx.ctx_d), si.batch, _ptr(block_idx), _ptr(out), _ptr(lse), *_ws_args(workspace), _stream())
+    st = lib().infllmv2_cache_attn(ctypes.byref(p), ctypes.byref(cache.c), q.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(),
+                                   cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch, _ptr(block_idx), out.data_ptr(), lse.data_ptr(),
+                                   *_ws_args(workspace), _stream())
     _check(st, "infllmv2_cache_attn")
     return out, lse

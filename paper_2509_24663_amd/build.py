@@ -37,6 +37,7 @@ EXTRA_FLAGS = {
     "attn_staged.hip": _VGPR_FORM,
     "block_scores.hip": _VGPR_FORM,
     "cache_attn.hip": _VGPR_FORM,
+    "cache_attn_tile.hip": _VGPR_FORM,
 }
 
 

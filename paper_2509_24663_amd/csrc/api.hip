@@ -17,7 +17,7 @@ int launch_decode_mfma(const infllmv2_params *p, const void *q, const void *k, c
                        int64_t kv_head_stride, int64_t kv_tok_stride, const float *kc, int64_t kc_head_stride,
                        const int32_t *ctx_h, const int32_t *ctx_d, int batch, int32_t *idx_out, void *out, float *lse,
                        void *ws, size_t ws_bytes, hipStream_t stream);
-size_t cache_attn_ws_bound(const infllmv2_params *p, int64_t tokens, int32_t max_ctx);
+size_t cache_attn_ws_bound(const infllmv2_params *p, int32_t batch, int64_t tokens, int32_t max_ctx);
 }  // namespace ifv2
 
 namespace ifv2 {
@@ -308,7 +308,7 @@ size_t infllmv2_workspace_bytes(int op, const infllmv2_params *p, int32_t batch,
         case INFLLMV2_OP_DENSE_ATTN_FWD: return attn_fwd_ws_bytes(p, t);
         case INFLLMV2_OP_SPARSE_ATTN_BWD: return attn_bwd_ws_bytes(p, t, true);
         case INFLLMV2_OP_SPARSE_ATTN_BWD_MIN: return attn_bwd_ws_bytes(p, t, false);
-        case INFLLMV2_OP_CACHE_ATTN: return cache_attn_ws_bound(p, total_tokens, max_seqlen);
+        case INFLLMV2_OP_CACHE_ATTN: return cache_attn_ws_bound(p, batch, total_tokens, max_seqlen);
         default: return 0;      // compress_k, compress_k_append, top-k: no scratch
     }
 }

@@ -1,0 +1,51 @@
+// What the two kernels of infllmv2_cache_attn share: cache_attn.hip (16 columns per workgroup, any data) and cache_attn_tile.hip (chunks of prompts, bf16).
+#pragma once
+#include "cache.h"
+#include "gen_unit.h"
+
+namespace ifv2 {
+namespace cache_attn {
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.4028234e38f;
+
+struct AttnArgs {
+    cache::Args c;
+    const char *q;
+    char *out;
+    float *lse;                        // or nullptr
+    const int32_t *cu, *ctx, *idx;     // idx: nullptr: all keys
+    int batch, hq, topk, dense_below;
+    int group_tokens;                  // of 16 columns over all keys (16 / G)
+    int wide_from;                     // sequences over all keys with so many queries are the tile kernel's
+    int tile_groups;                   // column groups of a tile of this launch (1: cache_attn.hip)
+    int pps;                           // pages of a split
+    int even;                          // > 0: one query token for each sequence, item = (sequence, head, split < even); slots alike
+    int multi;                         // some tile of cache_attn.hip has more than one token
+    float scale;
+    float *part;                       // [slots][16 tile_groups][D] sums, relative to the reference
+    float *ml;                         // [slots][16 tile_groups][2] reference, sum of weights
+    // how the n queries of a sequence of len tokens are cut
+    __host__ __device__ bool listed(int len) const { return idx != nullptr && len >= dense_below; }
+    __host__ __device__ int tile_tokens(int len) const { return listed(len) ? 1 : group_tokens * tile_groups; }
+    __host__ __device__ int tiles(int n, int len) const {
+        if ((tile_groups > 1) != (!listed(len) && n >= wide_from)) return 0;
+        const int t = tile_tokens(len);
+        return (n + t - 1) / t;
+    }
+    // pages (listed: entries) of the tile whose last token is at pos_last
+    __host__ __device__ int pages(int len, int pos_last) const {
+        const int all = pos_last / kBlock + 1;
+        return listed(len) && topk < (len + kBlock - 1) / kBlock ? topk : all;
+    }
+    __host__ __device__ int splits(int len, int pos_last) const { return (pages(len, pos_last) + pps - 1) / pps; }
+    __host__ __device__ int most_splits(int n, int len) const { return n == 0 ? 0 : splits(len, len - 1); }
+};
+
+// the rules of cache_attn_tile.hip
+int tile_wide_from(const infllmv2_params *p);           // least queries of a sequence, INT32_MAX: never
+int tile_groups(const infllmv2_params *p);
+int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream);
+
+}  // namespace cache_attn
+}  // namespace ifv2

@@ -9,43 +9,18 @@
 // A step's K is requested when the previous step's logits are done and its V when the previous step's sums are, so that one step is always
 // in flight.  The work of a (tile, KV head) is split along the keys over workgroups, and over the four wavefronts of each; partial results are joined in
 // LDS, then by cache_merge_kernel.
-#include "cache.h"
-#include "gen_unit.h"
+#include "cache_attn.h"
 
 namespace ifv2 {
 
 namespace {
 
 using namespace gen;
+using cache_attn::AttnArgs;
+using cache_attn::kLn2;
+using cache_attn::kLowest;
 
 constexpr int NW = 4;                  // wavefronts of a workgroup
-constexpr int kEntries = 256;          // pages that a workgroup lists at a time
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLowest = -3.4028234e38f;
-
-struct AttnArgs {
-    cache::Args c;
-    const char *q;
-    char *out;
-    float *lse;                        // or nullptr
-    const int32_t *cu, *ctx, *idx;     // idx: nullptr: all keys
-    int batch, hq, topk, dense_below;
-    int tokens;                        // of a tile over all keys (16 / G)
-    int pps;                           // pages of a split
-    int plain;                         // one query token for each sequence, no splits: item = (sequence, head)
-    float scale;
-    float *part;                       // [slots][16][D] sums, relative to the reference
-    float *ml;                         // [slots][16][2] reference, sum of weights
-    // how sequence s is cut
-    __host__ __device__ bool listed(int len) const { return idx != nullptr && len >= dense_below; }
-    __host__ __device__ int tiles(int n, int len) const { return listed(len) ? n : (n + tokens - 1) / tokens; }
-    __host__ __device__ int pages(int len) const {
-        const int all = (len + kBlock - 1) / kBlock;
-        return listed(len) && topk < all ? topk : all;
-    }
-    __host__ __device__ int splits(int n, int len) const { return n == 0 ? 0 : (pages(len) + pps - 1) / pps; }
-};
-
 __device__ inline float rows_max(float x) {          // over lanes with equal lane % 16
     x = fmaxf(x, __shfl_xor(x, 16));
     return fmaxf(x, __shfl_xor(x, 32));
@@ -68,15 +43,17 @@ __device__ inline uint32_t widen(uint32_t w, float scale) {
 template <typename T, int D, bool CODES> struct KeyTile;
 template <typename T, int D> struct KeyTile<T, D, false> {
     RowFrag<T, D> f;
-    __device__ inline void load(const char *row, int g) { f.load(reinterpret_cast<const T *>(row), g); }
+    static __device__ inline uint32_t lane_offset(int g) { return 16 * g; }
+    __device__ inline void load(const char *base, uint32_t off) { f.load_at(base, off); }
     __device__ inline RowFrag<T, D> operand(float) const { return f; }
     static __device__ inline void load_query(RowFrag<T, D> &q, const T *row, int g) { q.load(row, g); }
 };
 template <int D> struct KeyTile<bf16_t, D, true> {
     u32x4 raw[D / 64];                 // channels 64 s + 16 g .. + 15
-    __device__ inline void load(const char *row, int g) {
+    static __device__ inline uint32_t lane_offset(int g) { return 16 * g; }
+    __device__ inline void load(const char *base, uint32_t off) {
 #pragma unroll
-        for (int s = 0; s < D / 64; ++s) raw[s] = *reinterpret_cast<const u32x4 *>(row + 64 * s + 16 * g);
+        for (int s = 0; s < D / 64; ++s) raw[s] = *reinterpret_cast<const u32x4 *>(base + off + 64 * s);
     }
     __device__ inline RowFrag<bf16_t, D> operand(float scale) const {
         RowFrag<bf16_t, D> f;
@@ -95,9 +72,10 @@ template <int D> struct KeyTile<bf16_t, D, true> {
 };
 template <int D> struct KeyTile<float, D, true> {
     u32x4 raw[D / 64];
-    __device__ inline void load(const char *row, int g) {
+    static __device__ inline uint32_t lane_offset(int g) { return 16 * g; }
+    __device__ inline void load(const char *base, uint32_t off) {
 #pragma unroll
-        for (int s = 0; s < D / 64; ++s) raw[s] = *reinterpret_cast<const u32x4 *>(row + 64 * s + 16 * g);
+        for (int s = 0; s < D / 64; ++s) raw[s] = *reinterpret_cast<const u32x4 *>(base + off + 64 * s);
     }
     __device__ inline RowFrag<float, D> operand(float scale) const {
         RowFrag<float, D> f;
@@ -122,7 +100,7 @@ struct ValueRow {
     static constexpr int W = BYTES / 4;
     typedef uint32_t Words __attribute__((ext_vector_type(W)));
     Words raw;
-    __device__ inline void load(const char *row, int m) { raw = *reinterpret_cast<const Words *>(row + m * BYTES); }
+    __device__ inline void load(const char *base, uint32_t off) { raw = *reinterpret_cast<const Words *>(base + off); }
     __device__ inline uint32_t word(int i) const {
         if constexpr (W == 1) return raw[0];
         else return raw[i];
@@ -167,8 +145,15 @@ template <int TILES> struct Weights<float, TILES> {
 };
 
 // acc[j] += (rows' channel N (4 g + r) + j) x (weights of column m); rows v[4 t + r]: key 16 t + 4 g + r of the step
-template <int D, int TILES, bool CODES>
-__device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<bf16_t, TILES> &w, const ValueRow<bf16_t, D, CODES> (&v)[4 * TILES], float scale) {
+// SOLO: only into the columns (lanes) that take
+template <bool SOLO, int D, int TILES, bool CODES>
+__device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<bf16_t, TILES> &w, const ValueRow<bf16_t, D, CODES> (&v)[4 * TILES], float scale, bool take) {
+    auto add = [&](f32x4 &to, bf16x8 row, int t) {
+        f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.lo[t], to, 0, 0, 0);
+        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.hi[t], x, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[r] = !SOLO || take ? x[r] : to[r];
+    };
 #pragma unroll
     for (int t = 0; t < TILES / 2; ++t) {
         const ValueRow<bf16_t, D, CODES> *a = &v[8 * t];
@@ -187,9 +172,7 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<bf16_t, TI
                     u32x4 x;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) x[k] = j & 1 ? widen<true>(s[k], scale) : widen<false>(s[k], scale);
-                    const bf16x8 row = __builtin_bit_cast(bf16x8, x);
-                    acc[4 * i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.lo[t], acc[4 * i + j], 0, 0, 0);
-                    acc[4 * i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.hi[t], acc[4 * i + j], 0, 0, 0);
+                    add(acc[4 * i + j], __builtin_bit_cast(bf16x8, x), t);
                 }
             }
         } else {
@@ -200,21 +183,20 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<bf16_t, TI
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     x[k] = j & 1 ? upper_halves(a[2 * k].word(i), a[2 * k + 1].word(i)) : lower_halves(a[2 * k].word(i), a[2 * k + 1].word(i));
-                const bf16x8 row = __builtin_bit_cast(bf16x8, x);
-                acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.lo[t], acc[j], 0, 0, 0);
-                acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.hi[t], acc[j], 0, 0, 0);
+                add(acc[j], __builtin_bit_cast(bf16x8, x), t);
             }
         }
     }
 }
-template <int D, int TILES, bool CODES>
-__device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TILES> &w, const ValueRow<float, D, CODES> (&v)[4 * TILES], float) {
+template <bool SOLO, int D, int TILES, bool CODES>
+__device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TILES> &w, const ValueRow<float, D, CODES> (&v)[4 * TILES], float, bool take) {
 #pragma unroll
-    for (int t = 0; t < TILES; ++t)
+    for (int j = 0; j < D / 16; ++j) {
+        f32x4 sum = acc[j];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) {
+            for (int r = 0; r < 4; ++r) {
                 float x;
                 if constexpr (CODES) {
                     const auto two = (j & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)v[4 * t + r].word(j / 4), true)
@@ -223,50 +205,55 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TIL
                 } else {
                     x = __uint_as_float(v[4 * t + r].word(j));
                 }
-                acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, w.w[t][r], acc[j], 0, 0, 0);
+                sum = __builtin_amdgcn_mfma_f32_16x16x4f32(x, w.w[t][r], sum, 0, 0, 0);
             }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[j][r] = !SOLO || take ? sum[r] : acc[j][r];
+    }
 }
 
-struct Entry {
-    int page, key0;                    // key0: the page's first key
-    float ks, vs;
-};
-
 // ------------------------------------------------------------------------------------------ a split of a tile
-template <typename T, int D, bool CODES, int TILES>
-__global__ void __launch_bounds__(NW * 64) cache_attn_kernel(AttnArgs a) {
+// MULTI: tiles may have several tokens
+template <typename T, int D, bool CODES, int TILES, bool MULTI>
+__global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
     __shared__ int64_t s_item[3];
-    __shared__ Entry s_entry[kEntries];
-    __shared__ int s_count;
     __shared__ float s_m[NW][16], s_l[NW][16];
     __shared__ f32x4 s_o[NW][N][64];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv;
 
     // the item: sequence, tile, KV head, split; slot: where a partial result goes
-    int seq, rem;
-    int64_t slot0 = 0;
-    if (a.plain) {
-        seq = (int)(blockIdx.x / (unsigned)hkv);
-        rem = (int)(blockIdx.x - (unsigned)seq * (unsigned)hkv);
+    int seq, rem, row0, n;
+    int64_t slot = blockIdx.x;
+    if (a.even) {
+        seq = (int)(blockIdx.x / (unsigned)(hkv * a.even));
+        rem = (int)(blockIdx.x - (unsigned)seq * (unsigned)(hkv * a.even));
+        row0 = seq;
+        n = 1;
     } else {
+        int64_t slot0;
         seq = cache::find_item(a.batch, blockIdx.x, rem, slot0, s_item,
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
-                return (int64_t)a.tiles(n, len) * hkv * a.splits(n, len);
+                return (int64_t)a.tiles(n, len) * hkv * a.most_splits(n, len);
             },
             [&](int s) {
-                const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.splits(n, len);
+                const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
                 return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
             });
         if (seq >= a.batch) return;
+        slot = slot0 + rem;
+        row0 = a.cu[seq];
+        n = a.cu[seq + 1] - row0;
     }
-    const int row0 = a.cu[seq], n = a.cu[seq + 1] - row0, len = a.ctx[seq], nsplit = a.splits(n, len);
+    const int len = a.ctx[seq], per = a.even ? a.even : a.most_splits(n, len);
     const bool listed = a.listed(len);
-    const int split = rem % nsplit, th = rem / nsplit, h = th % hkv, tile = th / hkv;
-    const int T0 = listed ? 1 : a.tokens, first = tile * T0, ntok = min(T0, n - first);    // tokens of this tile
+    const int split = rem % per, th = rem / per, h = th % hkv, tile = th / hkv;
+    const int T0 = a.tile_tokens(len), first = tile * T0, ntok = min(T0, n - first);       // tokens of this tile
     const int pos0 = len - n + first, pos_last = pos0 + ntok - 1;
+    const int nsplit = a.splits(len, pos_last);
+    if (split >= nsplit) return;
     const int ti = m / G;                                                                // this lane's column
     const bool used = ti < ntok;
     const int pos = used ? pos0 + ti : -1;
@@ -283,72 +270,66 @@ __global__ void __launch_bounds__(NW * 64) cache_attn_kernel(AttnArgs a) {
     float ref = -INFINITY, sum = 0.f;            // reference in units of log2; this lane's share of the sum
     int low = INT32_MAX;                         // first key of any page that this wavefront went through
 
-    const int all = listed ? min(a.topk, (len + kBlock - 1) / kBlock) : pos_last / kBlock + 1;
-    const int e_end = min(all, (split + 1) * a.pps);
-    const int32_t *list = listed ? a.idx + (row * hkv + h) * a.topk : nullptr;
-    for (int e0 = split * a.pps; e0 < e_end; e0 += kEntries) {
-        // the pages of this part, those that are there side by side
-        __syncthreads();
-        if (w == 0) {
-            int count = 0;
-            for (int x0 = 0; x0 < kEntries && e0 + x0 < e_end; x0 += 64) {
-                const int e = e0 + x0 + lane;
-                int page = -1, j = -1;
-                if (e < e_end) {
-                    j = listed ? list[e] : e;
-                    if (j >= 0 && j <= pos_last / kBlock) page = a.c.page(seq, j);
-                }
-                const uint64_t there = __ballot(page >= 0);
-                if (page >= 0) {
-                    const int64_t at = (int64_t)page * hkv + h;
-                    s_entry[count + __popcll(there & ((1ull << lane) - 1ull))] = Entry{page, j * kBlock, CODES ? a.c.ks[at] : 1.f, CODES ? a.c.vs[at] : 1.f};
-                }
-                count += __popcll(there);
+    const int e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
+    const int32_t *list = a.idx + ((int64_t)(row0 + first) * hkv + h) * a.topk;
+    const uint32_t tok = (uint32_t)a.c.tok_stride;
+    const uint32_t k_off = m * tok + KeyTile<T, D, CODES>::lane_offset(g), v_off = 4 * g * tok + m * ValueRow<T, D, CODES>::BYTES;
+    // a wavefront takes every NW-th page of the split; lane l holds the l-th of the next 64: where it is, its first key, its scales
+    for (int e0 = split * a.pps + w; e0 < e_end; e0 += 64 * NW) {
+        const int e = e0 + lane * NW;
+        int my_page = -1, my_key0 = 0;
+        float my_ks = 1.f, my_vs = 1.f;
+        if (e < e_end) {
+            const int j = listed ? list[e] : e;
+            if (j >= 0 && j <= pos_last / kBlock) {
+                my_page = a.c.page(seq, j);
+                my_key0 = j * kBlock;
             }
-            if (lane == 0) s_count = count;
         }
-        __syncthreads();
-        const int count = __builtin_amdgcn_readfirstlane(s_count);
+        uint64_t there = __ballot(my_page >= 0);
+        if (there == 0) continue;
+        if (CODES && my_page >= 0) {
+            my_ks = a.c.ks[(int64_t)my_page * hkv + h];
+            my_vs = a.c.vs[(int64_t)my_page * hkv + h];
+        }
         KeyTile<T, D, CODES> k[TILES];
         ValueRow<T, D, CODES> v[4 * TILES];
-        auto entry = [&](int e) {
-            Entry x = s_entry[e];
-            x.page = __builtin_amdgcn_readfirstlane(x.page);
-            x.key0 = __builtin_amdgcn_readfirstlane(x.key0);
-            x.ks = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x.ks)));
-            x.vs = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x.vs)));
-            return x;
-        };
-        auto load_k = [&](const Entry &x, int part) {
-            const char *base = a.c.k + a.c.at(x.page, h);
+        auto base_of = [&](const char *p, int l) { return p + a.c.at(__builtin_amdgcn_readlane(my_page, l), h); };
+        auto load_k = [&](const char *base) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) k[t].load(base + (part * STEP + 16 * t + m) * a.c.tok_stride, g);
+            for (int t = 0; t < TILES; ++t) k[t].load(base + (int64_t)(16 * t) * tok, k_off);
         };
-        auto load_v = [&](const Entry &x, int part) {
-            const char *base = a.c.v + a.c.at(x.page, h);
+        auto load_v = [&](const char *base) {
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[4 * t + r].load(base + (part * STEP + 16 * t + 4 * g + r) * a.c.tok_stride, m);
+                for (int r = 0; r < 4; ++r) v[4 * t + r].load(base + (int64_t)(16 * t + r) * tok, v_off);
         };
-        Entry cur{};
-        if (w < count) {
-            cur = entry(w);
-            load_k(cur, 0);
-            load_v(cur, 0);
-        }
-        for (int e = w; e < count; e += NW) {
-            Entry next = cur;
-            low = min(low, cur.key0);
+        int l = __ffsll((long long)there) - 1;
+        const char *kb = base_of(a.c.k, l), *vb = base_of(a.c.v, l);
+        load_k(kb);
+        load_v(vb);
+        while (there) {
+            const int page_key0 = __builtin_amdgcn_readlane(my_key0, l);
+            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), l));
+            const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), l));
+            there &= there - 1;
+            low = min(low, page_key0);
+            if (there) l = __ffsll((long long)there) - 1;
 #pragma unroll 1
             for (int part = 0; part < STEPS; ++part) {
-                const int key0 = cur.key0 + part * STEP;
+                const int key0 = page_key0 + part * STEP;
                 f32x4 s[TILES];
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) s[t] = row_product<D>(k[t].operand(cur.ks), qf);
-                const bool last_part = part == STEPS - 1, more = !last_part || e + NW < count;
-                if (last_part && more) next = entry(e + NW);
-                if (more) load_k(last_part ? next : cur, last_part ? 0 : part + 1);
+                for (int t = 0; t < TILES; ++t) {
+                    s[t] = row_product<D>(k[t].operand(ks), qf);
+                    if (CODES && t % 2 == 1) __builtin_amdgcn_sched_barrier(0);      // (widened rows of two tiles at a time: registers)
+                }
+                const bool last_part = part == STEPS - 1, more = !last_part || there;
+                if (more) {
+                    kb = last_part ? base_of(a.c.k, l) : kb + (int64_t)STEP * tok;
+                    load_k(kb);
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 const bool edge = key0 + STEP - 1 > pos0;                        // keys behind a token
                 if (edge) {
@@ -382,8 +363,8 @@ __global__ void __launch_bounds__(NW * 64) cache_attn_kernel(AttnArgs a) {
                     }
                 sum += part_sum;
                 Weights<T, TILES> wt;
-                wt.set(s, cur.vs);
-                bool solo = false;
+                wt.set(s, vs);
+                int rounds = 1;
                 if (edge) {                                                      // rows that no token of the tile sees, and those that only some see
                     bool odd = false;
 #pragma unroll
@@ -391,33 +372,31 @@ __global__ void __launch_bounds__(NW * 64) cache_attn_kernel(AttnArgs a) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos_last);
-                            odd |= v[4 * t + r].odd();
+                            if (MULTI) odd |= v[4 * t + r].odd();
                         }
-                    solo = ntok > 1 && __any(odd);
+                    if (MULTI && __any(odd)) rounds = ntok;
                 }
-                if (!solo) {
-                    add_values<D, TILES, CODES>(acc, wt, v, cur.vs);
+                if (!MULTI) {
+                    add_values<false, D, TILES, CODES>(acc, wt, v, vs, true);
                 } else {
-                    // 0 x infinity: the sums of each token from the rows that it sees, latest token first
-                    for (int i = ntok - 1; i >= 0; --i) {
+                    // 0 x infinity: where rows are not finite, the sums of each token from the rows that it sees, latest token first
+#pragma unroll 1
+                    for (int i = rounds - 1; i >= 0; --i) {
+                        if (rounds > 1) {
 #pragma unroll
-                        for (int t = 0; t < TILES; ++t)
+                            for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos0 + i);
-                        f32x4 own[N];
-#pragma unroll
-                        for (int j = 0; j < N; ++j) own[j] = acc[j];
-                        add_values<D, TILES, CODES>(own, wt, v, cur.vs);
-#pragma unroll
-                        for (int j = 0; j < N; ++j)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) acc[j][r] = ti == i ? own[j][r] : acc[j][r];
+                                for (int r = 0; r < 4; ++r) v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos0 + i);
+                        }
+                        add_values<true, D, TILES, CODES>(acc, wt, v, vs, rounds == 1 || ti == i);
                     }
                 }
-                if (more) load_v(last_part ? next : cur, last_part ? 0 : part + 1);
+                if (more) {
+                    vb = last_part ? base_of(a.c.v, l) : vb + (int64_t)STEP * tok;
+                    load_v(vb);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            cur = next;
         }
     }
 
@@ -439,7 +418,6 @@ __global__ void __launch_bounds__(NW * 64) cache_attn_kernel(AttnArgs a) {
     __syncthreads();
     // wavefront w: results j = w, w + NW, ..: element r is channel N (4 g + r) + j of column m
     const bool direct = nsplit == 1;
-    const int64_t slot = slot0 + rem;
     const float inv = top == -INFINITY ? 0.f : 1.f / total;
 #pragma unroll
     for (int jj = 0; jj < N / NW; ++jj) {
@@ -470,71 +448,147 @@ __global__ void __launch_bounds__(NW * 64) cache_attn_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------ joining the splits of a tile
+// Four columns per workgroup, D / 4 threads of four channels each; up to kAhead splits are requested at once.
+constexpr int kMergeCols = 4, kAhead = 8;
+
 template <typename T, int D>
-__global__ void __launch_bounds__(256) cache_merge_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
     __shared__ int64_t s_item[3];
     const int tid = threadIdx.x, hkv = a.c.hkv, G = a.hq / hkv;
-    int th;
-    int64_t slot0;
-    const int seq = cache::find_item(a.batch, blockIdx.x, th, slot0, s_item,
-        [&](int s) {
-            const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
-            return a.splits(n, len) > 1 ? (int64_t)a.tiles(n, len) * hkv : 0;
-        },
-        [&](int s) {
-            const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.splits(n, len);
-            return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
-        });
-    if (seq >= a.batch) return;
-    const int row0 = a.cu[seq], n = a.cu[seq + 1] - row0, len = a.ctx[seq], nsplit = a.splits(n, len);
-    const int h = th % hkv, tile = th / hkv, T0 = a.listed(len) ? 1 : a.tokens, first = tile * T0, ntok = min(T0, n - first);
-    const int64_t slot = slot0 + (int64_t)th * nsplit;
-    constexpr int PER = D / 16;                          // channels per thread: 16 threads a column
-    const int m = tid >> 4, c0 = (tid & 15) * PER, ti = m / G;
-    if (ti >= ntok) return;
-    float top = -INFINITY, total = 0.f, o[PER];
+    int th, seq, row0, n;
+    int64_t slot;
+    if (a.even) {
+        seq = (int)(blockIdx.x / (unsigned)hkv);
+        th = (int)(blockIdx.x - (unsigned)seq * (unsigned)hkv);
+        slot = (int64_t)blockIdx.x * a.even;
+        row0 = seq;
+        n = 1;
+    } else {
+        seq = cache::find_item(a.batch, blockIdx.x, th, slot, s_item,
+            [&](int s) {
+                const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
+                return a.most_splits(n, len) > 1 ? (int64_t)a.tiles(n, len) * hkv : 0;
+            },
+            [&](int s) {
+                const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
+                return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
+            });
+        if (seq >= a.batch) return;
+        row0 = a.cu[seq];
+        n = a.cu[seq + 1] - row0;
+    }
+    const int len = a.ctx[seq], cols = 16 * a.tile_groups;
+    if (!a.even) slot += (int64_t)th * a.most_splits(n, len);
+    const int h = th % hkv, tile = th / hkv, T0 = a.tile_tokens(len), first = tile * T0, ntok = min(T0, n - first);
+    const int nsplit = a.splits(len, len - n + first + ntok - 1);
+    if (nsplit == 1) return;                             // (written by the split itself)
+    const int col = blockIdx.y * kMergeCols + tid / (D / 4), c0 = (tid % (D / 4)) * 4, m = col & 15;
+    const int in_group = m / G, ti = (col >> 4) * a.group_tokens + in_group;
+    if (in_group >= min(T0, a.group_tokens) || ti >= ntok) return;
+    const float *src = a.part + (slot * cols + col) * D + c0;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.ml) + slot * cols + col;
+    float top = -INFINITY, total = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < nsplit; s0 += kAhead) {
+        float2 x[kAhead];
+        f32x4 y[kAhead];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) o[i] = 0.f;
-    for (int s = 0; s < nsplit; ++s) {
-        const float ref = a.ml[((slot + s) * 16 + m) * 2], l = a.ml[((slot + s) * 16 + m) * 2 + 1];
-        const float to = fmaxf(top, ref), base = to == -INFINITY ? 0.f : to;
-        const float f0 = exp2_fast(top - base), f1 = exp2_fast(ref - base);
-        total = total * f0 + l * f1;
-        const float *src = a.part + ((slot + s) * 16 + m) * D + c0;
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t s = min(s0 + i, nsplit - 1);
+            x[i] = ml[s * cols];
+            y[i] = *reinterpret_cast<const f32x4 *>(src + s * cols * D);
+        }
+        float to = top;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) o[i] = o[i] * f0 + src[i] * f1;
+        for (int i = 0; i < kAhead; ++i) to = fmaxf(to, x[i].x);
+        const float base = to == -INFINITY ? 0.f : to, f0 = exp2_fast(top - base);
+        total *= f0;
+        o *= f0;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (s0 + i < nsplit) {
+                const float f = exp2_fast(x[i].x - base);
+                total += x[i].y * f;
+                o += y[i] * f;
+            }
+        }
         top = to;
     }
     const int64_t row = row0 + first + ti;
-    const int qh = h * G + m - ti * G;
+    const int qh = h * G + m - in_group * G;
     const float inv = top == -INFINITY ? 0.f : 1.f / total;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) o[i] *= inv;
-    gen::store_row<T, PER>(reinterpret_cast<T *>(a.out) + (row * a.hq + qh) * D + c0, o);
+    const float r[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    gen::store_row<T, 4>(reinterpret_cast<T *>(a.out) + (row * a.hq + qh) * D + c0, r);
     if (c0 == 0 && a.lse != nullptr) a.lse[row * a.hq + qh] = top == -INFINITY ? -INFINITY : top * kLn2 + logf(total);
+}
+
+template <typename T, int D>
+void merge(const AttnArgs &a, int64_t merges, hipStream_t stream) {
+    if (merges > 0)
+        hipLaunchKernelGGL((cache_merge_kernel<T, D>), dim3((unsigned)merges, 16 * a.tile_groups / kMergeCols), dim3(D), 0, stream, a);
 }
 
 template <typename T, int D, bool CODES, int TILES>
 int launch_t(const AttnArgs &a, int64_t items, int64_t merges, hipStream_t stream) {
-    hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES>), dim3((unsigned)items), dim3(NW * 64), 0, stream, a);
-    if (merges > 0) hipLaunchKernelGGL((cache_merge_kernel<T, D>), dim3((unsigned)merges), dim3(256), 0, stream, a);
+    if (a.multi) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, true>), dim3((unsigned)items), dim3(NW * 64), 0, stream, a);
+    else hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, false>), dim3((unsigned)items), dim3(NW * 64), 0, stream, a);
+    merge<T, D>(a, merges, stream);
     return hip_status(hipGetLastError());
 }
 
-constexpr int kTargetGroups = 1024;        // workgroups that a call is cut into: two rounds of two for each CU
-constexpr int kLeastPages = NW;            // a page for each wavefront
+constexpr int kTargetGroups = 2048;        // workgroups that a call is cut into: four rounds of two for each CU
+constexpr int kLeastPages = 2 * NW;        // two pages for each wavefront
+constexpr int kCus = 256;
 
-// Where splits are more than one, they are at most twice pages / pps, and pps >= all pages / kTargetGroups: at most 2 kTargetGroups partial results.
-size_t slot_bytes(int d) { return (size_t)16 * (d + 2) * sizeof(float); }
+// Splits of the tile kernel, whose workgroups (one on a CU) go over the CUs in rounds: the number s that makes (rounds) x (pages of a split and what a
+// split costs beside them) least.  A split's partial result, written and read again, takes the time of kSplitCost pages.
+constexpr int kSplitCost = 12, kMostSplits = 16, kMostTileSlots = 1024;
+int tile_pps(int64_t tiles, int most_pages) {
+    int64_t best = INT64_MAX;
+    int pps = most_pages;
+    for (int s = 1; s <= kMostSplits && s <= most_pages && (s == 1 || tiles * s <= kMostTileSlots); ++s) {
+        const int per = (most_pages + s - 1) / s;
+        const int64_t cost = (tiles * s + kCus - 1) / kCus * (per + (s > 1 ? kSplitCost : 0));
+        if (cost < best) best = cost, pps = per;
+    }
+    return pps;
+}
+
+// Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
+// kTargetGroups, so at most 2 kTargetGroups partial results.
+size_t slot_bytes(int d, int groups) { return (size_t)16 * groups * (d + 2) * sizeof(float); }
+size_t unit_bytes(const infllmv2_params *p, int64_t slots) { return align256((size_t)slots * slot_bytes(p->head_dim, 1)); }
+size_t tile_bytes(const infllmv2_params *p, int64_t slots) { return align256((size_t)slots * slot_bytes(p->head_dim, cache_attn::tile_groups(p))); }
+
+// what a launch covers: workgroups, tiles with several splits, their partial results
+struct Launches {
+    int64_t items = 0, merges = 0, slots = 0;
+    int most = 0;
+    void add(const AttnArgs &a, int n, int len) {
+        const int64_t t = (int64_t)a.tiles(n, len) * a.c.hkv;
+        if (t == 0) return;
+        const int sp = a.most_splits(n, len);
+        items += t * sp;
+        if (sp > 1) merges += t, slots += t * sp;
+        if (sp > most) most = sp;
+    }
+};
 
 }  // namespace
 
-size_t cache_attn_ws_bound(const infllmv2_params *p, int64_t tokens, int32_t max_ctx) {
+size_t cache_attn_ws_bound(const infllmv2_params *p, int32_t batch, int64_t tokens, int32_t max_ctx) {
     const int64_t most = (max_ctx + (int64_t)kBlock - 1) / kBlock, per = (most + kLeastPages - 1) / kLeastPages;
-    if (per <= 1) return 0;
     const int64_t units = tokens * p->num_kv_heads;
-    const int64_t slots = units < 2 * kTargetGroups && units * per < 2 * kTargetGroups ? units * per : 2 * kTargetGroups;
-    return align256((size_t)slots * slot_bytes(p->head_dim));
+    const int64_t slots = per <= 1 ? 0 : units < 2 * kTargetGroups && units * per < 2 * kTargetGroups ? units * per : 2 * kTargetGroups;
+    // the tile kernel: at most tokens / (tokens of a tile) tiles and one more for each sequence
+    const int64_t from = cache_attn::tile_wide_from(p);
+    int64_t tiles = 0;
+    if (tokens >= from && most > 1) {
+        const int64_t per_tile = kCols / (p->num_q_heads / p->num_kv_heads) * cache_attn::tile_groups(p), seqs = tokens / from < batch ? tokens / from : batch;
+        tiles = (tokens / per_tile + seqs) * p->num_kv_heads * (most < kMostSplits ? most : kMostSplits);
+        if (tiles > kMostTileSlots) tiles = kMostTileSlots;
+    }
+    return unit_bytes(p, slots) + tile_bytes(p, tiles);
 }
 
 }  // namespace ifv2
@@ -552,58 +606,86 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     if (st) return st;
     if (total == 0) return INFLLMV2_OK;
     if (q_d == nullptr || out_d == nullptr || ctx_lens_h == nullptr || ctx_lens_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
-    const int hkv = p->num_kv_heads, G = p->num_q_heads / hkv;
+    const int hkv = p->num_kv_heads;
     AttnArgs a{};
+    a.c.hkv = hkv;
     a.idx = block_idx_d;
+    a.batch = batch;
     a.topk = p->topk_total;
     a.dense_below = p->dense_threshold;
-    a.tokens = kCols / G;
-    int max_ctx = 0;
-    int64_t work = 0;                          // pages over all tiles and heads
+    a.group_tokens = kCols / (p->num_q_heads / hkv);
+    a.wide_from = cache_attn::tile_wide_from(p);
+    a.tile_groups = 1;
+    AttnArgs wide = a;                         // the tile kernel's launch
+    wide.tile_groups = cache_attn::tile_groups(p);
+    int max_ctx = 0, wide_pages = 0;
+    int64_t work = 0, wide_tiles = 0;          // pages over all tiles and heads of cache_attn.hip, tiles and heads of the other
     for (int b = 0; b < batch; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
         if (len < n || len > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
         if (n == 0) continue;
         if (len > max_ctx) max_ctx = len;
-        work += (int64_t)a.tiles(n, len) * hkv * a.pages(len);
+        const int64_t mine = (int64_t)a.tiles(n, len) * hkv, other = (int64_t)wide.tiles(n, len) * hkv;
+        const int pages = a.pages(len, len - 1);
+        work += mine * pages;
+        wide_tiles += other;
+        if (other > 0 && pages > wide_pages) wide_pages = pages;
+        if (mine > 0 && n > 1 && a.tile_tokens(len) > 1) a.multi = 1;
     }
     st = cache::check(p, c, max_ctx, true);
     if (st) return st;
-    const int64_t even = (work + kTargetGroups - 1) / kTargetGroups;
-    a.pps = even < kLeastPages ? kLeastPages : even > (1 << 24) ? 1 << 24 : (int)even;
-    int64_t items = 0, merges = 0, slots = 0;
-    bool plain = true;
+    // (rows of a page are addressed with 32-bit offsets)
+    if (c->tok_stride > (1ll << 24)) return INFLLMV2_ERR_UNSUPPORTED;
+    const int64_t share = (work + kTargetGroups - 1) / kTargetGroups;
+    a.pps = share < kLeastPages ? kLeastPages : share > (1 << 24) ? 1 << 24 : (int)share;
+    wide.pps = wide_tiles > 0 ? tile_pps(wide_tiles, wide_pages) : 1;
+    Launches mine, other;
+    bool single = true;                        // one query token for each sequence
     for (int b = 0; b < batch; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
-        const int sp = a.splits(n, len);
-        const int64_t t = n == 0 ? 0 : (int64_t)a.tiles(n, len) * hkv;
-        items += t * sp;
-        if (sp > 1) merges += t, slots += t * sp;
-        plain = plain && n == 1 && sp == 1;
+        mine.add(a, n, len);
+        other.add(wide, n, len);
+        single = single && n == 1;
     }
-    const size_t need = slots > 0 ? align256((size_t)slots * slot_bytes(p->head_dim)) : 0;
-    st = check_ws(workspace_d, workspace_bytes, need);
+    // as many workgroups for each (sequence, head), some with nothing to do: nothing has to be looked up
+    if (single && (int64_t)batch * hkv * mine.most <= 2 * kTargetGroups) {
+        a.even = mine.most;
+        mine.items = (int64_t)batch * hkv * mine.most;
+        mine.merges = mine.most > 1 ? (int64_t)batch * hkv : 0;
+        mine.slots = mine.most > 1 ? mine.items : 0;
+    }
+    const size_t need = unit_bytes(p, mine.slots), wide_need = tile_bytes(p, other.slots);
+    st = check_ws(workspace_d, workspace_bytes, need + wide_need);
     if (st) return st;
-    if (items >= (1ll << 31)) return INFLLMV2_ERR_UNSUPPORTED;
-    a.c = cache::args(p, c);
-    a.q = (const char *)q_d;
-    a.out = (char *)out_d;
-    a.lse = lse_d;
-    a.cu = cu_q_d;
-    a.ctx = ctx_lens_d;
-    a.batch = batch;
-    a.hq = p->num_q_heads;
-    a.plain = plain;
-    a.scale = p->softmax_scale;
+    if (mine.items >= (1ll << 31) || other.items >= (1ll << 31)) return INFLLMV2_ERR_UNSUPPORTED;
+    for (AttnArgs *x : {&a, &wide}) {
+        x->c = cache::args(p, c);
+        x->q = (const char *)q_d;
+        x->out = (char *)out_d;
+        x->lse = lse_d;
+        x->cu = cu_q_d;
+        x->ctx = ctx_lens_d;
+        x->hq = p->num_q_heads;
+        x->scale = p->softmax_scale;
+    }
     a.part = (float *)workspace_d;
-    a.ml = a.part + slots * 16 * p->head_dim;
+    a.ml = a.part + mine.slots * 16 * p->head_dim;
+    wide.part = (float *)((char *)workspace_d + need);
+    wide.ml = wide.part + other.slots * 16 * wide.tile_groups * p->head_dim;
     const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
     const hipStream_t s = (hipStream_t)stream;
+    if (other.items > 0) {
+        st = cache_attn::launch_tile(wide, p, codes, other.items, s);
+        if (st) return st;
+        if (p->head_dim == 128) merge<bf16_t, 128>(wide, other.merges, s);
+        else merge<bf16_t, 64>(wide, other.merges, s);
+        if (mine.items == 0) return hip_status(hipGetLastError());
+    }
     // keys of a step: 64 codes, 32 bf16, 16 fp32 rows take the same registers
     if (p->head_dim == 128) {
-        if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 128, true, 4>(a, items, merges, s) : launch_t<bf16_t, 128, false, 2>(a, items, merges, s);
-        return codes ? launch_t<float, 128, true, 2>(a, items, merges, s) : launch_t<float, 128, false, 1>(a, items, merges, s);
+        if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 128, true, 4>(a, mine.items, mine.merges, s) : launch_t<bf16_t, 128, false, 2>(a, mine.items, mine.merges, s);
+        return codes ? launch_t<float, 128, true, 2>(a, mine.items, mine.merges, s) : launch_t<float, 128, false, 1>(a, mine.items, mine.merges, s);
     }
-    if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 64, true, 4>(a, items, merges, s) : launch_t<bf16_t, 64, false, 4>(a, items, merges, s);
-    return codes ? launch_t<float, 64, true, 2>(a, items, merges, s) : launch_t<float, 64, false, 2>(a, items, merges, s);
+    if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 64, true, 4>(a, mine.items, mine.merges, s) : launch_t<bf16_t, 64, false, 4>(a, mine.items, mine.merges, s);
+    return codes ? launch_t<float, 64, true, 2>(a, mine.items, mine.merges, s) : launch_t<float, 64, false, 2>(a, mine.items, mine.merges, s);
 }

@@ -100,8 +100,9 @@ def rows_of(cache, scale, table, b, n, h):
 
 
 def attention(q, k, v, scales, table, news, ctxs, softmax_scale, blocks=None, dense_below=0):
-    """(out [T, hq, d], lse [T, hq]) in float64: one softmax per token and head, over the keys that it sees"""
+    """(out [T, hq, d], lse [T, hq], sum of weights times |v| [T, hq, d]) in float64: one softmax per token and head, over the keys that it sees"""
     T, hq, d = q.shape
+    mass = torch.zeros((T, hq, d), dtype=torch.float64, device=q.device)
     hkv = k.shape[1]
     G = hq // hkv
     out = torch.zeros((T, hq, d), dtype=torch.float64, device=q.device)
@@ -128,6 +129,7 @@ def attention(q, k, v, scales, table, news, ctxs, softmax_scale, blocks=None, de
                 z = q[t0 + i, h * G:(h + 1) * G].double() @ K[u].T * softmax_scale
                 p = torch.softmax(z, -1)
                 out[t0 + i, h * G:(h + 1) * G] = p @ V[u]
+                mass[t0 + i, h * G:(h + 1) * G] = p @ V[u].abs()
                 lse[t0 + i, h * G:(h + 1) * G] = torch.logsumexp(z, -1)
         t0 += n
-    return out, lse
+    return out, lse, mass
