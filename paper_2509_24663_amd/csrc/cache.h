@@ -80,9 +80,11 @@ __device__ inline int find_item(int batch, int64_t item, int &rem, int64_t &befo
         if (lane == 0) { s_out[0] = seq; s_out[1] = r; s_out[2] = bef; }
     }
     __syncthreads();
-    rem = (int)s_out[1];
-    before = s_out[2];
-    return (int)s_out[0];
+    // (uniform values, for the compiler as well: what follows from them stays in scalar registers)
+    rem = __builtin_amdgcn_readfirstlane((int)s_out[1]);
+    before = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s_out[2] >> 32)) << 32) |
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)s_out[2]));
+    return __builtin_amdgcn_readfirstlane((int)s_out[0]);
 }
 
 }  // namespace cache

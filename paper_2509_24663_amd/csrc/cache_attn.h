@@ -42,8 +42,7 @@ struct AttnArgs {
     __host__ __device__ int most_splits(int n, int len) const { return n == 0 ? 0 : splits(len, len - 1); }
 };
 
-// the rules of cache_attn_tile.hip
-int tile_wide_from(const infllmv2_params *p);           // least queries of a sequence, INT32_MAX: never
+// cache_attn_tile.hip
 int tile_groups(const infllmv2_params *p);
 int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream);
 

@@ -10,6 +10,7 @@
 // in flight.  The work of a (tile, KV head) is split along the keys over workgroups, and over the four wavefronts of each; partial results are joined in
 // LDS, then by cache_merge_kernel.
 #include "cache_attn.h"
+#include "launch_rules.h"
 
 namespace ifv2 {
 
@@ -538,25 +539,13 @@ int launch_t(const AttnArgs &a, int64_t items, int64_t merges, hipStream_t strea
 
 constexpr int kTargetGroups = 2048;        // workgroups that a call is cut into: four rounds of two for each CU
 constexpr int kLeastPages = 2 * NW;        // two pages for each wavefront
-constexpr int kCus = 256;
-
-// Splits of the tile kernel, whose workgroups (one on a CU) go over the CUs in rounds: the number s that makes (rounds) x (pages of a split and what a
-// split costs beside them) least.  A split's partial result, written and read again, takes the time of kSplitCost pages.
-constexpr int kSplitCost = 12, kMostSplits = 16, kMostTileSlots = 1024;
-int tile_pps(int64_t tiles, int most_pages) {
-    int64_t best = INT64_MAX;
-    int pps = most_pages;
-    for (int s = 1; s <= kMostSplits && s <= most_pages && (s == 1 || tiles * s <= kMostTileSlots); ++s) {
-        const int per = (most_pages + s - 1) / s;
-        const int64_t cost = (tiles * s + kCus - 1) / kCus * (per + (s > 1 ? kSplitCost : 0));
-        if (cost < best) best = cost, pps = per;
-    }
-    return pps;
-}
-
 // Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
 // kTargetGroups, so at most 2 kTargetGroups partial results.
 size_t slot_bytes(int d, int groups) { return (size_t)16 * groups * (d + 2) * sizeof(float); }
+// Least queries of a sequence for which the tile kernel is thought of (bf16 data)
+int tile_from(const infllmv2_params *p) {
+    return p->dtype == INFLLMV2_BF16 ? (rules::kTileFrom - 1) * (kCols / (p->num_q_heads / p->num_kv_heads)) + 1 : INT32_MAX;
+}
 size_t unit_bytes(const infllmv2_params *p, int64_t slots) { return align256((size_t)slots * slot_bytes(p->head_dim, 1)); }
 size_t tile_bytes(const infllmv2_params *p, int64_t slots) { return align256((size_t)slots * slot_bytes(p->head_dim, cache_attn::tile_groups(p))); }
 
@@ -581,12 +570,12 @@ size_t cache_attn_ws_bound(const infllmv2_params *p, int32_t batch, int64_t toke
     const int64_t units = tokens * p->num_kv_heads;
     const int64_t slots = per <= 1 ? 0 : units < 2 * kTargetGroups && units * per < 2 * kTargetGroups ? units * per : 2 * kTargetGroups;
     // the tile kernel: at most tokens / (tokens of a tile) tiles and one more for each sequence
-    const int64_t from = cache_attn::tile_wide_from(p);
+    const int64_t from = tile_from(p);
     int64_t tiles = 0;
     if (tokens >= from && most > 1) {
         const int64_t per_tile = kCols / (p->num_q_heads / p->num_kv_heads) * cache_attn::tile_groups(p), seqs = tokens / from < batch ? tokens / from : batch;
-        tiles = (tokens / per_tile + seqs) * p->num_kv_heads * (most < kMostSplits ? most : kMostSplits);
-        if (tiles > kMostTileSlots) tiles = kMostTileSlots;
+        tiles = (tokens / per_tile + seqs) * p->num_kv_heads * (most < rules::kMostTileSplits ? most : rules::kMostTileSplits);
+        if (tiles > rules::kMostTileResults) tiles = rules::kMostTileResults;
     }
     return unit_bytes(p, slots) + tile_bytes(p, tiles);
 }
@@ -614,23 +603,32 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     a.topk = p->topk_total;
     a.dense_below = p->dense_threshold;
     a.group_tokens = kCols / (p->num_q_heads / hkv);
-    a.wide_from = cache_attn::tile_wide_from(p);
+    a.wide_from = tile_from(p);
     a.tile_groups = 1;
     AttnArgs wide = a;                         // the tile kernel's launch
     wide.tile_groups = cache_attn::tile_groups(p);
     int max_ctx = 0, wide_pages = 0;
-    int64_t work = 0, wide_tiles = 0;          // pages over all tiles and heads of cache_attn.hip, tiles and heads of the other
+    int64_t work = 0, wide_work = 0, wide_tiles = 0;       // pages over column groups (or listed tokens) and heads of each kernel's sequences; tiles and heads
     for (int b = 0; b < batch; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
         if (len < n || len > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
         if (n == 0) continue;
         if (len > max_ctx) max_ctx = len;
-        const int64_t mine = (int64_t)a.tiles(n, len) * hkv, other = (int64_t)wide.tiles(n, len) * hkv;
         const int pages = a.pages(len, len - 1);
-        work += mine * pages;
+        const int64_t other = (int64_t)wide.tiles(n, len) * hkv;
+        const int64_t groups = (int64_t)((n + a.tile_tokens(len) - 1) / a.tile_tokens(len)) * hkv * pages;
+        (other > 0 ? wide_work : work) += groups;
         wide_tiles += other;
         if (other > 0 && pages > wide_pages) wide_pages = pages;
-        if (mine > 0 && n > 1 && a.tile_tokens(len) > 1) a.multi = 1;
+    }
+    if (!rules::tile_pays(wide_tiles, wide_pages, wide_work)) {
+        a.wide_from = wide.wide_from = INT32_MAX;
+        work += wide_work;
+        wide_tiles = 0;
+    }
+    for (int b = 0; b < batch && !a.multi; ++b) {
+        const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
+        a.multi = n > 1 && a.tiles(n, len) > 0 && a.tile_tokens(len) > 1;
     }
     st = cache::check(p, c, max_ctx, true);
     if (st) return st;
@@ -638,7 +636,7 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     if (c->tok_stride > (1ll << 24)) return INFLLMV2_ERR_UNSUPPORTED;
     const int64_t share = (work + kTargetGroups - 1) / kTargetGroups;
     a.pps = share < kLeastPages ? kLeastPages : share > (1 << 24) ? 1 << 24 : (int)share;
-    wide.pps = wide_tiles > 0 ? tile_pps(wide_tiles, wide_pages) : 1;
+    wide.pps = wide_tiles > 0 ? rules::tile_splits(wide_tiles, wide_pages).pps : 1;
     Launches mine, other;
     bool single = true;                        // one query token for each sequence
     for (int b = 0; b < batch; ++b) {

@@ -1,14 +1,23 @@
 // Attention of a chunk of a prompt over its paged cache, bf16 data: tiles of 8 x CG groups of 16 columns (a column is a token and a head of one KV head).
 //
-// The workgroup's eight wavefronts go through the pages together and each keeps CG column groups (CG = 3, head dim 64: 4) with their queries and sums in
-// registers, so that an operand read from LDS feeds CG products; the other way round (one group per wavefront) LDS reads bound the kernel at half the
-// matrix cores' rate.  S^T = K Q^T and O^T += V^T P^T on 16x16x32 products; a lane's logits of a half page are eight consecutive keys of one
-// column, which is the operand that the second product wants.
-// A page is requested while the one before it is worked on: half of the wavefronts hold its K, half its V, in registers, widen them (codes times
-// the page's scale: exact in bf16) and write them to the other of two LDS buffers, V transposed: a thread holds 8 keys of 4 channels, so it
-// writes whole 16-byte operand pieces.  One barrier per page.
-// Rounding: weights go into the second product as bf16 (2^-9 of each, as the output's own rounding); their sum takes them as they are.  References move only
-// where eight weights of a lane add up to more than kSlack, so a weight is below it.
+// The workgroup's eight wavefronts go through the pages together and each keeps CG column groups (CG = 2; head dim 64: 4) with their queries and sums in
+// registers, so that an operand read from LDS feeds CG products.  S^T = K Q^T and O^T += V^T P^T on 16x16x32 products; a lane's logits of a
+// half page are eight consecutive keys of one column, which is the operand that the second product wants.
+// Half a page is a step: its logits, then the sums of the half before it with the weights of this one between the products (they do not depend on
+// each other: the vector unit works while the matrix core does).  A page is requested two pages ahead: K rows into registers, V rows (asynchronously) into a
+// buffer of the wavefront's own, from where transposing reads give a lane eight keys of a channel.  Beside the products of a first half they are widened
+// (codes times the page's scale: exact in bf16) and written as bf16 K and V^T pages, two and three buffers: one barrier per page.
+// Rounding: weights go into the second product as bf16 (2^-9 of each at most, like the output's own rounding); their sum takes them as they are.  References
+// move only where eight weights of a lane add up to more than kSlack, so a weight is below it.
+//
+// What bounds it: LDS and the matrix cores together.  2048 tokens over 34816, 32 heads on 2, e4m3: 966 to 996 us, 1130 to 1170 TFLOP/s (a large library
+// product reaches 1212 on this card); without LDS reads 786, without the rows' way through LDS 822, products and weights alone 656, products
+// alone 591.  Steps on the way: rows through registers by role and phases in lockstep 1208; queries waited for in front of the loop (their wait stood in
+// it and waited for the pages) 1102; the rows' work between the products 1043; the step of this form 1017; V through LDS with transposing reads 985; the second four
+// wavefronts ahead in first halves 966.  Measured and not taken: CG = 3 (two thirds of the LDS reads: 1013; fewer, larger tiles leave
+// CUs idle), the wavefronts of a SIMD taking turns behind barriers (1043), operands eight ahead (994).
+#include <type_traits>
+
 #include "attn_unit.h"
 #include "cache_attn.h"
 
@@ -25,7 +34,8 @@ using cache_attn::kLowest;
 constexpr int NW = 8;
 constexpr int kThreads = NW * 64;
 constexpr float kSlack = 64.f, kNoReference = -1e38f;
-constexpr int groups_of(int d) { return d == 128 ? 3 : 4; }
+constexpr int groups_of(int d) { return d == 128 ? 2 : 4; }
+constexpr int kAhead = 4;                  // operands requested in front of their product
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <bool UPPER>
@@ -59,20 +69,20 @@ __device__ inline void lds_write16(uint32_t at, u32x4 x) {
 // of K, 16 consecutive rows of V^T, one logical chunk) and the lanes of a write take different positions.
 template <int D>
 struct Page {
-    static constexpr uint32_t kKBytes = 64 * D * 2, kBytes = 2 * kKBytes;
+    static constexpr uint32_t kBytes = 64 * D * 2;                // of K or of V
     static __device__ inline uint32_t k_swizzle(int row) {
         return D == 128 ? 4 * ((row >> 3) & 3) + (row & 3) : 2 * ((row >> 3) & 3) + ((row >> 1) & 1);
     }
     static __device__ inline uint32_t v_swizzle(int ch) { return ((ch >> 1) & 7) ^ ((ch >> 4) & 1); }
     static __device__ inline uint32_t k_at(int row, int chunk) { return (uint32_t)row * (2 * D) + ((chunk ^ k_swizzle(row)) << 4); }
-    static __device__ inline uint32_t v_at(int ch, int octet) { return kKBytes + (uint32_t)ch * 128 + ((octet ^ v_swizzle(ch)) << 4); }
+    static __device__ inline uint32_t v_at(int ch, int octet) { return (uint32_t)ch * 128 + ((octet ^ v_swizzle(ch)) << 4); }
 };
 
-template <int D, int CG, bool CODES>
+template <int D, int CG, int W, bool CODES>
 __global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a) {
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int KB = CODES ? 1 : 2;                               // bytes of an element
-    extern __shared__ __attribute__((aligned(1024))) char smem[];   // two pages
+    extern __shared__ __attribute__((aligned(1024))) char smem[];   // two K pages, three V pages, rows of V as they come
     __shared__ int64_t s_item[3];
     __shared__ int s_odd;                                           // a value of a page's edge (see write) is not finite
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -112,8 +122,12 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8_u *>(q + 32 * s + 8 * g));
     }
-    const int wave_first = w * CG * GT;                             // tokens of this wavefront: from here ..
-    const int wave_last = min(wave_first + CG * GT, ntok) - 1;      // .. to here (none: last < first)
+    // (the queries have landed here: left to the first product, the wait for them stands in the loop and waits for the pages requested ahead as well)
+#pragma unroll
+    for (int x = 0; x < CG; ++x)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[x][s]));
+    const int wave_first = w * CG * GT;                             // first token of this wavefront
     const float c = a.scale * kLog2e;
 
     f32x4 acc[CG][DT];
@@ -129,182 +143,274 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a
     const uint32_t lds = __builtin_amdgcn_readfirstlane(attn_unit::lds_address(smem));
     const uint32_t k_lane = Page<D>::k_at(8 * (m >> 2) + (m & 3), g), v_lane = Page<D>::v_at(m, g);
     const uint32_t tok = (uint32_t)a.c.tok_stride;
-    // what this thread brings of a page: threads 0..255 a quarter of a K row, the next 2 D eight keys of four channels of V
-    const bool is_k = w < 4, is_v = tid >= 256 && tid < 256 + 2 * D;
-    const int k_row = tid >> 2, quarter = tid & 3, vid = tid - 256, octet = vid / (D / 4), ch0 = vid % (D / 4) * 4;
-    const uint32_t from = is_k ? k_row * tok + quarter * (D / 4 * KB) : 8 * octet * tok + ch0 * KB;
-    constexpr int KW = D / 4 * KB / 16, VW = KB;
-    uint32_t raw[4 * KW > 8 * VW ? 4 * KW : 8 * VW];
-    auto bring = [&](int page) {
-        const char *base = (is_k ? a.c.k : a.c.v) + a.c.at(page, h);
-        if (is_k) {
+    // What a wavefront brings of a page: eight rows of K (a lane an eighth of one, through registers) and of V (copied to an LDS buffer of its own, from where
+    // transposing reads give a lane the eight keys of a channel).
+    constexpr int CV = D / 64, KP = D / 64;                         // channels of V; 16-byte pieces of K in LDS
+    constexpr int KL = D / 8 * KB > 16 ? 2 : 1, KW = D / 8 * KB / KL / 4;            // requests for K, words of one
+    constexpr int VL = 8 * D * KB > 1024 ? 2 : 1, VW = 2 * KB;      // copies of V, words of eight keys
+    constexpr uint32_t kRawBytes = 8 * D * KB;                      // of V
+    const int k_row = tid >> 3, eighth = tid & 7;
+    const uint32_t k_from = k_row * tok + eighth * (D / 8 * KB);
+    const uint32_t k_to_lane = Page<D>::k_at(k_row, eighth * KP), v_to_lane = Page<D>::v_at(lane, w);
+    constexpr int RL = D * KB / 16;                                 // lanes of a V row
+    const uint32_t v_from = (8 * w + lane / RL) * tok + lane % RL * 16;
+    const uint32_t raw_at = lds + 5 * Page<D>::kBytes + w * kRawBytes;
+    // (codes: lane 2 r + c of a group of sixteen points at half c of row r's sixteen bytes; bf16: lane 4 r + c at quarter c of row r's 32 bytes)
+    const uint32_t raw_lane = raw_at + (CODES ? (m >> 1) * (D * KB) + g * 16 + (m & 1) * 8 : (m >> 2) * (D * KB) + g * 32 + (m & 3) * 8);
+    uint32_t raw_k[KL * KW], raw_v[CV][VW];
+    struct Where {                                                  // a page: offset of its rows, first key, scales
+        int64_t at;
+        int key0;
+        float ks, vs;
+    };
+    auto request = [&](int i, const Where &p) {                     // i < KL + VL
+        if (i < KL) {
+            typedef uint32_t Words __attribute__((ext_vector_type(KW)));
+            const Words x = *reinterpret_cast<const Words *>(a.c.k + p.at + k_from + 16 * i);
 #pragma unroll
-            for (int i = 0; i < KW; ++i) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(base + from + 16 * i);
+            for (int e = 0; e < KW; ++e) raw_k[KW * i + e] = x[e];
+        } else if (RL * 8 >= 64 || lane < RL * 8) {
+            attn_unit::async_copy16(a.c.v + p.at + (int64_t)((i - KL) * (64 / RL)) * tok, v_from, raw_at + (i - KL) * 1024);
+        }
+    };
+    // The rows that were requested are here: V from the wavefront's buffer.
+    auto collect = [&]() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-                for (int e = 0; e < 4; ++e) raw[4 * i + e] = x[e];
-            }
-        } else if (is_v) {
+        for (int q = 0; q < CV; ++q) {
+            if constexpr (CODES) {
+                typedef int Two __attribute__((ext_vector_type(2)));
+                typedef __attribute__((address_space(3))) Two lds_two;
+                const Two x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_two *)(uintptr_t)(raw_lane + 64 * q));
+                raw_v[q][0] = x[0], raw_v[q][1] = x[1];
+            } else {
+                typedef short Four __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) Four lds_four;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (CODES) {
-                    raw[i] = *reinterpret_cast<const uint32_t *>(base + from + i * tok);
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2 *>(base + from + i * tok);
-                    raw[2 * i] = x.x, raw[2 * i + 1] = x.y;
+                for (int k = 0; k < 2; ++k) {
+                    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_four *)(uintptr_t)(raw_lane + 128 * q + 4 * k * D * KB)));
+                    raw_v[q][2 * k] = x.x, raw_v[q][2 * k + 1] = x.y;
                 }
             }
         }
     };
-    auto write = [&](int buf, int key0, float scale) {
-        const uint32_t at = lds + buf * Page<D>::kBytes;
-        if (is_k) {
+    auto clean = [&](int key0) {                                    // a page of which not all is visible to all tokens of the tile
+        uint32_t odd = 0;
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {                      // 8 channels at a time
-                u32x4 x;
-                if constexpr (CODES) x = u32x4{widen<false>(raw[2 * i], scale), widen<true>(raw[2 * i], scale), widen<false>(raw[2 * i + 1], scale), widen<true>(raw[2 * i + 1], scale)};
-                else x = u32x4{raw[4 * i], raw[4 * i + 1], raw[4 * i + 2], raw[4 * i + 3]};
-                lds_write16(at + Page<D>::k_at(k_row, quarter * (D / 32) + i), x);
+        for (int q = 0; q < CV; ++q)
+#pragma unroll
+            for (int k = 0; k < VW; ++k) {
+                constexpr int PER = 4 / KB;                         // keys of a word
+                const int seen = pos_last + 1 - (key0 + 8 * w + PER * k);            // .. that some token sees
+                const uint32_t keep = seen >= PER ? ~0u : seen <= 0 ? 0u : (1u << (8 * KB * seen)) - 1u;
+                const uint32_t o = not_finite<CODES>(raw_v[q][k]);
+                odd |= o & keep;
+                raw_v[q][k] &= ~o & keep;
             }
-        } else if (is_v) {
-            if (key0 + kBlock - 1 > pos0) {                         // a page of which not all is visible to all tokens of the tile
-                uint32_t odd = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int e = 0; e < VW; ++e) {
-                        uint32_t &x = raw[VW * i + e];
-                        const uint32_t o = not_finite<CODES>(x);
-                        const bool any_sees = key0 + 8 * octet + i <= pos_last;
-                        odd |= any_sees ? o : 0u;
-                        x = any_sees ? x & ~o : 0u;
-                    }
-                if (odd != 0) s_odd = 1;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u32x4 x;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if constexpr (CODES) {
-                        const uint32_t two = __builtin_amdgcn_perm(raw[2 * k + 1], raw[2 * k], j < 2 ? 0x05010400u : 0x07030602u);
-                        x[k] = j & 1 ? widen<true>(two, scale) : widen<false>(two, scale);
-                    } else {
-                        const uint32_t lo = raw[4 * k + j / 2], hi = raw[4 * k + 2 + j / 2];
-                        x[k] = j & 1 ? upper_halves(lo, hi) : lower_halves(lo, hi);
-                    }
-                }
-                lds_write16(at + Page<D>::v_at(ch0 + j, octet), x);
-            }
+        if (odd != 0) s_odd = 1;
+    };
+    auto write = [&](int i, uint32_t k_to, uint32_t v_to, float ks, float vs) {      // i < KP + CV
+        u32x4 x;
+        if (i < KP) {                                               // 8 channels of a row
+            if constexpr (CODES) x = u32x4{widen<false>(raw_k[2 * i], ks), widen<true>(raw_k[2 * i], ks), widen<false>(raw_k[2 * i + 1], ks), widen<true>(raw_k[2 * i + 1], ks)};
+            else x = u32x4{raw_k[4 * i], raw_k[4 * i + 1], raw_k[4 * i + 2], raw_k[4 * i + 3]};
+            lds_write16((k_to + k_to_lane) ^ (16u * i), x);         // (KP = 2: the lower bit of the piece's number)
+        } else {                                                    // 8 keys of channel 64 q + lane
+            const int q = i - KP;
+            if constexpr (CODES) x = u32x4{widen<false>(raw_v[q][0], vs), widen<true>(raw_v[q][0], vs), widen<false>(raw_v[q][1], vs), widen<true>(raw_v[q][1], vs)};
+            else x = u32x4{raw_v[q][0], raw_v[q][1], raw_v[q][2], raw_v[q][3]};
+            lds_write16(v_to + v_to_lane + 8192u * q, x);           // (64 rows on: one swizzle)
         }
     };
 
     // the pages of the split: lane l holds the l-th of the next 64
     const int e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
-    int e0 = split * a.pps, list_page, list_key0 = 0;
-    float list_scale = 1.f;
+    int e0 = split * a.pps, list_key0 = 0;
+    int64_t list_at = 0;
+    float list_ks = 1.f, list_vs = 1.f;
     uint64_t there = 0;
-    auto next = [&](int &page, int &key0, float &scale) -> bool {   // the next page that is there
-        while (there == 0) {
-            if (e0 >= e_end) return false;
-            const int j = e0 + lane;
-            list_page = j < e_end ? a.c.page(seq, j) : -1;
+    auto refill = [&]() {
+        while (there == 0 && e0 < e_end) {
+            const int j = e0 + lane, page = j < e_end ? a.c.page(seq, j) : -1;
+            list_at = a.c.at(page, h);
             list_key0 = j * kBlock;
-            if (CODES && list_page >= 0) list_scale = (is_k ? a.c.ks : a.c.vs)[(int64_t)list_page * hkv + h];
-            there = __ballot(list_page >= 0);
+            if (CODES && page >= 0) {
+                list_ks = a.c.ks[(int64_t)page * hkv + h];
+                list_vs = a.c.vs[(int64_t)page * hkv + h];
+            }
+            there = __ballot(page >= 0);
             e0 += 64;
         }
+    };
+    auto next = [&](Where &p) {                                     // the next page of the list, which is not empty
         const int l = __ffsll((long long)there) - 1;
         there &= there - 1;
-        page = __builtin_amdgcn_readlane(list_page, l);
-        key0 = __builtin_amdgcn_readlane(list_key0, l);
-        scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list_scale), l));
-        return true;
+        p.at = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(list_at >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)list_at, l));
+        p.key0 = __builtin_amdgcn_readlane(list_key0, l);
+        p.ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list_ks), l));
+        p.vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list_vs), l));
     };
-    int page, key0 = 0, next_key0 = 0, low = INT32_MAX;
-    float scale = 1.f;
-    bool here = next(page, key0, scale), more = false;
     if (tid == 0) s_odd = 0;
-    if (here) {
-        bring(page);
-        __syncthreads();                                            // (s_odd)
-        write(0, key0, scale);
-        more = next(page, next_key0, scale);
-        if (more) bring(page);
-        low = key0;
-        __syncthreads();
-    }
-    for (int buf = 0; here; buf ^= 1) {
-        const bool edge = key0 + kBlock - 1 > pos0;
-        if (wave_first <= wave_last && key0 <= pos0 + wave_last) {
-            const uint32_t kp = lds + buf * Page<D>::kBytes + k_lane, vp = lds + buf * Page<D>::kBytes + v_lane;
+
+    // The walk, in steps of half a page k (32 keys): logits of k; then sums of the weights of k - 1 and, between those products, the weights of k.
+    constexpr int LOGITS = 8 * CG, KF = 2 * KS;                     // logits of a lane, K operands of a step
+    f32x4 s[CG][2];
+    uint32_t pb[2][CG][4];                                          // by the parity of k
+    bf16x8 f[W];                                                    // operands, requested W ahead: KF of K, then DT of V^T
+    static_assert((KF + DT) % W == 0, "an operand's place does not depend on the step");
+    const uint32_t k_at = lds + k_lane, v_at = lds + 2 * Page<D>::kBytes + v_lane;
+    auto k_half = [&](int p2, int hb) { return k_at + p2 * Page<D>::kBytes + hb * (32 * 2 * D); };
+    auto v_half = [&](int p3, int hb) { return (v_at + p3 * Page<D>::kBytes) ^ (uint32_t)(64 * hb); };
+    auto fetch_k = [&](int j, uint32_t kb) { f[j % W] = lds_read16((kb ^ (uint32_t)(64 * (j % KS))) + (uint32_t)(4 * (j / KS) * 2 * D)); };
+    auto fetch_v = [&](int j, uint32_t vb) { f[(KF + j) % W] = lds_read16((vb ^ (uint32_t)(16 * (j & 1))) + (uint32_t)(2048 * j)); };
+    auto sums = [&](int j, const uint32_t (&w)[CG][4]) {
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb) {
-                f32x4 s[CG][2];
+        for (int x = 0; x < CG; ++x) {
+            const bf16x8 wt = __builtin_bit_cast(bf16x8, (u32x4){w[x][0], w[x][1], w[x][2], w[x][3]});
+            acc[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[(KF + j) % W], wt, acc[x][j], 0, 0, 0);
+        }
+    };
+    // kb: K of k; vb: V of k - 1; kb_on: K of k + 1 where it is there already (ON); beside(j): what else is issued at K operand j
+    auto step = [&](auto parity, auto on, int first_key, uint32_t kb, uint32_t vb, uint32_t kb_on, auto beside) {
+        constexpr int P = decltype(parity)::value;
+        constexpr bool ON = decltype(on)::value;
+#pragma unroll
+        for (int j = 0; j < KF; ++j) {
+            const int kt = j / KS, ks = j % KS;
+#pragma unroll
+            for (int x = 0; x < CG; ++x)
+                s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j % W], qf[x][ks], ks ? s[x][kt] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            if (j + W < KF) fetch_k(j + W, kb);
+            else fetch_v(j + W - KF, vb);
+            beside(j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (first_key + 31 > pos0 + wave_first) {                   // keys behind a token
+#pragma unroll
+            for (int x = 0; x < CG; ++x) {
+                const int lim = used[x] ? pos0 + ti[x] - (first_key + 8 * g) : -1;
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        const bf16x8 f = lds_read16((kp ^ (uint32_t)(64 * ks)) + (uint32_t)((32 * hb + 4 * kt) * 2 * D));
+                    for (int r = 0; r < 4; ++r) s[x][kt][r] = 4 * kt + r <= lim ? s[x][kt][r] : -INFINITY;
+            }
+        }
+        float part[CG], last = 0.f;
 #pragma unroll
-                        for (int x = 0; x < CG; ++x)
-                            s[x][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, qf[x][ks], ks ? s[x][kt] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                    }
-                if (edge) {
+        for (int j = 0; j < DT; ++j) {
+            sums(j, pb[1 - P]);
+            if (j + W < DT) fetch_v(j + W, vb);
+            else if (ON) fetch_k(j + W - DT, kb_on);
 #pragma unroll
-                    for (int x = 0; x < CG; ++x) {
-                        const int lim = used[x] ? pos0 + ti[x] - (key0 + 32 * hb + 8 * g) : -1;
+            for (int n = j * LOGITS / DT; n < (j + 1) * LOGITS / DT; ++n) {
+                const int x = n / 8, i = n % 8;
+                const float p = exp2_fast(__builtin_fmaf(s[x][i >> 2][i & 3], c, -ref[x]));
+                part[x] = i ? part[x] + p : p;
+                asm volatile("" : "+v"(part[x]));                   // (added here: left alone, all weights are kept to the end of the step)
+                if (i & 1) pb[P][x][i >> 1] = pack(last, p);
+                last = p;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // references move where weights are large: the sums so far are those of k - 1, the weights are formed again
+        float largest = part[0];
 #pragma unroll
-                        for (int kt = 0; kt < 2; ++kt)
+        for (int x = 1; x < CG; ++x) largest = fmaxf(largest, part[x]);
+        if (__any(largest > kSlack)) {
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) s[x][kt][r] = 4 * kt + r <= lim ? s[x][kt][r] : -INFINITY;
-                    }
-                }
-                bf16x8 pb[CG];
+            for (int x = 0; x < CG; ++x) {
+                float mx = s[x][0][0];
 #pragma unroll
-                for (int x = 0; x < CG; ++x) {
-                    float p[8], part = 0.f;
+                for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[x][i >> 2][i & 3]);
+                const float to = fmaxf(ref[x], rows_max(mx) * c), down = exp2_fast(ref[x] - to);
+                ref[x] = to;
+                sum[x] *= down;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        p[i] = exp2_fast(__builtin_fmaf(s[x][i >> 2][i & 3], c, -ref[x]));
-                        part += p[i];
-                    }
-                    if (__any(part > kSlack)) {
-                        float mx = s[x][0][0];
+                for (int i = 0; i < DT; ++i) acc[x][i] *= down;
+                part[x] = 0.f;
 #pragma unroll
-                        for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[x][i >> 2][i & 3]);
-                        const float to = fmaxf(ref[x], rows_max(mx) * c), f = exp2_fast(ref[x] - to);
-                        ref[x] = to;
-                        sum[x] *= f;
-#pragma unroll
-                        for (int i = 0; i < DT; ++i) acc[x][i] *= f;
-                        part = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            p[i] = exp2_fast(__builtin_fmaf(s[x][i >> 2][i & 3], c, -to));
-                            part += p[i];
-                        }
-                    }
-                    sum[x] += part;
-                    pb[x] = __builtin_bit_cast(bf16x8, (u32x4){pack(p[0], p[1]), pack(p[2], p[3]), pack(p[4], p[5]), pack(p[6], p[7])});
-                }
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    const bf16x8 f = lds_read16((vp ^ (uint32_t)(64 * hb) ^ (uint32_t)(16 * (i & 1))) + (uint32_t)(2048 * i));
-#pragma unroll
-                    for (int x = 0; x < CG; ++x) acc[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pb[x], acc[x][i], 0, 0, 0);
+                for (int i = 0; i < 8; ++i) {
+                    const float p = exp2_fast(__builtin_fmaf(s[x][i >> 2][i & 3], c, -to));
+                    part[x] += p;
+                    if (i & 1) pb[P][x][i >> 1] = pack(last, p);
+                    last = p;
                 }
             }
         }
-        here = more;
-        if (more) {
-            key0 = next_key0;
-            low = min(low, key0);
-            write(buf ^ 1, key0, scale);
-            more = next(page, next_key0, scale);
-            if (more) bring(page);
+#pragma unroll
+        for (int x = 0; x < CG; ++x) sum[x] += part[x];
+    };
+    constexpr int PIECES = KP + CV + KL + VL, PER_STEP = (PIECES + KF - 1) / KF;
+
+    // Between two barriers K and V of page p and V of p - 1 are read, K and V of p + 1 written to the other buffers (two of K, three of V) from the registers
+    // that hold them, and p + 2 is requested.
+    Where now{}, then{}, after{};                                   // pages p, p + 1, p + 2 (those that are not there repeat the last)
+    refill();
+    const bool here = there != 0;
+    int low = INT32_MAX;
+    if (here) {
+        next(now);
+        low = now.key0;
+        refill();
+        then = now;
+        bool more = there != 0;                                     // p + 1 is there
+        if (more) next(then);
+#pragma unroll
+        for (int i = 0; i < KL + VL; ++i) request(i, now);
+        // V of "page -1", for the sums of the weights 0 in front of the first: zeros
+        for (uint32_t at = 16 * tid; at < Page<D>::kBytes; at += 16 * kThreads) lds_write16(lds + 4 * Page<D>::kBytes + at, u32x4{0, 0, 0, 0});
+        __syncthreads();                                            // (s_odd)
+        collect();
+        if (now.key0 + kBlock - 1 > pos0) clean(now.key0);
+#pragma unroll
+        for (int i = 0; i < KP + CV; ++i) write(i, lds, lds + 2 * Page<D>::kBytes, now.ks, now.vs);
+#pragma unroll
+        for (int i = 0; i < KL + VL; ++i) request(i, then);
+#pragma unroll
+        for (int x = 0; x < CG; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pb[1][x][i] = 0u;
+        int p2 = 0, p3 = 0, before = 2;                             // buffers of page p (K, V) and of V of p - 1
+        for (;;) {
+            collect();
+            refill();
+            after = then;
+            const bool most = there != 0;
+            if (most) next(after);
+            const int ahead3 = p3 == 2 ? 0 : p3 + 1;
+            if (then.key0 + kBlock - 1 > pos0) clean(then.key0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (what this wavefront wrote)
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int j = 0; j < W; ++j) fetch_k(j, k_half(p2, 0));
+            if (w >= 4) __builtin_amdgcn_s_setprio(1);              // (of two wavefronts of a SIMD the older wins otherwise, and waits at the barrier)
+            const uint32_t k_to = lds + (p2 ^ 1) * Page<D>::kBytes, v_to = lds + (2 + ahead3) * Page<D>::kBytes;
+            step(std::integral_constant<int, 0>(), std::true_type(), now.key0, k_half(p2, 0), v_half(before, 1), k_half(p2, 1), [&](int j) {
+#pragma unroll
+                for (int i = j * PER_STEP; i < (j + 1) * PER_STEP && i < PIECES; ++i) {
+                    if (i < KP + CV) write(i, k_to, v_to, then.ks, then.vs);
+                    else request(i - KP - CV, after);
+                }
+            });
+            __builtin_amdgcn_s_setprio(0);
+            step(std::integral_constant<int, 1>(), std::false_type(), now.key0 + 32, k_half(p2, 1), v_half(p3, 0), 0, [](int) {});
+            before = p3;
+            p3 = ahead3;
+            p2 ^= 1;
+            if (!more) break;
+            now = then;
+            then = after;
+            more = most;
         }
-        __syncthreads();
+        // sums of the last half
+#pragma unroll
+        for (int j = 0; j < DT; ++j) {
+            fetch_v(j, v_half(before, 1));
+            sums(j, pb[1]);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (no copy is under way into LDS that this workgroup gives back)
+        __syncthreads();                                            // (s_odd)
     }
 
 #pragma unroll
@@ -374,8 +480,8 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a
 
 template <int D, bool CODES>
 int launch_d(const AttnArgs &a, int64_t items, hipStream_t stream) {
-    constexpr int CG = groups_of(D), LDS = 2 * Page<D>::kBytes;
-    const auto kernel = cache_attn_tile_kernel<D, CG, CODES>;
+    constexpr int CG = groups_of(D), LDS = 5 * Page<D>::kBytes + 64 * D * (CODES ? 1 : 2);
+    const auto kernel = cache_attn_tile_kernel<D, CG, kAhead, CODES>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
         return INFLLMV2_ERR_HIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(kThreads), LDS, stream, a);
@@ -387,12 +493,6 @@ int launch_d(const AttnArgs &a, int64_t items, hipStream_t stream) {
 namespace cache_attn {
 
 int tile_groups(const infllmv2_params *p) { return NW * groups_of(p->head_dim); }
-
-// From half a tile of column groups on.
-int tile_wide_from(const infllmv2_params *p) {
-    if (p->dtype != INFLLMV2_BF16) return INT32_MAX;
-    return (kCols / (p->num_q_heads / p->num_kv_heads)) * tile_groups(p) / 2;
-}
 
 int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream) {
     if (p->head_dim == 128) return codes ? launch_d<128, true>(a, items, stream) : launch_d<128, false>(a, items, stream);

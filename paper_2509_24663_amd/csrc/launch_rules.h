@@ -381,5 +381,31 @@ inline DecodeSplits decode_splits(int64_t pairs, int entries, int waves) {
     return {(int)bpw, (int)std::max<int64_t>((entries + bpw - 1) / bpw, 1)};
 }
 
+// Paged cache, chunks of prompts: splits along the keys of the tile kernel (cache_attn_tile.hip), whose workgroups go over the 256 CUs in rounds, one on a
+// CU; `pages`: of the longest tile.  A page takes 1.85 us, a workgroup 3 us before and after its pages, a call 9; several splits cost a
+// launch of 4 us and 0.05 us for each partial result (128 KB written and read).  Measured (G 16, d 128, 33000 cached tokens), 2 / 16 / 130 / 512 / 2048 tokens:
+// see the table at tile_pays.
+constexpr int kMostTileSplits = 64, kMostTileResults = 1024;
+struct TileSplits {
+    int pps;               // pages of a split
+    double us;             // what the launch is taken to cost
+};
+inline TileSplits tile_splits(int64_t tiles, int pages) {
+    TileSplits best{pages, 0};
+    for (int s = 1; s <= kMostTileSplits && s <= pages && (s == 1 || tiles * s <= kMostTileResults); ++s) {
+        const int per = (pages + s - 1) / s;
+        const double us = 9 + (double)((tiles * s + 255) / 256) * (1.85 * per + 3) + (s > 1 ? 4 + 0.05 * tiles * s : 0);
+        if (s == 1 || us < best.us) best = {per, us};
+    }
+    return best;
+}
+// Whether the tile kernel pays for sequences with at least kTileFrom column groups (16 columns) of queries, against the kernel of 16 columns: group_pages is
+// what that one goes through, pages over all column groups and KV heads; 3.5 ns each while they fill the chip a few times, 1.4 once rows come from the L2.
+constexpr int kTileFrom = 4;
+inline bool tile_pays(int64_t tiles, int pages, int64_t group_pages) {
+    const double few = group_pages < 20000 ? (double)group_pages : 20000.;
+    return tiles > 0 && tile_splits(tiles, pages).us < 12 + 3.5e-3 * few + 1.4e-3 * (group_pages - few);
+}
+
 }  // namespace rules
 }  // namespace ifv2
