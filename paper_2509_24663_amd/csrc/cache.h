@@ -35,24 +35,26 @@ __device__ inline float scale_for(float top) {
 }
 __device__ inline float reciprocal_of_power(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
 
-// two values, in units of the scale, as two codes (nearest, ties to even; saturating; NaN and infinities as NaN)
+// a value in units of the scale as a code: nearest, ties to even; saturating; NaN and infinities as NaN
 __device__ inline uint32_t code(float x) {
     return fabsf(x) <= 3.4028234e38f ? (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fminf(fmaxf(x, -kTop), kTop), 0.f, 0, false) & 0xffu : 0x7fu;
 }
-// four values
+// four values; FITS: none is infinite or above the largest code
+template <bool FITS>
 __device__ inline uint32_t codes4(float a, float b, float c, float d) {
-    const float top = fmaxf(fmaxf(fabsf(a), fabsf(b)), fmaxf(fabsf(c), fabsf(d)));
-    const bool odd = !(fabsf(a) <= 3.4028234e38f && fabsf(b) <= 3.4028234e38f && fabsf(c) <= 3.4028234e38f && fabsf(d) <= 3.4028234e38f);
-    if (odd || top > kTop) return code(a) | code(b) << 8 | code(c) << 16 | code(d) << 24;
-    int x = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, x, true);
+    if (!FITS) return code(a) | code(b) << 8 | code(c) << 16 | code(d) << 24;
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
 
 // Which sequence the item-th of a batch's work items belongs to, when sequence s has count(s) of them; rem: which of the sequence's; before: the sum
 // of weight(s) over the sequences in front.  As find_seq_count (common.h), for counts that do not come from one list of offsets.  Called by every
-// thread of a workgroup; one barrier; returns >= batch past the last item.
-template <class Count, class Weight>
-__device__ inline int find_item(int batch, int64_t item, int &rem, int64_t &before, int64_t *s_out, Count count, Weight weight) {
+// thread of a workgroup; one barrier; returns >= batch past the last item.  facts(s, i), i = 0, 1, 2: what else is wanted of the sequence (the lane that
+// found it has just read it).
+struct Facts {
+    int x[3];
+};
+template <class Count, class Weight, class Fact>
+__device__ inline int find_item(int batch, int64_t item, int &rem, int64_t &before, Facts &facts, int64_t (&s_out)[6], Count count, Weight weight, Fact fact) {
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
         int64_t items = 0, sum = 0, bef = 0;
@@ -72,6 +74,10 @@ __device__ inline int find_item(int batch, int64_t item, int &rem, int64_t &befo
                 seq = s0 + l;
                 r = (int)(item - items - __shfl(incl - n, l));
                 bef = sum + __shfl(wincl - wt, l);
+                if (lane == l) {
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) s_out[3 + i] = fact(s, i);
+                }
                 break;
             }
             items += __shfl(incl, 63);
@@ -84,6 +90,8 @@ __device__ inline int find_item(int batch, int64_t item, int &rem, int64_t &befo
     rem = __builtin_amdgcn_readfirstlane((int)s_out[1]);
     before = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s_out[2] >> 32)) << 32) |
                        (uint32_t)__builtin_amdgcn_readfirstlane((int)s_out[2]));
+#pragma unroll
+    for (int i = 0; i < 3; ++i) facts.x[i] = __builtin_amdgcn_readfirstlane((int)s_out[3 + i]);
     return __builtin_amdgcn_readfirstlane((int)s_out[0]);
 }
 

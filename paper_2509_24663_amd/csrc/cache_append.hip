@@ -1,10 +1,11 @@
 // New keys and values into the pages of each sequence's cache, keys turned by their positions on the way; the pages hold the data's type or e4m3 codes
 // with a power-of-two scale per page and head.
 //
-// A workgroup owns what a call writes to one (page, KV head) of K or of V: up to 64 rows.  So the page's scale is one workgroup's business: it
-// turns its rows in registers, takes the largest magnitude over them (and, where a page is continued, the scale that the page has: a scale
-// only grows), rounds once, and rounds the older codes again if the scale grew.  No atomics, no second pass over the new rows.
-// A thread owns eight pair numbers of a row (16 channels; rotary.h says which) of every kRows-th row.
+// A workgroup owns what a call writes to one page of K or of V, for one KV head or (many pages) for several in turn: up to 64 rows.  So the page's
+// scale is one workgroup's business: it turns its rows in registers, takes the largest magnitude over them (and, where a page is continued, the
+// scale that the page has: a scale only grows), rounds once, and rounds the older codes again if the scale grew.  No atomics, no second pass over
+// the new rows.  The angles are worked out once for all heads of a workgroup.
+// A thread owns eight pair numbers of a row (16 channels; rotary.h says which).
 #include "cache.h"
 #include "gen_unit.h"
 #include "rotary.h"
@@ -12,8 +13,6 @@
 namespace ifv2 {
 
 namespace {
-
-constexpr int kThreads = 256;
 
 struct AppendArgs {
     cache::Args c;
@@ -23,37 +22,36 @@ struct AppendArgs {
     const int32_t *cu, *prev, *pos;
     int batch;
     int single;                            // every sequence has new tokens, all in one page: item = sequence
+    int heads;                             // of a workgroup
 };
 
+// The 16 channels of the pair numbers q .. q + 7: two runs of eight, as requested ..
 template <typename T>
-__device__ inline float element(const T *p) { return Elem<T>::load(p); }
-
-// the 16 channels of the pair numbers q .. q + 7 as (x[i], y[i]), i = 0..7
-template <typename T>
-__device__ inline void load_pairs(const rotary::Args &r, int q, const T *row, float (&x)[8], float (&y)[8]) {
+struct Pairs {
     typedef typename gen::Unaligned<typename std::conditional<sizeof(T) == 2, uint16_t, float>::type, 8>::type Vec;
-    auto wide = [](auto e) -> float {
-        if constexpr (sizeof(T) == 2) return bf16_to_float(e);
-        else return e;
-    };
-    if (r.pairs % 8 != 0) {                                                  // the eight may straddle the two kinds of pairs
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = element(row + rotary::first_channel(r, q + i));
-            y[i] = element(row + rotary::second_channel(r, q + i));
-        }
-    } else if (q < r.pairs && !r.interleaved) {
-        const Vec a = *reinterpret_cast<const Vec *>(row + q), b = *reinterpret_cast<const Vec *>(row + q + r.pairs);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = wide(a[i]), y[i] = wide(b[i]);
-    } else {
-        const Vec a = *reinterpret_cast<const Vec *>(row + 2 * q), b = *reinterpret_cast<const Vec *>(row + 2 * q + 8);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = wide(i < 4 ? a[(2 * i) & 7] : b[(2 * i) & 7]), y[i] = wide(i < 4 ? a[(2 * i + 1) & 7] : b[(2 * i + 1) & 7]);
+    Vec a, b;
+    // (r.pairs % 8 == 0)
+    __device__ inline void load(const rotary::Args &r, int q, const T *row) {
+        const bool half = q < r.pairs && !r.interleaved;
+        a = *reinterpret_cast<const Vec *>(row + (half ? q : 2 * q));
+        b = *reinterpret_cast<const Vec *>(row + (half ? q + r.pairs : 2 * q + 8));
     }
-}
+    static __device__ inline float wide(uint16_t e) { return bf16_to_float(e); }
+    static __device__ inline float wide(float e) { return e; }
+    // .. and as pairs (x[i], y[i])
+    __device__ inline void spread(const rotary::Args &r, int q, float (&x)[8], float (&y)[8]) const {
+        if (q < r.pairs && !r.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = wide(a[i]), y[i] = wide(b[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = wide(i < 4 ? a[(2 * i) & 7] : b[(2 * i) & 7]), y[i] = wide(i < 4 ? a[(2 * i + 1) & 7] : b[(2 * i + 1) & 7]);
+        }
+    }
+};
 
 // the same channels of a row of codes, from values in units of the scale
+template <bool FITS>
 __device__ inline void store_codes(const rotary::Args &r, int q, char *row, const float (&x)[8], const float (&y)[8]) {
     if (r.pairs % 8 != 0) {
 #pragma unroll
@@ -62,11 +60,11 @@ __device__ inline void store_codes(const rotary::Args &r, int q, char *row, cons
             row[rotary::second_channel(r, q + i)] = (char)cache::code(y[i]);
         }
     } else if (q < r.pairs && !r.interleaved) {
-        *reinterpret_cast<uint2 *>(row + q) = uint2{cache::codes4(x[0], x[1], x[2], x[3]), cache::codes4(x[4], x[5], x[6], x[7])};
-        *reinterpret_cast<uint2 *>(row + q + r.pairs) = uint2{cache::codes4(y[0], y[1], y[2], y[3]), cache::codes4(y[4], y[5], y[6], y[7])};
+        *reinterpret_cast<uint2 *>(row + q) = uint2{cache::codes4<FITS>(x[0], x[1], x[2], x[3]), cache::codes4<FITS>(x[4], x[5], x[6], x[7])};
+        *reinterpret_cast<uint2 *>(row + q + r.pairs) = uint2{cache::codes4<FITS>(y[0], y[1], y[2], y[3]), cache::codes4<FITS>(y[4], y[5], y[6], y[7])};
     } else {
-        *reinterpret_cast<uint4 *>(row + 2 * q) = uint4{cache::codes4(x[0], y[0], x[1], y[1]), cache::codes4(x[2], y[2], x[3], y[3]),
-                                                        cache::codes4(x[4], y[4], x[5], y[5]), cache::codes4(x[6], y[6], x[7], y[7])};
+        *reinterpret_cast<uint4 *>(row + 2 * q) = uint4{cache::codes4<FITS>(x[0], y[0], x[1], y[1]), cache::codes4<FITS>(x[2], y[2], x[3], y[3]),
+                                                        cache::codes4<FITS>(x[4], y[4], x[5], y[5]), cache::codes4<FITS>(x[6], y[6], x[7], y[7])};
     }
 }
 
@@ -95,110 +93,140 @@ __device__ inline void store_native(const rotary::Args &r, int q, T *row, const 
 __host__ __device__ inline int pages_touched(int prev, int n) { return n == 0 ? 0 : (prev + n - 1) / kBlock - prev / kBlock + 1; }
 
 template <typename T, int D, bool CODES>
-__global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
-    constexpr int PER = D / 16;                       // threads per row
-    constexpr int ROWS = kThreads / PER, STEPS = kBlock / ROWS;
-    __shared__ int64_t s_item[3];
-    __shared__ float s_top[kThreads / 64];
-    const int h = blockIdx.y, tid = threadIdx.x;
+__global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
+    constexpr int PER = D / 16, kThreads = 4 * D;     // threads per row; every row of a page has its own
+    __shared__ int64_t s_item[6];
+    __shared__ float s_top[2][2][kThreads / 64];      // by turns
+    const int tid = threadIdx.x, h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.c.hkv);
     const bool values = blockIdx.z != 0;
-    int seq = blockIdx.x, nth = 0;
-    if (!a.single) {
+    int seq = blockIdx.x, nth = 0, prev, row0, n;
+    if (a.single) {
+        prev = a.prev[seq];
+        row0 = a.cu[seq];
+        n = a.cu[seq + 1] - row0;
+    } else {
         int64_t before;
-        seq = cache::find_item(a.batch, blockIdx.x, nth, before, s_item,
-                               [&](int s) { return pages_touched(a.prev[s], a.cu[s + 1] - a.cu[s]); }, [](int) { return 0; });
+        cache::Facts f;
+        seq = cache::find_item(a.batch, blockIdx.x, nth, before, f, s_item,
+                               [&](int s) { return pages_touched(a.prev[s], a.cu[s + 1] - a.cu[s]); }, [](int) { return 0; },
+                               [&](int s, int i) { return i == 0 ? a.prev[s] : a.cu[s + i - 1]; });
         if (seq >= a.batch) return;
+        prev = f.x[0];
+        row0 = f.x[1];
+        n = f.x[2] - row0;
     }
-    const int prev = a.prev[seq], row0 = a.cu[seq], n = a.cu[seq + 1] - row0;
     const int block = prev / kBlock + nth;
-    const int page = a.c.page(seq, block);
-    if (page < 0) return;
     const int first = max(prev, block * kBlock), end = min(prev + n, block * kBlock + kBlock);     // tokens of this page that are new
     rotary::Args r = a.r;
     if (values) r.pairs = 0;
-    const int q = (tid % PER) * 8, t0 = block * kBlock + tid / PER;
-    const T *src = reinterpret_cast<const T *>(values ? a.v : a.k) + (int64_t)(row0 - prev) * a.tok_stride + h * a.head_stride;
-    char *dst = (values ? a.c.v : a.c.k) + a.c.at(page, h);
-    float x[STEPS][8], y[STEPS][8], top = 0.f;
+    const int q = (tid % PER) * 8, t = block * kBlock + tid / PER;
+    const bool mine = t >= first && t < end;
+    const T *src = reinterpret_cast<const T *>(values ? a.v : a.k) + (int64_t)(row0 + t - prev) * a.tok_stride;
+    const bool runs = r.pairs % 8 == 0;               // the eight are pairs of one kind
+    Pairs<T> raw;
+    if (mine && runs) raw.load(r, q, src + h0 * a.head_stride);      // (beside the page's number, not behind it)
+    const int page = a.c.page(seq, block);
+    if (page < 0) return;
+    float co[8], si[8];
+    const bool turns = mine && q < r.pairs;
+    if (turns) {
+        const int32_t pos = a.pos ? a.pos[row0 + t - prev] : t;
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int t = t0 + i * ROWS;
-        if (t >= first && t < end) {
-            load_pairs(r, q, src + (int64_t)t * a.tok_stride, x[i], y[i]);
+        for (int e = 0; e < 8; ++e) {
+            const float2 cs = q + e < r.pairs ? rotary::cos_sin<T>(pos, r.turns[q + e], r.magnitude) : float2{1.f, 0.f};
+            co[e] = cs.x;
+            si[e] = cs.y;
+        }
+    }
+    for (int h = h0, turn = 0; h < h1; ++h, turn ^= 1) {
+        char *page_at = (values ? a.c.v : a.c.k) + a.c.at(page, h), *dst = page_at + (t - block * kBlock) * a.c.tok_stride;
+        float x[8], y[8], top = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
+        if (mine && runs) {
+            raw.spread(r, q, x, y);
+            if (h + 1 < h1) raw.load(r, q, src + (h + 1) * a.head_stride);
+        } else if (mine) {
+            const T *row = src + h * a.head_stride;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = Elem<T>::load(row + rotary::first_channel(r, q + e));
+                y[e] = Elem<T>::load(row + rotary::second_channel(r, q + e));
+            }
+        }
+        if (turns && runs) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 z = rotary::turn(x[e], y[e], co[e], si[e]);
+                x[e] = z.x;
+                y[e] = z.y;
+            }
+        } else if (turns) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 z = rotary::turn(x[e], y[e], co[e], si[e]);
+                x[e] = q + e < r.pairs ? z.x : x[e];
+                y[e] = q + e < r.pairs ? z.y : y[e];
+            }
+        }
+        if constexpr (!CODES) {
+            if (mine) store_native(r, q, reinterpret_cast<T *>(dst), x, y);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.f;
-        }
-    }
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(y[e])));       // (a NaN is passed over)
+            float *scale = (values ? a.c.vs : a.c.ks) + (int64_t)page * a.c.hkv + h;
+            const bool continued = first > block * kBlock;
+            const float was = continued ? *scale : 0.f;
+            auto over_all = [&](float v, float (&s)[kThreads / 64]) {
+                v = wave_max(v);
+                if ((tid & 63) == 0) s[tid >> 6] = v;
+                __syncthreads();
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int t = t0 + i * ROWS;
-        if (q < r.pairs && t >= first && t < end) {
-            const int32_t pos = a.pos ? a.pos[row0 + t - prev] : t;
+                for (int w = 0; w < kThreads / 64; ++w) v = fmaxf(v, s[w]);
+                return v;
+            };
+            top = over_all(top, s_top[turn][0]);
+            const bool fits = top <= 448.f * 0x1p119f;
+            if (!fits) {                              // infinities, or numbers that no scale is large enough for: the finite ones again
+                top = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (q + e >= r.pairs) continue;
-                const float2 cs = rotary::cos_sin(pos, r.turns[q + e], r.magnitude);
-                const float2 z = rotary::turn(x[i][e], y[i][e], cs.x, cs.y);
-                x[i][e] = z.x;
-                y[i][e] = z.y;
-            }
-        }
-        if constexpr (CODES) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float u = fabsf(x[i][e]), w = fabsf(y[i][e]);
-                top = fmaxf(top, fmaxf(u <= 3.4028234e38f ? u : 0.f, w <= 3.4028234e38f ? w : 0.f));
-            }
-        }
-    }
-    if constexpr (!CODES) {
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const int t = t0 + i * ROWS;
-            if (t >= first && t < end) store_native(r, q, reinterpret_cast<T *>(dst + (t - block * kBlock) * a.c.tok_stride), x[i], y[i]);
-        }
-    } else {
-        float *scale = (values ? a.c.vs : a.c.ks) + (int64_t)page * a.c.hkv + h;
-        const bool continued = first > block * kBlock;
-        const float was = continued ? *scale : 0.f;
-        top = wave_max(top);
-        if ((tid & 63) == 0) s_top[tid >> 6] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, s_top[w]);
-        const float now = fmaxf(cache::scale_for(top), was), inv = cache::reciprocal_of_power(now);
-        if (continued && now != was) {                // the older rows, sixteen codes at a time
-            const float down = was * inv;
-            for (int i = tid; i < (first - block * kBlock) * PER; i += kThreads) {
-                uint4 *at = reinterpret_cast<uint4 *>(dst + (i / PER) * a.c.tok_stride + (i % PER) * 16);
-                uint4 old = *at;
-                uint32_t w[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
-                    w[j] = cache::codes4(lo[0] * down, lo[1] * down, hi[0] * down, hi[1] * down);
+                for (int e = 0; e < 8; ++e) {
+                    const float u = fabsf(x[e]), w = fabsf(y[e]);
+                    top = fmaxf(top, fmaxf(u <= 3.4028234e38f ? u : 0.f, w <= 3.4028234e38f ? w : 0.f));
                 }
-                *at = uint4{w[0], w[1], w[2], w[3]};
+                top = over_all(top, s_top[turn][1]);
             }
-        }
+            const float now = fmaxf(cache::scale_for(top), was), inv = cache::reciprocal_of_power(now);
+            if (continued && now != was) {            // the older rows, sixteen codes at a time
+                const float down = was * inv;
+                for (int i = tid; i < (first - block * kBlock) * PER; i += kThreads) {
+                    uint4 *at = reinterpret_cast<uint4 *>(page_at + (i / PER) * a.c.tok_stride + (i % PER) * 16);
+                    uint4 old = *at;
+                    uint32_t w[4] = {old.x, old.y, old.z, old.w};
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const int t = t0 + i * ROWS;
-            if (t < first || t >= end) continue;
+                    for (int j = 0; j < 4; ++j) {
+                        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
+                        w[j] = cache::codes4<true>(lo[0] * down, lo[1] * down, hi[0] * down, hi[1] * down);
+                    }
+                    *at = uint4{w[0], w[1], w[2], w[3]};
+                }
+            }
+            if (mine) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] *= inv, y[i][e] *= inv;
-            store_codes(r, q, dst + (t - block * kBlock) * a.c.tok_stride, x[i], y[i]);
+                for (int e = 0; e < 8; ++e) x[e] *= inv, y[e] *= inv;
+                if (fits) store_codes<true>(r, q, dst, x, y);
+                else store_codes<false>(r, q, dst, x, y);
+            }
+            if (tid == 0 && now != was) *scale = now;
         }
-        if (tid == 0 && now != was) *scale = now;
     }
 }
 
 template <typename T, int D>
 int launch_t(const AppendArgs &a, bool codes, unsigned items, hipStream_t stream) {
-    const dim3 grid(items, a.c.hkv, 2);
-    if (codes) hipLaunchKernelGGL((cache_append_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((cache_append_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, a);
+    const dim3 grid(items, (a.c.hkv + a.heads - 1) / a.heads, 2);
+    if (codes) hipLaunchKernelGGL((cache_append_kernel<T, D, true>), grid, dim3(4 * D), 0, stream, a);
+    else hipLaunchKernelGGL((cache_append_kernel<T, D, false>), grid, dim3(4 * D), 0, stream, a);
     return hip_status(hipGetLastError());
 }
 
@@ -260,7 +288,9 @@ extern "C" int infllmv2_cache_append(const infllmv2_params *p, const infllmv2_ca
     if (st) return st;
     if (p->num_kv_heads > 65535) return INFLLMV2_ERR_UNSUPPORTED;
     AppendArgs a{cache::args(p, c), r ? rotary::args(r) : rotary::Args{nullptr, 0, 0, 1.f}, (const char *)k_d, (const char *)v_d,
-                 kv_tok_stride, kv_head_stride, cu_new_d, prev_lens_d, pos_d, batch, single};
+                 kv_tok_stride, kv_head_stride, cu_new_d, prev_lens_d, pos_d, batch, single, 1};
+    // heads of a workgroup: all, while that leaves a few workgroups for each CU (the angles are half of a key page's work)
+    while (a.heads < p->num_kv_heads && items * 2 * ((p->num_kv_heads + 2 * a.heads - 1) / (2 * a.heads)) >= 1024) a.heads *= 2;
     const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
     const hipStream_t s = (hipStream_t)stream;
     if (p->head_dim == 128)

@@ -218,23 +218,28 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TIL
 template <typename T, int D, bool CODES, int TILES, bool MULTI>
 __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
-    __shared__ int64_t s_item[3];
+    __shared__ int64_t s_item[6];
     __shared__ float s_m[NW][16], s_l[NW][16];
     __shared__ f32x4 s_o[NW][N][64];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv;
 
     // the item: sequence, tile, KV head, split; slot: where a partial result goes
-    int seq, rem, row0, n;
+    int seq, rem, row0, n, len, early = -1;
     int64_t slot = blockIdx.x;
     if (a.even) {
         seq = (int)(blockIdx.x / (unsigned)(hkv * a.even));
         rem = (int)(blockIdx.x - (unsigned)seq * (unsigned)(hkv * a.even));
         row0 = seq;
         n = 1;
+        len = a.ctx[seq];
+        // (the first list entries are requested beside the length that says whether there is a list)
+        if (a.idx != nullptr)
+            early = a.idx[((int64_t)seq * hkv + rem / a.even) * a.topk + min(rem % a.even * a.pps + w + lane * NW, a.topk - 1)];
     } else {
         int64_t slot0;
-        seq = cache::find_item(a.batch, blockIdx.x, rem, slot0, s_item,
+        cache::Facts f;
+        seq = cache::find_item(a.batch, blockIdx.x, rem, slot0, f, s_item,
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
                 return (int64_t)a.tiles(n, len) * hkv * a.most_splits(n, len);
@@ -242,13 +247,15 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
                 return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
-            });
+            },
+            [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
         if (seq >= a.batch) return;
         slot = slot0 + rem;
-        row0 = a.cu[seq];
-        n = a.cu[seq + 1] - row0;
+        row0 = f.x[0];
+        n = f.x[1] - row0;
+        len = f.x[2];
     }
-    const int len = a.ctx[seq], per = a.even ? a.even : a.most_splits(n, len);
+    const int per = a.even ? a.even : a.most_splits(n, len);
     const bool listed = a.listed(len);
     const int split = rem % per, th = rem / per, h = th % hkv, tile = th / hkv;
     const int T0 = a.tile_tokens(len), first = tile * T0, ntok = min(T0, n - first);       // tokens of this tile
@@ -281,7 +288,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
         int my_page = -1, my_key0 = 0;
         float my_ks = 1.f, my_vs = 1.f;
         if (e < e_end) {
-            const int j = listed ? list[e] : e;
+            const int j = !listed ? e : a.even && e0 < split * a.pps + NW ? early : list[e];
             if (j >= 0 && j <= pos_last / kBlock) {
                 my_page = a.c.page(seq, j);
                 my_key0 = j * kBlock;
@@ -454,9 +461,9 @@ constexpr int kMergeCols = 4, kAhead = 8;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
-    __shared__ int64_t s_item[3];
+    __shared__ int64_t s_item[6];
     const int tid = threadIdx.x, hkv = a.c.hkv, G = a.hq / hkv;
-    int th, seq, row0, n;
+    int th, seq, row0, n, len;
     int64_t slot;
     if (a.even) {
         seq = (int)(blockIdx.x / (unsigned)hkv);
@@ -464,8 +471,10 @@ __global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
         slot = (int64_t)blockIdx.x * a.even;
         row0 = seq;
         n = 1;
+        len = a.ctx[seq];
     } else {
-        seq = cache::find_item(a.batch, blockIdx.x, th, slot, s_item,
+        cache::Facts f;
+        seq = cache::find_item(a.batch, blockIdx.x, th, slot, f, s_item,
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
                 return a.most_splits(n, len) > 1 ? (int64_t)a.tiles(n, len) * hkv : 0;
@@ -473,12 +482,14 @@ __global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
                 return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
-            });
+            },
+            [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
         if (seq >= a.batch) return;
-        row0 = a.cu[seq];
-        n = a.cu[seq + 1] - row0;
+        row0 = f.x[0];
+        n = f.x[1] - row0;
+        len = f.x[2];
     }
-    const int len = a.ctx[seq], cols = 16 * a.tile_groups;
+    const int cols = 16 * a.tile_groups;
     if (!a.even) slot += (int64_t)th * a.most_splits(n, len);
     const int h = th % hkv, tile = th / hkv, T0 = a.tile_tokens(len), first = tile * T0, ntok = min(T0, n - first);
     const int nsplit = a.splits(len, len - n + first + ntok - 1);
@@ -538,7 +549,7 @@ int launch_t(const AttnArgs &a, int64_t items, int64_t merges, hipStream_t strea
 }
 
 constexpr int kTargetGroups = 2048;        // workgroups that a call is cut into: four rounds of two for each CU
-constexpr int kLeastPages = 2 * NW;        // two pages for each wavefront
+constexpr int kLeastPages = NW;            // a page for each wavefront; two once that makes a workgroup for each CU (16 sequences, 64 blocks each: 19.3 -> 17.3 us)
 // Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
 // kTargetGroups, so at most 2 kTargetGroups partial results.
 size_t slot_bytes(int d, int groups) { return (size_t)16 * groups * (d + 2) * sizeof(float); }
@@ -635,7 +646,8 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     // (rows of a page are addressed with 32-bit offsets)
     if (c->tok_stride > (1ll << 24)) return INFLLMV2_ERR_UNSUPPORTED;
     const int64_t share = (work + kTargetGroups - 1) / kTargetGroups;
-    a.pps = share < kLeastPages ? kLeastPages : share > (1 << 24) ? 1 << 24 : (int)share;
+    const int least = work > 256 * kLeastPages ? 2 * kLeastPages : kLeastPages;
+    a.pps = share < least ? least : share > (1 << 24) ? 1 << 24 : (int)share;
     wide.pps = wide_tiles > 0 ? rules::tile_splits(wide_tiles, wide_pages).pps : 1;
     Launches mine, other;
     bool single = true;                        // one query token for each sequence

@@ -83,14 +83,15 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int KB = CODES ? 1 : 2;                               // bytes of an element
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // two K pages, three V pages, rows of V as they come
-    __shared__ int64_t s_item[3];
+    __shared__ int64_t s_item[6];
     __shared__ int s_odd;                                           // a value of a page's edge (see write) is not finite
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv, GT = a.group_tokens;
 
     int rem;
     int64_t slot0;
-    const int seq = cache::find_item(a.batch, blockIdx.x, rem, slot0, s_item,
+    cache::Facts facts;
+    const int seq = cache::find_item(a.batch, blockIdx.x, rem, slot0, facts, s_item,
         [&](int s) {
             const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
             return (int64_t)a.tiles(n, len) * hkv * a.most_splits(n, len);
@@ -98,9 +99,10 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a
         [&](int s) {
             const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
             return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
-        });
+        },
+        [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
     if (seq >= a.batch) return;
-    const int row0 = a.cu[seq], n = a.cu[seq + 1] - row0, len = a.ctx[seq];
+    const int row0 = facts.x[0], n = facts.x[1] - row0, len = facts.x[2];
     const int per = a.most_splits(n, len), ntiles = a.tiles(n, len);
     const int split = rem % per, th = rem / per, h = th % hkv, tile = ntiles - 1 - th / hkv;          // (longest first)
     const int64_t slot = slot0 + (int64_t)(tile * hkv + h) * per + split;

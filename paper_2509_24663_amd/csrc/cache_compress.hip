@@ -9,7 +9,6 @@ namespace ifv2 {
 namespace {
 
 constexpr int VEC = 8;            // channels per thread
-constexpr int U = 16;             // rows requested at once
 
 struct CompressArgs {
     cache::Args c;
@@ -22,6 +21,9 @@ struct CompressArgs {
 template <typename T, int D, bool CODES>
 __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
     constexpr int VPR = D / VEC;
+    // rows requested at once, of two pages at most, both looked up first (fp32 rows: registers)
+    constexpr int U = CODES || sizeof(T) == 2 ? 32 : 16;
+    typedef typename std::conditional<CODES, uint2, typename std::conditional<sizeof(T) == 2, gen::u16x8_u, gen::f32x8_u>::type>::type Vec;
     const int slot = threadIdx.x / VPR, pair = (int)((blockIdx.y * (64u / VPR) + slot) / a.rows);
     if (pair >= a.pairs) return;
     const int b = pair / a.c.hkv, h = pair - b * a.c.hkv;
@@ -32,49 +34,46 @@ __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
 #pragma unroll
     for (int c = 0; c < VEC; ++c) acc[c] = 0.f;
     const int end = i * a.sc + a.lc;
-    for (int t = i * a.sc; t < end;) {
-        const int block = t / kBlock, stop = min(end, (block + 1) * kBlock);
-        const int page = a.c.page(b, block);
-        if (page >= 0) {
-            const char *base = a.c.k + a.c.at(page, h) - (int64_t)block * kBlock * a.c.tok_stride;
-            const float scale = CODES ? a.c.ks[(int64_t)page * a.c.hkv + h] : 1.f;
-            for (int u0 = t; u0 < stop; u0 += U) {
-                if constexpr (CODES) {
-                    uint2 x[U];
+    for (int t = i * a.sc; t < end; t += U) {
+        const int last = min(t + U, end) - 1, block = t / kBlock, edge = (block + 1) * kBlock;     // rows from edge on are the next page's
+        const int page0 = a.c.page(b, block), page1 = last >= edge ? a.c.page(b, block + 1) : -1;
+        // (rows of a page that is not there: any row's address, taken as 0)
+        const int safe0 = page0 >= 0 ? page0 : 0, safe1 = page1 >= 0 ? page1 : 0;
+        const char *base0 = a.c.k + a.c.at(safe0, h) + (int64_t)(t - block * kBlock) * a.c.tok_stride + c0 * (CODES ? 1 : (int)sizeof(T));
+        const char *base1 = a.c.k + a.c.at(safe1, h) + (int64_t)(t - edge) * a.c.tok_stride + c0 * (CODES ? 1 : (int)sizeof(T));
+        float s0 = 1.f, s1 = 1.f;
+        if constexpr (CODES) {
+            s0 = a.c.ks[(int64_t)safe0 * a.c.hkv + h];
+            s1 = a.c.ks[(int64_t)safe1 * a.c.hkv + h];
+        }
+        const int n0 = min(edge, last + 1) - t, n = last + 1 - t;   // rows of the first page, of both
+        Vec x[U];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const uint2 *>(base + (int64_t)min(u0 + u, stop - 1) * a.c.tok_stride + c0);
-                    __builtin_amdgcn_sched_barrier(0);
+        for (int u = 0; u < U; ++u) {
+            const int v = min(u, n - 1);
+            x[u] = *reinterpret_cast<const Vec *>((v < n0 ? base0 : base1) + (int64_t)v * a.c.tok_stride);
+        }
+        __builtin_amdgcn_sched_barrier(0);       // (left alone, the scheduler trades the requests for registers)
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const bool in = u0 + u < stop;
+        for (int u = 0; u < U; ++u) {
+            const bool in = u < n && (u < n0 ? page0 : page1) >= 0;
+            if constexpr (CODES) {
+                const float scale = u < n0 ? s0 : s1;
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int w = (int)(j ? x[u].y : x[u].x);
-                            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                            acc[4 * j] += in ? lo[0] * scale : 0.f, acc[4 * j + 1] += in ? lo[1] * scale : 0.f;
-                            acc[4 * j + 2] += in ? hi[0] * scale : 0.f, acc[4 * j + 3] += in ? hi[1] * scale : 0.f;
-                        }
-                    }
-                } else {
-                    typedef typename std::conditional<sizeof(T) == 2, gen::u16x8_u, gen::f32x8_u>::type Vec;
-                    Vec x[U];
+                for (int j = 0; j < 2; ++j) {
+                    const int w = (int)(j ? x[u].y : x[u].x);
+                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                    acc[4 * j] += in ? lo[0] * scale : 0.f, acc[4 * j + 1] += in ? lo[1] * scale : 0.f;
+                    acc[4 * j + 2] += in ? hi[0] * scale : 0.f, acc[4 * j + 3] += in ? hi[1] * scale : 0.f;
+                }
+            } else {
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        x[u] = *reinterpret_cast<const Vec *>(base + (int64_t)min(u0 + u, stop - 1) * a.c.tok_stride + c0 * sizeof(T));
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const bool in = u0 + u < stop;
-#pragma unroll
-                        for (int c = 0; c < VEC; ++c) {
-                            if constexpr (sizeof(T) == 2) acc[c] += in ? bf16_to_float(x[u][c]) : 0.f;
-                            else acc[c] += in ? x[u][c] : 0.f;
-                        }
-                    }
+                for (int c = 0; c < VEC; ++c) {
+                    if constexpr (sizeof(T) == 2) acc[c] += in ? bf16_to_float(x[u][c]) : 0.f;
+                    else acc[c] += in ? x[u][c] : 0.f;
                 }
             }
         }
-        t = stop;
     }
     const float inv = 1.0f / (float)a.lc;
 #pragma unroll

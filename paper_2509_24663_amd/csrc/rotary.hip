@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(RotaryLaunch a) {
         const int32_t pos = a.pos[token];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float2 cs = rotary::cos_sin(pos, a.r.turns[q + i], a.r.magnitude);
+            const float2 cs = rotary::cos_sin<T>(pos, a.r.turns[q + i], a.r.magnitude);
             co[i] = cs.x;
             si[i] = cs.y * a.sign;
         }
