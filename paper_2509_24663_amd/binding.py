@@ -509,10 +509,16 @@ class PagedCache:
         for s in (k_scale, v_scale) if coded else ():
             assert s.dtype == torch.float32 and s.is_contiguous() and s.shape == k.shape[:2]
         self.k, self.v, self.page_table, self.k_scale, self.v_scale = k, v, page_table, k_scale, v_scale
-        self.batch = page_table.shape[0]
+        self.batch, blocks = page_table.shape
+        self.rows = (p.num_kv_heads, p.head_dim, p.dtype)
+        # (rows of a table that is part of a wider one end before the library's check of their stride does)
+        self.room = blocks * p.block_size if self.batch > 1 and page_table.stride(0) > blocks else None
         self.c = _CacheC(CACHE_E4M3 if coded else CACHE_NATIVE, k.shape[0], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                          k.stride(2), _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(),
-                         page_table.stride(0) if self.batch > 1 else page_table.shape[1], 0)
+                         page_table.stride(0) if self.batch > 1 else blocks, 0)
+
+    def _holds(self, p: Params, max_ctx: int) -> bool:
+        return self.rows == (p.num_kv_heads, p.head_dim, p.dtype) and (self.room is None or max_ctx <= self.room)
 
     @staticmethod
     def empty(p: Params, num_pages: int, page_table: torch.Tensor, kv_type: str = "e4m3") -> "PagedCache":
@@ -538,6 +544,7 @@ def cache_append(p: Params, cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
     assert one == 1 and v.stride() == stride and k.dtype is dtype and v.dtype is dtype
     assert k.shape == v.shape == (p.num_kv_heads, si.total, p.head_dim) and batch == pv.batch <= cache.batch
     assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == si.total)
+    assert cache._holds(p, 0 if cache.room is None else max((n and n + t for n, t in zip(si.lens, pv.ctx_h.tolist())), default=0))
     st = lib().infllmv2_cache_append(ctypes.byref(p), ctypes.byref(cache.c), ctypes.byref(rotary.c) if rotary is not None else None,
                                      k.data_ptr(), v.data_ptr(), ts, hs, si.cu_h.data_ptr(), si.cu_d.data_ptr(), pv.ctx_h.data_ptr(),
                                      pv.ctx_d.data_ptr(), _ptr(positions), batch, _stream())
@@ -550,7 +557,7 @@ def cache_compress_k(p: Params, cache: PagedCache, kc_cache: torch.Tensor, prev_
     pv, cx = _decode_info(prev_lens), _decode_info(ctx_lens)
     planes, hkv, rows, d = kc_cache.shape
     assert kc_cache.is_contiguous() and kc_cache.dtype is torch.float32 and hkv == p.num_kv_heads and d == p.head_dim
-    assert pv.batch == cx.batch <= cache.batch and cx.batch <= planes
+    assert pv.batch == cx.batch <= cache.batch and cx.batch <= planes and cache._holds(p, cx.max_ctx)
     st = lib().infllmv2_cache_compress_k(ctypes.byref(p), ctypes.byref(cache.c), kc_cache.data_ptr(), rows * d, pv.ctx_h.data_ptr(),
                                          pv.ctx_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), cx.batch, _stream())
     _check(st, "infllmv2_cache_compress_k")
@@ -563,9 +570,10 @@ def decode_blocks(p: Params, q: torch.Tensor, kc_cache: torch.Tensor, ctx_lens, 
     di = _decode_info(ctx_lens)
     assert q.is_contiguous() and q.dtype == p.torch_dtype and q.shape == (di.batch, p.num_q_heads, p.head_dim)
     assert kc_cache.dim() == 4 and kc_cache.is_contiguous() and kc_cache.dtype == torch.float32 and kc_cache.shape[0] >= di.batch
+    assert kc_cache.shape[1] == p.num_kv_heads and kc_cache.shape[3] == p.head_dim
     if out is None:
         out = torch.empty((di.batch, p.num_kv_heads, p.topk_total), dtype=torch.int32, device=q.device)
-    assert out.is_contiguous() and out.dtype == torch.int32
+    assert out.is_contiguous() and out.dtype == torch.int32 and out.shape == (di.batch, p.num_kv_heads, p.topk_total)
     if workspace is None:
         need = workspace_bytes(OP_DECODE_BLOCKS, p, di.batch, 0, di.max_ctx)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
@@ -583,7 +591,7 @@ def cache_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q, ctx_
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     tokens, hq, _ = shape = q.shape
     assert q.is_contiguous() and q.dtype is p.torch_dtype and shape == (si.total, p.num_q_heads, p.head_dim)
-    assert si.batch == cx.batch <= cache.batch
+    assert si.batch == cx.batch <= cache.batch and cache._holds(p, cx.max_ctx)
     if block_idx is not None:
         assert block_idx.is_contiguous() and block_idx.dtype is torch.int32 and block_idx.shape == (tokens, p.num_kv_heads, p.topk_total)
     if out is None:

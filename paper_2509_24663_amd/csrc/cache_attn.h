@@ -33,7 +33,7 @@ struct AttnArgs {
         const int t = tile_tokens(len);
         return (n + t - 1) / t;
     }
-    // pages (listed: entries) of the tile whose last token is at pos_last
+    // pages of the tile whose last token is at pos_last: at most so many are there (listed: a list may hold them anywhere)
     __host__ __device__ int pages(int len, int pos_last) const {
         const int all = pos_last / kBlock + 1;
         return listed(len) && topk < (len + kBlock - 1) / kBlock ? topk : all;

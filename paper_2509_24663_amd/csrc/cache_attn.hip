@@ -262,6 +262,9 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     const int pos0 = len - n + first, pos_last = pos0 + ntok - 1;
     const int nsplit = a.splits(len, pos_last);
     if (split >= nsplit) return;
+    // the entries of this split: a list that is longer than the pages there can be is cut into as many equal parts
+    const int pages = a.pages(len, pos_last), entries = listed ? a.topk : pages, each = entries > pages ? (entries + nsplit - 1) / nsplit : a.pps;
+    const int e_first = split * each, e_end = min(entries, e_first + each);
     const int ti = m / G;                                                                // this lane's column
     const bool used = ti < ntok;
     const int pos = used ? pos0 + ti : -1;
@@ -278,17 +281,16 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     float ref = -INFINITY, sum = 0.f;            // reference in units of log2; this lane's share of the sum
     int low = INT32_MAX;                         // first key of any page that this wavefront went through
 
-    const int e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
     const int32_t *list = a.idx + ((int64_t)(row0 + first) * hkv + h) * a.topk;
     const uint32_t tok = (uint32_t)a.c.tok_stride;
     const uint32_t k_off = m * tok + KeyTile<T, D, CODES>::lane_offset(g), v_off = 4 * g * tok + m * ValueRow<T, D, CODES>::BYTES;
     // a wavefront takes every NW-th page of the split; lane l holds the l-th of the next 64: where it is, its first key, its scales
-    for (int e0 = split * a.pps + w; e0 < e_end; e0 += 64 * NW) {
+    for (int e0 = e_first + w; e0 < e_end; e0 += 64 * NW) {
         const int e = e0 + lane * NW;
         int my_page = -1, my_key0 = 0;
         float my_ks = 1.f, my_vs = 1.f;
         if (e < e_end) {
-            const int j = !listed ? e : a.even && e0 < split * a.pps + NW ? early : list[e];
+            const int j = !listed ? e : a.even && each == a.pps && e0 < e_first + NW ? early : list[e];
             if (j >= 0 && j <= pos_last / kBlock) {
                 my_page = a.c.page(seq, j);
                 my_key0 = j * kBlock;
@@ -550,6 +552,7 @@ int launch_t(const AttnArgs &a, int64_t items, int64_t merges, hipStream_t strea
 
 constexpr int kTargetGroups = 2048;        // workgroups that a call is cut into: four rounds of two for each CU
 constexpr int kLeastPages = NW;            // a page for each wavefront; two once that makes a workgroup for each CU (16 sequences, 64 blocks each: 19.3 -> 17.3 us)
+constexpr int kMostPages = 1 << 25;        // of a context: with so many to a split there is one split
 // Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
 // kTargetGroups, so at most 2 kTargetGroups partial results.
 size_t slot_bytes(int d, int groups) { return (size_t)16 * groups * (d + 2) * sizeof(float); }
@@ -647,7 +650,7 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     if (c->tok_stride > (1ll << 24)) return INFLLMV2_ERR_UNSUPPORTED;
     const int64_t share = (work + kTargetGroups - 1) / kTargetGroups;
     const int least = work > 256 * kLeastPages ? 2 * kLeastPages : kLeastPages;
-    a.pps = share < least ? least : share > (1 << 24) ? 1 << 24 : (int)share;
+    a.pps = share < least ? least : share > kMostPages ? kMostPages : (int)share;
     wide.pps = wide_tiles > 0 ? rules::tile_splits(wide_tiles, wide_pages).pps : 1;
     Launches mine, other;
     bool single = true;                        // one query token for each sequence

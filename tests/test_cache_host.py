@@ -2,11 +2,13 @@
 are not device memory: a call that went on would fault)."""
 import ctypes
 import math
+import random
 
 import numpy as np
 import pytest
+import torch
 
-INVALID, UNSUPPORTED, TOO_SMALL = -1, -2, -3
+INVALID, UNSUPPORTED, TOO_SMALL, HIP = -1, -2, -3, -4
 one = ctypes.c_void_p(256)
 
 
@@ -161,6 +163,31 @@ def test_attention_refusals_and_scratch(m):
     assert call(big, ctx=(40000,), ws=None) == INVALID and call(big, ctx=(40000,), ws=ctypes.c_void_p(264)) == INVALID
     assert call(big, ctx=(40000,), nbytes=1024) == TOO_SMALL
     assert m.workspace_bytes(m.OP_CACHE_ATTN, m.Params.make("bf16", 8, 2, 96), 1, 1, 40000) == 0
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls whose arguments are in order must end at the launch: no GPU")
+def test_scratch_that_was_asked_for_is_enough(m):
+    """The size from a batch's totals alone covers what any batch of these totals needs: single tokens, chunks, both, over lists and not."""
+    rng = random.Random(3)
+    for i in range(400):
+        dtype, hq, hkv, d = rng.choice([("bf16", 32, 2, 128), ("bf16", 8, 2, 64), ("bf16", 5, 5, 64), ("fp32", 4, 1, 64), ("bf16", 16, 16, 128)])
+        p = m.Params.make(dtype, hq, hkv, d, topk_total=rng.choice([4, 64, 1024]), n_init=1, n_local=1, dense_threshold=rng.choice([0, 4000, 1 << 30]))
+        batch = rng.choice([1, 2, 7, 64, 700])
+        far = rng.choice([100, 5000, 200000, 100000000])
+        news = [rng.choice([0, 1, 1, 1, 3, 30, 200, 5000] if rng.random() < 0.5 else [1]) for _ in range(batch)]
+        if rng.random() < 0.3:
+            news = [1] * batch
+        ctx = [max(n, int(far ** rng.random())) for n in news]
+        cu = [0]
+        for n in news:
+            cu.append(cu[-1] + n)
+        if cu[-1] == 0:
+            continue
+        c = _cache(m, stride=(max(ctx) + 63) // 64, tok=128, head=64 * 128, page=16 * 64 * 128)
+        need = m.workspace_bytes(m.OP_CACHE_ATTN, p, batch, cu[-1], max(ctx))
+        (_a, cu_h), (_b, cx) = _ints(cu), _ints(ctx)
+        st = m.lib().infllmv2_cache_attn(ctypes.byref(p), ctypes.byref(c), one, cu_h, one, cx, one, batch, rng.choice([None, one]), one, None, one, need, None)
+        assert st == HIP, (i, st, dtype, hq, hkv, d, news[:8], ctx[:8])
 
 
 def test_decode_blocks_refusals(m):

@@ -261,6 +261,31 @@ def test_attention_over_lists(m, kv, dtype, hq, hkv, d):
 
 
 @pytest.mark.parametrize("kv", ["e4m3", "native"])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", 32, 2, 128), ("fp32", 4, 1, 64)])
+@pytest.mark.parametrize("topk,ctxs", [(24, [130, 64, 1, 900]), (600, [700, 1, 5000, 20000])])
+def test_lists_longer_than_the_pages(m, kv, dtype, hq, hkv, d, topk, ctxs):
+    """A list's blocks may stand anywhere in it, also where it has more entries than the sequence has blocks."""
+    p = _params(m, dtype, hq, hkv, d, topk_total=topk)
+    c, _, _ = _filled(m, p, ctxs, kv, 33)
+    gen = torch.Generator().manual_seed(topk)
+    for news in ([1] * 4, [1, 1, 0, 7]):
+        blocks = torch.full((sum(news), hkv, topk), -1, dtype=torch.int32)
+        row = 0
+        for n, L in zip(news, ctxs):
+            for i in range(n):
+                own = (L - n + i) // PAGE
+                for h in range(hkv):
+                    here = torch.randperm(own + 1, generator=gen)[:topk - 3].to(torch.int32)
+                    here = torch.cat([here[:len(here) - len(here) // 3], torch.tensor([own + 1, 1 << 30, -5], dtype=torch.int32)])
+                    blocks[row, h, torch.randperm(topk, generator=gen)[:len(here)]] = here
+                    blocks[row, h, topk - 1], last = here[0], blocks[row, h, topk - 1].clone()       # (one of them last of all)
+                    blocks[row, h, :topk - 1][blocks[row, h, :topk - 1] == here[0]] = last
+                row += 1
+        q = torch.randn((sum(news), hq, d), generator=_gen(16), device="cuda").to(p.torch_dtype)
+        _check_attn(m, p, c, q, news, ctxs, blocks.cuda())
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "native"])
 @pytest.mark.parametrize("dtype,hq,hkv,d,news,ctxs", [
     ("bf16", 32, 2, 128, [1], [9001]), ("bf16", 8, 2, 64, [1, 2], [5000, 20000]), ("fp32", 4, 1, 64, [1, 1], [6000, 130]),
     ("bf16", 32, 2, 128, [150], [3000]), ("bf16", 16, 2, 128, [40, 1, 333, 1], [40, 2000, 700, 1]), ("bf16", 8, 2, 64, [700], [1100])])
@@ -455,3 +480,88 @@ def test_captured_and_on_other_streams(m):
         torch.cuda.synchronize()
         for s, w in zip(steps, want):
             assert torch.equal(s["out"], w[0]) and torch.equal(s["lse"], w[1]) and torch.equal(s["blocks"], w[2])
+
+
+def test_chunks_captured(m):
+    """A chunk of a prompt for the tiles of 8 wavefronts and a few proposed tokens, appended and attended to in one captured graph."""
+    p = _params(m, "bf16", 32, 2, 128)
+    rot = m.Rotary(m.rotary_turns(128), 128)
+    news, prev = [200, 3], [5000, 700]
+    ctxs = [5200, 703]
+    c, _, _ = _filled(m, p, prev, "e4m3", 81)
+    table = torch.full((2, 82), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.page_table.shape[1]] = c.page_table
+    pages = c.k.shape[0]
+    c = m.PagedCache(p, *(torch.cat([x.view(torch.uint8), x.view(torch.uint8)[:8]]).view(torch.float8_e4m3fn) for x in (c.k, c.v)), table,
+                     *(torch.cat([x, x[:8]]) for x in (c.k_scale, c.v_scale)))
+    table[0, 79:82] = torch.tensor([pages, pages + 1, pages + 2], dtype=torch.int32)
+    cu, pv, cx = m.SeqInfo([0, 200, 203]), m.DecodeInfo(prev), m.DecodeInfo(ctxs)
+    k, v = (torch.empty((2, 203, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q, out = (torch.empty((203, 32, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    lse = torch.empty((203, 32), device="cuda")
+    ws = torch.empty(m.workspace_bytes(m.OP_CACHE_ATTN, p, 2, 203, 5200), dtype=torch.uint8, device="cuda")
+    pages = [x.view(torch.uint8) for x in (c.k, c.v)] + [c.k_scale, c.v_scale]
+    before = [x.clone() for x in pages]
+
+    def call():
+        m.cache_append(p, c, k, v, cu, pv, rot)
+        m.cache_attn(p, c, q, cu, cx, out=out, lse=lse, workspace=ws)
+
+    def inputs(seed):
+        gen = _gen(seed)
+        for x in (k, v, q):
+            x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+        for x, y in zip(pages, before):
+            x.copy_(y)
+        out.zero_()
+
+    inputs(1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for seed in (2, 3, 4):
+        inputs(seed)
+        call()
+        torch.cuda.synchronize()
+        want = [x.clone() for x in [out, lse] + pages]
+        inputs(seed)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip([out, lse] + pages, want))
+    sc = (c.k_scale, c.v_scale)
+    exact, exact_lse, mass = paged.attention(q, c.k, c.v, sc, table, news, ctxs, p.softmax_scale)
+    assert bool(((out.double() - exact).abs() <= 2.0 ** -8 * exact.abs() + 6 * 2.0 ** -12 + 2.0 ** -8 * mass).all())
+    assert float((lse.double() - exact_lse).abs().max()) <= 1e-4
+
+
+def test_arguments_that_do_not_fit(m):
+    """Refused before a call: another dtype or number of heads than the cache's, a table without room, wrong shapes."""
+    p = _params(m, "bf16", 8, 2, 64)
+    c, k, v = _filled(m, p, [100, 300], "native", 91)
+    q = torch.zeros((2, 8, 64), dtype=torch.bfloat16, device="cuda")
+    kc = torch.zeros((2, 2, 20, 64), device="cuda")
+    new = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    wide = torch.full((2, 100), 0, dtype=torch.int32, device="cuda")
+    part = m.PagedCache(p, c.k, c.v, wide[:, :5])              # room for 320 tokens each
+    other = _params(m, "bf16", 16, 4, 64)
+    fp32 = _params(m, "fp32", 8, 2, 64)
+    for call in (lambda: m.cache_attn(other, c, torch.zeros((2, 16, 64), dtype=torch.bfloat16, device="cuda"), [0, 1, 2], [100, 300]),
+                 lambda: m.cache_attn(fp32, c, q.float(), [0, 1, 2], [100, 300]),
+                 lambda: m.cache_attn(p, part, q, [0, 1, 2], [100, 321]),
+                 lambda: m.cache_attn(p, c, q[:, :4], [0, 1, 2], [100, 300]),
+                 lambda: m.cache_append(fp32, c, new.float(), new.float(), [0, 1, 2], [100, 300]),
+                 lambda: m.cache_append(p, part, new, new, [0, 1, 2], [100, 320]),
+                 lambda: m.cache_compress_k(p, part, kc, [100, 300], [100, 321]),
+                 lambda: m.cache_compress_k(other, c, torch.zeros((2, 4, 20, 64), device="cuda"), [0, 0], [100, 300]),
+                 lambda: m.decode_blocks(p, q, kc[:, :1].contiguous(), [100, 300]),
+                 lambda: m.decode_blocks(p, q, kc, [100, 300], out=torch.empty((2, 2, 3), dtype=torch.int32, device="cuda"))):
+        with pytest.raises(AssertionError):
+            call()
+    m.cache_append(p, part, new[:, :1], new[:, :1], [0, 1, 1], [319, 320])   # the last row that fits
+    with pytest.raises(m.InfllmV2Error):
+        m.cache_attn(p, c, q, [0, 1, 2], [100, 100000])
