@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
         len = a.ctx[seq];
         // (the first list entries are requested beside the length that says whether there is a list)
         if (a.idx != nullptr)
-            early = a.idx[((int64_t)seq * hkv + rem / a.even) * a.topk + min(rem % a.even * a.pps + w + lane * NW, a.topk - 1)];
+            early = a.idx[((int64_t)seq * hkv + rem / a.even) * a.topk + min(rem % a.even * NW + w + lane * NW * a.even, a.topk - 1)];
     } else {
         int64_t slot0;
         cache::Facts f;
@@ -262,9 +262,10 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     const int pos0 = len - n + first, pos_last = pos0 + ntok - 1;
     const int nsplit = a.splits(len, pos_last);
     if (split >= nsplit) return;
-    // the entries of this split: a list that is longer than the pages there can be is cut into as many equal parts
-    const int pages = a.pages(len, pos_last), entries = listed ? a.topk : pages, each = entries > pages ? (entries + nsplit - 1) / nsplit : a.pps;
-    const int e_first = split * each, e_end = min(entries, e_first + each);
+    // the entries of this wavefront: of all pages a run for each split; of a list (which may be longer than the pages there can be, and hold them
+    // anywhere) every (NW x nsplit)-th
+    const int e_first = listed ? split * NW + w : split * a.pps + w, e_step = listed ? NW * nsplit : NW;
+    const int e_end = listed ? a.topk : min(a.pages(len, pos_last), (split + 1) * a.pps);
     const int ti = m / G;                                                                // this lane's column
     const bool used = ti < ntok;
     const int pos = used ? pos0 + ti : -1;
@@ -284,13 +285,13 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     const int32_t *list = a.idx + ((int64_t)(row0 + first) * hkv + h) * a.topk;
     const uint32_t tok = (uint32_t)a.c.tok_stride;
     const uint32_t k_off = m * tok + KeyTile<T, D, CODES>::lane_offset(g), v_off = 4 * g * tok + m * ValueRow<T, D, CODES>::BYTES;
-    // a wavefront takes every NW-th page of the split; lane l holds the l-th of the next 64: where it is, its first key, its scales
-    for (int e0 = e_first + w; e0 < e_end; e0 += 64 * NW) {
-        const int e = e0 + lane * NW;
+    // lane l holds the l-th of the next 64 pages: where it is, its first key, its scales
+    for (int e0 = e_first; e0 < e_end; e0 += 64 * e_step) {
+        const int e = e0 + lane * e_step;
         int my_page = -1, my_key0 = 0;
         float my_ks = 1.f, my_vs = 1.f;
         if (e < e_end) {
-            const int j = !listed ? e : a.even && each == a.pps && e0 < e_first + NW ? early : list[e];
+            const int j = !listed ? e : nsplit == a.even && e0 == e_first ? early : list[e];
             if (j >= 0 && j <= pos_last / kBlock) {
                 my_page = a.c.page(seq, j);
                 my_key0 = j * kBlock;
@@ -552,6 +553,12 @@ int launch_t(const AttnArgs &a, int64_t items, int64_t merges, hipStream_t strea
 
 constexpr int kTargetGroups = 2048;        // workgroups that a call is cut into: four rounds of two for each CU
 constexpr int kLeastPages = NW;            // a page for each wavefront; two once that makes a workgroup for each CU (16 sequences, 64 blocks each: 19.3 -> 17.3 us)
+// Pages that a call does not split, to save the second launch: 256 KB of them (fp32 data: as if of the data's type, the products take longer than the
+// rows).  One token of 2 sequences, split / whole: e4m3, d 128, 12 pages 15 / 12 us, 16 pages 15.3 / 12.9, 24 pages 15.2 / 15.4; bf16 pages, 8
+// pages 15.3 / 11.4, 16 pages 15 / 15.9; fp32, d 128, 8 pages 15.9 / 17.2, 16 pages 16 / 27.
+int whole_pages(const infllmv2_params *p, bool codes) {
+    return 256 * 1024 / (2 * kBlock * p->head_dim * (p->dtype == INFLLMV2_FP32 ? 4 : codes ? 1 : 2));
+}
 constexpr int kMostPages = 1 << 25;        // of a context: with so many to a split there is one split
 // Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
 // kTargetGroups, so at most 2 kTargetGroups partial results.
@@ -621,7 +628,7 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     a.tile_groups = 1;
     AttnArgs wide = a;                         // the tile kernel's launch
     wide.tile_groups = cache_attn::tile_groups(p);
-    int max_ctx = 0, wide_pages = 0;
+    int max_ctx = 0, wide_pages = 0, most_pages = 0;
     int64_t work = 0, wide_work = 0, wide_tiles = 0;       // pages over column groups (or listed tokens) and heads of each kernel's sequences; tiles and heads
     for (int b = 0; b < batch; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
@@ -634,10 +641,12 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
         (other > 0 ? wide_work : work) += groups;
         wide_tiles += other;
         if (other > 0 && pages > wide_pages) wide_pages = pages;
+        if (other == 0 && pages > most_pages) most_pages = pages;
     }
     if (!rules::tile_pays(wide_tiles, wide_pages, wide_work)) {
         a.wide_from = wide.wide_from = INT32_MAX;
         work += wide_work;
+        if (wide_pages > most_pages) most_pages = wide_pages;
         wide_tiles = 0;
     }
     for (int b = 0; b < batch && !a.multi; ++b) {
@@ -651,6 +660,8 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     const int64_t share = (work + kTargetGroups - 1) / kTargetGroups;
     const int least = work > 256 * kLeastPages ? 2 * kLeastPages : kLeastPages;
     a.pps = share < least ? least : share > kMostPages ? kMostPages : (int)share;
+    const int whole = whole_pages(p, c->kv_type == INFLLMV2_CACHE_E4M3);
+    if (most_pages <= whole && a.pps < whole) a.pps = whole;
     wide.pps = wide_tiles > 0 ? rules::tile_splits(wide_tiles, wide_pages).pps : 1;
     Launches mine, other;
     bool single = true;                        // one query token for each sequence
