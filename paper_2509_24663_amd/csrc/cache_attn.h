@@ -18,7 +18,7 @@ struct AttnArgs {
     int batch, hq, topk, dense_below;
     int group_tokens;                  // of 16 columns over all keys (16 / G)
     int wide_from;                     // sequences over all keys with so many queries are the tile kernel's
-    int tile_groups;                   // column groups of a tile of this launch (1: cache_attn.hip)
+    int tile_groups;                   // column groups of a tile of this launch (1: cache_attn.hip; rules::tile_size)
     int pps;                           // pages of a split
     int even;                          // > 0: one query token for each sequence, item = (sequence, head, split < even); slots alike
     int multi;                         // some tile of cache_attn.hip has more than one token
@@ -43,7 +43,6 @@ struct AttnArgs {
 };
 
 // cache_attn_tile.hip
-int tile_groups(const infllmv2_params *p);
 int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream);
 
 }  // namespace cache_attn

@@ -459,13 +459,18 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------ joining the splits of a tile
-// Four columns per workgroup, D / 4 threads of four channels each; up to kAhead splits are requested at once.
-constexpr int kMergeCols = 4, kAhead = 8;
+// COLS columns per workgroup, D / 4 threads of four channels each for SG shares of the splits; up to kAhead splits are requested at once by each.
+// Four columns and one share where that is all of the splits or there are columns enough for the chip, else one column and 16 shares (one token of one
+// sequence, 33000 keys, 65 splits: 20.7 -> 16.0 us; 130 tokens, 4608 columns, 15 splits: 92.8 -> 112.8).
+constexpr int kAhead = 8;
 
-template <typename T, int D>
-__global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
+template <typename T, int D, int SG, int COLS>
+__global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs a) {
+    constexpr int kThreads = D / 4 * COLS;               // of a share
     __shared__ int64_t s_item[6];
-    const int tid = threadIdx.x, hkv = a.c.hkv, G = a.hq / hkv;
+    __shared__ f32x4 s_o[SG == 1 ? 1 : SG - 1][SG == 1 ? 1 : kThreads];
+    __shared__ float2 s_ml[SG == 1 ? 1 : SG - 1][COLS];
+    const int tid = threadIdx.x % kThreads, sg = threadIdx.x / kThreads, hkv = a.c.hkv, G = a.hq / hkv;
     int th, seq, row0, n, len;
     int64_t slot;
     if (a.even) {
@@ -497,14 +502,14 @@ __global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
     const int h = th % hkv, tile = th / hkv, T0 = a.tile_tokens(len), first = tile * T0, ntok = min(T0, n - first);
     const int nsplit = a.splits(len, len - n + first + ntok - 1);
     if (nsplit == 1) return;                             // (written by the split itself)
-    const int col = blockIdx.y * kMergeCols + tid / (D / 4), c0 = (tid % (D / 4)) * 4, m = col & 15;
+    const int col = blockIdx.y * COLS + tid / (D / 4), c0 = (tid % (D / 4)) * 4, m = col & 15;
     const int in_group = m / G, ti = (col >> 4) * a.group_tokens + in_group;
-    if (in_group >= min(T0, a.group_tokens) || ti >= ntok) return;
+    const bool used = in_group < min(T0, a.group_tokens) && ti < ntok;
     const float *src = a.part + (slot * cols + col) * D + c0;
     const float2 *ml = reinterpret_cast<const float2 *>(a.ml) + slot * cols + col;
     float top = -INFINITY, total = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < nsplit; s0 += kAhead) {
+    for (int s0 = sg * kAhead; used && s0 < nsplit; s0 += SG * kAhead) {
         float2 x[kAhead];
         f32x4 y[kAhead];
 #pragma unroll
@@ -529,6 +534,29 @@ __global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
         }
         top = to;
     }
+    if constexpr (SG > 1) {                              // the shares' results, by the threads of the first
+        if (sg > 0) {
+            s_o[sg - 1][tid] = o;
+            if (c0 == 0) s_ml[sg - 1][tid / (D / 4)] = float2{top, total};
+        }
+        __syncthreads();
+        if (sg > 0) return;
+        float to = top;
+#pragma unroll
+        for (int i = 0; i < SG - 1; ++i) to = fmaxf(to, s_ml[i][tid / (D / 4)].x);
+        const float base = to == -INFINITY ? 0.f : to, f0 = exp2_fast(top - base);
+        total *= f0;
+        o *= f0;
+#pragma unroll
+        for (int i = 0; i < SG - 1; ++i) {
+            const float2 x = s_ml[i][tid / (D / 4)];
+            const float f = exp2_fast(x.x - base);
+            total += x.y * f;
+            o += s_o[i][tid] * f;
+        }
+        top = to;
+    }
+    if (!used) return;
     const int64_t row = row0 + first + ti;
     const int qh = h * G + m - in_group * G;
     const float inv = top == -INFINITY ? 0.f : 1.f / total;
@@ -536,39 +564,6 @@ __global__ void __launch_bounds__(D) cache_merge_kernel(AttnArgs a) {
     gen::store_row<T, 4>(reinterpret_cast<T *>(a.out) + (row * a.hq + qh) * D + c0, r);
     if (c0 == 0 && a.lse != nullptr) a.lse[row * a.hq + qh] = top == -INFINITY ? -INFINITY : top * kLn2 + logf(total);
 }
-
-template <typename T, int D>
-void merge(const AttnArgs &a, int64_t merges, hipStream_t stream) {
-    if (merges > 0)
-        hipLaunchKernelGGL((cache_merge_kernel<T, D>), dim3((unsigned)merges, 16 * a.tile_groups / kMergeCols), dim3(D), 0, stream, a);
-}
-
-template <typename T, int D, bool CODES, int TILES>
-int launch_t(const AttnArgs &a, int64_t items, int64_t merges, hipStream_t stream) {
-    if (a.multi) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, true>), dim3((unsigned)items), dim3(NW * 64), 0, stream, a);
-    else hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, false>), dim3((unsigned)items), dim3(NW * 64), 0, stream, a);
-    merge<T, D>(a, merges, stream);
-    return hip_status(hipGetLastError());
-}
-
-constexpr int kTargetGroups = 2048;        // workgroups that a call is cut into: four rounds of two for each CU
-constexpr int kLeastPages = NW;            // a page for each wavefront; two once that makes a workgroup for each CU (16 sequences, 64 blocks each: 19.3 -> 17.3 us)
-// Pages that a call does not split, to save the second launch: 256 KB of them (fp32 data: as if of the data's type, the products take longer than the
-// rows).  One token of 2 sequences, split / whole: e4m3, d 128, 12 pages 15 / 12 us, 16 pages 15.3 / 12.9, 24 pages 15.2 / 15.4; bf16 pages, 8
-// pages 15.3 / 11.4, 16 pages 15 / 15.9; fp32, d 128, 8 pages 15.9 / 17.2, 16 pages 16 / 27.
-int whole_pages(const infllmv2_params *p, bool codes) {
-    return 256 * 1024 / (2 * kBlock * p->head_dim * (p->dtype == INFLLMV2_FP32 ? 4 : codes ? 1 : 2));
-}
-constexpr int kMostPages = 1 << 25;        // of a context: with so many to a split there is one split
-// Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
-// kTargetGroups, so at most 2 kTargetGroups partial results.
-size_t slot_bytes(int d, int groups) { return (size_t)16 * groups * (d + 2) * sizeof(float); }
-// Least queries of a sequence for which the tile kernel is thought of (bf16 data)
-int tile_from(const infllmv2_params *p) {
-    return p->dtype == INFLLMV2_BF16 ? (rules::kTileFrom - 1) * (kCols / (p->num_q_heads / p->num_kv_heads)) + 1 : INT32_MAX;
-}
-size_t unit_bytes(const infllmv2_params *p, int64_t slots) { return align256((size_t)slots * slot_bytes(p->head_dim, 1)); }
-size_t tile_bytes(const infllmv2_params *p, int64_t slots) { return align256((size_t)slots * slot_bytes(p->head_dim, cache_attn::tile_groups(p))); }
 
 // what a launch covers: workgroups, tiles with several splits, their partial results
 struct Launches {
@@ -584,21 +579,53 @@ struct Launches {
     }
 };
 
+template <typename T, int D>
+void merge(const AttnArgs &a, const Launches &l, hipStream_t stream) {
+    if (l.merges == 0) return;
+    const unsigned cols = 16 * a.tile_groups;
+    if (l.most <= kAhead || l.merges * cols > 1024) hipLaunchKernelGGL((cache_merge_kernel<T, D, 1, 4>), dim3((unsigned)l.merges, cols / 4), dim3(D), 0, stream, a);
+    else hipLaunchKernelGGL((cache_merge_kernel<T, D, 16, 1>), dim3((unsigned)l.merges, cols), dim3(4 * D), 0, stream, a);
+}
+
+template <typename T, int D, bool CODES, int TILES>
+int launch_t(const AttnArgs &a, const Launches &l, hipStream_t stream) {
+    if (a.multi) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, true>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
+    else hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, false>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
+    merge<T, D>(a, l, stream);
+    return hip_status(hipGetLastError());
+}
+
+constexpr int kMostGroups = 2048;          // a workgroup has at least all pages / kMostGroups
+constexpr int kLeastPages = NW;            // .. and a page for each wavefront
+constexpr int kMostPages = 1 << 25;        // of a context: with so many to a split there is one split
+// Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
+// kMostGroups, so at most 2 kMostGroups partial results.
+size_t slot_bytes(int d, int groups) { return (size_t)16 * groups * (d + 2) * sizeof(float); }
+// Least queries of a sequence for which the tile kernel is thought of (bf16 data)
+int tile_from(const infllmv2_params *p) {
+    return p->dtype == INFLLMV2_BF16 ? (rules::kTileFrom - 1) * (kCols / (p->num_q_heads / p->num_kv_heads)) + 1 : INT32_MAX;
+}
+size_t unit_bytes(const infllmv2_params *p, int64_t slots) { return align256((size_t)slots * slot_bytes(p->head_dim, 1)); }
+size_t tile_bytes(const infllmv2_params *p, int64_t slots, int groups) { return align256((size_t)slots * slot_bytes(p->head_dim, groups)); }
+
 }  // namespace
 
 size_t cache_attn_ws_bound(const infllmv2_params *p, int32_t batch, int64_t tokens, int32_t max_ctx) {
     const int64_t most = (max_ctx + (int64_t)kBlock - 1) / kBlock, per = (most + kLeastPages - 1) / kLeastPages;
     const int64_t units = tokens * p->num_kv_heads;
-    const int64_t slots = per <= 1 ? 0 : units < 2 * kTargetGroups && units * per < 2 * kTargetGroups ? units * per : 2 * kTargetGroups;
+    const int64_t slots = per <= 1 ? 0 : units < 2 * kMostGroups && units * per < 2 * kMostGroups ? units * per : 2 * kMostGroups;
     // the tile kernel: at most tokens / (tokens of a tile) tiles and one more for each sequence
     const int64_t from = tile_from(p);
-    int64_t tiles = 0;
-    if (tokens >= from && most > 1) {
-        const int64_t per_tile = kCols / (p->num_q_heads / p->num_kv_heads) * cache_attn::tile_groups(p), seqs = tokens / from < batch ? tokens / from : batch;
-        tiles = (tokens / per_tile + seqs) * p->num_kv_heads * (most < rules::kMostTileSplits ? most : rules::kMostTileSplits);
-        if (tiles > rules::kMostTileResults) tiles = rules::kMostTileResults;
+    int64_t groups = 0;
+    for (bool small : {false, true}) {
+        if (tokens < from || most <= 1) break;
+        const int64_t tile = rules::tile_size(p->head_dim, small).groups, per_tile = kCols / (p->num_q_heads / p->num_kv_heads) * tile;
+        const int64_t seqs = tokens / from < batch ? tokens / from : batch;
+        const int64_t n = (tokens / per_tile + seqs) * p->num_kv_heads * (most < rules::kMostTileSplits ? most : rules::kMostTileSplits) * tile;
+        if (n > groups) groups = n;
     }
-    return unit_bytes(p, slots) + tile_bytes(p, tiles);
+    if (groups > rules::kMostTileGroups) groups = rules::kMostTileGroups;
+    return unit_bytes(p, slots) + tile_bytes(p, groups, 1);
 }
 
 }  // namespace ifv2
@@ -626,28 +653,39 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     a.group_tokens = kCols / (p->num_q_heads / hkv);
     a.wide_from = tile_from(p);
     a.tile_groups = 1;
-    AttnArgs wide = a;                         // the tile kernel's launch
-    wide.tile_groups = cache_attn::tile_groups(p);
-    int max_ctx = 0, wide_pages = 0, most_pages = 0;
-    int64_t work = 0, wide_work = 0, wide_tiles = 0;       // pages over column groups (or listed tokens) and heads of each kernel's sequences; tiles and heads
+    AttnArgs wide = a;                         // the tile kernel's launch, with large tiles or small ones
+    const rules::TileSize size[2] = {rules::tile_size(p->head_dim, false), rules::tile_size(p->head_dim, true)};
+    int max_ctx = 0, wide_pages = 0;
+    rules::PageWork work, wide_work;           // of the kernel of 16 columns; of the sequences that could be either's, if they are its own as well
+    int64_t tiles[2] = {0, 0}, tile_pages[2] = {0, 0}, unit_pages = 0;       // of the sequences that could be either's: what they are in tiles, pages in all
     for (int b = 0; b < batch; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
         if (len < n || len > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
         if (n == 0) continue;
         if (len > max_ctx) max_ctx = len;
         const int pages = a.pages(len, len - 1);
-        const int64_t other = (int64_t)wide.tiles(n, len) * hkv;
-        const int64_t groups = (int64_t)((n + a.tile_tokens(len) - 1) / a.tile_tokens(len)) * hkv * pages;
-        (other > 0 ? wide_work : work) += groups;
-        wide_tiles += other;
-        if (other > 0 && pages > wide_pages) wide_pages = pages;
-        if (other == 0 && pages > most_pages) most_pages = pages;
+        const int64_t groups = (int64_t)((n + a.tile_tokens(len) - 1) / a.tile_tokens(len)) * hkv;
+        if (a.listed(len) || n < a.wide_from) {
+            work.add(groups, pages, a.listed(len) ? groups * pages : (int64_t)hkv * pages);
+            continue;
+        }
+        wide_work.add(groups, pages, (int64_t)hkv * pages);
+        if (pages > wide_pages) wide_pages = pages;
+        const int first = (len - n) / kBlock + 1;                            // pages that the first token sees
+        unit_pages += groups * (first + pages) / 2;
+        for (int i = 0; i < 2; ++i) {
+            const int t0 = a.group_tokens * size[i].groups, t = (n + t0 - 1) / t0, low = t > 1 ? (len - n + t0 - 1) / kBlock + 1 : pages;
+            tiles[i] += (int64_t)t * hkv;
+            tile_pages[i] += (int64_t)t * hkv * (low + pages) / 2;
+        }
     }
-    if (!rules::tile_pays(wide_tiles, wide_pages, wide_work)) {
+    const rules::TileSplits large = rules::tile_splits(size[0], tiles[0], wide_pages, tile_pages[0]), small = rules::tile_splits(size[1], tiles[1], wide_pages, tile_pages[1]);
+    const bool use_small = small.us < large.us;
+    wide.tile_groups = size[use_small].groups;
+    wide.pps = use_small ? small.pps : large.pps;
+    if (tiles[0] == 0 || rules::unit_us(p->head_dim, wide_pages, unit_pages) <= (use_small ? small.us : large.us)) {
         a.wide_from = wide.wide_from = INT32_MAX;
-        work += wide_work;
-        if (wide_pages > most_pages) most_pages = wide_pages;
-        wide_tiles = 0;
+        work.add(wide_work);
     }
     for (int b = 0; b < batch && !a.multi; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
@@ -657,12 +695,9 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     if (st) return st;
     // (rows of a page are addressed with 32-bit offsets)
     if (c->tok_stride > (1ll << 24)) return INFLLMV2_ERR_UNSUPPORTED;
-    const int64_t share = (work + kTargetGroups - 1) / kTargetGroups;
-    const int least = work > 256 * kLeastPages ? 2 * kLeastPages : kLeastPages;
-    a.pps = share < least ? least : share > kMostPages ? kMostPages : (int)share;
-    const int whole = whole_pages(p, c->kv_type == INFLLMV2_CACHE_E4M3);
-    if (most_pages <= whole && a.pps < whole) a.pps = whole;
-    wide.pps = wide_tiles > 0 ? rules::tile_splits(wide_tiles, wide_pages).pps : 1;
+    const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3, fp32 = p->dtype == INFLLMV2_FP32;
+    const int64_t share = (work.sum + kMostGroups - 1) / kMostGroups;
+    a.pps = share >= kMostPages ? kMostPages : rules::unit_pps(work, p->head_dim, fp32, codes ? 1 : fp32 ? 4 : 2, share);
     Launches mine, other;
     bool single = true;                        // one query token for each sequence
     for (int b = 0; b < batch; ++b) {
@@ -671,14 +706,16 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
         other.add(wide, n, len);
         single = single && n == 1;
     }
-    // as many workgroups for each (sequence, head), some with nothing to do: nothing has to be looked up
-    if (single && (int64_t)batch * hkv * mine.most <= 2 * kTargetGroups) {
+    // as many workgroups for each (sequence, head): nothing has to be looked up.  Where those with nothing to do are few, or a CU each: others are placed
+    // beside them, not evenly (16 sequences of 1000 to 33000 keys: 54.5 us, looked up 41.4)
+    const int64_t alike = (int64_t)batch * hkv * mine.most;
+    if (single && alike <= 2 * kMostGroups && (alike <= 256 || 10 * alike <= 11 * mine.items)) {
         a.even = mine.most;
-        mine.items = (int64_t)batch * hkv * mine.most;
+        mine.items = alike;
         mine.merges = mine.most > 1 ? (int64_t)batch * hkv : 0;
         mine.slots = mine.most > 1 ? mine.items : 0;
     }
-    const size_t need = unit_bytes(p, mine.slots), wide_need = tile_bytes(p, other.slots);
+    const size_t need = unit_bytes(p, mine.slots), wide_need = tile_bytes(p, other.slots, wide.tile_groups);
     st = check_ws(workspace_d, workspace_bytes, need + wide_need);
     if (st) return st;
     if (mine.items >= (1ll << 31) || other.items >= (1ll << 31)) return INFLLMV2_ERR_UNSUPPORTED;
@@ -696,20 +733,19 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     a.ml = a.part + mine.slots * 16 * p->head_dim;
     wide.part = (float *)((char *)workspace_d + need);
     wide.ml = wide.part + other.slots * 16 * wide.tile_groups * p->head_dim;
-    const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
     const hipStream_t s = (hipStream_t)stream;
     if (other.items > 0) {
         st = cache_attn::launch_tile(wide, p, codes, other.items, s);
         if (st) return st;
-        if (p->head_dim == 128) merge<bf16_t, 128>(wide, other.merges, s);
-        else merge<bf16_t, 64>(wide, other.merges, s);
+        if (p->head_dim == 128) merge<bf16_t, 128>(wide, other, s);
+        else merge<bf16_t, 64>(wide, other, s);
         if (mine.items == 0) return hip_status(hipGetLastError());
     }
     // keys of a step: 64 codes, 32 bf16, 16 fp32 rows take the same registers
     if (p->head_dim == 128) {
-        if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 128, true, 4>(a, mine.items, mine.merges, s) : launch_t<bf16_t, 128, false, 2>(a, mine.items, mine.merges, s);
-        return codes ? launch_t<float, 128, true, 2>(a, mine.items, mine.merges, s) : launch_t<float, 128, false, 1>(a, mine.items, mine.merges, s);
+        if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 128, true, 4>(a, mine, s) : launch_t<bf16_t, 128, false, 2>(a, mine, s);
+        return codes ? launch_t<float, 128, true, 2>(a, mine, s) : launch_t<float, 128, false, 1>(a, mine, s);
     }
-    if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 64, true, 4>(a, mine.items, mine.merges, s) : launch_t<bf16_t, 64, false, 4>(a, mine.items, mine.merges, s);
-    return codes ? launch_t<float, 64, true, 2>(a, mine.items, mine.merges, s) : launch_t<float, 64, false, 2>(a, mine.items, mine.merges, s);
+    if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 64, true, 4>(a, mine, s) : launch_t<bf16_t, 64, false, 4>(a, mine, s);
+    return codes ? launch_t<float, 64, true, 2>(a, mine, s) : launch_t<float, 64, false, 2>(a, mine, s);
 }

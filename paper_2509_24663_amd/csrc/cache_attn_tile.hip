@@ -1,6 +1,7 @@
-// Attention of a chunk of a prompt over its paged cache, bf16 data: tiles of 8 x CG groups of 16 columns (a column is a token and a head of one KV head).
+// Attention of a chunk of a prompt over its paged cache, bf16 data: tiles of 8 x CG groups of 16 columns (a column is a token and a head of one KV head); CG = 2
+// (head dim 64: 4), or 1 where large tiles are too few for the chip (launch_rules.h).
 //
-// The workgroup's eight wavefronts go through the pages together and each keeps CG column groups (CG = 2; head dim 64: 4) with their queries and sums in
+// The workgroup's eight wavefronts go through the pages together and each keeps CG column groups with their queries and sums in
 // registers, so that an operand read from LDS feeds CG products.  S^T = K Q^T and O^T += V^T P^T on 16x16x32 products; a lane's logits of a
 // half page are eight consecutive keys of one column, which is the operand that the second product wants.
 // Half a page is a step: its logits, then the sums of the half before it with the weights of this one between the products (they do not depend on
@@ -20,6 +21,7 @@
 
 #include "attn_unit.h"
 #include "cache_attn.h"
+#include "launch_rules.h"
 
 namespace ifv2 {
 
@@ -34,7 +36,6 @@ using cache_attn::kLowest;
 constexpr int NW = 8;
 constexpr int kThreads = NW * 64;
 constexpr float kSlack = 64.f, kNoReference = -1e38f;
-constexpr int groups_of(int d) { return d == 128 ? 2 : 4; }
 constexpr int kAhead = 4;                  // operands requested in front of their product
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -79,7 +80,7 @@ struct Page {
 };
 
 template <int D, int CG, int W, bool CODES>
-__global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_attn_tile_kernel(AttnArgs a) {
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int KB = CODES ? 1 : 2;                               // bytes of an element
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // two K pages, three V pages, rows of V as they come
@@ -480,9 +481,9 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_tile_kernel(AttnArgs a
     }
 }
 
-template <int D, bool CODES>
+template <int D, int CG, bool CODES>
 int launch_d(const AttnArgs &a, int64_t items, hipStream_t stream) {
-    constexpr int CG = groups_of(D), LDS = 5 * Page<D>::kBytes + 64 * D * (CODES ? 1 : 2);
+    constexpr int LDS = 5 * Page<D>::kBytes + 64 * D * (CODES ? 1 : 2);
     const auto kernel = cache_attn_tile_kernel<D, CG, kAhead, CODES>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
         return INFLLMV2_ERR_HIP;
@@ -494,11 +495,16 @@ int launch_d(const AttnArgs &a, int64_t items, hipStream_t stream) {
 
 namespace cache_attn {
 
-int tile_groups(const infllmv2_params *p) { return NW * groups_of(p->head_dim); }
-
 int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream) {
-    if (p->head_dim == 128) return codes ? launch_d<128, true>(a, items, stream) : launch_d<128, false>(a, items, stream);
-    return codes ? launch_d<64, true>(a, items, stream) : launch_d<64, false>(a, items, stream);
+    static_assert(rules::tile_size(128, false).groups == 2 * NW && rules::tile_size(64, false).groups == 4 * NW, "the tiles that the rules count with");
+    static_assert(rules::tile_size(128, true).groups == NW && rules::tile_size(64, true).groups == NW, "the tiles that the rules count with");
+    const bool small = a.tile_groups == NW;
+    if (p->head_dim == 128) {
+        if (small) return codes ? launch_d<128, 1, true>(a, items, stream) : launch_d<128, 1, false>(a, items, stream);
+        return codes ? launch_d<128, 2, true>(a, items, stream) : launch_d<128, 2, false>(a, items, stream);
+    }
+    if (small) return codes ? launch_d<64, 1, true>(a, items, stream) : launch_d<64, 1, false>(a, items, stream);
+    return codes ? launch_d<64, 4, true>(a, items, stream) : launch_d<64, 4, false>(a, items, stream);
 }
 
 }  // namespace cache_attn

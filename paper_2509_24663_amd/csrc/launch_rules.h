@@ -3,6 +3,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 namespace ifv2 {
 namespace rules {
@@ -381,31 +382,104 @@ inline DecodeSplits decode_splits(int64_t pairs, int entries, int waves) {
     return {(int)bpw, (int)std::max<int64_t>((entries + bpw - 1) / bpw, 1)};
 }
 
-// Paged cache, chunks of prompts: splits along the keys of the tile kernel (cache_attn_tile.hip), whose workgroups go over the 256 CUs in rounds, one on a
-// CU; `pages`: of the longest tile.  A page takes 1.85 us, a workgroup 3 us before and after its pages, a call 9; several splits cost a
-// launch of 4 us and 0.05 us for each partial result (128 KB written and read).  Measured (G 16, d 128, 33000 cached tokens), 2 / 16 / 130 / 512 / 2048 tokens:
-// see the table at tile_pays.
-constexpr int kMostTileSplits = 64, kMostTileResults = 1024;
+// Paged cache, workgroups of 16 columns (cache_attn.hip): what a call goes through, by how many pages a unit (a column group or listed token of a KV head) has.
+struct PageWork {
+    static constexpr int kKinds = 16;        // different numbers of pages that are counted exactly
+    int kinds = 0, most = 0, pages[kKinds];
+    int64_t units[kKinds], all = 0, sum = 0; // units, and pages over them, of all kinds
+    int64_t read = 0;                        // pages that come from memory
+    void add(int64_t n, int p, int64_t r) {
+        all += n;
+        sum += n * p;
+        read += r;
+        if (p > most) most = p;
+        int i = 0;
+        while (i < kinds && i < kKinds && pages[i] != p) ++i;
+        if (i < kinds && i < kKinds) units[i] += n;
+        else if (kinds++ < kKinds) pages[i] = p, units[i] = n;
+    }
+    void add(const PageWork &o) {
+        const int64_t n = all + o.all, p = sum + o.sum;
+        for (int i = 0; i < o.kinds && i < kKinds; ++i) add(o.units[i], o.pages[i], 0);
+        all = n;
+        sum = p;
+        read += o.read;
+        if (o.most > most) most = o.most;
+        if (o.kinds > kKinds) kinds = kKinds + 1;
+    }
+    // workgroups of pps pages each
+    int64_t groups(int pps) const {
+        if (kinds > kKinds) return sum / pps + all / 2 + 1;
+        int64_t n = 0;
+        for (int i = 0; i < kinds; ++i) n += units[i] * ((pages[i] + pps - 1) / pps);
+        return n;
+    }
+};
+// Pages of a workgroup (whose four wavefronts take them in turn).  Few: every CU has work soon; many: less to start and to join.  512 workgroups run at
+// once, two on a CU; starting those of each 256 is taken to cost 2.5 us, a page of a wavefront 0.6 us and 0.75 for each 16 KB of K and V (fp32 data, whose products take
+// longer: 2.6 for each 64 channels) or its share of 6 TB/s, less where the last workgroups leave CUs idle (sequences of many
+// lengths even out); a partial result 7 ns, the launch that joins
+// them 5 us.  Measured, one call, us, by pages 4 / 8 / 16 / 32 / 64 (one token each, 2 KV heads, d 128): 1 sequence of 33000 keys, e4m3 16.7 / 16.0 / 18.1 /
+// 22.7 / 32.9, bf16 19.6 / 17.5 / 21.1 / 29.3 / 46.4, fp32 27.9 / 23.9 / 34 / 54 / 96; of 500000, e4m3 107 / 77 / 65 / 58 / 56; 16 of 8000 29 / 24 / 21 / 23 /
+// 32; 64 of 16384 to 65536 478 / 347 / 294 / 315 / 285.  Split or not: 2 sequences, e4m3, 12 pages 15 / 12, 24 pages 15.2 / 15.4; bf16, 8 pages 15.3 /
+// 11.4, 16 pages 15 / 15.9; fp32, 8 pages 15.9 / 17.2.
+inline int unit_pps(const PageWork &w, int d, bool fp32, int bytes, int64_t least) {
+    const int64_t from = (least + 3) / 4 * 4 < 4 ? 4 : (least + 3) / 4 * 4, whole = ((int64_t)w.most + 3) / 4 * 4;
+    if (from >= whole) return (int)from;
+    const double page_bytes = 2. * 64 * d * bytes, page_us = fp32 ? 2.6 * d / 64 : 0.6 + 0.75 * page_bytes / 16384;
+    int64_t best = from;
+    double best_us = 0;
+    for (int64_t pps = from;; pps = pps < 8 ? 8 : pps < 32 ? pps + 8 : pps * 3 / 2 / 4 * 4) {
+        if (pps > 128 || pps > whole) pps = whole;
+        const int64_t n = w.groups((int)pps), rounds = (n + 511) / 512;
+        const double idle = std::sqrt((double)((n + 255) / 256 * 256) / n), uneven = n > 256 && w.kinds <= 4 ? idle : std::sqrt(idle);
+        const double way = page_us * (pps / 4) * rounds, bytes_us = w.read * page_bytes / 6e6 * uneven;
+        const double us = 2.5 + 2.5 * ((n + 255) / 256) + (way > bytes_us ? way : bytes_us) + 0.007 * n + (pps < w.most ? 5 : 0);
+        if (pps == from || us < best_us) best = pps, best_us = us;
+        if (pps == whole) break;
+    }
+    return (int)best;
+}
+
+// Paged cache, chunks of prompts: cache_attn_tile.hip takes a sequence's queries in tiles of `groups` column groups (16 columns each), a workgroup over the
+// pages of one.  Two sizes: large tiles read the least of LDS for a product, small ones fill the chip where there are few of them.
+struct TileSize {
+    int groups;
+    double page_us, result_us;      // a page of a workgroup; a partial result written and read (128 KB; head dim 64: 128, small 34 to 66)
+};
+constexpr TileSize tile_size(int d, bool small) {
+    if (small) return d == 128 ? TileSize{8, 1.13, 0.03} : TileSize{8, 0.75, 0.01};
+    return d == 128 ? TileSize{16, 1.75, 0.05} : TileSize{32, 1.9, 0.05};
+}
+// Splits along the keys for `tiles` workgroups with up to `pages` pages, `sum` in all, on 256 CUs.  A call is taken to cost 14.7 us and its longest way:
+// rounds of workgroups, or where tiles differ (a prompt from its first token) their sum dealt out; several splits 1.5 us for the second launch and
+// result_us each.  Measured, one call, us (G 16, d 128, e4m3, 512 tokens over 8000, 1 / 2 / 4 splits): large tiles 231 / 134 / 84.6, small
+// 156 / 94.8 / 105; 300 over 1300, 1 / 3: 52 / 36, 36 / 30; G 4, d 64, 72 over 6800, 1 / 4 / 12: 219 / 71 / 37.5, 94 / 35 / 22.7.
+constexpr int kMostTileSplits = 64, kMostTileGroups = 16384;        // splits of a tile; column groups of all partial results
 struct TileSplits {
     int pps;               // pages of a split
     double us;             // what the launch is taken to cost
 };
-inline TileSplits tile_splits(int64_t tiles, int pages) {
+inline TileSplits tile_splits(const TileSize &z, int64_t tiles, int pages, int64_t sum) {
     TileSplits best{pages, 0};
-    for (int s = 1; s <= kMostTileSplits && s <= pages && (s == 1 || tiles * s <= kMostTileResults); ++s) {
+    for (int s = 1; s <= kMostTileSplits && s <= pages && (s == 1 || tiles * s * z.groups <= kMostTileGroups); ++s) {
         const int per = (pages + s - 1) / s;
-        const double us = 9 + (double)((tiles * s + 255) / 256) * (1.85 * per + 3) + (s > 1 ? 4 + 0.05 * tiles * s : 0);
+        const int64_t rounds = (tiles * s + 255) / 256;
+        const double dealt = (double)sum / 256 + per / 2., way = rounds > 1 && dealt < (double)rounds * per ? dealt : (double)rounds * per;
+        const double us = 14.7 + z.page_us * way + 3. * (rounds - 1) + (s > 1 ? 1.5 + z.result_us * tiles * s : 0);
         if (s == 1 || us < best.us) best = {per, us};
     }
     return best;
 }
-// Whether the tile kernel pays for sequences with at least kTileFrom column groups (16 columns) of queries, against the kernel of 16 columns: group_pages is
-// what that one goes through, pages over all column groups and KV heads; 3.5 ns each while they fill the chip a few times, 1.4 once rows come from the L2.
-constexpr int kTileFrom = 4;
-inline bool tile_pays(int64_t tiles, int pages, int64_t group_pages) {
-    const double few = group_pages < 20000 ? (double)group_pages : 20000.;
-    return tiles > 0 && tile_splits(tiles, pages).us < 12 + 3.5e-3 * few + 1.4e-3 * (group_pages - few);
+// What the kernel of 16 columns (cache_attn.hip) is taken to cost: `sum`: pages over all its column groups and KV heads; once there are many, rows come from
+// the L2; long ones cost the joining of many splits.  d 128: 600 groups over 21 pages 55 us, 2200 over 18 (half of them, on average) 75, 1024 over 126 200, 8 over 516 38; d 64: 366 over 9 17 us,
+// 256 over 125 50.
+inline double unit_us(int d, int pages, int64_t sum) {
+    const double few = sum < 20000 ? (double)sum : 20000.;
+    return 13 + 0.02 * (pages < 500 ? pages : 500) + (d == 128 ? 3.2e-3 : 1.2e-3) * few + (d == 128 ? 1.4e-3 : 1.2e-3) * (sum - few);
 }
+// The sequences that tiles are thought of for: those with at least so many column groups of queries
+constexpr int kTileFrom = 4;
 
 }  // namespace rules
 }  // namespace ifv2

@@ -7,9 +7,10 @@ from test_gpu_cache import _check_attn, _filled, _gen, _params, m  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
-# 20000 and more pages over column groups of 16 and KV heads: the kernel of 16 columns is thought to take four times as long
+# Small tiles (launch_rules.h), then large ones: one split and several
 SHAPES = [(32, 2, 128, [150], [6001]), (8, 2, 64, [701], [6000]), (5, 5, 64, [703], [5990]), (12, 4, 128, [303], [6010]), (6, 6, 128, [257, 700], [2000, 5000]),
-          (16, 1, 64, [400], [5000]), (14, 2, 64, [333], [5050])]
+          (16, 1, 64, [400], [5000]), (14, 2, 64, [333], [5050]),
+          (32, 2, 128, [1400], [3001]), (12, 4, 128, [901], [7000]), (14, 2, 64, [905], [9000]), (5, 5, 64, [1703], [9001]), (8, 2, 64, [2000, 2005], [6000, 2005])]
 
 
 @pytest.mark.parametrize("kv", ["e4m3", "native"])
@@ -22,19 +23,19 @@ def test_chunks(m, kv, hq, hkv, d, news, ctxs):  # noqa: F811
 
 
 @pytest.mark.parametrize("kv", ["e4m3", "native"])
-@pytest.mark.parametrize("hq,hkv,d", [(32, 2, 128), (8, 2, 64)])
-def test_beside_single_tokens_and_lists(m, kv, hq, hkv, d):  # noqa: F811
+@pytest.mark.parametrize("hq,hkv,d,n,L", [(32, 2, 128, 130, 2990), (8, 2, 64, 600, 2990), (32, 2, 128, 700, 8100), (8, 2, 64, 1500, 8990)])
+def test_beside_single_tokens_and_lists(m, kv, hq, hkv, d, n, L):  # noqa: F811
     """One call: a chunk, single tokens, a skipped sequence, and (second) sequences with block lists; pages that are not there."""
     p = _params(m, "bf16", hq, hkv, d, topk_total=8, dense_threshold=3000)
-    n = 130 if hq == 32 else 600
-    news, ctxs = [1, n, 0, 1, n, 7], [2000, 2990, 100, 6000, n, 2900]
+    news, ctxs = [1, n, 0, 1, n, 7], [2000, L, 100, 6000, n, 2900]
     c, _, _ = _filled(m, p, ctxs, kv, 91)
     c.page_table[1, 0] = c.page_table[1, 7] = c.page_table[1, 20] = -1
-    c.page_table[1, (2990 - n // 2) // 64] = c.k.shape[0] + 5
+    c.page_table[1, (L - n // 2) // 64] = c.k.shape[0] + 5
     q = torch.randn((sum(news), hq, d), generator=_gen(16), device="cuda").to(torch.bfloat16)
     _check_attn(m, p, c, q, news, ctxs)
     blocks = torch.full((sum(news), hkv, 8), -1, dtype=torch.int32, device="cuda")
     blocks[n + 1, :, :3] = torch.tensor([93, 5, 40], dtype=torch.int32)
+    blocks[1:n + 1, :, 2] = 3                                # (L over the threshold: the chunk's as well)
     _check_attn(m, p, c, q, news, ctxs, blocks)
 
 
@@ -49,7 +50,8 @@ def test_no_page_at_all(m):  # noqa: F811
 
 
 @pytest.mark.parametrize("kv", ["e4m3", "native"])
-@pytest.mark.parametrize("hq,hkv,d,n,ctx", [(32, 2, 128, 150, 6001), (8, 2, 64, 701, 6000), (5, 5, 64, 703, 5990)])
+@pytest.mark.parametrize("hq,hkv,d,n,ctx", [(32, 2, 128, 150, 6001), (8, 2, 64, 701, 6000), (5, 5, 64, 703, 5990),
+                                            (32, 2, 128, 700, 7990), (14, 2, 64, 902, 9000)])
 def test_values_that_are_not_finite(m, kv, hq, hkv, d, n, ctx):  # noqa: F811
     """Rows behind a token, of the last page's end and one channel of an earlier row hold infinities and NaN: who does not see them is as if they were not
     there, bit for bit; who does gets them in their channels."""
