@@ -7,8 +7,12 @@
 // the keys.  Codes are widened on the way: K codes to bf16 with their page's scale (exact, a 3-bit mantissa times a power of two), V codes
 // after the permute, two keys of a channel per instruction.
 // A step's K is requested when the previous step's logits are done and its V when the previous step's sums are, so that one step is always
-// in flight.  The work of a (tile, KV head) is split along the keys over workgroups, and over the four wavefronts of each; partial results are joined in
-// LDS, then by cache_merge_kernel.
+// in flight.  The work of a (tile, KV head) is split along the keys over workgroups (launch_rules.h: unit_pps), and over the four wavefronts of each; partial
+// results are joined in LDS, then by cache_merge_kernel.
+//
+// Bound: HBM where the pages are many (64 sequences of 16384 to 65536 keys, 16 heads on 1, e4m3: 262 + 8 us for 1.37 GB, 5.1 TB/s; one of 500000: 55 us for 256 MB),
+// else a chain of trips to memory: length, page number, rows, partial results, joined results (16 sequences, 64 listed blocks each: 12 + 4 us; 5 sequences of 300 to
+// 2011 keys with 4 tokens each, fp32: 11 + 4.8).  fp32 data: the products, 2.6 us for a page of 64 channels and wavefront.
 #include "cache_attn.h"
 #include "launch_rules.h"
 
@@ -595,7 +599,7 @@ int launch_t(const AttnArgs &a, const Launches &l, hipStream_t stream) {
     return hip_status(hipGetLastError());
 }
 
-constexpr int kMostGroups = 2048;          // a workgroup has at least all pages / kMostGroups
+constexpr int kMostGroups = 2048;          // a workgroup has at least all pages / kMostGroups (64 sequences of 16384 to 65536 keys: 480 313 us, 2048 272)
 constexpr int kLeastPages = NW;            // .. and a page for each wavefront
 constexpr int kMostPages = 1 << 25;        // of a context: with so many to a split there is one split
 // Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /

@@ -8,15 +8,16 @@
 // each other: the vector unit works while the matrix core does).  A page is requested two pages ahead: K rows into registers, V rows (asynchronously) into a
 // buffer of the wavefront's own, from where transposing reads give a lane eight keys of a channel.  Beside the products of a first half they are widened
 // (codes times the page's scale: exact in bf16) and written as bf16 K and V^T pages, two and three buffers: one barrier per page.
-// Rounding: weights go into the second product as bf16 (2^-9 of each at most, like the output's own rounding); their sum takes them as they are.  References
+// Rounding: weights go into the second product as bf16 (2^-8 of each at most, like the output's own rounding); their sum takes them as they are.  References
 // move only where eight weights of a lane add up to more than kSlack, so a weight is below it.
 //
-// What bounds it: LDS and the matrix cores together.  2048 tokens over 34816, 32 heads on 2, e4m3: 966 to 996 us, 1130 to 1170 TFLOP/s (a large library
+// What bounds it: LDS and the matrix cores together.  2048 tokens over 34816, 32 heads on 2, e4m3: 946 to 996 us on different cards, 1140 to 1200 TFLOP/s (a large library
 // product reaches 1212 on this card); without LDS reads 786, without the rows' way through LDS 822, products and weights alone 656, products
 // alone 591.  Steps on the way: rows through registers by role and phases in lockstep 1208; queries waited for in front of the loop (their wait stood in
 // it and waited for the pages) 1102; the rows' work between the products 1043; the step of this form 1017; V through LDS with transposing reads 985; the second four
 // wavefronts ahead in first halves 966.  Measured and not taken: CG = 3 (two thirds of the LDS reads: 1013; fewer, larger tiles leave
-// CUs idle), the wavefronts of a SIMD taking turns behind barriers (1043), operands eight ahead (994).
+// CUs idle), the wavefronts of a SIMD taking turns behind barriers (1043), operands eight ahead (994).  A page takes a workgroup 1.75 us with CG = 2
+// and 1.13 with CG = 1 (head dim 64: 1.9 with CG = 4, 0.75 with CG = 1): a small tile has half or a quarter of the columns, so it is taken where the call is short of workgroups.
 #include <type_traits>
 
 #include "attn_unit.h"
