@@ -122,10 +122,13 @@ int rotary_common(const infllmv2_params *p, const infllmv2_rotary *r, const void
     if (tokens < 0 || heads < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (tokens == 0 || heads == 0) return INFLLMV2_OK;
     if (x == nullptr || y == nullptr || pos == nullptr || r->turns_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
-    const int64_t d = p->head_dim, span_t = (tokens - 1) * y_tok, span_h = (heads - 1) * y_head;
+    const int64_t d = p->head_dim;
+    int64_t span_t, span_h;
+    if (__builtin_mul_overflow(tokens - 1, y_tok, &span_t) || __builtin_mul_overflow((int64_t)heads - 1, y_head, &span_h)) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (tokens > 0xffffff00ll || heads > (1 << 24)) return INFLLMV2_ERR_UNSUPPORTED;      // (thread numbers are 32 bits)
     if (x_tok < 0 || x_head < 0 || y_tok < 0 || y_head < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
     // rows of the output stand apart: one of the two strides steps over everything that the other reaches
-    if (tokens > 1 && heads > 1 && !(y_head >= d && y_tok >= span_h + d) && !(y_tok >= d && y_head >= span_t + d))
+    if (tokens > 1 && heads > 1 && !(y_head >= d && y_tok - d >= span_h) && !(y_tok >= d && y_head - d >= span_t))
         return INFLLMV2_ERR_INVALID_ARGUMENT;
     if ((tokens > 1 && y_tok < d) || (heads > 1 && y_head < d)) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (x == y && ((tokens > 1 && x_tok != y_tok) || (heads > 1 && x_head != y_head))) return INFLLMV2_ERR_INVALID_ARGUMENT;
@@ -136,7 +139,7 @@ int rotary_common(const infllmv2_params *p, const infllmv2_rotary *r, const void
     // heads per thread: as many as leave every CU its 2048 threads
     while (a.per < 8 && tokens * ((heads + 2 * a.per - 1) / (2 * a.per)) * groups >= 256 * 2048) a.per *= 2;
     a.slices = (heads + a.per - 1) / a.per;
-    if (tokens > (int64_t)0xffffff00u / (a.slices * groups)) return INFLLMV2_ERR_UNSUPPORTED;     // (thread numbers are 32 bits)
+    if (tokens > (int64_t)0xffffff00u / (a.slices * groups)) return INFLLMV2_ERR_UNSUPPORTED;
     return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t>(a, n, (hipStream_t)stream) : launch_t<float>(a, n, (hipStream_t)stream);
 }
 

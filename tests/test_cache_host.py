@@ -88,6 +88,7 @@ def test_rotary_refusals(m):
             assert call(fn, **kw) == INVALID, kw
         assert call(fn, r=(64, 2, 1.0, 0, 256)) == UNSUPPORTED
         assert call(fn, tokens=1 << 40, yt=512, xt=0) == UNSUPPORTED
+        assert call(fn, heads=2 ** 31 - 1, xt=1 << 50, yt=1 << 50) == UNSUPPORTED and call(fn, tokens=1 << 40, yt=1 << 40) == INVALID
         assert call(fn, tokens=0, x=None, y=None, pos=None) == 0 and call(fn, heads=0) == 0
 
 
