@@ -94,6 +94,20 @@ __device__ inline void store_native(const rotary::Args &r, int q, T *row, const 
     }
 }
 
+// The bits of |x|: as whole numbers they are in the order of the magnitudes, infinities above every number and NaN above those, and a maximum of them is one instruction
+// for three (of floats the compiler has every input made quiet first).
+__device__ inline uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// over the wavefront, for all of it
+__device__ inline uint32_t wave_top(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));      // row_shr:1, 2, 4, 8 (zeros shifted in)
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));     // row_bcast:15 into rows 1 and 3
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));     // row_bcast:31 into rows 2 and 3
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
 // pages that n new tokens behind prev cached ones fall into
 __host__ __device__ inline int pages_touched(int prev, int n) { return n == 0 ? 0 : (prev + n - 1) / kBlock - prev / kBlock + 1; }
 
@@ -101,7 +115,7 @@ template <typename T, int D, bool CODES>
 __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
     constexpr int PER = D / 16, kThreads = 4 * D;     // threads per row; every row of a page has its own
     __shared__ int64_t s_item[6];
-    __shared__ float s_top[2][2][kThreads / 64];      // by turns
+    __shared__ uint32_t s_top[2][2][kThreads / 64];   // by turns
     const int tid = threadIdx.x, h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.c.hkv);
     const bool values = blockIdx.z != 0;
     int seq = blockIdx.x, nth = 0, prev, row0, n;
@@ -136,18 +150,19 @@ __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
     const bool turns = mine && q < r.pairs;
     if (turns) {
         const int32_t pos = a.pos ? a.pos[row0 + t - prev] : t;
+        uint64_t f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = r.turns[runs ? q + e : min(q + e, r.pairs - 1)];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float2 cs = q + e < r.pairs ? rotary::cos_sin<T>(pos, r.turns[q + e], r.magnitude) : float2{1.f, 0.f};
+            const float2 cs = rotary::cos_sin<T>(pos, f[e], r.magnitude);
             co[e] = cs.x;
             si[e] = cs.y;
         }
     }
     for (int h = h0, turn = 0; h < h1; ++h, turn ^= 1) {
         char *page_at = (values ? a.c.v : a.c.k) + a.c.at(page, h), *dst = page_at + (t - block * kBlock) * a.c.tok_stride;
-        float x[8], y[8], top = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
+        float x[8], y[8];                             // (of a row that is not written: nothing)
         if (mine && runs) {
             raw.spread(r, q, x, y);
             if (h + 1 < h1) raw.load(r, q, src + (h + 1) * a.head_stride);
@@ -177,31 +192,36 @@ __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
         if constexpr (!CODES) {
             if (mine) store_native(r, q, reinterpret_cast<T *>(dst), x, y);
         } else {
+            uint32_t bits = 0;
+            if (mine) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(y[e])));       // (a NaN is passed over)
+                for (int e = 0; e < 8; ++e) bits = max(bits, max(magnitude_bits(x[e]), magnitude_bits(y[e])));
+            }
             float *scale = (values ? a.c.vs : a.c.ks) + (int64_t)page * a.c.hkv + h;
             const bool continued = first > block * kBlock;
             const float was = continued ? *scale : 0.f;
-            auto over_all = [&](float v, float (&s)[kThreads / 64]) {
-                v = wave_max(v);
+            auto over_all = [&](uint32_t v, uint32_t (&s)[kThreads / 64]) {
+                v = wave_top(v);
                 if ((tid & 63) == 0) s[tid >> 6] = v;
                 __syncthreads();
 #pragma unroll
-                for (int w = 0; w < kThreads / 64; ++w) v = fmaxf(v, s[w]);
+                for (int w = 0; w < kThreads / 64; ++w) v = max(v, s[w]);
                 return v;
             };
-            top = over_all(top, s_top[turn][0]);
-            const bool fits = top <= 448.f * 0x1p119f;
-            if (!fits) {                              // infinities, or numbers that no scale is large enough for: the finite ones again
-                top = 0.f;
+            bits = over_all(bits, s_top[turn][0]);
+            const bool fits = bits <= __float_as_uint(448.f * 0x1p119f);
+            if (!fits) {                              // infinities, NaN, or numbers that no scale is large enough for: the finite ones again
+                bits = 0;
+                if (mine) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float u = fabsf(x[e]), w = fabsf(y[e]);
-                    top = fmaxf(top, fmaxf(u <= 3.4028234e38f ? u : 0.f, w <= 3.4028234e38f ? w : 0.f));
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t u = magnitude_bits(x[e]), w = magnitude_bits(y[e]);
+                        bits = max(bits, max(u < 0x7f800000u ? u : 0u, w < 0x7f800000u ? w : 0u));
+                    }
                 }
-                top = over_all(top, s_top[turn][1]);
+                bits = over_all(bits, s_top[turn][1]);
             }
-            const float now = fmaxf(cache::scale_for(top), was), inv = cache::reciprocal_of_power(now);
+            const float now = fmaxf(cache::scale_for(__uint_as_float(bits)), was), inv = cache::reciprocal_of_power(now);
             if (continued && now != was) {            // the older rows, sixteen codes at a time
                 const float down = was * inv;
                 for (int i = tid; i < (first - block * kBlock) * PER; i += kThreads) {
