@@ -8,9 +8,10 @@
 // A thread owns eight pair numbers of a row (16 channels; rotary.h says which); a page's 64 rows have a thread each, so that a page is requested at once, and
 // in front of the page's number, which is one more trip to memory.
 //
-// Bound: HBM for prompts, with the vector unit close behind (some 260 instructions for a wavefront's rows: widening, angles, the maximum, codes).  6 prompts of 24001 tokens, 2 heads of
-// 128, bf16 to e4m3, 175 MB: 49.2 us, 3.6 TB/s read and written, of the 4.9 of a large copy (rows behind the page's number, half the threads: 53.8).  One token of
-// 16 sequences: 4.8 us (5.6); 3 x 511 tokens, fp32, d 64: 6.2: launch, page lookup and rows, one after the other.
+// Bound: HBM for prompts.  6 prompts of 24001 tokens, 2 heads of 128, bf16 to e4m3, 175 MB: 41.2 us, 4.25 TB/s read and written, of the 4.9 of a large copy.
+// Before: rows behind the page's number, half the threads 53.8; maxima of floats, each made quiet first, frequencies one by one 49.2; the addresses of
+// single channels kept beside (122 registers for 90) 45.5.  One token of 16 sequences: 3.8 us; 3 x 511 tokens, fp32, d 64: 5.0: launch, page lookup and
+// rows, one after the other.
 #include "cache.h"
 #include "gen_unit.h"
 #include "rotary.h"
@@ -56,9 +57,9 @@ struct Pairs {
 };
 
 // the same channels of a row of codes, from values in units of the scale
-template <bool FITS>
+template <bool FITS, bool RUNS>
 __device__ inline void store_codes(const rotary::Args &r, int q, char *row, const float (&x)[8], const float (&y)[8]) {
-    if (r.pairs % 8 != 0) {
+    if (!RUNS && r.pairs % 8 != 0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             row[rotary::first_channel(r, q + i)] = (char)cache::code(x[i]);
@@ -74,9 +75,9 @@ __device__ inline void store_codes(const rotary::Args &r, int q, char *row, cons
 }
 
 // the same channels of a row of the data's type
-template <typename T>
+template <typename T, bool RUNS>
 __device__ inline void store_native(const rotary::Args &r, int q, T *row, const float (&x)[8], const float (&y)[8]) {
-    if (r.pairs % 8 != 0) {
+    if (!RUNS && r.pairs % 8 != 0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             Elem<T>::store(row + rotary::first_channel(r, q + i), x[i]);
@@ -111,7 +112,8 @@ __device__ inline uint32_t wave_top(uint32_t x) {
 // pages that n new tokens behind prev cached ones fall into
 __host__ __device__ inline int pages_touched(int prev, int n) { return n == 0 ? 0 : (prev + n - 1) / kBlock - prev / kBlock + 1; }
 
-template <typename T, int D, bool CODES>
+// RUNS: the pairs that are turned are a multiple of eight (the single channels' addresses of the other form take registers and instructions)
+template <typename T, int D, bool CODES, bool RUNS>
 __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
     constexpr int PER = D / 16, kThreads = 4 * D;     // threads per row; every row of a page has its own
     __shared__ int64_t s_item[6];
@@ -141,7 +143,7 @@ __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
     const int q = (tid % PER) * 8, t = block * kBlock + tid / PER;
     const bool mine = t >= first && t < end;
     const T *src = reinterpret_cast<const T *>(values ? a.v : a.k) + (int64_t)(row0 + t - prev) * a.tok_stride;
-    const bool runs = r.pairs % 8 == 0;               // the eight are pairs of one kind
+    const bool runs = RUNS || r.pairs % 8 == 0;             // the eight are pairs of one kind
     Pairs<T> raw;
     if (mine && runs) raw.load(r, q, src + h0 * a.head_stride);      // (beside the page's number, not behind it)
     const int page = a.c.page(seq, block);
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
             }
         }
         if constexpr (!CODES) {
-            if (mine) store_native(r, q, reinterpret_cast<T *>(dst), x, y);
+            if (mine) store_native<T, RUNS>(r, q, reinterpret_cast<T *>(dst), x, y);
         } else {
             uint32_t bits = 0;
             if (mine) {
@@ -239,8 +241,8 @@ __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
             if (mine) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] *= inv, y[e] *= inv;
-                if (fits) store_codes<true>(r, q, dst, x, y);
-                else store_codes<false>(r, q, dst, x, y);
+                if (fits) store_codes<true, RUNS>(r, q, dst, x, y);
+                else store_codes<false, RUNS>(r, q, dst, x, y);
             }
             if (tid == 0 && now != was) *scale = now;
         }
@@ -250,8 +252,10 @@ __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
 template <typename T, int D>
 int launch_t(const AppendArgs &a, bool codes, unsigned items, hipStream_t stream) {
     const dim3 grid(items, (a.c.hkv + a.heads - 1) / a.heads, 2);
-    if (codes) hipLaunchKernelGGL((cache_append_kernel<T, D, true>), grid, dim3(4 * D), 0, stream, a);
-    else hipLaunchKernelGGL((cache_append_kernel<T, D, false>), grid, dim3(4 * D), 0, stream, a);
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(4 * D), 0, stream, a); };
+    const bool runs = a.r.pairs % 8 == 0;
+    if (codes) launch(runs ? cache_append_kernel<T, D, true, true> : cache_append_kernel<T, D, true, false>);
+    else launch(runs ? cache_append_kernel<T, D, false, true> : cache_append_kernel<T, D, false, false>);
     return hip_status(hipGetLastError());
 }
 
