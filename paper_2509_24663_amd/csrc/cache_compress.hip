@@ -4,6 +4,8 @@
 //
 // Bound: memory latency.  A window's rows are requested together, behind one lookup of the pages they are in.  128 sequences with a new row each: 5.7 us (fewer
 // rows at a time: 7.3); 65536 tokens of 2 heads of 128, e4m3, 21 MB: 8.8 us (9.5), every row read for two windows.
+#include <type_traits>
+
 #include "cache.h"
 #include "gen_unit.h"
 
@@ -57,26 +59,32 @@ __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
             x[u] = *reinterpret_cast<const Vec *>((v < n0 ? base0 : base1) + (int64_t)v * a.c.tok_stride);
         }
         __builtin_amdgcn_sched_barrier(0);       // (left alone, the scheduler trades the requests for registers)
+        auto add = [&](auto some) {                                  // some: rows that are not the window's or of no page are among them
+            constexpr bool SOME = decltype(some)::value;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool in = u < n && (u < n0 ? page0 : page1) >= 0;
-            if constexpr (CODES) {
-                const float scale = u < n0 ? s0 : s1;
+            for (int u = 0; u < U; ++u) {
+                const bool in = !SOME || (u < n && (u < n0 ? page0 : page1) >= 0);
+                if constexpr (CODES) {
+                    const float scale = u < n0 ? s0 : s1;            // (a power of two: the product is exact, fused or not)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int w = (int)(j ? x[u].y : x[u].x);
-                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                    acc[4 * j] += in ? lo[0] * scale : 0.f, acc[4 * j + 1] += in ? lo[1] * scale : 0.f;
-                    acc[4 * j + 2] += in ? hi[0] * scale : 0.f, acc[4 * j + 3] += in ? hi[1] * scale : 0.f;
-                }
-            } else {
+                    for (int j = 0; j < 2; ++j) {
+                        const int w = (int)(j ? x[u].y : x[u].x);
+                        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                        const float v[4] = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
-                for (int c = 0; c < VEC; ++c) {
-                    if constexpr (sizeof(T) == 2) acc[c] += in ? bf16_to_float(x[u][c]) : 0.f;
-                    else acc[c] += in ? x[u][c] : 0.f;
+                        for (int i = 0; i < 4; ++i) acc[4 * j + i] = in ? __builtin_fmaf(v[i], scale, acc[4 * j + i]) : acc[4 * j + i];
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) {
+                        if constexpr (sizeof(T) == 2) acc[c] += in ? bf16_to_float(x[u][c]) : 0.f;
+                        else acc[c] += in ? x[u][c] : 0.f;
+                    }
                 }
             }
-        }
+        };
+        if (__all(n == U && page0 >= 0 && (n0 == n || page1 >= 0))) add(std::false_type());
+        else add(std::true_type());
     }
     const float inv = 1.0f / (float)a.lc;
 #pragma unroll
