@@ -2,8 +2,8 @@
 // from prev[b] to ctx[b] tokens, from the keys as the pages hold them.  As the append of compress_k.hip, with a page looked up for every 64
 // tokens of a window; the additions are in the order of the window, in 32 bits.
 //
-// Bound: memory latency.  A window's rows are requested together, behind one lookup of the pages they are in.  128 sequences with a new row each: 5.7 us (fewer
-// rows at a time: 7.3); 65536 tokens of 2 heads of 128, e4m3, 21 MB: 8.8 us (9.5), every row read for two windows.
+// Bound: memory latency.  A window's rows are requested together, behind one lookup of the pages they are in.  128 sequences with a new row each: 4.8 us (fewer
+// rows at a time: 7.3; every row asked whether it is there: 5.7); 65536 tokens of 2 heads of 128, e4m3, 21 MB: 7.4 us (9.5; 8.8), every row read for two windows.
 #include <type_traits>
 
 #include "cache.h"
