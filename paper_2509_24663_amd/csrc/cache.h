@@ -47,52 +47,55 @@ __device__ inline uint32_t codes4(float a, float b, float c, float d) {
 }
 
 // Which sequence the item-th of a batch's work items belongs to, when sequence s has count(s) of them; rem: which of the sequence's; before: the sum
-// of weight(s) over the sequences in front.  As find_seq_count (common.h), for counts that do not come from one list of offsets.  Called by every
+// of weight(s) over the sequences in front.  Both sums are below 2^31 (the host has seen to it).  As find_seq_count (common.h), for counts that do not come from one list of offsets.  Called by every
 // thread of a workgroup; one barrier; returns >= batch past the last item.  facts(s, i), i = 0, 1, 2: what else is wanted of the sequence (the lane that
 // found it has just read it).
 struct Facts {
     int x[3];
 };
+// sums over the lanes up to a lane's own
+__device__ inline int wave_sums(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr:1, 2, 4, 8 (zeros shifted in)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);     // row_bcast:31 into rows 2 and 3
+    return x;
+}
 template <class Count, class Weight, class Fact>
-__device__ inline int find_item(int batch, int64_t item, int &rem, int64_t &before, Facts &facts, int64_t (&s_out)[6], Count count, Weight weight, Fact fact) {
+__device__ inline int find_item(int batch, int item, int &rem, int &before, Facts &facts, int (&s_out)[6], Count count, Weight weight, Fact fact) {
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
-        int64_t items = 0, sum = 0, bef = 0;
-        int seq = batch, r = 0;
+        int items = 0, sum = 0, bef = 0, seq = batch, r = 0;
         for (int s0 = 0; s0 < batch; s0 += 64) {
             const int s = s0 + lane;
-            const int64_t n = s < batch ? count(s) : 0, wt = s < batch ? weight(s) : 0;
-            int64_t incl = n, wincl = wt;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int64_t up = __shfl_up(incl, o), wup = __shfl_up(wincl, o);
-                if (lane >= o) { incl += up; wincl += wup; }
-            }
+            const int n = s < batch ? count(s) : 0, wt = s < batch ? weight(s) : 0;
+            const int incl = wave_sums(n), wincl = wave_sums(wt);
             const uint64_t hit = __ballot(items + incl > item);
             if (hit) {
                 const int l = __ffsll((long long)hit) - 1;
                 seq = s0 + l;
-                r = (int)(item - items - __shfl(incl - n, l));
-                bef = sum + __shfl(wincl - wt, l);
+                r = item - items - __builtin_amdgcn_readlane(incl - n, l);
+                bef = sum + __builtin_amdgcn_readlane(wincl - wt, l);
                 if (lane == l) {
 #pragma unroll
                     for (int i = 0; i < 3; ++i) s_out[3 + i] = fact(s, i);
                 }
                 break;
             }
-            items += __shfl(incl, 63);
-            sum += __shfl(wincl, 63);
+            items += __builtin_amdgcn_readlane(incl, 63);
+            sum += __builtin_amdgcn_readlane(wincl, 63);
         }
         if (lane == 0) { s_out[0] = seq; s_out[1] = r; s_out[2] = bef; }
     }
     __syncthreads();
     // (uniform values, for the compiler as well: what follows from them stays in scalar registers)
-    rem = __builtin_amdgcn_readfirstlane((int)s_out[1]);
-    before = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s_out[2] >> 32)) << 32) |
-                       (uint32_t)__builtin_amdgcn_readfirstlane((int)s_out[2]));
+    rem = __builtin_amdgcn_readfirstlane(s_out[1]);
+    before = __builtin_amdgcn_readfirstlane(s_out[2]);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) facts.x[i] = __builtin_amdgcn_readfirstlane((int)s_out[3 + i]);
-    return __builtin_amdgcn_readfirstlane((int)s_out[0]);
+    for (int i = 0; i < 3; ++i) facts.x[i] = __builtin_amdgcn_readfirstlane(s_out[3 + i]);
+    return __builtin_amdgcn_readfirstlane(s_out[0]);
 }
 
 }  // namespace cache

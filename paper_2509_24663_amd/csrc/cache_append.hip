@@ -8,9 +8,10 @@
 // A thread owns eight pair numbers of a row (16 channels; rotary.h says which); a page's 64 rows have a thread each, so that a page is requested at once, and
 // in front of the page's number, which is one more trip to memory.
 //
-// Bound: HBM for prompts.  6 prompts of 24001 tokens, 2 heads of 128, bf16 to e4m3, 175 MB: 41.2 us, 4.25 TB/s read and written, of the 4.9 of a large copy.
+// Bound: HBM for prompts.  6 prompts of 24001 tokens, 2 heads of 128, bf16 to e4m3, 175 MB: 38.1 us, 4.6 TB/s read and written, of the 4.9 of a large copy.
 // Before: rows behind the page's number, half the threads 53.8; maxima of floats, each made quiet first, frequencies one by one 49.2; the addresses of
-// single channels kept beside (122 registers for 90) 45.5.  One token of 16 sequences: 3.8 us; 3 x 511 tokens, fp32, d 64: 5.0: launch, page lookup and
+// single channels kept beside (122 registers for 90) 45.5; sums over the
+// batch in 64 bits through LDS 41.2.  One token of 16 sequences: 3.8 us; 3 x 511 tokens, fp32, d 64: 4.6: launch, page lookup and
 // rows, one after the other.
 #include "cache.h"
 #include "gen_unit.h"
@@ -116,19 +117,19 @@ __host__ __device__ inline int pages_touched(int prev, int n) { return n == 0 ? 
 template <typename T, int D, bool CODES, bool RUNS>
 __global__ void __launch_bounds__(4 * D) cache_append_kernel(AppendArgs a) {
     constexpr int PER = D / 16, kThreads = 4 * D;     // threads per row; every row of a page has its own
-    __shared__ int64_t s_item[6];
+    __shared__ int s_item[6];
     __shared__ uint32_t s_top[2][2][kThreads / 64];   // by turns
     const int tid = threadIdx.x, h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.c.hkv);
     const bool values = blockIdx.z != 0;
-    int seq = blockIdx.x, nth = 0, prev, row0, n;
+    int seq = (int)blockIdx.x, nth = 0, prev, row0, n;
     if (a.single) {
         prev = a.prev[seq];
         row0 = a.cu[seq];
         n = a.cu[seq + 1] - row0;
     } else {
-        int64_t before;
+        int before;
         cache::Facts f;
-        seq = cache::find_item(a.batch, blockIdx.x, nth, before, f, s_item,
+        seq = cache::find_item(a.batch, (int)blockIdx.x, nth, before, f, s_item,
                                [&](int s) { return pages_touched(a.prev[s], a.cu[s + 1] - a.cu[s]); }, [](int) { return 0; },
                                [&](int s, int i) { return i == 0 ? a.prev[s] : a.cu[s + i - 1]; });
         if (seq >= a.batch) return;

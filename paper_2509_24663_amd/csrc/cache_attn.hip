@@ -222,7 +222,7 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TIL
 template <typename T, int D, bool CODES, int TILES, bool MULTI>
 __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
-    __shared__ int64_t s_item[6];
+    __shared__ int s_item[6];
     __shared__ float s_m[NW][16], s_l[NW][16];
     __shared__ f32x4 s_o[NW][N][64];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -241,20 +241,20 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
         if (a.idx != nullptr)
             early = a.idx[((int64_t)seq * hkv + rem / a.even) * a.topk + min(rem % a.even * NW + w + lane * NW * a.even, a.topk - 1)];
     } else {
-        int64_t slot0;
+        int slot0;
         cache::Facts f;
-        seq = cache::find_item(a.batch, blockIdx.x, rem, slot0, f, s_item,
+        seq = cache::find_item(a.batch, (int)blockIdx.x, rem, slot0, f, s_item,
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
-                return (int64_t)a.tiles(n, len) * hkv * a.most_splits(n, len);
+                return a.tiles(n, len) * hkv * a.most_splits(n, len);
             },
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
-                return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
+                return sp > 1 ? a.tiles(n, len) * hkv * sp : 0;
             },
             [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
         if (seq >= a.batch) return;
-        slot = slot0 + rem;
+        slot = (int64_t)slot0 + rem;
         row0 = f.x[0];
         n = f.x[1] - row0;
         len = f.x[2];
@@ -471,7 +471,7 @@ constexpr int kAhead = 8;
 template <typename T, int D, int SG, int COLS>
 __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs a) {
     constexpr int kThreads = D / 4 * COLS;               // of a share
-    __shared__ int64_t s_item[6];
+    __shared__ int s_item[6];
     __shared__ f32x4 s_o[SG == 1 ? 1 : SG - 1][SG == 1 ? 1 : kThreads];
     __shared__ float2 s_ml[SG == 1 ? 1 : SG - 1][COLS];
     const int tid = threadIdx.x % kThreads, sg = threadIdx.x / kThreads, hkv = a.c.hkv, G = a.hq / hkv;
@@ -486,17 +486,19 @@ __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs
         len = a.ctx[seq];
     } else {
         cache::Facts f;
-        seq = cache::find_item(a.batch, blockIdx.x, th, slot, f, s_item,
+        int slot0;
+        seq = cache::find_item(a.batch, (int)blockIdx.x, th, slot0, f, s_item,
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
-                return a.most_splits(n, len) > 1 ? (int64_t)a.tiles(n, len) * hkv : 0;
+                return a.most_splits(n, len) > 1 ? a.tiles(n, len) * hkv : 0;
             },
             [&](int s) {
                 const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
-                return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
+                return sp > 1 ? a.tiles(n, len) * hkv * sp : 0;
             },
             [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
         if (seq >= a.batch) return;
+        slot = slot0;
         row0 = f.x[0];
         n = f.x[1] - row0;
         len = f.x[2];

@@ -85,22 +85,22 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int KB = CODES ? 1 : 2;                               // bytes of an element
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // two K pages, three V pages, rows of V as they come
-    __shared__ int64_t s_item[6];
+    __shared__ int s_item[6];
     __shared__ int s_odd;                                           // a value of a page's edge (see write) is not finite
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv, GT = a.group_tokens;
 
     int rem;
-    int64_t slot0;
+    int slot0;
     cache::Facts facts;
-    const int seq = cache::find_item(a.batch, blockIdx.x, rem, slot0, facts, s_item,
+    const int seq = cache::find_item(a.batch, (int)blockIdx.x, rem, slot0, facts, s_item,
         [&](int s) {
             const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
-            return (int64_t)a.tiles(n, len) * hkv * a.most_splits(n, len);
+            return a.tiles(n, len) * hkv * a.most_splits(n, len);
         },
         [&](int s) {
             const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
-            return sp > 1 ? (int64_t)a.tiles(n, len) * hkv * sp : 0;
+            return sp > 1 ? a.tiles(n, len) * hkv * sp : 0;
         },
         [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
     if (seq >= a.batch) return;
