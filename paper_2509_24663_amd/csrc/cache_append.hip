@@ -5,7 +5,7 @@
 // scale is one workgroup's business: it turns its rows in registers, takes the largest magnitude over them (and, where a page is continued, the
 // scale that the page has: a scale only grows), rounds once, and rounds the older codes again if the scale grew.  No atomics, no second pass over
 // the new rows.  The angles are worked out once for all heads of a workgroup.
-// A thread owns eight pair numbers of a row (16 channels; rotary.h says which); a page's 64 rows have a thread each, so that a page is requested at once, and
+// A thread owns eight pair numbers of a row (16 channels; rotary.h says which); all 64 rows of a page have threads of their own, so that a page is requested at once, and
 // in front of the page's number, which is one more trip to memory.
 //
 // Bound: HBM for prompts.  6 prompts of 24001 tokens, 2 heads of 128, bf16 to e4m3, 175 MB: 38.1 us, 4.6 TB/s read and written, of the 4.9 of a large copy.

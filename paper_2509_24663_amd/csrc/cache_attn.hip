@@ -223,8 +223,8 @@ template <typename T, int D, bool CODES, int TILES, bool MULTI>
 __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
     __shared__ int s_item[6];
-    __shared__ float s_m[NW][16], s_l[NW][16];
-    __shared__ f32x4 s_o[NW][N][64];
+    __shared__ float s_m[NW][16], s_l[NW][16], s_inv[16];
+    __shared__ __attribute__((aligned(16))) float s_o[NW][16][D + 4];          // (rows four banks apart)
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv;
 
@@ -428,29 +428,33 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
 #pragma unroll
     for (int x = 0; x < NW; ++x) total += s_l[x][m] * exp2_fast(s_m[x][m] - base);
     const float f = exp2_fast(ref - base);
+    // (element r of acc[j]: channel N (4 g + r) + j of column m)
 #pragma unroll
-    for (int j = 0; j < N; ++j) s_o[w][j][lane] = acc[j] * f;
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < N; j += 4)
+            *reinterpret_cast<f32x4 *>(&s_o[w][m][N * (4 * g + r) + j]) = f32x4{acc[j][r], acc[j + 1][r], acc[j + 2][r], acc[j + 3][r]} * f;
+    if (w == 0 && lane < 16) s_inv[m] = top == -INFINITY ? 0.f : 1.f / total;
     __syncthreads();
-    // wavefront w: results j = w, w + NW, ..: element r is channel N (4 g + r) + j of column m
+    // a thread: PER channels of a column
+    constexpr int PER = 16 * D / (NW * 64);
     const bool direct = nsplit == 1;
-    const float inv = top == -INFINITY ? 0.f : 1.f / total;
+    const int col = tid / (D / PER), ch = tid % (D / PER) * PER, ci = col / G;
+    float o[PER];
 #pragma unroll
-    for (int jj = 0; jj < N / NW; ++jj) {
-        const int j = jj * NW + w;
-        f32x4 o = s_o[0][j][lane];
+    for (int i = 0; i < PER; i += 4) {
+        f32x4 v = *reinterpret_cast<const f32x4 *>(&s_o[0][col][ch + i]);
 #pragma unroll
-        for (int x = 1; x < NW; ++x) o += s_o[x][j][lane];
-        if (direct) {
-            if (used) {
-                T *dst = reinterpret_cast<T *>(a.out) + (row * a.hq + qh) * D;
+        for (int x = 1; x < NW; ++x) v += *reinterpret_cast<const f32x4 *>(&s_o[x][col][ch + i]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) Elem<T>::store(dst + N * (4 * g + r) + j, o[r] * inv);
-            }
-        } else {
-            float *dst = a.part + (slot * 16 + m) * D;
+        for (int e = 0; e < 4; ++e) o[i + e] = v[e];
+    }
+    if (!direct) {
+        store_row<float, PER>(a.part + (slot * 16 + col) * D + ch, o);
+    } else if (ci < ntok) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dst[N * (4 * g + r) + j] = o[r];
-        }
+        for (int i = 0; i < PER; ++i) o[i] *= s_inv[col];
+        store_row<T, PER>(reinterpret_cast<T *>(a.out) + (((int64_t)row0 + first + ci) * a.hq + h * G + col - ci * G) * D + ch, o);
     }
     if (w == 0 && lane < 16) {
         if (direct) {
