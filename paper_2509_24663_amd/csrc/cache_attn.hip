@@ -11,8 +11,10 @@
 // results are joined in LDS, then by cache_merge_kernel.
 //
 // Bound: HBM where the pages are many (64 sequences of 16384 to 65536 keys, 16 heads on 1, e4m3: 262 + 8 us for 1.37 GB, 5.1 TB/s; one of 500000: 55 us for 256 MB),
-// else a chain of trips to memory: length, page number, rows, partial results, joined results (16 sequences, 64 listed blocks each: 12 + 4 us; 5 sequences of 300 to
-// 2011 keys with 4 tokens each, fp32: 11 + 4.8).  fp32 data: the products, 2.6 us for a page of 64 channels and wavefront.
+// else a chain of trips to memory: length, page number, rows, partial results, joined results (16 sequences, 64 listed blocks each: 10.4 + 3.8 us, of which 0.5 to the
+// length, 1.4 to the page, 1.7 to its first logits, 2.8 for the rest of two pages, 0.5 in LDS; 5 sequences of 300 to 2011 keys with 4 tokens each, fp32: 10.8 + 4.1).
+// fp32 data: the products, 2.6 us for a page of 64 channels and wavefront.  Measured and not taken: a word of each line of the page after the next requested
+// ahead, for the L2 (16 sequences of 33000 keys: 56 -> 64 us).
 #include "cache_attn.h"
 #include "launch_rules.h"
 
