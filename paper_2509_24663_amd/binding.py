@@ -465,34 +465,35 @@ class Rotary:
         assert turns.dtype == torch.int64 and turns.is_contiguous() and turns.numel() == int(rot_dim) // 2
         self.turns = turns
         self.c = _RotaryC(int(rot_dim), LAYOUTS[layout], float(magnitude), 0, turns.data_ptr())
+        self.ref = ctypes.byref(self.c)
 
 
 # (The checks below take shapes and strides as whole tuples: each question to a tensor is 0.1 to 0.3 us, and these calls are short.)
-def _rotary(name, p: Params, rot: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor]):
+def _rotary(fn, p: Params, rot: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor]):
     tokens, heads, d = x.shape
     x_tok, x_head, one = x.stride()
     assert one == 1 and d == p.head_dim and x.dtype is p.torch_dtype
     assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (tokens,)
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
         y_tok, y_head = heads * d, d
+        out = torch.empty_like(x) if x_tok == y_tok and x_head == d else torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
         y_tok, y_head, one = out.stride()
         assert one == 1 and out.shape == x.shape and out.dtype is x.dtype
-    st = getattr(lib(), name)(ctypes.byref(p), ctypes.byref(rot.c), x.data_ptr(), x_tok, x_head, out.data_ptr(), y_tok, y_head,
-                              positions.data_ptr(), tokens, heads, _stream())
-    _check(st, name)
+    st = fn(ctypes.byref(p), rot.ref, x.data_ptr(), x_tok, x_head, out.data_ptr(), y_tok, y_head, positions.data_ptr(), tokens, heads, _stream())
+    if st:
+        _check(st, fn.__name__)
     return out
 
 
 def rotary_fwd(p: Params, rot: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None):
     """x [T, heads, d] (any strides, d contiguous) turned by positions (device int32 [T]).  out: optional buffer, x itself allowed."""
-    return _rotary("infllmv2_rotary_fwd", p, rot, x, positions, out)
+    return _rotary(lib().infllmv2_rotary_fwd, p, rot, x, positions, out)
 
 
 def rotary_bwd(p: Params, rot: Rotary, dy: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None):
     """Gradient of rotary_fwd with respect to its input, from that of its output."""
-    return _rotary("infllmv2_rotary_bwd", p, rot, dy, positions, out)
+    return _rotary(lib().infllmv2_rotary_bwd, p, rot, dy, positions, out)
 
 
 # ---------------------------------------------------------------------------------- the paged cache
@@ -516,6 +517,7 @@ class PagedCache:
         self.c = _CacheC(CACHE_E4M3 if coded else CACHE_NATIVE, k.shape[0], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                          k.stride(2), _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(),
                          page_table.stride(0) if self.batch > 1 else blocks, 0)
+        self.ref = ctypes.byref(self.c)
 
     def _holds(self, p: Params, max_ctx: int) -> bool:
         return self.rows == (p.num_kv_heads, p.head_dim, p.dtype) and (self.room is None or max_ctx <= self.room)
@@ -545,7 +547,7 @@ def cache_append(p: Params, cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
     assert k.shape == v.shape == (p.num_kv_heads, si.total, p.head_dim) and batch == pv.batch <= cache.batch
     assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == si.total)
     assert cache._holds(p, 0 if cache.room is None else max((n and n + t for n, t in zip(si.lens, pv.ctx_h.tolist())), default=0))
-    st = lib().infllmv2_cache_append(ctypes.byref(p), ctypes.byref(cache.c), ctypes.byref(rotary.c) if rotary is not None else None,
+    st = lib().infllmv2_cache_append(ctypes.byref(p), cache.ref, rotary.ref if rotary is not None else None,
                                      k.data_ptr(), v.data_ptr(), ts, hs, si.cu_h.data_ptr(), si.cu_d.data_ptr(), pv.ctx_h.data_ptr(),
                                      pv.ctx_d.data_ptr(), _ptr(positions), batch, _stream())
     _check(st, "infllmv2_cache_append")
@@ -558,7 +560,7 @@ def cache_compress_k(p: Params, cache: PagedCache, kc_cache: torch.Tensor, prev_
     planes, hkv, rows, d = kc_cache.shape
     assert kc_cache.is_contiguous() and kc_cache.dtype is torch.float32 and hkv == p.num_kv_heads and d == p.head_dim
     assert pv.batch == cx.batch <= cache.batch and cx.batch <= planes and cache._holds(p, cx.max_ctx)
-    st = lib().infllmv2_cache_compress_k(ctypes.byref(p), ctypes.byref(cache.c), kc_cache.data_ptr(), rows * d, pv.ctx_h.data_ptr(),
+    st = lib().infllmv2_cache_compress_k(ctypes.byref(p), cache.ref, kc_cache.data_ptr(), rows * d, pv.ctx_h.data_ptr(),
                                          pv.ctx_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), cx.batch, _stream())
     _check(st, "infllmv2_cache_compress_k")
     return kc_cache
@@ -605,7 +607,7 @@ def cache_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q, ctx_
     if workspace is None:
         need = workspace_bytes(OP_CACHE_ATTN, p, si.batch, si.total, cx.max_ctx)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    st = lib().infllmv2_cache_attn(ctypes.byref(p), ctypes.byref(cache.c), q.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(),
+    st = lib().infllmv2_cache_attn(ctypes.byref(p), cache.ref, q.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(),
                                    cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch, _ptr(block_idx), out.data_ptr(), lse.data_ptr(),
                                    *_ws_args(workspace), _stream())
     _check(st, "infllmv2_cache_attn")
