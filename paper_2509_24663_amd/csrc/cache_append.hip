@@ -10,9 +10,8 @@
 //
 // Bound: HBM for prompts.  6 prompts of 24001 tokens, 2 heads of 128, bf16 to e4m3, 175 MB: 38.1 us, 4.6 TB/s read and written, of the 4.9 of a large copy.
 // Before: rows behind the page's number, half the threads 53.8; maxima of floats, each made quiet first, frequencies one by one 49.2; the addresses of
-// single channels kept beside (122 registers for 90) 45.5; sums over the
-// batch in 64 bits through LDS 41.2.  One token of 16 sequences: 3.8 us; 3 x 511 tokens, fp32, d 64: 4.6: launch, page lookup and
-// rows, one after the other.
+// single channels kept beside (122 registers for 90) 45.5; sums over the batch in 64 bits through LDS 41.2.  One token of 16 sequences: 3.6 us; 3 x 511
+// tokens, fp32, d 64: 4.6: launch, page lookup and rows, one after the other.
 #include "cache.h"
 #include "gen_unit.h"
 #include "rotary.h"
@@ -319,7 +318,7 @@ extern "C" int infllmv2_cache_append(const infllmv2_params *p, const infllmv2_ca
     if (p->num_kv_heads > 65535) return INFLLMV2_ERR_UNSUPPORTED;
     AppendArgs a{cache::args(p, c), r ? rotary::args(r) : rotary::Args{nullptr, 0, 0, 1.f}, (const char *)k_d, (const char *)v_d,
                  kv_tok_stride, kv_head_stride, cu_new_d, prev_lens_d, pos_d, batch, single, 1};
-    // heads of a workgroup: all, while that leaves a few workgroups for each CU (the angles are half of a key page's work)
+    // heads of a workgroup: all, while that leaves a few workgroups for each CU (the angles of a key page are worked out once for them)
     while (a.heads < p->num_kv_heads && items * 2 * ((p->num_kv_heads + 2 * a.heads - 1) / (2 * a.heads)) >= 1024) a.heads *= 2;
     const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
     const hipStream_t s = (hipStream_t)stream;

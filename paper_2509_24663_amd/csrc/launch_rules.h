@@ -416,11 +416,11 @@ struct PageWork {
     }
 };
 // Pages of a workgroup (whose four wavefronts take them in turn).  Few: every CU has work soon; many: less to start and to join.  512 workgroups run at
-// once, two on a CU; starting those of each 256 is taken to cost 2.5 us, a page of a wavefront 0.6 us and 0.75 for each 16 KB of K and V (fp32 data, whose products take
-// longer: 2.6 for each 64 channels) or its share of 6 TB/s, less where the last workgroups leave CUs idle (sequences of many
-// lengths even out); a partial result 7 ns, the launch that joins
-// them 5 us.  Measured, one call, us, by pages 4 / 8 / 16 / 32 / 64 (one token each, 2 KV heads, d 128): 1 sequence of 33000 keys, e4m3 16.7 / 16.0 / 18.1 /
-// 22.7 / 32.9, bf16 19.6 / 17.5 / 21.1 / 29.3 / 46.4, fp32 27.9 / 23.9 / 34 / 54 / 96; of 500000, e4m3 107 / 77 / 65 / 58 / 56; 16 of 8000 29 / 24 / 21 / 23 /
+// once, two on a CU; starting those of each 256 is taken to cost 2.5 us, a page of a wavefront 0.6 us and 0.75 for each 16 KB of K and V (fp32 data, whose
+// products take longer: 2.6 for each 64 channels) or its share of 6 TB/s, less where the last workgroups leave CUs idle (sequences of many lengths even
+// out); a partial result 7 ns, the launch that joins them 5 us.
+// Measured before the last steps, one call, us, by pages 4 / 8 / 16 / 32 / 64 (one token each, 2 KV heads, d 128): 1 sequence of 33000 keys, e4m3 16.7 / 16.0 /
+// 18.1 / 22.7 / 32.9, bf16 19.6 / 17.5 / 21.1 / 29.3 / 46.4, fp32 27.9 / 23.9 / 34 / 54 / 96; of 500000, e4m3 107 / 77 / 65 / 58 / 56; 16 of 8000 29 / 24 / 21 / 23 /
 // 32; 64 of 16384 to 65536 478 / 347 / 294 / 315 / 285.  Split or not: 2 sequences, e4m3, 12 pages 15 / 12, 24 pages 15.2 / 15.4; bf16, 8 pages 15.3 /
 // 11.4, 16 pages 15 / 15.9; fp32, 8 pages 15.9 / 17.2.
 inline int unit_pps(const PageWork &w, int d, bool fp32, int bytes, int64_t least) {
