@@ -129,17 +129,24 @@ struct ValueRow {
     }
 };
 
-// Weights of a step as operands: bf16 data as two bf16 pieces (the upper 16 bits and the rest, 2^-16 of the weight left), so that the sums round like
-// sums of 32-bit weights and an output is off by its own rounding only; fp32 data as they are.
+// Weights of a step as operands: bf16 data as two bf16 pieces (the upper 16 bits and the rest, 2^-15 of the weight left), so that an output is off by
+// little more than its own rounding; fp32 data as they are.  The first piece is that of the next smaller float: below the weight, also where 16 bits hold
+// it, so that the second is above 0 and both products with an infinite value are that infinity (0 x infinity is not a number).
 template <typename T, int TILES> struct Weights;
 template <int TILES> struct Weights<bf16_t, TILES> {
     bf16x8 hi[TILES / 2], lo[TILES / 2];
     __device__ inline void set(const f32x4 (&p)[TILES], float) {
 #pragma unroll
         for (int t = 0; t < TILES / 2; ++t) {
-            f32x4 a = p[2 * t], b = p[2 * t + 1];
-            hi[t] = take_piece32<true>(a, b);
-            lo[t] = take_piece32<true>(a, b);
+            uint32_t u[8], r[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = p[2 * t + i / 4][i % 4];
+                u[i] = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u);                    // (0 stays 0)
+                r[i] = __float_as_uint(x - __uint_as_float(u[i] & 0xffff0000u));
+            }
+            hi[t] = __builtin_bit_cast(bf16x8, (u32x4){upper_halves(u[0], u[1]), upper_halves(u[2], u[3]), upper_halves(u[4], u[5]), upper_halves(u[6], u[7])});
+            lo[t] = __builtin_bit_cast(bf16x8, (u32x4){upper_halves(r[0], r[1]), upper_halves(r[2], r[3]), upper_halves(r[4], r[5]), upper_halves(r[6], r[7])});
         }
     }
 };
