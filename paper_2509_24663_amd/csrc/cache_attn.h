@@ -9,6 +9,12 @@ namespace cache_attn {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.4028234e38f;
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t pack(float a, float b) {          // nearest even
+    const bf16x2 x = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, x);
+}
+
 struct AttnArgs {
     cache::Args c;
     const char *q;

@@ -26,6 +26,7 @@ using namespace gen;
 using cache_attn::AttnArgs;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
+using cache_attn::pack;
 
 constexpr int NW = 4;                  // wavefronts of a workgroup
 __device__ inline float rows_max(float x) {          // over lanes with equal lane % 16
@@ -36,8 +37,6 @@ __device__ inline float rows_add(float x) {
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
 }
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // two codes (the lower or the upper half of w) as two bf16 values
 template <bool UPPER>
@@ -129,24 +128,28 @@ struct ValueRow {
     }
 };
 
-// Weights of a step as operands: bf16 data as two bf16 pieces (the upper 16 bits and the rest, 2^-15 of the weight left), so that an output is off by
-// little more than its own rounding; fp32 data as they are.  The first piece is that of the next smaller float: below the weight, also where 16 bits hold
-// it, so that the second is above 0 and both products with an infinite value are that infinity (0 x infinity is not a number).
+// Weights of a step as operands: bf16 data as two bf16 pieces, the upper 16 bits and the rest rounded to nearest (off by at most 2^-16 of the weight, either
+// way), so that an output is off by little more than its own rounding; fp32 data as they are.  The first piece is that of the next smaller float: below the
+// weight, also where 16 bits hold it, so that the second is above 0 and both products with an infinite value are that infinity (0 x infinity is not a
+// number).
 template <typename T, int TILES> struct Weights;
 template <int TILES> struct Weights<bf16_t, TILES> {
     bf16x8 hi[TILES / 2], lo[TILES / 2];
     __device__ inline void set(const f32x4 (&p)[TILES], float) {
 #pragma unroll
         for (int t = 0; t < TILES / 2; ++t) {
-            uint32_t u[8], r[8];
+            uint32_t u[8], r[4];
+            float rest[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float x = p[2 * t + i / 4][i % 4];
                 u[i] = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u);                    // (0 stays 0)
-                r[i] = __float_as_uint(x - __uint_as_float(u[i] & 0xffff0000u));
+                rest[i] = x - __uint_as_float(u[i] & 0xffff0000u);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = pack(rest[2 * i], rest[2 * i + 1]);
             hi[t] = __builtin_bit_cast(bf16x8, (u32x4){upper_halves(u[0], u[1]), upper_halves(u[2], u[3]), upper_halves(u[4], u[5]), upper_halves(u[6], u[7])});
-            lo[t] = __builtin_bit_cast(bf16x8, (u32x4){upper_halves(r[0], r[1]), upper_halves(r[2], r[3]), upper_halves(r[4], r[5]), upper_halves(r[6], r[7])});
+            lo[t] = __builtin_bit_cast(bf16x8, (u32x4){r[0], r[1], r[2], r[3]});
         }
     }
 };

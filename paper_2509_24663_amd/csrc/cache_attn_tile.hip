@@ -33,20 +33,16 @@ using attn_unit::lds_read16;
 using cache_attn::AttnArgs;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
+using cache_attn::pack;
 
 constexpr int NW = 8;
 constexpr int kThreads = NW * 64;
 constexpr float kSlack = 64.f, kNoReference = -1e38f;
 constexpr int kAhead = 4;                  // operands requested in front of their product
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <bool UPPER>
 __device__ inline uint32_t widen(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER));
-}
-__device__ inline uint32_t pack(float a, float b) {          // nearest even
-    const bf16x2 x = {(__bf16)a, (__bf16)b};
-    return __builtin_bit_cast(uint32_t, x);
 }
 // all ones in the elements of w that are infinities or NaN
 template <bool CODES>

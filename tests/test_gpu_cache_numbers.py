@@ -1,7 +1,9 @@
-"""Attention over the paged cache with numbers at the edges of their types: infinities among the values."""
+"""Attention over the paged cache with numbers at the edges of their types: infinities among the values, and how exact
+the weights are."""
 import pytest
 import torch
 
+import paged
 from test_gpu_cache import _filled, _gen, _params, m  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -38,3 +40,45 @@ def test_infinite_values_keep_their_sign(m, dtype, hq, hkv, d, n, ctx):  # noqa:
         rest = [x for x in range(d) if x != ch]
         assert torch.equal(out[..., rest], clean[..., rest]) and torch.equal(out[~sees], clean[~sees])
         c.v[page, :, row, ch] = was
+
+
+@pytest.mark.parametrize("kv", ["native", "e4m3"])
+@pytest.mark.parametrize("n,ctx", [(1, 200), (1, 33000), (2, 200), (8, 500)])
+def test_weights_of_a_few_tokens(m, kv, n, ctx):  # noqa: F811
+    """Values that cancel show the weights alone.  Channel i is made for column i (a token and a head of KV head 0): four keys B of value 1 and weight w below
+    1, five keys A of weight 1 whose values add up to -4 w as nearly as five rounded numbers do, every other key of weight 0.
+    Derivation, bf16 data: a weight enters as two bf16 pieces, the second rounded to nearest: off by at most 2^-16 of it, either way; 1 is the sum of two such
+    pieces, and B's are half of the sum of p |v|: 2^-17 of that.  9 terms in 32 bits whose sum stays below that half: 9 * 2^-24 / 2 < 2^-21.8; w itself (the
+    exponential, the scale's rounding): 2^-22 of a half and less.  A result's own rounding: 2^-8 of it.  Roundings to nearest are as often up as down: over N
+    weights their mean is within 4 / sqrt(N) of the largest."""
+    hq, hkv, d, few, many = 32, 2, 128, 5, 4
+    p = _params(m, "bf16", hq, hkv, d, softmax_scale=1.0)
+    pages = (ctx + 63) // 64
+    c = m.PagedCache.empty(p, pages, torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous(), kv)
+    a, b = torch.arange(2, 2 + few), torch.arange(30, 30 + many)
+    columns = [(ch % (16 * n) // 16, ch % 16) for ch in range(d)]
+    seeds, errors = 8 if ctx <= 500 else 1, 0.0
+    for seed in range(seeds):
+        z = (-torch.rand((n, hq), generator=_gen(seed), device="cuda") * 2).to(torch.bfloat16)
+        q = torch.zeros((n, hq, d), device="cuda", dtype=torch.bfloat16)
+        q[..., 0], q[..., 1] = z, 200.0                     # logits: z for B, 0 for A, -200 for the others
+        k, v = torch.zeros((ctx, d), device="cuda"), torch.zeros((ctx, d), device="cuda", dtype=torch.float64)
+        k[:, 1] = -1.0
+        k[a] = k[b] = 0.0
+        k[b, 0] = 1.0
+        w = torch.stack([z[i, h].double().exp() for i, h in columns])
+        v[b] = 1.0
+        left, s = -many * w, paged.scale_for(float(many * w.max()))
+        for t in a.tolist():
+            v[t] = left.to(torch.bfloat16).double() if kv == "native" else paged.to_codes(left / s).double() * s
+            left = left - v[t]
+        m.cache_append(p, c, *(x[None].expand(hkv, -1, -1).to(torch.bfloat16) for x in (k, v)), [0, ctx], [0])
+        sc = None if kv == "native" else c.v_scale
+        assert torch.equal(paged.rows_of(c.v, sc, c.page_table, 0, ctx, 0)[0], v)
+        out, _ = m.cache_attn(p, c, q, [0, n], [ctx])
+        got = torch.stack([out[i, h, ch] for ch, (i, h) in enumerate(columns)]).double()
+        want, mass = (many * w + v[a].sum(0)) / (few + many * w), (many * w + v[a].abs().sum(0)) / (few + many * w)
+        tol = 2.0 ** -8 * want.abs() + (2.0 ** -17 + 2.0 ** -21.8 + 2.0 ** -23) * mass
+        assert bool(((got - want).abs() <= tol).all()), float(((got - want).abs() / tol).max())
+        errors += float(((got - want) / mass).mean()) / seeds
+    assert abs(errors) <= 2.0 ** -17 * 4 / (seeds * min(d, 16 * n)) ** 0.5 + 2.0 ** -21.8 + 2.0 ** -23
