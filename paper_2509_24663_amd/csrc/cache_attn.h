@@ -14,6 +14,16 @@ __device__ inline uint32_t pack(float a, float b) {          // nearest even
     const bf16x2 x = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, x);
 }
+// Two weights as two bf16 pieces each, the upper 16 bits and the rest rounded to nearest: off by at most 2^-16 of the weight, either way.  The first piece is
+// that of the next smaller float: below the weight, also where 16 bits hold it, so that the second is above 0 and both products with an infinite value are
+// that infinity (0 x infinity is not a number).
+struct Pieces {
+    uint32_t hi, lo;
+};
+__device__ inline Pieces pieces(float a, float b) {
+    const uint32_t u = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u), v = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);      // (0 stays 0)
+    return Pieces{gen::upper_halves(u, v), pack(a - __uint_as_float(u & 0xffff0000u), b - __uint_as_float(v & 0xffff0000u))};
+}
 
 struct AttnArgs {
     cache::Args c;
@@ -25,6 +35,7 @@ struct AttnArgs {
     int group_tokens;                  // of 16 columns over all keys (16 / G)
     int wide_from;                     // sequences over all keys with so many queries are the tile kernel's
     int tile_groups;                   // column groups of a tile of this launch (1: cache_attn.hip; rules::tile_size)
+    int fine;                          // tile kernel: weights of two pieces (small tiles)
     int pps;                           // pages of a split
     int even;                          // > 0: one query token for each sequence, item = (sequence, head, split < even); slots alike
     int multi;                         // some tile of cache_attn.hip has more than one token

@@ -26,7 +26,6 @@ using namespace gen;
 using cache_attn::AttnArgs;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
-using cache_attn::pack;
 
 constexpr int NW = 4;                  // wavefronts of a workgroup
 __device__ inline float rows_max(float x) {          // over lanes with equal lane % 16
@@ -128,28 +127,23 @@ struct ValueRow {
     }
 };
 
-// Weights of a step as operands: bf16 data as two bf16 pieces, the upper 16 bits and the rest rounded to nearest (off by at most 2^-16 of the weight, either
-// way), so that an output is off by little more than its own rounding; fp32 data as they are.  The first piece is that of the next smaller float: below the
-// weight, also where 16 bits hold it, so that the second is above 0 and both products with an infinite value are that infinity (0 x infinity is not a
-// number).
+// Weights of a step as operands: bf16 data as two bf16 pieces, so that an output is off by little more than its own rounding; fp32 data as they are.
 template <typename T, int TILES> struct Weights;
 template <int TILES> struct Weights<bf16_t, TILES> {
     bf16x8 hi[TILES / 2], lo[TILES / 2];
     __device__ inline void set(const f32x4 (&p)[TILES], float) {
 #pragma unroll
         for (int t = 0; t < TILES / 2; ++t) {
-            uint32_t u[8], r[4];
-            float rest[8];
+            u32x4 h, l;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = p[2 * t + i / 4][i % 4];
-                u[i] = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u);                    // (0 stays 0)
-                rest[i] = x - __uint_as_float(u[i] & 0xffff0000u);
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 x = p[2 * t + i / 2];
+                const cache_attn::Pieces w = cache_attn::pieces(x[2 * (i & 1)], x[2 * (i & 1) + 1]);
+                h[i] = w.hi;
+                l[i] = w.lo;
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = pack(rest[2 * i], rest[2 * i + 1]);
-            hi[t] = __builtin_bit_cast(bf16x8, (u32x4){upper_halves(u[0], u[1]), upper_halves(u[2], u[3]), upper_halves(u[4], u[5]), upper_halves(u[6], u[7])});
-            lo[t] = __builtin_bit_cast(bf16x8, (u32x4){r[0], r[1], r[2], r[3]});
+            hi[t] = __builtin_bit_cast(bf16x8, h);
+            lo[t] = __builtin_bit_cast(bf16x8, l);
         }
     }
 };
@@ -677,9 +671,15 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     a.tile_groups = 1;
     AttnArgs wide = a;                         // the tile kernel's launch, with large tiles or small ones
     const rules::TileSize size[2] = {rules::tile_size(p->head_dim, false), rules::tile_size(p->head_dim, true)};
-    int max_ctx = 0, wide_pages = 0;
-    rules::PageWork work, wide_work;           // of the kernel of 16 columns; of the sequences that could be either's, if they are its own as well
-    int64_t tiles[2] = {0, 0}, tile_pages[2] = {0, 0}, unit_pages = 0;       // of the sequences that could be either's: what they are in tiles, pages in all
+    int max_ctx = 0;
+    rules::PageWork work;                      // of the kernel of 16 columns
+    // The sequences that could be either kernel's: what they are as its work, in large and in small tiles, their pages in all.  few: those of kFewTokens and
+    // fewer, whose weights keep 16 bits in any batch: tiles with weights of two pieces if the batch has no longer ones, else the kernel of 16 columns.
+    struct Either {
+        rules::PageWork work;
+        int most = 0;
+        int64_t tiles[2] = {0, 0}, tile_pages[2] = {0, 0}, unit_pages = 0;
+    } chunks, few;
     for (int b = 0; b < batch; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
         if (len < n || len > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
@@ -691,23 +691,31 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
             work.add(groups, pages, a.listed(len) ? groups * pages : (int64_t)hkv * pages);
             continue;
         }
-        wide_work.add(groups, pages, (int64_t)hkv * pages);
-        if (pages > wide_pages) wide_pages = pages;
+        Either &e = n > rules::kFewTokens ? chunks : few;
+        e.work.add(groups, pages, (int64_t)hkv * pages);
+        if (pages > e.most) e.most = pages;
         const int first = (len - n) / kBlock + 1;                            // pages that the first token sees
-        unit_pages += groups * (first + pages) / 2;
+        e.unit_pages += groups * (first + pages) / 2;
         for (int i = 0; i < 2; ++i) {
             const int t0 = a.group_tokens * size[i].groups, t = (n + t0 - 1) / t0, low = t > 1 ? (len - n + t0 - 1) / kBlock + 1 : pages;
-            tiles[i] += (int64_t)t * hkv;
-            tile_pages[i] += (int64_t)t * hkv * (low + pages) / 2;
+            e.tiles[i] += (int64_t)t * hkv;
+            e.tile_pages[i] += (int64_t)t * hkv * (low + pages) / 2;
         }
     }
-    const rules::TileSplits large = rules::tile_splits(size[0], tiles[0], wide_pages, tile_pages[0]), small = rules::tile_splits(size[1], tiles[1], wide_pages, tile_pages[1]);
-    const bool use_small = small.us < large.us;
+    wide.fine = chunks.tiles[0] == 0;
+    const Either &tiled = wide.fine ? few : chunks;
+    const rules::TileSplits large = rules::tile_splits(size[0], tiled.tiles[0], tiled.most, tiled.tile_pages[0]);
+    const rules::TileSplits small = rules::tile_splits(wide.fine ? rules::fine_tile_size(p->head_dim) : size[1], tiled.tiles[1], tiled.most, tiled.tile_pages[1]);
+    const bool use_small = wide.fine || small.us < large.us;
     wide.tile_groups = size[use_small].groups;
     wide.pps = use_small ? small.pps : large.pps;
-    if (tiles[0] == 0 || rules::unit_us(p->head_dim, wide_pages, unit_pages) <= (use_small ? small.us : large.us)) {
+    if (tiled.tiles[0] == 0 || rules::unit_us(p->head_dim, tiled.most, tiled.unit_pages) <= (use_small ? small.us : large.us)) {
         a.wide_from = wide.wide_from = INT32_MAX;
-        work.add(wide_work);
+        work.add(chunks.work);
+        work.add(few.work);
+    } else if (!wide.fine) {
+        a.wide_from = wide.wide_from = a.wide_from > rules::kFewTokens ? a.wide_from : rules::kFewTokens + 1;
+        work.add(few.work);
     }
     for (int b = 0; b < batch && !a.multi; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];

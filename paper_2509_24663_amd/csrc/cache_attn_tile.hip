@@ -76,7 +76,8 @@ struct Page {
     static __device__ inline uint32_t v_at(int ch, int octet) { return (uint32_t)ch * 128 + ((octet ^ v_swizzle(ch)) << 4); }
 };
 
-template <int D, int CG, int W, bool CODES>
+// PIECES: bf16 pieces of a weight in the second product
+template <int D, int CG, int W, int PIECES, bool CODES>
 __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_attn_tile_kernel(AttnArgs a) {
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int KB = CODES ? 1 : 2;                               // bytes of an element
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     // The walk, in steps of half a page k (32 keys): logits of k; then sums of the weights of k - 1 and, between those products, the weights of k.
     constexpr int LOGITS = 8 * CG, KF = 2 * KS;                     // logits of a lane, K operands of a step
     f32x4 s[CG][2];
-    uint32_t pb[2][CG][4];                                          // by the parity of k
+    uint32_t pb[2][CG][PIECES][4];                                  // by the parity of k
     bf16x8 f[W];                                                    // operands, requested W ahead: KF of K, then DT of V^T
     static_assert((KF + DT) % W == 0, "an operand's place does not depend on the step");
     const uint32_t k_at = lds + k_lane, v_at = lds + 2 * Page<D>::kBytes + v_lane;
@@ -263,11 +264,22 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     auto v_half = [&](int p3, int hb) { return (v_at + p3 * Page<D>::kBytes) ^ (uint32_t)(64 * hb); };
     auto fetch_k = [&](int j, uint32_t kb) { f[j % W] = lds_read16((kb ^ (uint32_t)(64 * (j % KS))) + (uint32_t)(4 * (j / KS) * 2 * D)); };
     auto fetch_v = [&](int j, uint32_t vb) { f[(KF + j) % W] = lds_read16((vb ^ (uint32_t)(16 * (j & 1))) + (uint32_t)(2048 * j)); };
-    auto sums = [&](int j, const uint32_t (&w)[CG][4]) {
+    auto sums = [&](int j, const uint32_t (&w)[CG][PIECES][4]) {
 #pragma unroll
-        for (int x = 0; x < CG; ++x) {
-            const bf16x8 wt = __builtin_bit_cast(bf16x8, (u32x4){w[x][0], w[x][1], w[x][2], w[x][3]});
-            acc[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[(KF + j) % W], wt, acc[x][j], 0, 0, 0);
+        for (int x = 0; x < CG; ++x)
+#pragma unroll
+            for (int i = PIECES - 1; i >= 0; --i) {
+                const bf16x8 wt = __builtin_bit_cast(bf16x8, (u32x4){w[x][i][0], w[x][i][1], w[x][i][2], w[x][i][3]});
+                acc[x][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[(KF + j) % W], wt, acc[x][j], 0, 0, 0);
+            }
+    };
+    auto set = [&](uint32_t (&w)[PIECES][4], int i, float a, float b) {
+        if constexpr (PIECES == 2) {
+            const cache_attn::Pieces two = cache_attn::pieces(a, b);
+            w[0][i] = two.hi;
+            w[1][i] = two.lo;
+        } else {
+            w[0][i] = pack(a, b);
         }
     };
     // kb: K of k; vb: V of k - 1; kb_on: K of k + 1 where it is there already (ON); beside(j): what else is issued at K operand j
@@ -307,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                 const float p = exp2_fast(__builtin_fmaf(s[x][i >> 2][i & 3], c, -ref[x]));
                 part[x] = i ? part[x] + p : p;
                 asm volatile("" : "+v"(part[x]));                   // (added here: left alone, all weights are kept to the end of the step)
-                if (i & 1) pb[P][x][i >> 1] = pack(last, p);
+                if (i & 1) set(pb[P][x], i >> 1, last, p);
                 last = p;
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -332,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                 for (int i = 0; i < 8; ++i) {
                     const float p = exp2_fast(__builtin_fmaf(s[x][i >> 2][i & 3], c, -to));
                     part[x] += p;
-                    if (i & 1) pb[P][x][i >> 1] = pack(last, p);
+                    if (i & 1) set(pb[P][x], i >> 1, last, p);
                     last = p;
                 }
             }
@@ -340,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
 #pragma unroll
         for (int x = 0; x < CG; ++x) sum[x] += part[x];
     };
-    constexpr int PIECES = KP + CV + KL + VL, PER_STEP = (PIECES + KF - 1) / KF;
+    constexpr int MOVES = KP + CV + KL + VL, PER_STEP = (MOVES + KF - 1) / KF;
 
     // Between two barriers K and V of page p and V of p - 1 are read, K and V of p + 1 written to the other buffers (two of K, three of V) from the registers
     // that hold them, and p + 2 is requested.
@@ -369,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
 #pragma unroll
         for (int x = 0; x < CG; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pb[1][x][i] = 0u;
+            for (int i = 0; i < 4 * PIECES; ++i) pb[1][x][i / 4][i % 4] = 0u;
         int p2 = 0, p3 = 0, before = 2;                             // buffers of page p (K, V) and of V of p - 1
         for (;;) {
             collect();
@@ -388,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             const uint32_t k_to = lds + (p2 ^ 1) * Page<D>::kBytes, v_to = lds + (2 + ahead3) * Page<D>::kBytes;
             step(std::integral_constant<int, 0>(), std::true_type(), now.key0, k_half(p2, 0), v_half(before, 1), k_half(p2, 1), [&](int j) {
 #pragma unroll
-                for (int i = j * PER_STEP; i < (j + 1) * PER_STEP && i < PIECES; ++i) {
+                for (int i = j * PER_STEP; i < (j + 1) * PER_STEP && i < MOVES; ++i) {
                     if (i < KP + CV) write(i, k_to, v_to, then.ks, then.vs);
                     else request(i - KP - CV, after);
                 }
@@ -478,10 +490,10 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     }
 }
 
-template <int D, int CG, bool CODES>
+template <int D, int CG, int PIECES, bool CODES>
 int launch_d(const AttnArgs &a, int64_t items, hipStream_t stream) {
     constexpr int LDS = 5 * Page<D>::kBytes + 64 * D * (CODES ? 1 : 2);
-    const auto kernel = cache_attn_tile_kernel<D, CG, kAhead, CODES>;
+    const auto kernel = cache_attn_tile_kernel<D, CG, kAhead, PIECES, CODES>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
         return INFLLMV2_ERR_HIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(kThreads), LDS, stream, a);
@@ -495,13 +507,18 @@ namespace cache_attn {
 int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream) {
     static_assert(rules::tile_size(128, false).groups == 2 * NW && rules::tile_size(64, false).groups == 4 * NW, "the tiles that the rules count with");
     static_assert(rules::tile_size(128, true).groups == NW && rules::tile_size(64, true).groups == NW, "the tiles that the rules count with");
+    const auto launch = [&](auto d, auto groups, auto pieces) {
+        constexpr int D = decltype(d)::value, CG = decltype(groups)::value, PIECES = decltype(pieces)::value;
+        return codes ? launch_d<D, CG, PIECES, true>(a, items, stream) : launch_d<D, CG, PIECES, false>(a, items, stream);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 4> four;
+    const std::integral_constant<int, 64> d64;
+    const std::integral_constant<int, 128> d128;
     const bool small = a.tile_groups == NW;
-    if (p->head_dim == 128) {
-        if (small) return codes ? launch_d<128, 1, true>(a, items, stream) : launch_d<128, 1, false>(a, items, stream);
-        return codes ? launch_d<128, 2, true>(a, items, stream) : launch_d<128, 2, false>(a, items, stream);
-    }
-    if (small) return codes ? launch_d<64, 1, true>(a, items, stream) : launch_d<64, 1, false>(a, items, stream);
-    return codes ? launch_d<64, 4, true>(a, items, stream) : launch_d<64, 4, false>(a, items, stream);
+    if (p->head_dim == 128) return !small ? launch(d128, two, one) : a.fine ? launch(d128, one, two) : launch(d128, one, one);
+    return !small ? launch(d64, four, one) : a.fine ? launch(d64, one, two) : launch(d64, one, one);
 }
 
 }  // namespace cache_attn

@@ -451,6 +451,8 @@ constexpr TileSize tile_size(int d, bool small) {
     if (small) return d == 128 ? TileSize{8, 1.13, 0.03} : TileSize{8, 0.75, 0.01};
     return d == 128 ? TileSize{16, 1.75, 0.05} : TileSize{32, 1.9, 0.05};
 }
+// small, with weights of two pieces (half as many products again)
+constexpr TileSize fine_tile_size(int d) { return d == 128 ? TileSize{8, 1.35, 0.03} : TileSize{8, 0.95, 0.01}; }
 // Splits along the keys for `tiles` workgroups with up to `pages` pages, `sum` in all, on 256 CUs.  A call is taken to cost 14.7 us and its longest way:
 // rounds of workgroups, or where tiles differ (a prompt from its first token) their sum dealt out; several splits 1.5 us for the second launch and
 // result_us each.  Measured, one call, us (G 16, d 128, e4m3, 512 tokens over 8000, 1 / 2 / 4 splits): large tiles 231 / 134 / 84.6, small
@@ -478,8 +480,9 @@ inline double unit_us(int d, int pages, int64_t sum) {
     const double few = sum < 20000 ? (double)sum : 20000.;
     return 13 + 0.02 * (pages < 500 ? pages : 500) + (d == 128 ? 3.2e-3 : 1.2e-3) * few + (d == 128 ? 1.4e-3 : 1.2e-3) * (sum - few);
 }
-// The sequences that tiles are thought of for: those with at least so many column groups of queries
-constexpr int kTileFrom = 4;
+// The sequences that tiles are thought of for: those with at least so many column groups of queries.  Up to kFewTokens queries (a decode step, proposed
+// tokens) keep weights of 16 bits, so tiles of theirs are small ones with weights of two pieces; more are a chunk, whose weights may be rounded to 8 bits.
+constexpr int kTileFrom = 4, kFewTokens = 8;
 
 }  // namespace rules
 }  // namespace ifv2

@@ -43,7 +43,7 @@ def test_infinite_values_keep_their_sign(m, dtype, hq, hkv, d, n, ctx):  # noqa:
 
 
 @pytest.mark.parametrize("kv", ["native", "e4m3"])
-@pytest.mark.parametrize("n,ctx", [(1, 200), (1, 33000), (2, 200), (8, 500)])
+@pytest.mark.parametrize("n,ctx", [(1, 200), (1, 33000), (2, 200), (4, 33000), (5, 33000), (8, 33000), (8, 500)])
 def test_weights_of_a_few_tokens(m, kv, n, ctx):  # noqa: F811
     """Values that cancel show the weights alone.  Channel i is made for column i (a token and a head of KV head 0): four keys B of value 1 and weight w below
     1, five keys A of weight 1 whose values add up to -4 w as nearly as five rounded numbers do, every other key of weight 0.
