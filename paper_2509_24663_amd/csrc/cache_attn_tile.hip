@@ -37,7 +37,7 @@ using cache_attn::pack;
 
 constexpr int NW = 8;
 constexpr int kThreads = NW * 64;
-constexpr float kSlack = 64.f, kNoReference = -1e38f;
+constexpr float kSlack = 64.f;
 constexpr int kAhead = 4;                  // operands requested in front of their product
 
 template <bool UPPER>
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     float ref[CG], sum[CG];
 #pragma unroll
     for (int x = 0; x < CG; ++x) {
-        ref[x] = kNoReference;
+        ref[x] = kLowest;                                           // (below every logit)
         sum[x] = 0.f;
 #pragma unroll
         for (int i = 0; i < DT; ++i) acc[x][i] = f32x4{0.f, 0.f, 0.f, 0.f};

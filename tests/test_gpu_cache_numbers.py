@@ -1,5 +1,7 @@
-"""Attention over the paged cache with numbers at the edges of their types: infinities among the values, and how exact
-the weights are."""
+"""Attention over the paged cache with numbers at the edges of their types: infinities among the values, sums next to the largest float, logits far
+below zero, and how exact the weights are."""
+import math
+
 import pytest
 import torch
 
@@ -82,3 +84,38 @@ def test_weights_of_a_few_tokens(m, kv, n, ctx):  # noqa: F811
         assert bool(((got - want).abs() <= tol).all()), float(((got - want).abs() / tol).max())
         errors += float(((got - want) / mass).mean()) / seeds
     assert abs(errors) <= 2.0 ** -17 * 4 / (seeds * min(d, 16 * n)) ** 0.5 + 2.0 ** -21.8 + 2.0 ** -23
+
+
+def _large(m, dtype, kv, hq, hkv, d, ctx, seed=5):  # noqa: F811
+    """A cache of one sequence whose logits are its first key channel alone"""
+    p = _params(m, dtype, hq, hkv, d, softmax_scale=1.0)
+    c, _, _ = _filled(m, p, [ctx], kv, seed)
+    pages = (ctx + 63) // 64
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous()
+    return p, m.PagedCache.empty(p, pages, table, kv)
+
+
+def _write(m, p, c, k0, v):  # noqa: F811
+    """keys with k0 [ctx] in channel 0 and nothing else, values v [ctx, d], for every KV head"""
+    ctx, d = v.shape
+    k = torch.zeros((p.num_kv_heads, ctx, d), device="cuda")
+    k[..., 0] = k0
+    m.cache_append(p, c, k.to(p.torch_dtype), v[None].expand(p.num_kv_heads, -1, -1).contiguous().to(p.torch_dtype), [0, ctx], [0])
+
+
+@pytest.mark.parametrize("n,ctx", FORMS)
+def test_logits_far_below_zero(m, n, ctx):  # noqa: F811
+    """All logits at -2^127 ln 2, -1.7e38 in units of log2: a softmax over equal logits is a mean, wherever they are."""
+    hq, hkv, d = 32, 2, 128
+    p = _params(m, "bf16", hq, hkv, d, softmax_scale=math.log(2.0))
+    _, c = _large(m, "bf16", "native", hq, hkv, d, ctx)
+    q = torch.zeros((n, hq, d), device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = -(2.0 ** 64)
+    v = torch.randn((ctx, d), generator=_gen(2), device="cuda").to(torch.bfloat16)
+    _write(m, p, c, torch.full((ctx,), 2.0 ** 63, device="cuda"), v.float())
+    out, lse = m.cache_attn(p, c, q, [0, n], [ctx])
+    want = (v.double().cumsum(0) / torch.arange(1, ctx + 1, device="cuda")[:, None])[ctx - n:, None]
+    mass = (v.double().abs().cumsum(0) / torch.arange(1, ctx + 1, device="cuda")[:, None])[ctx - n:, None]
+    # equal weights: exact; sums in 32 bits of up to 6001 terms; the result's own rounding
+    assert bool(((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + ctx * 2.0 ** -24 * mass).all())
+    assert float((lse.double() / -(2.0 ** 127 * math.log(2.0)) - 1).abs().max()) <= 1e-6
