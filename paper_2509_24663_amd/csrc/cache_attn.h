@@ -9,6 +9,18 @@ namespace cache_attn {
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.4028234e38f;
 
+// Sums of weights times values are finite wherever the result is: a mean of values.  Relative to the largest logit, or one near it, they may pass the
+// largest float although their quotient by the sum of the weights does not, so
+//  - elements of a walk's sums that are not finite are taken from a second walk whose references lie kLift binary orders above the largest logit (2^34 keys of weight
+//    2^6 x 2^-kLift stay below 1; the others keep the first walk's, whose small weights reach 40 orders further down),
+//  - sums are joined as means: each divided by its own weights, then added up with its share of all weights.
+constexpr float kLift = 40.f;
+// (a factor that is formed before it is multiplied with anything else)
+__device__ inline float formed(float x) {
+    asm("" : "+v"(x));
+    return x;
+}
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ inline uint32_t pack(float a, float b) {          // nearest even
     const bf16x2 x = {(__bf16)a, (__bf16)b};
@@ -40,23 +52,23 @@ struct AttnArgs {
     int even;                          // > 0: one query token for each sequence, item = (sequence, head, split < even); slots alike
     int multi;                         // some tile of cache_attn.hip has more than one token
     float scale;
-    float *part;                       // [slots][16 tile_groups][D] sums, relative to the reference
+    float *part;                       // [slots][16 tile_groups][D] means over the split's keys
     float *ml;                         // [slots][16 tile_groups][2] reference, sum of weights
-    // how the n queries of a sequence of len tokens are cut
-    __host__ __device__ bool listed(int len) const { return idx != nullptr && len >= dense_below; }
-    __host__ __device__ int tile_tokens(int len) const { return listed(len) ? 1 : group_tokens * tile_groups; }
-    __host__ __device__ int tiles(int n, int len) const {
+    // how the n queries of a sequence of len tokens are cut (always inlined: a call in a kernel that is long already takes registers from all of it)
+    __host__ __device__ __attribute__((always_inline)) bool listed(int len) const { return idx != nullptr && len >= dense_below; }
+    __host__ __device__ __attribute__((always_inline)) int tile_tokens(int len) const { return listed(len) ? 1 : group_tokens * tile_groups; }
+    __host__ __device__ __attribute__((always_inline)) int tiles(int n, int len) const {
         if ((tile_groups > 1) != (!listed(len) && n >= wide_from)) return 0;
         const int t = tile_tokens(len);
         return (n + t - 1) / t;
     }
     // pages of the tile whose last token is at pos_last: at most so many are there (listed: a list may hold them anywhere)
-    __host__ __device__ int pages(int len, int pos_last) const {
+    __host__ __device__ __attribute__((always_inline)) int pages(int len, int pos_last) const {
         const int all = pos_last / kBlock + 1;
         return listed(len) && topk < (len + kBlock - 1) / kBlock ? topk : all;
     }
-    __host__ __device__ int splits(int len, int pos_last) const { return (pages(len, pos_last) + pps - 1) / pps; }
-    __host__ __device__ int most_splits(int n, int len) const { return n == 0 ? 0 : splits(len, len - 1); }
+    __host__ __device__ __attribute__((always_inline)) int splits(int len, int pos_last) const { return (pages(len, pos_last) + pps - 1) / pps; }
+    __host__ __device__ __attribute__((always_inline)) int most_splits(int n, int len) const { return n == 0 ? 0 : splits(len, len - 1); }
 };
 
 // cache_attn_tile.hip

@@ -15,6 +15,8 @@
 // length, 1.4 to the page, 1.7 to its first logits, 2.8 for the rest of two pages, 0.5 in LDS; 5 sequences of 300 to 2011 keys with 4 tokens each, fp32: 10.8 + 4.1).
 // fp32 data: the products, 2.6 us for a page of 64 channels and wavefront.  Measured and not taken: a word of each line of the page after the next requested
 // ahead, for the L2 (16 sequences of 33000 keys: 56 -> 64 us).
+#include <type_traits>
+
 #include "cache_attn.h"
 #include "launch_rules.h"
 
@@ -24,6 +26,8 @@ namespace {
 
 using namespace gen;
 using cache_attn::AttnArgs;
+using cache_attn::formed;
+using cache_attn::kLift;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
 
@@ -229,7 +233,7 @@ template <typename T, int D, bool CODES, int TILES, bool MULTI>
 __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
     __shared__ int s_item[6];
-    __shared__ float s_m[NW][16], s_l[NW][16], s_inv[16];
+    __shared__ float s_m[NW][16], s_l[NW][16];
     __shared__ __attribute__((aligned(16))) float s_o[NW][16][D + 4];          // (rows four banks apart)
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv;
@@ -287,145 +291,177 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     const float c = a.scale * kLog2e;
 
     f32x4 acc[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float ref = -INFINITY, sum = 0.f;            // reference in units of log2; this lane's share of the sum
+    float ref, sum;                              // reference in units of log2; this lane's share of the sum, then the column's
     int low = INT32_MAX;                         // first key of any page that this wavefront went through
 
     const int32_t *list = a.idx + ((int64_t)(row0 + first) * hkv + h) * a.topk;
     const uint32_t tok = (uint32_t)a.c.tok_stride;
     const uint32_t k_off = m * tok + KeyTile<T, D, CODES>::lane_offset(g), v_off = 4 * g * tok + m * ValueRow<T, D, CODES>::BYTES;
-    // lane l holds the l-th of the next 64 pages: where it is, its first key, its scales
-    for (int e0 = e_first; e0 < e_end; e0 += 64 * e_step) {
-        const int e = e0 + lane * e_step;
-        int my_page = -1, my_key0 = 0;
-        float my_ks = 1.f, my_vs = 1.f;
-        if (e < e_end) {
-            const int j = !listed ? e : nsplit == a.even && e0 == e_first ? early : list[e];
-            if (j >= 0 && j <= pos_last / kBlock) {
-                my_page = a.c.page(seq, j);
-                my_key0 = j * kBlock;
+    // (a walk as a loop's body instead of twice in the code keeps some 24 more registers)
+    auto walk = [&](auto second) {
+        constexpr float lift = decltype(second)::value ? kLift : 0.f;
+        ref = -INFINITY;
+        sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // lane l holds the l-th of the next 64 pages: where it is, its first key, its scales
+        for (int e0 = e_first; e0 < e_end; e0 += 64 * e_step) {
+            const int e = e0 + lane * e_step;
+            int my_page = -1, my_key0 = 0;
+            float my_ks = 1.f, my_vs = 1.f;
+            if (e < e_end) {
+                const int j = !listed ? e : nsplit == a.even && e0 == e_first ? early : list[e];
+                if (j >= 0 && j <= pos_last / kBlock) {
+                    my_page = a.c.page(seq, j);
+                    my_key0 = j * kBlock;
+                }
             }
-        }
-        uint64_t there = __ballot(my_page >= 0);
-        if (there == 0) continue;
-        if (CODES && my_page >= 0) {
-            my_ks = a.c.ks[(int64_t)my_page * hkv + h];
-            my_vs = a.c.vs[(int64_t)my_page * hkv + h];
-        }
-        KeyTile<T, D, CODES> k[TILES];
-        ValueRow<T, D, CODES> v[4 * TILES];
-        auto base_of = [&](const char *p, int l) { return p + a.c.at(__builtin_amdgcn_readlane(my_page, l), h); };
-        auto load_k = [&](const char *base) {
+            uint64_t there = __ballot(my_page >= 0);
+            if (there == 0) continue;
+            if (CODES && my_page >= 0) {
+                my_ks = a.c.ks[(int64_t)my_page * hkv + h];
+                my_vs = a.c.vs[(int64_t)my_page * hkv + h];
+            }
+            KeyTile<T, D, CODES> k[TILES];
+            ValueRow<T, D, CODES> v[4 * TILES];
+            auto base_of = [&](const char *p, int l) { return p + a.c.at(__builtin_amdgcn_readlane(my_page, l), h); };
+            auto load_k = [&](const char *base) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t) k[t].load(base + (int64_t)(16 * t) * tok, k_off);
-        };
-        auto load_v = [&](const char *base) {
+                for (int t = 0; t < TILES; ++t) k[t].load(base + (int64_t)(16 * t) * tok, k_off);
+            };
+            auto load_v = [&](const char *base) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t)
+                for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[4 * t + r].load(base + (int64_t)(16 * t + r) * tok, v_off);
-        };
-        int l = __ffsll((long long)there) - 1;
-        const char *kb = base_of(a.c.k, l), *vb = base_of(a.c.v, l);
-        load_k(kb);
-        load_v(vb);
-        while (there) {
-            const int page_key0 = __builtin_amdgcn_readlane(my_key0, l);
-            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), l));
-            const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), l));
-            there &= there - 1;
-            low = min(low, page_key0);
-            if (there) l = __ffsll((long long)there) - 1;
+                    for (int r = 0; r < 4; ++r) v[4 * t + r].load(base + (int64_t)(16 * t + r) * tok, v_off);
+            };
+            int l = __ffsll((long long)there) - 1;
+            const char *kb = base_of(a.c.k, l), *vb = base_of(a.c.v, l);
+            load_k(kb);
+            load_v(vb);
+            while (there) {
+                const int page_key0 = __builtin_amdgcn_readlane(my_key0, l);
+                const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), l));
+                const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), l));
+                there &= there - 1;
+                low = min(low, page_key0);
+                if (there) l = __ffsll((long long)there) - 1;
 #pragma unroll 1
-            for (int part = 0; part < STEPS; ++part) {
-                const int key0 = page_key0 + part * STEP;
-                f32x4 s[TILES];
+                for (int part = 0; part < STEPS; ++part) {
+                    const int key0 = page_key0 + part * STEP;
+                    f32x4 s[TILES];
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    s[t] = row_product<D>(k[t].operand(ks), qf);
-                    if (CODES && t % 2 == 1) __builtin_amdgcn_sched_barrier(0);      // (widened rows of two tiles at a time: registers)
-                }
-                const bool last_part = part == STEPS - 1, more = !last_part || there;
-                if (more) {
-                    kb = last_part ? base_of(a.c.k, l) : kb + (int64_t)STEP * tok;
-                    load_k(kb);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                const bool edge = key0 + STEP - 1 > pos0;                        // keys behind a token
-                if (edge) {
+                    for (int t = 0; t < TILES; ++t) {
+                        s[t] = row_product<D>(k[t].operand(ks), qf);
+                        if (CODES && t % 2 == 1) __builtin_amdgcn_sched_barrier(0);      // (widened rows of two tiles at a time: registers)
+                    }
+                    const bool last_part = part == STEPS - 1, more = !last_part || there;
+                    if (more) {
+                        kb = last_part ? base_of(a.c.k, l) : kb + (int64_t)STEP * tok;
+                        load_k(kb);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    const bool edge = key0 + STEP - 1 > pos0;                        // keys behind a token
+                    if (edge) {
+#pragma unroll
+                        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[t][r] = key0 + 16 * t + 4 * g + r <= pos ? s[t][r] : -INFINITY;
+                    }
+                    float mx = s[0][0];
 #pragma unroll
                     for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[t][r] = key0 + 16 * t + 4 * g + r <= pos ? s[t][r] : -INFINITY;
-                }
-                float mx = s[0][0];
+                        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[t][r]);
+                    mx = __builtin_fmaf(rows_max(mx), c, lift);
+                    if (__any(mx > ref)) {
+                        const float to = fmaxf(ref, mx), base = to == -INFINITY ? 0.f : to;
+                        const float f = exp2_fast(ref - base);
+                        ref = to;
+                        sum *= f;
 #pragma unroll
-                for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[t][r]);
-                mx = rows_max(mx) * c;
-                if (__any(mx > ref)) {
-                    const float to = fmaxf(ref, mx), base = to == -INFINITY ? 0.f : to;
-                    const float f = exp2_fast(ref - base);
-                    ref = to;
-                    sum *= f;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) acc[j] *= f;
-                }
-                const float base = ref == -INFINITY ? 0.f : ref;
-                float part_sum = 0.f;
-#pragma unroll
-                for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[t][r] = exp2_fast(__builtin_fmaf(s[t][r], c, -base));
-                        part_sum += s[t][r];
+                        for (int j = 0; j < N; ++j) acc[j] *= f;
                     }
-                sum += part_sum;
-                Weights<T, TILES> wt;
-                wt.set(s, vs);
-                int rounds = 1;
-                if (edge) {                                                      // rows that no token of the tile sees, and those that only some see
-                    bool odd = false;
+                    const float base = ref == -INFINITY ? 0.f : ref;
+                    float part_sum = 0.f;
 #pragma unroll
                     for (int t = 0; t < TILES; ++t)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos_last);
-                            if (MULTI) odd |= v[4 * t + r].odd();
+                            s[t][r] = exp2_fast(__builtin_fmaf(s[t][r], c, -base));
+                            part_sum += s[t][r];
                         }
-                    if (MULTI && __any(odd)) rounds = ntok;
-                }
-                if (!MULTI) {
-                    add_values<false, D, TILES, CODES>(acc, wt, v, vs, true);
-                } else {
-                    // 0 x infinity: where rows are not finite, the sums of each token from the rows that it sees, latest token first
-#pragma unroll 1
-                    for (int i = rounds - 1; i >= 0; --i) {
-                        if (rounds > 1) {
+                    sum += part_sum;
+                    Weights<T, TILES> wt;
+                    wt.set(s, vs);
+                    int rounds = 1;
+                    if (edge) {                                                      // rows that no token of the tile sees, and those that only some see
+                        bool odd = false;
 #pragma unroll
-                            for (int t = 0; t < TILES; ++t)
+                        for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos0 + i);
-                        }
-                        add_values<true, D, TILES, CODES>(acc, wt, v, vs, rounds == 1 || ti == i);
+                            for (int r = 0; r < 4; ++r) {
+                                v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos_last);
+                                if (MULTI) odd |= v[4 * t + r].odd();
+                            }
+                        if (MULTI && __any(odd)) rounds = ntok;
                     }
+                    if (!MULTI) {
+                        add_values<false, D, TILES, CODES>(acc, wt, v, vs, true);
+                    } else {
+                        // 0 x infinity: where rows are not finite, the sums of each token from the rows that it sees, latest token first
+#pragma unroll 1
+                        for (int i = rounds - 1; i >= 0; --i) {
+                            if (rounds > 1) {
+#pragma unroll
+                                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos0 + i);
+                            }
+                            add_values<true, D, TILES, CODES>(acc, wt, v, vs, rounds == 1 || ti == i);
+                        }
+                    }
+                    if (more) {
+                        vb = last_part ? base_of(a.c.v, l) : vb + (int64_t)STEP * tok;
+                        load_v(vb);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if (more) {
-                    vb = last_part ? base_of(a.c.v, l) : vb + (int64_t)STEP * tok;
-                    load_v(vb);
-                }
-                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        sum = rows_add(sum);
+    };
+    walk(std::false_type());
+    // sums that are not finite: a second walk (cache_attn.h)
+    uint32_t again = 0;                          // elements 4 j + r that are the second walk's
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) again |= finite(acc[j][r]) ? 0u : 1u << (4 * j + r);
+    again = used ? again : 0u;
+    const bool twice = __any(again != 0u);
+    float more = 1.f;                            // the second walk's share of the first's sums
+    if (twice) {
+        const float first_ref = ref, first_sum = sum;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < N; ++j) s_o[w][m][N * (4 * g + r) + j] = acc[j][r];
+        walk(std::true_type());
+        more = first_sum / sum;
+        ref = first_ref;
+        sum = first_sum;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j][r] = (again >> (4 * j + r)) & 1u ? acc[j][r] : s_o[w][m][N * (4 * g + r) + j];
     }
 
     // the four wavefronts' results together
-    sum = rows_add(sum);
     if (ref == -INFINITY && low <= pos) ref = kLowest;       // only logits of minus infinity (0 / 0 below), not no key at all
     if (lane < 16) s_m[w][m] = ref, s_l[w][m] = sum;
     __syncthreads();
+    const bool direct = nsplit == 1;
     float top = s_m[0][m];
 #pragma unroll
     for (int x = 1; x < NW; ++x) top = fmaxf(top, s_m[x][m]);
@@ -433,18 +469,28 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     float total = 0.f;
 #pragma unroll
     for (int x = 0; x < NW; ++x) total += s_l[x][m] * exp2_fast(s_m[x][m] - base);
-    const float f = exp2_fast(ref - base);
+    // (a split without weight is 0 with no weight: others of the column may have some)
+    const float inv = top == -INFINITY || (!direct && total == 0.f) ? 0.f : 1.f / total;
+    const float f = formed(exp2_fast(ref - base) * inv);
     // (element r of acc[j]: channel N (4 g + r) + j of column m)
+    if (twice) {
+        const float f2 = formed(f * more);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j][r] *= (again >> (4 * j + r)) & 1u ? f2 : f;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] *= f;
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int j = 0; j < N; j += 4)
-            *reinterpret_cast<f32x4 *>(&s_o[w][m][N * (4 * g + r) + j]) = f32x4{acc[j][r], acc[j + 1][r], acc[j + 2][r], acc[j + 3][r]} * f;
-    if (w == 0 && lane < 16) s_inv[m] = top == -INFINITY ? 0.f : 1.f / total;
+            *reinterpret_cast<f32x4 *>(&s_o[w][m][N * (4 * g + r) + j]) = f32x4{acc[j][r], acc[j + 1][r], acc[j + 2][r], acc[j + 3][r]};
     __syncthreads();
     // a thread: PER channels of a column
     constexpr int PER = 16 * D / (NW * 64);
-    const bool direct = nsplit == 1;
     const int col = tid / (D / PER), ch = tid % (D / PER) * PER, ci = col / G;
     float o[PER];
 #pragma unroll
@@ -458,8 +504,6 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     if (!direct) {
         store_row<float, PER>(a.part + (slot * 16 + col) * D + ch, o);
     } else if (ci < ntok) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) o[i] *= s_inv[col];
         store_row<T, PER>(reinterpret_cast<T *>(a.out) + (((int64_t)row0 + first + ci) * a.hq + h * G + col - ci * G) * D + ch, o);
     }
     if (w == 0 && lane < 16) {
@@ -524,7 +568,8 @@ __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs
     const float *src = a.part + (slot * cols + col) * D + c0;
     const float2 *ml = reinterpret_cast<const float2 *>(a.ml) + slot * cols + col;
     float top = -INFINITY, total = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};                      // the mean so far
+    auto part_of = [](float sum) { return sum == 0.f ? 0.f : 1.f / sum; };
     for (int s0 = sg * kAhead; used && s0 < nsplit; s0 += SG * kAhead) {
         float2 x[kAhead];
         f32x4 y[kAhead];
@@ -537,17 +582,19 @@ __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs
         float to = top;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) to = fmaxf(to, x[i].x);
-        const float base = to == -INFINITY ? 0.f : to, f0 = exp2_fast(top - base);
-        total *= f0;
-        o *= f0;
+        const float base = to == -INFINITY ? 0.f : to, before = total * exp2_fast(top - base);
+        total = before;
+        float f[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (s0 + i < nsplit) {
-                const float f = exp2_fast(x[i].x - base);
-                total += x[i].y * f;
-                o += y[i] * f;
-            }
+            f[i] = s0 + i < nsplit ? x[i].y * exp2_fast(x[i].x - base) : 0.f;
+            total += f[i];
         }
+        const float inv = part_of(total);
+        o *= formed(before * inv);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (s0 + i < nsplit) o += y[i] * formed(f[i] * inv);
         top = to;
     }
     if constexpr (SG > 1) {                              // the shares' results, by the threads of the first
@@ -560,23 +607,27 @@ __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs
         float to = top;
 #pragma unroll
         for (int i = 0; i < SG - 1; ++i) to = fmaxf(to, s_ml[i][tid / (D / 4)].x);
-        const float base = to == -INFINITY ? 0.f : to, f0 = exp2_fast(top - base);
-        total *= f0;
-        o *= f0;
+        const float base = to == -INFINITY ? 0.f : to, before = total * exp2_fast(top - base);
+        total = before;
+        float f[SG - 1];
 #pragma unroll
         for (int i = 0; i < SG - 1; ++i) {
             const float2 x = s_ml[i][tid / (D / 4)];
-            const float f = exp2_fast(x.x - base);
-            total += x.y * f;
-            o += s_o[i][tid] * f;
+            f[i] = x.y * exp2_fast(x.x - base);
+            total += f[i];
         }
+        const float inv = part_of(total);
+        o *= formed(before * inv);
+#pragma unroll
+        for (int i = 0; i < SG - 1; ++i) o += s_o[i][tid] * formed(f[i] * inv);
         top = to;
     }
     if (!used) return;
     const int64_t row = row0 + first + ti;
     const int qh = h * G + m - in_group * G;
-    const float inv = top == -INFINITY ? 0.f : 1.f / total;
-    const float r[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    // (only logits of minus infinity: 0 / 0, not no key at all)
+    const float none = top != -INFINITY && total == 0.f ? NAN : 0.f;
+    const float r[4] = {o[0] + none, o[1] + none, o[2] + none, o[3] + none};
     gen::store_row<T, 4>(reinterpret_cast<T *>(a.out) + (row * a.hq + qh) * D + c0, r);
     if (c0 == 0 && a.lse != nullptr) a.lse[row * a.hq + qh] = top == -INFINITY ? -INFINITY : top * kLn2 + logf(total);
 }

@@ -31,6 +31,7 @@ namespace {
 using namespace gen;
 using attn_unit::lds_read16;
 using cache_attn::AttnArgs;
+using cache_attn::kLift;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
 using cache_attn::pack;
@@ -84,6 +85,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // two K pages, three V pages, rows of V as they come
     __shared__ int s_item[6];
     __shared__ int s_odd;                                           // a value of a page's edge (see write) is not finite
+    __shared__ int s_again;                                         // sums are not finite ..
+    __shared__ uint32_t s_bad[CG][kThreads];                        // .. a thread's: bit 4 i + r (registers: kept here through the second walk)
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv, GT = a.group_tokens;
 
@@ -133,13 +136,6 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
 
     f32x4 acc[CG][DT];
     float ref[CG], sum[CG];
-#pragma unroll
-    for (int x = 0; x < CG; ++x) {
-        ref[x] = kLowest;                                           // (below every logit)
-        sum[x] = 0.f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) acc[x][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
 
     const uint32_t lds = __builtin_amdgcn_readfirstlane(attn_unit::lds_address(smem));
     const uint32_t k_lane = Page<D>::k_at(8 * (m >> 2) + (m & 3), g), v_lane = Page<D>::v_at(m, g);
@@ -226,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
 
     // the pages of the split: lane l holds the l-th of the next 64
     const int e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
-    int e0 = split * a.pps, list_key0 = 0;
+    int e0 = 0, list_key0 = 0;
     int64_t list_at = 0;
     float list_ks = 1.f, list_vs = 1.f;
     uint64_t there = 0;
@@ -251,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
         p.ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list_ks), l));
         p.vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list_vs), l));
     };
-    if (tid == 0) s_odd = 0;
+    if (tid == 0) s_odd = s_again = 0;
 
     // The walk, in steps of half a page k (32 keys): logits of k; then sums of the weights of k - 1 and, between those products, the weights of k.
     constexpr int LOGITS = 8 * CG, KF = 2 * KS;                     // logits of a lane, K operands of a step
@@ -283,7 +279,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
         }
     };
     // kb: K of k; vb: V of k - 1; kb_on: K of k + 1 where it is there already (ON); beside(j): what else is issued at K operand j
-    auto step = [&](auto parity, auto on, int first_key, uint32_t kb, uint32_t vb, uint32_t kb_on, auto beside) {
+    // slack, lift: see pass
+    auto step = [&](auto parity, auto on, float slack, float lift, int first_key, uint32_t kb, uint32_t vb, uint32_t kb_on, auto beside) __attribute__((always_inline)) {
         constexpr int P = decltype(parity)::value;
         constexpr bool ON = decltype(on)::value;
 #pragma unroll
@@ -328,13 +325,13 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
         float largest = part[0];
 #pragma unroll
         for (int x = 1; x < CG; ++x) largest = fmaxf(largest, part[x]);
-        if (__any(largest > kSlack)) {
+        if (__any(largest > slack)) {
 #pragma unroll
             for (int x = 0; x < CG; ++x) {
                 float mx = s[x][0][0];
 #pragma unroll
                 for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[x][i >> 2][i & 3]);
-                const float to = fmaxf(ref[x], rows_max(mx) * c), down = exp2_fast(ref[x] - to);
+                const float to = fmaxf(ref[x], __builtin_fmaf(rows_max(mx), c, lift)), down = exp2_fast(ref[x] - to);
                 ref[x] = to;
                 sum[x] *= down;
 #pragma unroll
@@ -356,102 +353,147 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
 
     // Between two barriers K and V of page p and V of p - 1 are read, K and V of p + 1 written to the other buffers (two of K, three of V) from the registers
     // that hold them, and p + 2 is requested.
-    Where now{}, then{}, after{};                                   // pages p, p + 1, p + 2 (those that are not there repeat the last)
-    refill();
-    const bool here = there != 0;
     int low = INT32_MAX;
-    if (here) {
-        next(now);
-        low = now.key0;
+    // (the pass as a loop's body instead of twice in the code keeps 30 to 50 more registers)
+    auto pass = [&](auto second) __attribute__((always_inline)) {
+        constexpr float lift = decltype(second)::value ? kLift : 0.f, slack = decltype(second)::value ? kSlack * 0x1p-40f : kSlack;
+#pragma unroll
+        for (int x = 0; x < CG; ++x) {
+            ref[x] = kLowest;                                       // (below every logit)
+            sum[x] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) acc[x][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        Where now{}, then{}, after{};                                   // pages p, p + 1, p + 2 (those that are not there repeat the last)
+        e0 = split * a.pps;
+        there = 0;
         refill();
-        then = now;
-        bool more = there != 0;                                     // p + 1 is there
-        if (more) next(then);
-#pragma unroll
-        for (int i = 0; i < KL + VL; ++i) request(i, now);
-        // V of "page -1", for the sums of the weights 0 in front of the first: zeros
-        for (uint32_t at = 16 * tid; at < Page<D>::kBytes; at += 16 * kThreads) lds_write16(lds + 4 * Page<D>::kBytes + at, u32x4{0, 0, 0, 0});
-        __syncthreads();                                            // (s_odd)
-        collect();
-        if (now.key0 + kBlock - 1 > pos0) clean(now.key0);
-#pragma unroll
-        for (int i = 0; i < KP + CV; ++i) write(i, lds, lds + 2 * Page<D>::kBytes, now.ks, now.vs);
-#pragma unroll
-        for (int i = 0; i < KL + VL; ++i) request(i, then);
-#pragma unroll
-        for (int x = 0; x < CG; ++x)
-#pragma unroll
-            for (int i = 0; i < 4 * PIECES; ++i) pb[1][x][i / 4][i % 4] = 0u;
-        int p2 = 0, p3 = 0, before = 2;                             // buffers of page p (K, V) and of V of p - 1
-        for (;;) {
-            collect();
+        const bool here = there != 0;
+        low = INT32_MAX;
+        if (here) {
+            next(now);
+            low = now.key0;
             refill();
-            after = then;
-            const bool most = there != 0;
-            if (most) next(after);
-            const int ahead3 = p3 == 2 ? 0 : p3 + 1;
-            if (then.key0 + kBlock - 1 > pos0) clean(then.key0);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (what this wavefront wrote)
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
+            then = now;
+            bool more = there != 0;                                     // p + 1 is there
+            if (more) next(then);
 #pragma unroll
-            for (int j = 0; j < W; ++j) fetch_k(j, k_half(p2, 0));
-            if (w >= 4) __builtin_amdgcn_s_setprio(1);              // (of two wavefronts of a SIMD the older wins otherwise, and waits at the barrier)
-            const uint32_t k_to = lds + (p2 ^ 1) * Page<D>::kBytes, v_to = lds + (2 + ahead3) * Page<D>::kBytes;
-            step(std::integral_constant<int, 0>(), std::true_type(), now.key0, k_half(p2, 0), v_half(before, 1), k_half(p2, 1), [&](int j) {
+            for (int i = 0; i < KL + VL; ++i) request(i, now);
+            // V of "page -1", for the sums of the weights 0 in front of the first: zeros
+            for (uint32_t at = 16 * tid; at < Page<D>::kBytes; at += 16 * kThreads) lds_write16(lds + 4 * Page<D>::kBytes + at, u32x4{0, 0, 0, 0});
+            __syncthreads();                                            // (s_odd)
+            collect();
+            if (now.key0 + kBlock - 1 > pos0) clean(now.key0);
 #pragma unroll
-                for (int i = j * PER_STEP; i < (j + 1) * PER_STEP && i < MOVES; ++i) {
-                    if (i < KP + CV) write(i, k_to, v_to, then.ks, then.vs);
-                    else request(i - KP - CV, after);
+            for (int i = 0; i < KP + CV; ++i) write(i, lds, lds + 2 * Page<D>::kBytes, now.ks, now.vs);
+#pragma unroll
+            for (int i = 0; i < KL + VL; ++i) request(i, then);
+#pragma unroll
+            for (int x = 0; x < CG; ++x)
+#pragma unroll
+                for (int i = 0; i < 4 * PIECES; ++i) pb[1][x][i / 4][i % 4] = 0u;
+            int p2 = 0, p3 = 0, before = 2;                             // buffers of page p (K, V) and of V of p - 1
+            for (;;) {
+                collect();
+                refill();
+                after = then;
+                const bool most = there != 0;
+                if (most) next(after);
+                const int ahead3 = p3 == 2 ? 0 : p3 + 1;
+                if (then.key0 + kBlock - 1 > pos0) clean(then.key0);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (what this wavefront wrote)
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < W; ++j) fetch_k(j, k_half(p2, 0));
+                if (w >= 4) __builtin_amdgcn_s_setprio(1);              // (of two wavefronts of a SIMD the older wins otherwise, and waits at the barrier)
+                const uint32_t k_to = lds + (p2 ^ 1) * Page<D>::kBytes, v_to = lds + (2 + ahead3) * Page<D>::kBytes;
+                step(std::integral_constant<int, 0>(), std::true_type(), slack, lift, now.key0, k_half(p2, 0), v_half(before, 1), k_half(p2, 1), [&](int j) {
+#pragma unroll
+                    for (int i = j * PER_STEP; i < (j + 1) * PER_STEP && i < MOVES; ++i) {
+                        if (i < KP + CV) write(i, k_to, v_to, then.ks, then.vs);
+                        else request(i - KP - CV, after);
+                    }
+                });
+                __builtin_amdgcn_s_setprio(0);
+                step(std::integral_constant<int, 1>(), std::false_type(), slack, lift, now.key0 + 32, k_half(p2, 1), v_half(p3, 0), 0, [](int) {});
+                before = p3;
+                p3 = ahead3;
+                p2 ^= 1;
+                if (!more) break;
+                now = then;
+                then = after;
+                more = most;
+            }
+            // sums of the last half
+#pragma unroll
+            for (int j = 0; j < DT; ++j) {
+                fetch_v(j, v_half(before, 1));
+                sums(j, pb[1]);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (no copy is under way into LDS that this workgroup gives back)
+            if (lift == 0.f) {
+#pragma unroll
+                for (int x = 0; x < CG; ++x) {
+                    uint32_t bad = 0u;
+#pragma unroll
+                    for (int i = 0; i < DT; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) bad |= finite(acc[x][i][r]) ? 0u : 1u << (4 * i + r);
+                    bad = used[x] ? bad : 0u;
+                    s_bad[x][tid] = bad;
+                    if (bad != 0u) s_again = 1;
                 }
-            });
-            __builtin_amdgcn_s_setprio(0);
-            step(std::integral_constant<int, 1>(), std::false_type(), now.key0 + 32, k_half(p2, 1), v_half(p3, 0), 0, [](int) {});
-            before = p3;
-            p3 = ahead3;
-            p2 ^= 1;
-            if (!more) break;
-            now = then;
-            then = after;
-            more = most;
+            }
+            __syncthreads();                                            // (s_odd, s_again)
         }
-        // sums of the last half
-#pragma unroll
-        for (int j = 0; j < DT; ++j) {
-            fetch_v(j, v_half(before, 1));
-            sums(j, pb[1]);
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // (no copy is under way into LDS that this workgroup gives back)
-        __syncthreads();                                            // (s_odd)
-    }
 
 #pragma unroll
-    for (int x = 0; x < CG; ++x) {
-        const float total = rows_add(sum[x]);
-        const bool seen = used[x] && low <= pos0 + ti[x];
-        if (nsplit == 1) {
-            if (!used[x]) continue;
-            const int64_t row = row0 + first + ti[x];
-            const int qh = h * G + m % G;
-            const float inv = seen ? 1.f / total : 0.f;
-            bf16_t *dst = reinterpret_cast<bf16_t *>(a.out) + (row * a.hq + qh) * D + 4 * g;
+        for (int x = 0; x < CG; ++x) {
+            int t = ti[x];
+            asm volatile("" : "+v"(t));                             // (addresses are formed here: kept through the second walk they take registers)
+            const float total = rows_add(sum[x]);
+            const bool seen = used[x] && low <= pos0 + t;
+            // (a split without weight is 0 with no weight: others of the column may have some)
+            const float inv = seen && (nsplit == 1 || total != 0.f) ? 1.f / total : 0.f;
+            const uint32_t kept = lift != 0.f ? ~s_bad[x][tid] : 0u;                     // elements that are the first walk's
+            if (nsplit == 1) {
+                if (!used[x]) continue;
+                const int64_t row = row0 + first + t;
+                const int qh = h * G + m % G;
+                bf16_t *dst = reinterpret_cast<bf16_t *>(a.out) + (row * a.hq + qh) * D + 4 * g;
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                const float o[4] = {acc[x][i][0] * inv, acc[x][i][1] * inv, acc[x][i][2] * inv, acc[x][i][3] * inv};
-                store_row<bf16_t, 4>(dst + 16 * i, o);
-            }
-            if (g == 0 && a.lse != nullptr) a.lse[row * a.hq + qh] = seen ? ref[x] * kLn2 + logf(total) : -INFINITY;
-        } else {
-            const int64_t col = slot * (16 * NW * CG) + (w * CG + x) * 16 + m;
-            float *dst = a.part + col * D + 4 * g;
+                for (int i = 0; i < DT; ++i) {
+                    float o[4] = {acc[x][i][0] * inv, acc[x][i][1] * inv, acc[x][i][2] * inv, acc[x][i][3] * inv};
+                    if (lift != 0.f) {
 #pragma unroll
-            for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4 *>(dst + 16 * i) = acc[x][i];
-            if (g == 0) {
-                a.ml[col * 2] = seen ? ref[x] : -INFINITY;
-                a.ml[col * 2 + 1] = total;
+                        for (int r = 0; r < 4; ++r) o[r] = (kept >> (4 * i + r)) & 1u ? Elem<bf16_t>::load(dst + 16 * i + r) : o[r];
+                    }
+                    store_row<bf16_t, 4>(dst + 16 * i, o);
+                }
+                if (lift == 0.f && g == 0 && a.lse != nullptr) a.lse[row * a.hq + qh] = seen ? ref[x] * kLn2 + logf(total) : -INFINITY;
+            } else {
+                const int64_t col = slot * (16 * NW * CG) + (w * CG + x) * 16 + m + (t - ti[x]);
+                float *dst = a.part + col * D + 4 * g;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    f32x4 o = acc[x][i] * inv;
+                    if (lift != 0.f) {
+                        const f32x4 was = *reinterpret_cast<const f32x4 *>(dst + 16 * i);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[r] = (kept >> (4 * i + r)) & 1u ? was[r] : o[r];
+                    }
+                    *reinterpret_cast<f32x4 *>(dst + 16 * i) = o;
+                }
+                if (lift == 0.f && g == 0) {
+                    a.ml[col * 2] = seen ? ref[x] : -INFINITY;
+                    a.ml[col * 2 + 1] = total;
+                }
             }
         }
-    }
+        return here;
+    };
+    if (pass(std::false_type()) && s_again != 0) pass(std::true_type());
     if (low == INT32_MAX || s_odd == 0) return;
     // Values that are not finite were taken as 0 in pages that some tokens see further than others (0 x infinity): the tokens that do see them get them now.
     __threadfence_block();

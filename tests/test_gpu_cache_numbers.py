@@ -103,6 +103,71 @@ def _write(m, p, c, k0, v):  # noqa: F811
     m.cache_append(p, c, k.to(p.torch_dtype), v[None].expand(p.num_kv_heads, -1, -1).contiguous().to(p.torch_dtype), [0, ctx], [0])
 
 
+@pytest.mark.parametrize("kv", ["native", "e4m3"])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", *HEADS[0]), ("bf16", *HEADS[1]), ("bf16", 5, 5, 64), ("fp32", 4, 1, 64), ("fp32", 6, 2, 128)])
+@pytest.mark.parametrize("n,ctx", FORMS + [(700, 6001)])
+def test_sums_of_large_values_stay_finite(m, kv, dtype, hq, hkv, d, n, ctx):  # noqa: F811
+    """A mean of values next to the largest float is one of them, however many keys and whatever the softmax is taken relative to; values of other
+    channels are not touched by that, bit for bit."""
+    p, c = _large(m, dtype, kv, hq, hkv, d, ctx)
+    q = torch.zeros((n, hq, d), device="cuda", dtype=p.torch_dtype)
+    q[..., 0] = 1.0
+    gen = _gen(11)
+    v = torch.zeros((ctx, d), device="cuda")
+    v[:, 8:] = torch.randn((ctx, d - 8), generator=gen, device="cuda")
+    k0 = torch.randn(ctx, generator=gen, device="cuda") * 0.25
+    _write(m, p, c, k0, v)
+    top = 1.75 * 2.0 ** 127 if dtype == "bf16" or kv == "e4m3" else 3.0e38
+    if kv == "e4m3":                # (the scale of a page that holds such values: the others are zeros in it)
+        v[:, 8:] = 0
+        _write(m, p, c, k0, v)
+    clean, clean_lse = m.cache_attn(p, c, q, [0, n], [ctx])
+    v[:, 0], v[:, 1], v[:, 2], v[:, 3] = top, -top, 2.0 ** 120, top / 2
+    _write(m, p, c, k0, v)
+    out, lse = m.cache_attn(p, c, q, [0, n], [ctx])
+    assert torch.equal(lse, clean_lse) and torch.equal(out[..., 8:], clean[..., 8:])
+    for ch, x in ((0, top), (1, -top), (2, 2.0 ** 120), (3, top / 2)):
+        # a mean of equal values: the weights' rounding (2^-8 each at most, bf16 tiles) and the result's own
+        worst = (out[..., ch].double() / x - 1).abs().max()
+        assert bool(worst <= (2.0 ** -7 if dtype == "bf16" else 1e-4)), (ch, float(worst))
+
+
+@pytest.mark.parametrize("hq,hkv,d,n,ctx", [(32, 2, 128, 200, 6001), (8, 2, 64, 701, 6000), (32, 2, 128, 1400, 3001), (32, 2, 128, 1, 9001), (32, 2, 128, 3, 100)])
+def test_references_behind_the_largest_logit(m, hq, hkv, d, n, ctx):  # noqa: F811
+    """One key of weight 1 and two of 59.75 in different half pages, V = 2^122: sums relative to the first key would be 2^128.9."""
+    p, c = _large(m, "bf16", "native", hq, hkv, d, ctx)
+    q = torch.zeros((n, hq, d), device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    k0 = torch.full((ctx,), -100.0, device="cuda")
+    k0[0], k0[10], k0[40] = 0.0, 4.09375, 4.09375
+    _write(m, p, c, k0, torch.full((ctx, d), 2.0 ** 122, device="cuda"))
+    out, lse = m.cache_attn(p, c, q, [0, n], [ctx])
+    assert bool((out.double() / 2.0 ** 122 - 1).abs().max() <= 2.0 ** -7)
+    want = math.log(1 + 2 * math.exp(4.09375))
+    assert float((lse.double() - want).abs().max()) <= 1e-5
+
+
+@pytest.mark.parametrize("n,ctx", FORMS)
+def test_small_weights_of_large_values_count(m, n, ctx):  # noqa: F811
+    """A key 2^-100 times as heavy as another and of a value 2^110 times as large: most of the result.  (The other way round, weights that are cut off far
+    below the largest would lose it.)"""
+    hq, hkv, d = 32, 2, 128
+    p, c = _large(m, "bf16", "native", hq, hkv, d, ctx)
+    q = torch.zeros((n, hq, d), device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    k0 = torch.full((ctx,), -1000.0, device="cuda")
+    v = torch.zeros((ctx, d), device="cuda")
+    k0[0], v[0] = 0.0, 1.0
+    want = 1.0
+    if ctx - n >= 70:
+        k0[69], v[69] = -69.5, 2.0 ** 110
+        want += math.exp(-69.5) * 2.0 ** 110
+    _write(m, p, c, k0, v)
+    out, _ = m.cache_attn(p, c, q, [0, n], [ctx])
+    # the weights' rounding and the result's: 2^-8 each; a logit of -69.5 in units of log2 (-100.27) to 2^-17 of a binary order
+    assert bool((out.double() / want - 1).abs().max() <= 2.0 ** -7 + 2.0 ** -16)
+
+
 @pytest.mark.parametrize("n,ctx", FORMS)
 def test_logits_far_below_zero(m, n, ctx):  # noqa: F811
     """All logits at -2^127 ln 2, -1.7e38 in units of log2: a softmax over equal logits is a mean, wherever they are."""
