@@ -414,6 +414,7 @@ typedef struct infllmv2_cache {
  *   cu_new_h/d    host / device int32 [batch + 1]; prev_lens_h/d host / device int32 [batch]
  * A page is written by one sequence at a time: the pages that new tokens fall into must not be listed twice.  Rows that
  * do not belong to the new tokens stay as they are, up to the larger scale of a page that is continued.
+ * One call writes to fewer than 2^30 / head_dim pages (8.4 million of 128 channels), else UNSUPPORTED.
  */
 int infllmv2_cache_append(const infllmv2_params *p, const infllmv2_cache *c, const infllmv2_rotary *r, const void *k_d,
                           const void *v_d, int64_t kv_tok_stride, int64_t kv_head_stride, const int32_t *cu_new_h,
@@ -452,6 +453,7 @@ int infllmv2_decode_blocks(const infllmv2_params *p, const void *q_d, const floa
  *   lse_d          device float32 [total, num_q_heads] or NULL
  *   A token that has no key at all (empty list, or no page) gets zeros and lse = -infinity.
  *   workspace_d    device scratch (INFLLMV2_OP_CACHE_ATTN)
+ * A call that no launch holds (2^32 threads: 8 million tokens with lists and 2 KV heads) is UNSUPPORTED.
  */
 int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h,
                         const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,

@@ -20,6 +20,8 @@ struct Args {
 };
 
 int check(const infllmv2_params *p, const infllmv2_cache *c, int max_ctx, bool values);
+// a launch's threads are counted in 32 bits
+inline bool fits_launch(int64_t workgroups, int threads) { return workgroups < (1ll << 32) / threads; }
 Args args(const infllmv2_params *p, const infllmv2_cache *c);
 
 constexpr float kTop = 448.f;                          // largest e4m3 magnitude

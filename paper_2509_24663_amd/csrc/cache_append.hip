@@ -315,7 +315,7 @@ extern "C" int infllmv2_cache_append(const infllmv2_params *p, const infllmv2_ca
     }
     st = cache::check(p, c, max_ctx, true);
     if (st) return st;
-    if (p->num_kv_heads > 65535) return INFLLMV2_ERR_UNSUPPORTED;
+    if (p->num_kv_heads > 65535 || !cache::fits_launch(items, 4 * p->head_dim)) return INFLLMV2_ERR_UNSUPPORTED;
     AppendArgs a{cache::args(p, c), r ? rotary::args(r) : rotary::Args{nullptr, 0, 0, 1.f}, (const char *)k_d, (const char *)v_d,
                  kv_tok_stride, kv_head_stride, cu_new_d, prev_lens_d, pos_d, batch, single, 1};
     // heads of a workgroup: all, while that leaves a few workgroups for each CU (the angles of a key page are worked out once for them)

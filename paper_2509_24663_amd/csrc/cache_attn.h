@@ -72,6 +72,7 @@ struct AttnArgs {
 };
 
 // cache_attn_tile.hip
+constexpr int kTileThreads = 512;
 int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream);
 
 }  // namespace cache_attn

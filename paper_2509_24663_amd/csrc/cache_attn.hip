@@ -799,7 +799,7 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     const size_t need = unit_bytes(p, mine.slots), wide_need = tile_bytes(p, other.slots, wide.tile_groups);
     st = check_ws(workspace_d, workspace_bytes, need + wide_need);
     if (st) return st;
-    if (mine.items >= (1ll << 31) || other.items >= (1ll << 31)) return INFLLMV2_ERR_UNSUPPORTED;
+    if (!cache::fits_launch(mine.items, NW * 64) || !cache::fits_launch(other.items, cache_attn::kTileThreads)) return INFLLMV2_ERR_UNSUPPORTED;
     for (AttnArgs *x : {&a, &wide}) {
         x->c = cache::args(p, c);
         x->q = (const char *)q_d;

@@ -37,7 +37,8 @@ using cache_attn::kLowest;
 using cache_attn::pack;
 
 constexpr int NW = 8;
-constexpr int kThreads = NW * 64;
+constexpr int kThreads = cache_attn::kTileThreads;
+static_assert(kThreads == NW * 64, "eight wavefronts");
 constexpr float kSlack = 64.f;
 constexpr int kAhead = 4;                  // operands requested in front of their product
 
