@@ -20,19 +20,41 @@ struct CompressArgs {
     float *kc;
     int64_t kc_head_stride;
     const int32_t *prev, *ctx;
-    int pairs, lc, sc, rows;
+    int batch;
+    int64_t pairs;
+    int lc, sc, rows;
 };
 
-template <typename T, int D, bool CODES>
+// workgroups of a head of a sequence that has grown
+__host__ __device__ inline int items(int prev, int ctx, int lc, int sc, int per) { return (num_cmp(ctx, lc, sc) - num_cmp(prev, lc, sc) + per - 1) / per; }
+
+// LOOKUP: workgroups are those of the new rows, each finds its sequence; else as many for every sequence, those past its rows with nothing to do
+template <typename T, int D, bool CODES, bool LOOKUP>
 __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
     constexpr int VPR = D / VEC;
     // rows requested at once, of two pages at most, both looked up first (fp32 rows: registers)
     constexpr int U = CODES || sizeof(T) == 2 ? 32 : 16;
     typedef typename std::conditional<CODES, uint2, typename std::conditional<sizeof(T) == 2, gen::u16x8_u, gen::f32x8_u>::type>::type Vec;
-    const int slot = threadIdx.x / VPR, pair = (int)((blockIdx.y * (64u / VPR) + slot) / a.rows);
-    if (pair >= a.pairs) return;
-    const int b = pair / a.c.hkv, h = pair - b * a.c.hkv;
-    const int i = num_cmp(a.prev[b], a.lc, a.sc) + (int)blockIdx.x * a.rows + (slot & (a.rows - 1));
+    const int slot = threadIdx.x / VPR;
+    int b, h, i;
+    int64_t pair;
+    if constexpr (LOOKUP) {
+        __shared__ int s_item[6];
+        constexpr int PER = 64 / VPR;
+        int rem, before;
+        cache::Facts f;
+        b = cache::find_item(a.batch, (int)blockIdx.x, rem, before, f, s_item, [&](int s) { return items(a.prev[s], a.ctx[s], a.lc, a.sc, PER) * a.c.hkv; },
+                             [](int) { return 0; }, [&](int s, int) { return num_cmp(a.prev[s], a.lc, a.sc); });
+        if (b >= a.batch) return;
+        h = rem % a.c.hkv;
+        pair = (int64_t)b * a.c.hkv + h;
+        i = f.x[0] + rem / a.c.hkv * PER + slot;
+    } else {
+        pair = (blockIdx.y * (64u / VPR) + slot) / (unsigned)a.rows;
+        if (pair >= a.pairs) return;
+        b = (int)pair / a.c.hkv, h = (int)pair - b * a.c.hkv;
+        i = num_cmp(a.prev[b], a.lc, a.sc) + (int)blockIdx.x * a.rows + (slot & (a.rows - 1));
+    }
     if (i >= num_cmp(a.ctx[b], a.lc, a.sc)) return;
     const int c0 = (threadIdx.x % VPR) * VEC;
     float acc[VEC];
@@ -89,20 +111,32 @@ __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
     const float inv = 1.0f / (float)a.lc;
 #pragma unroll
     for (int c = 0; c < VEC; ++c) acc[c] *= inv;
-    gen::store_row<float, VEC>(a.kc + (int64_t)pair * a.kc_head_stride + (int64_t)i * D + c0, acc);
+    gen::store_row<float, VEC>(a.kc + pair * a.kc_head_stride + (int64_t)i * D + c0, acc);
 }
 
 template <typename T, int D>
-int launch_t(CompressArgs a, bool codes, int max_new, hipStream_t stream) {
+int launch_t(CompressArgs a, bool codes, const int32_t *prev, const int32_t *ctx, int max_new, hipStream_t stream) {
     // consecutive new rows of a pair share a workgroup
     const int per = 64 / (D / VEC);
     a.rows = 1;
     while (a.rows < per && a.rows < max_new) a.rows *= 2;
-    const int64_t y = ((int64_t)a.pairs * a.rows + per - 1) / per;
-    if (y > 65535) return INFLLMV2_ERR_UNSUPPORTED;
-    const dim3 grid((max_new + a.rows - 1) / a.rows, (unsigned)y);
-    if (codes) hipLaunchKernelGGL((cache_compress_kernel<T, D, true>), grid, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((cache_compress_kernel<T, D, false>), grid, dim3(64), 0, stream, a);
+    const int64_t x = ((int64_t)max_new + a.rows - 1) / a.rows, y = (a.pairs * a.rows + per - 1) / per;
+    // As many workgroups for every sequence and head need no search, but those of short ones stand idle, some 1000 a microsecond.  Both ways, us a call: one prompt of
+    // 65536 tokens beside 127 sequences with a new row 89.6, looked up 8.3; of 4096 beside 63 11.3 / 5.8; of 65536 beside one 9.0 / 7.6 (2046 idle); 16 of 4000 to
+    // 64000 42.5 / 35.0; of 1024 beside 63 5.8 / 6.0 (1890 idle); alike 65536 6.6 / 6.9.
+    int64_t n = 0;
+    for (int b = 0; b < a.batch; ++b) n += items(prev[b], ctx[b], a.lc, a.sc, per);
+    n *= a.c.hkv;
+    if (y > 65535 || x * y - n > 2000) {
+        if (!cache::fits_launch(n, 64)) return INFLLMV2_ERR_UNSUPPORTED;
+        if (codes) hipLaunchKernelGGL((cache_compress_kernel<T, D, true, true>), dim3((unsigned)n), dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL((cache_compress_kernel<T, D, false, true>), dim3((unsigned)n), dim3(64), 0, stream, a);
+    } else {
+        if (!cache::fits_launch(x, 64)) return INFLLMV2_ERR_UNSUPPORTED;
+        const dim3 grid((unsigned)x, (unsigned)y);
+        if (codes) hipLaunchKernelGGL((cache_compress_kernel<T, D, true, false>), grid, dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL((cache_compress_kernel<T, D, false, false>), grid, dim3(64), 0, stream, a);
+    }
     return hip_status(hipGetLastError());
 }
 
@@ -133,10 +167,10 @@ extern "C" int infllmv2_cache_compress_k(const infllmv2_params *p, const infllmv
     if (kc_cache_d == nullptr || kc_head_stride < (int64_t)max_nc * p->head_dim) return INFLLMV2_ERR_INVALID_ARGUMENT;
     st = cache::check(p, c, max_ctx, false);
     if (st) return st;
-    CompressArgs a{cache::args(p, c), kc_cache_d, kc_head_stride, prev_lens_d, ctx_lens_d, batch * p->num_kv_heads, p->cmp_len, p->cmp_stride, 1};
+    CompressArgs a{cache::args(p, c), kc_cache_d, kc_head_stride, prev_lens_d, ctx_lens_d, batch, (int64_t)batch * p->num_kv_heads, p->cmp_len, p->cmp_stride, 1};
     const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
     const hipStream_t s = (hipStream_t)stream;
     if (p->head_dim == 128)
-        return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 128>(a, codes, max_new, s) : launch_t<float, 128>(a, codes, max_new, s);
-    return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 64>(a, codes, max_new, s) : launch_t<float, 64>(a, codes, max_new, s);
+        return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 128>(a, codes, prev_lens_h, ctx_lens_h, max_new, s) : launch_t<float, 128>(a, codes, prev_lens_h, ctx_lens_h, max_new, s);
+    return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 64>(a, codes, prev_lens_h, ctx_lens_h, max_new, s) : launch_t<float, 64>(a, codes, prev_lens_h, ctx_lens_h, max_new, s);
 }
