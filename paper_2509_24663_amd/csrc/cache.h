@@ -55,15 +55,19 @@ __device__ inline uint32_t codes4(float a, float b, float c, float d) {
 struct Facts {
     int x[3];
 };
-// sums over the lanes up to a lane's own
-__device__ inline int wave_sums(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr:1, 2, 4, 8 (zeros shifted in)
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast:15 into rows 1 and 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);     // row_bcast:31 into rows 2 and 3
+// op over the lanes up to a lane's own (0: what op leaves as it is)
+template <class Op>
+__device__ inline int wave_scan(int x, Op op) {
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));      // row_shr:1, 2, 4, 8 (zeros shifted in)
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));     // row_bcast:15 into rows 1 and 3
+    x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));     // row_bcast:31 into rows 2 and 3
     return x;
+}
+__device__ inline int wave_sums(int x) {
+    return wave_scan(x, [](int a, int b) { return a + b; });
 }
 template <class Count, class Weight, class Fact>
 __device__ inline int find_item(int batch, int item, int &rem, int &before, Facts &facts, int (&s_out)[6], Count count, Weight weight, Fact fact) {

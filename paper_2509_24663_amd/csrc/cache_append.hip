@@ -100,13 +100,7 @@ __device__ inline void store_native(const rotary::Args &r, int q, T *row, const 
 __device__ inline uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 // over the wavefront, for all of it
 __device__ inline uint32_t wave_top(uint32_t x) {
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));      // row_shr:1, 2, 4, 8 (zeros shifted in)
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true));
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));     // row_bcast:15 into rows 1 and 3
-    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));     // row_bcast:31 into rows 2 and 3
-    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+    return (uint32_t)__builtin_amdgcn_readlane(cache::wave_scan((int)x, [](int a, int b) { return (int)max((uint32_t)a, (uint32_t)b); }), 63);
 }
 
 // pages that n new tokens behind prev cached ones fall into

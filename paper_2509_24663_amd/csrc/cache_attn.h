@@ -21,6 +21,20 @@ __device__ inline float formed(float x) {
     return x;
 }
 
+// over lanes with equal lane % 16
+__device__ inline float rows_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float rows_add(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+// two codes (the lower or the upper half of w) as two bf16 values; of the scale, a power of two, the exponent counts
+template <bool UPPER>
+__device__ inline uint32_t widen(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER));
+}
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ inline uint32_t pack(float a, float b) {          // nearest even
     const bf16x2 x = {(__bf16)a, (__bf16)b};

@@ -30,22 +30,11 @@ using cache_attn::formed;
 using cache_attn::kLift;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
+using cache_attn::rows_add;
+using cache_attn::rows_max;
+using cache_attn::widen;
 
 constexpr int NW = 4;                  // wavefronts of a workgroup
-__device__ inline float rows_max(float x) {          // over lanes with equal lane % 16
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ inline float rows_add(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
-
-// two codes (the lower or the upper half of w) as two bf16 values
-template <bool UPPER>
-__device__ inline uint32_t widen(uint32_t w, float scale) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER));
-}
 
 // ------------------------------------------------------------------------------------------ rows of a page, by element type and store
 // Keys: sixteen rows of a product, as loaded; the channels that a lane group takes are those of the query operand (load_query).

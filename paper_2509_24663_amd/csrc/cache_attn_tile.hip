@@ -35,6 +35,9 @@ using cache_attn::kLift;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
 using cache_attn::pack;
+using cache_attn::rows_add;
+using cache_attn::rows_max;
+using cache_attn::widen;
 
 constexpr int NW = 8;
 constexpr int kThreads = cache_attn::kTileThreads;
@@ -42,23 +45,11 @@ static_assert(kThreads == NW * 64, "eight wavefronts");
 constexpr float kSlack = 64.f;
 constexpr int kAhead = 4;                  // operands requested in front of their product
 
-template <bool UPPER>
-__device__ inline uint32_t widen(uint32_t w, float scale) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER));
-}
 // all ones in the elements of w that are infinities or NaN
 template <bool CODES>
 __device__ inline uint32_t not_finite(uint32_t w) {
     if (CODES) return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
     return ((((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
-}
-__device__ inline float rows_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ inline float rows_add(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
 }
 __device__ inline void lds_write16(uint32_t at, u32x4 x) {
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
