@@ -25,9 +25,6 @@ struct CompressArgs {
     int lc, sc, rows;
 };
 
-// workgroups of a head of a sequence that has grown
-__host__ __device__ inline int items(int prev, int ctx, int lc, int sc, int per) { return (num_cmp(ctx, lc, sc) - num_cmp(prev, lc, sc) + per - 1) / per; }
-
 // LOOKUP: workgroups are those of the new rows, each finds its sequence; else as many for every sequence, those past its rows with nothing to do
 template <typename T, int D, bool CODES, bool LOOKUP>
 __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
@@ -43,7 +40,7 @@ __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
         constexpr int PER = 64 / VPR;
         int rem, before;
         cache::Facts f;
-        b = cache::find_item(a.batch, (int)blockIdx.x, rem, before, f, s_item, [&](int s) { return items(a.prev[s], a.ctx[s], a.lc, a.sc, PER) * a.c.hkv; },
+        b = cache::find_item(a.batch, (int)blockIdx.x, rem, before, f, s_item, [&](int s) { return (num_cmp(a.ctx[s], a.lc, a.sc) - num_cmp(a.prev[s], a.lc, a.sc) + PER - 1) / PER * a.c.hkv; },
                              [](int) { return 0; }, [&](int s, int) { return num_cmp(a.prev[s], a.lc, a.sc); });
         if (b >= a.batch) return;
         h = rem % a.c.hkv;
@@ -115,18 +112,15 @@ __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
 }
 
 template <typename T, int D>
-int launch_t(CompressArgs a, bool codes, const int32_t *prev, const int32_t *ctx, int max_new, hipStream_t stream) {
-    // consecutive new rows of a pair share a workgroup
-    const int per = 64 / (D / VEC);
+int launch_t(CompressArgs a, bool codes, int max_new, int64_t n, hipStream_t stream) {
+    // consecutive new rows of a pair share a workgroup; n: workgroups that have rows then
+    constexpr int per = 64 / (D / VEC);
     a.rows = 1;
     while (a.rows < per && a.rows < max_new) a.rows *= 2;
     const int64_t x = ((int64_t)max_new + a.rows - 1) / a.rows, y = (a.pairs * a.rows + per - 1) / per;
     // As many workgroups for every sequence and head need no search, but those of short ones stand idle, some 1000 a microsecond.  Both ways, us a call: one prompt of
     // 65536 tokens beside 127 sequences with a new row 89.6, looked up 8.3; of 4096 beside 63 11.3 / 5.8; of 65536 beside one 9.0 / 7.6 (2046 idle); 16 of 4000 to
     // 64000 42.5 / 35.0; of 1024 beside 63 5.8 / 6.0 (1890 idle); alike 65536 6.6 / 6.9.
-    int64_t n = 0;
-    for (int b = 0; b < a.batch; ++b) n += items(prev[b], ctx[b], a.lc, a.sc, per);
-    n *= a.c.hkv;
     if (y > 65535 || x * y - n > 2000) {
         if (!cache::fits_launch(n, 64)) return INFLLMV2_ERR_UNSUPPORTED;
         if (codes) hipLaunchKernelGGL((cache_compress_kernel<T, D, true, true>), dim3((unsigned)n), dim3(64), 0, stream, a);
@@ -155,11 +149,14 @@ extern "C" int infllmv2_cache_compress_k(const infllmv2_params *p, const infllmv
     if (prev_lens_h == nullptr || prev_lens_d == nullptr || ctx_lens_h == nullptr || ctx_lens_d == nullptr)
         return INFLLMV2_ERR_INVALID_ARGUMENT;
     int max_new = 0, max_nc = 0, max_ctx = 0;
+    const int shift = p->head_dim == 128 ? 2 : 3;            // rows of a workgroup, as in the kernel
+    int64_t items = 0;
     for (int b = 0; b < batch; ++b) {
         if (prev_lens_h[b] < 0 || ctx_lens_h[b] < prev_lens_h[b] || ctx_lens_h[b] > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
         const int n1 = num_cmp(ctx_lens_h[b], p->cmp_len, p->cmp_stride);
         const int grown = n1 - num_cmp(prev_lens_h[b], p->cmp_len, p->cmp_stride);
         if (grown > max_new) max_new = grown;
+        items += ((int64_t)grown + (1 << shift) - 1) >> shift;
         if (n1 > max_nc) max_nc = n1;
         if (ctx_lens_h[b] > max_ctx) max_ctx = ctx_lens_h[b];
     }
@@ -167,10 +164,11 @@ extern "C" int infllmv2_cache_compress_k(const infllmv2_params *p, const infllmv
     if (kc_cache_d == nullptr || kc_head_stride < (int64_t)max_nc * p->head_dim) return INFLLMV2_ERR_INVALID_ARGUMENT;
     st = cache::check(p, c, max_ctx, false);
     if (st) return st;
+    items *= p->num_kv_heads;
     CompressArgs a{cache::args(p, c), kc_cache_d, kc_head_stride, prev_lens_d, ctx_lens_d, batch, (int64_t)batch * p->num_kv_heads, p->cmp_len, p->cmp_stride, 1};
     const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
     const hipStream_t s = (hipStream_t)stream;
     if (p->head_dim == 128)
-        return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 128>(a, codes, prev_lens_h, ctx_lens_h, max_new, s) : launch_t<float, 128>(a, codes, prev_lens_h, ctx_lens_h, max_new, s);
-    return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 64>(a, codes, prev_lens_h, ctx_lens_h, max_new, s) : launch_t<float, 64>(a, codes, prev_lens_h, ctx_lens_h, max_new, s);
+        return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 128>(a, codes, max_new, items, s) : launch_t<float, 128>(a, codes, max_new, items, s);
+    return p->dtype == INFLLMV2_BF16 ? launch_t<bf16_t, 64>(a, codes, max_new, items, s) : launch_t<float, 64>(a, codes, max_new, items, s);
 }
