@@ -387,7 +387,9 @@ int infllmv2_rotary_bwd(const infllmv2_params *p, const infllmv2_rotary *r, cons
  *                          3-bit-mantissa float (relative error at most 2^-4) unless it is over 2^13 times smaller than
  *                          the largest of its page.  A page that is continued keeps its scale or gets a larger one, and the
  *                          codes that it holds are then rounded again (exact unless they become subnormal).  NaN and
- *                          infinities are stored as NaN.
+ *                          infinities are stored as NaN.  Pages that are filled by other means must have such scales too:
+ *                          with others infllmv2_cache_attn of bf16 data (which reads their exponents) and the other
+ *                          readers differ.
  */
 #define INFLLMV2_CACHE_NATIVE 0
 #define INFLLMV2_CACHE_E4M3 1
@@ -449,9 +451,14 @@ int infllmv2_decode_blocks(const infllmv2_params *p, const void *q_d, const floa
  *   cu_q_h/d       host / device int32 [batch + 1]; ctx_lens_h/d host / device int32 [batch]
  *   block_idx_d    device int32 [total, num_kv_heads, topk_total]: the blocks that a token attends to, each listed once, in
  *                  any order (entries outside 0 .. the token's own block are skipped); sequences with
- *                  ctx_lens[b] < dense_threshold attend to every key.  NULL: all sequences do.
+ *                  ctx_lens[b] < dense_threshold attend to every key.  NULL: all sequences do.  infllmv2_decode_blocks makes
+ *                  the lists of a decode step; those of several tokens of a sequence are the caller's own (no call here
+ *                  makes them behind a cached context, and infllmv2_topk_blocks' lists are [num_kv_heads, total, topk_total]).
  *   lse_d          device float32 [total, num_q_heads] or NULL
  *   A token that has no key at all (empty list, or no page) gets zeros and lse = -infinity.
+ *   Rounding, bf16 data: the weights p of sequences with up to 8 queries, and of block lists, are taken to 2^-16 (an output
+ *                  is off by its own rounding and 2^-16 of the sum of p |v|).  Longer chunks over all keys may be taken to
+ *                  2^-8, like the output itself; whether they are, and how the keys are split, depends on the whole batch.
  *   workspace_d    device scratch (INFLLMV2_OP_CACHE_ATTN)
  * A call that no launch holds (2^32 threads: 8 million tokens with lists and 2 KV heads) is UNSUPPORTED.
  */

@@ -588,8 +588,8 @@ def decode_blocks(p: Params, q: torch.Tensor, kc_cache: torch.Tensor, ctx_lens, 
 def cache_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q, ctx_lens, block_idx: Optional[torch.Tensor] = None,
                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Attention of the newest tokens of each sequence over its pages.  q [T, hq, d], packed by cu_seqlens_q; sequence b has ctx_lens[b]
-    cached tokens, its queries the last of them.  block_idx [T, hkv, topk_total] int32 or None (all keys).  Returns (out [T, hq, d],
-    lse [T, hq])."""
+    cached tokens, its queries the last of them.  block_idx [T, hkv, topk_total] int32 (decode_blocks makes that of a decode step) or None (all
+    keys).  Returns (out [T, hq, d], lse [T, hq])."""
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     tokens, hq, _ = shape = q.shape
     assert q.is_contiguous() and q.dtype is p.torch_dtype and shape == (si.total, p.num_q_heads, p.head_dim)

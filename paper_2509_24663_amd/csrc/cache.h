@@ -49,9 +49,9 @@ __device__ inline uint32_t codes4(float a, float b, float c, float d) {
 }
 
 // Which sequence the item-th of a batch's work items belongs to, when sequence s has count(s) of them; rem: which of the sequence's; before: the sum
-// of weight(s) over the sequences in front.  Both sums are below 2^31 (the host has seen to it).  As find_seq_count (common.h), for counts that do not come from one list of offsets.  Called by every
-// thread of a workgroup; one barrier; returns >= batch past the last item.  facts(s, i), i = 0, 1, 2: what else is wanted of the sequence (the lane that
-// found it has just read it).
+// of weight(s) over the sequences in front.  Both sums are below 2^31 (fits_launch).  As find_seq_count (common.h), for counts that do not come from one
+// list of offsets.  Called by every thread of a workgroup; one barrier; returns >= batch past the last item.  facts(s, i), i = 0, 1, 2: what else is wanted of
+// the sequence (the lane that found it has just read it).
 struct Facts {
     int x[3];
 };

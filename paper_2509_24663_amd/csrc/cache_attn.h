@@ -1,4 +1,5 @@
-// What the two kernels of infllmv2_cache_attn share: cache_attn.hip (16 columns per workgroup, any data) and cache_attn_tile.hip (chunks of prompts, bf16).
+// What the two kernels of infllmv2_cache_attn share: cache_attn.hip (16 columns per workgroup, any data) and cache_attn_tile.hip (chunks of prompts and a few
+// tokens over long contexts, bf16).
 #pragma once
 #include "cache.h"
 #include "gen_unit.h"
@@ -11,8 +12,8 @@ constexpr float kLowest = -3.4028234e38f;
 
 // Sums of weights times values are finite wherever the result is: a mean of values.  Relative to the largest logit, or one near it, they may pass the
 // largest float although their quotient by the sum of the weights does not, so
-//  - elements of a walk's sums that are not finite are taken from a second walk whose references lie kLift binary orders above the largest logit (2^34 keys of weight
-//    2^6 x 2^-kLift stay below 1; the others keep the first walk's, whose small weights reach 40 orders further down),
+//  - elements of a walk's sums that are not finite are taken from a second walk whose references lie kLift binary orders above the largest logit (2^34 keys
+//    of weight 2^6 x 2^-kLift add up to 1; the other elements keep the first walk's, whose small weights reach 40 orders further down),
 //  - sums are joined as means: each divided by its own weights, then added up with its share of all weights.
 constexpr float kLift = 40.f;
 // (a factor that is formed before it is multiplied with anything else)

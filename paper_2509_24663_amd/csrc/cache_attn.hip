@@ -10,11 +10,11 @@
 // in flight.  The work of a (tile, KV head) is split along the keys over workgroups (launch_rules.h: unit_pps), and over the four wavefronts of each; partial
 // results are joined in LDS, then by cache_merge_kernel.
 //
-// Bound: HBM where the pages are many (64 sequences of 16384 to 65536 keys, 16 heads on 1, e4m3: 262 + 8 us for 1.37 GB, 5.1 TB/s; one of 500000: 55 us for 256 MB),
-// else a chain of trips to memory: length, page number, rows, partial results, joined results (16 sequences, 64 listed blocks each: 10.4 + 3.8 us, of which 0.5 to the
-// length, 1.4 to the page, 1.7 to its first logits, 2.8 for the rest of two pages, 0.5 in LDS; 5 sequences of 300 to 2011 keys with 4 tokens each, fp32: 10.8 + 4.1).
-// fp32 data: the products, 2.6 us for a page of 64 channels and wavefront.  Measured and not taken: a word of each line of the page after the next requested
-// ahead, for the L2 (16 sequences of 33000 keys: 56 -> 64 us).
+// Bound: HBM where the pages are many (64 sequences of 16384 to 65536 keys, 16 heads on 1, e4m3: 258 + 8 us for 1.37 GB, 5.2 TB/s, the matrix cores busy for 10 % of
+// it; one of 500000: 54 us for 256 MB), else a chain of trips to memory: length, page number, rows, partial results, joined results (16 sequences, 64 listed
+// blocks each: 11.0 + 4.0 us traced, of which some 0.5 to the length, 1.4 to the page, 1.7 to its first logits, 2.8 for the rest of two pages, 0.5 in LDS; 5
+// sequences of 300 to 2011 keys with 4 tokens each, fp32: 10.6 + 3.9).  fp32 data: the products, 2.6 us for a page of 64 channels and wavefront.  Measured and
+// not taken: a word of each line of the page after the next requested ahead, for the L2 (16 sequences of 33000 keys: 56 -> 64 us).
 #include <type_traits>
 
 #include "cache_attn.h"
@@ -749,7 +749,9 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     const bool use_small = wide.fine || small.us < large.us;
     wide.tile_groups = size[use_small].groups;
     wide.pps = use_small ? small.pps : large.pps;
-    if (tiled.tiles[0] == 0 || rules::unit_us(p->head_dim, tiled.most, tiled.unit_pages) <= (use_small ? small.us : large.us)) {
+    const double unit_us = wide.fine ? rules::few_us(p->head_dim * (c != nullptr && c->kv_type == INFLLMV2_CACHE_E4M3 ? 1 : 2), tiled.most, tiled.unit_pages)
+                                     : rules::unit_us(p->head_dim, tiled.most, tiled.unit_pages);
+    if (tiled.tiles[0] == 0 || unit_us <= (use_small ? small.us : large.us)) {
         a.wide_from = wide.wide_from = INT32_MAX;
         work.add(chunks.work);
         work.add(few.work);

@@ -1,5 +1,5 @@
-// Attention of a chunk of a prompt over its paged cache, bf16 data: tiles of 8 x CG groups of 16 columns (a column is a token and a head of one KV head); CG = 2
-// (head dim 64: 4), or 1 where large tiles are too few for the chip (launch_rules.h).
+// Attention of a chunk of a prompt, or of a few tokens over a long context, bf16 data: tiles of 8 x CG groups of 16 columns (a column is a token and a head of
+// one KV head); CG = 2 (head dim 64: 4), or 1 where large tiles are too few for the chip (launch_rules.h).
 //
 // The workgroup's eight wavefronts go through the pages together and each keeps CG column groups with their queries and sums in
 // registers, so that an operand read from LDS feeds CG products.  S^T = K Q^T and O^T += V^T P^T on 16x16x32 products; a lane's logits of a
@@ -8,16 +8,19 @@
 // each other: the vector unit works while the matrix core does).  A page is requested two pages ahead: K rows into registers, V rows (asynchronously) into a
 // buffer of the wavefront's own, from where transposing reads give a lane eight keys of a channel.  Beside the products of a first half they are widened
 // (codes times the page's scale: exact in bf16) and written as bf16 K and V^T pages, two and three buffers: one barrier per page.
-// Rounding: weights go into the second product as bf16 (2^-8 of each at most, like the output's own rounding); their sum takes them as they are.  References
-// move only where eight weights of a lane add up to more than kSlack, so a weight is below it.
+// Rounding: a chunk's weights go into the second product as bf16 (2^-8 of each at most, like the output's own rounding), those of up to eight tokens as two
+// bf16 pieces (2^-16); their sum takes them as they are.  Two pieces for chunks: 2048 tokens over 34816 943 -> 1330 us, 512 over 8000 84 -> 106.  References
+// move only where eight weights of a lane add up to more than kSlack, so a weight is below it; sums that pass the largest float for that: cache_attn.h.
 //
-// What bounds it: LDS and the matrix cores together.  2048 tokens over 34816, 32 heads on 2, e4m3: 946 to 996 us on different cards, 1140 to 1200 TFLOP/s (a large library
-// product reaches 1212 on this card); without LDS reads 786, without the rows' way through LDS 822, products and weights alone 656, products
-// alone 591.  Steps on the way: rows through registers by role and phases in lockstep 1208; queries waited for in front of the loop (their wait stood in
-// it and waited for the pages) 1102; the rows' work between the products 1043; the step of this form 1017; V through LDS with transposing reads 985; the second four
-// wavefronts ahead in first halves 966.  Measured and not taken: CG = 3 (two thirds of the LDS reads: 1013; fewer, larger tiles leave
-// CUs idle), the wavefronts of a SIMD taking turns behind barriers (1043), operands eight ahead (994).  A page takes a workgroup 1.75 us with CG = 2
-// and 1.13 with CG = 1 (head dim 64: 1.9 with CG = 4, 0.75 with CG = 1): a small tile has half or a quarter of the columns, so it is taken where the call is short of workgroups.
+// What bounds it: LDS and the matrix cores together, at the clocks that the products leave.  2048 tokens over 34816, 32 heads on 2, e4m3: 943 to 996 us on
+// different cards, 1140 to 1200 TFLOP/s (a large library product reaches 1212 on this card); the matrix cores are busy 49 % of the clocks and LDS 40 %, conflicts 8 %
+// (counters).  Parts left out, when the whole took 966: without LDS reads 786, without the rows' way through LDS 822, products and weights alone 656,
+// products alone 591.  Steps on the way: rows through registers by role and phases in lockstep 1208; queries waited for in front of the loop (their wait
+// stood in it and waited for the pages) 1102; the rows' work between the products 1043; the step of this form 1017; V through LDS with transposing reads
+// 985; the second four wavefronts ahead in first halves 966.  Measured and not taken: CG = 3 (two thirds of the LDS reads: 1013; fewer, larger tiles leave
+// CUs idle), the wavefronts of a SIMD taking turns behind barriers (1043), operands eight ahead (994).  A page takes a workgroup 1.75 us with CG = 2 and 1.13
+// with CG = 1, 1.46 with two pieces (head dim 64: 1.9 with CG = 4, 0.75 with CG = 1): a small tile has half or a quarter of the columns, so it is taken
+// where the call is short of workgroups.
 #include <type_traits>
 
 #include "attn_unit.h"

@@ -2,8 +2,9 @@
 // from prev[b] to ctx[b] tokens, from the keys as the pages hold them.  As the append of compress_k.hip, with a page looked up for every 64
 // tokens of a window; the additions are in the order of the window, in 32 bits.
 //
-// Bound: memory latency.  A window's rows are requested together, behind one lookup of the pages they are in.  128 sequences with a new row each: 4.8 us (fewer
-// rows at a time: 7.3; every row asked whether it is there: 5.7); 65536 tokens of 2 heads of 128, e4m3, 21 MB: 7.4 us (9.5; 8.8), every row read for two windows.
+// Bound: memory latency.  A window's rows are requested together, behind one lookup of the pages they are in.  128 sequences with a new row each: 4.6 us (fewer
+// rows at a time: 7.3; every row asked whether it is there: 5.7); 65536 tokens of 2 heads of 128, e4m3, 21 MB: 7.3 us (9.5; 8.8), every row read for two
+// windows.  (Adding each run of stride rows once would be half the requests, and another order of additions than that of compress_k.hip, whose rows these equal.)
 #include <type_traits>
 
 #include "cache.h"
@@ -40,7 +41,8 @@ __global__ void __launch_bounds__(64) cache_compress_kernel(CompressArgs a) {
         constexpr int PER = 64 / VPR;
         int rem, before;
         cache::Facts f;
-        b = cache::find_item(a.batch, (int)blockIdx.x, rem, before, f, s_item, [&](int s) { return (num_cmp(a.ctx[s], a.lc, a.sc) - num_cmp(a.prev[s], a.lc, a.sc) + PER - 1) / PER * a.c.hkv; },
+        b = cache::find_item(a.batch, (int)blockIdx.x, rem, before, f, s_item,
+                             [&](int s) { return (num_cmp(a.ctx[s], a.lc, a.sc) - num_cmp(a.prev[s], a.lc, a.sc) + PER - 1) / PER * a.c.hkv; },
                              [](int) { return 0; }, [&](int s, int) { return num_cmp(a.prev[s], a.lc, a.sc); });
         if (b >= a.batch) return;
         h = rem % a.c.hkv;
@@ -118,9 +120,9 @@ int launch_t(CompressArgs a, bool codes, int max_new, int64_t n, hipStream_t str
     a.rows = 1;
     while (a.rows < per && a.rows < max_new) a.rows *= 2;
     const int64_t x = ((int64_t)max_new + a.rows - 1) / a.rows, y = (a.pairs * a.rows + per - 1) / per;
-    // As many workgroups for every sequence and head need no search, but those of short ones stand idle, some 1000 a microsecond.  Both ways, us a call: one prompt of
-    // 65536 tokens beside 127 sequences with a new row 89.6, looked up 8.3; of 4096 beside 63 11.3 / 5.8; of 65536 beside one 9.0 / 7.6 (2046 idle); 16 of 4000 to
-    // 64000 42.5 / 35.0; of 1024 beside 63 5.8 / 6.0 (1890 idle); alike 65536 6.6 / 6.9.
+    // As many workgroups for every sequence and head need no search, but those of short ones stand idle, some 1000 a microsecond.  Both ways, us a call: one
+    // prompt of 65536 tokens beside 127 sequences with a new row 89.6, looked up 8.3; of 4096 beside 63 11.3 / 5.8; of 65536 beside one 9.0 / 7.6 (2046 idle);
+    // 16 of 4000 to 64000 42.5 / 35.0; of 1024 beside 63 5.8 / 6.0 (1890 idle); 65536 alone 6.6 / 6.9.
     if (y > 65535 || x * y - n > 2000) {
         if (!cache::fits_launch(n, 64)) return INFLLMV2_ERR_UNSUPPORTED;
         if (codes) hipLaunchKernelGGL((cache_compress_kernel<T, D, true, true>), dim3((unsigned)n), dim3(64), 0, stream, a);

@@ -419,10 +419,11 @@ struct PageWork {
 // once, two on a CU; starting those of each 256 is taken to cost 2.5 us, a page of a wavefront 0.6 us and 0.75 for each 16 KB of K and V (fp32 data, whose
 // products take longer: 2.6 for each 64 channels) or its share of 6 TB/s, less where the last workgroups leave CUs idle (sequences of many lengths even
 // out); a partial result 7 ns, the launch that joins them 5 us.
-// Measured before the last steps, one call, us, by pages 4 / 8 / 16 / 32 / 64 (one token each, 2 KV heads, d 128): 1 sequence of 33000 keys, e4m3 16.7 / 16.0 /
-// 18.1 / 22.7 / 32.9, bf16 19.6 / 17.5 / 21.1 / 29.3 / 46.4, fp32 27.9 / 23.9 / 34 / 54 / 96; of 500000, e4m3 107 / 77 / 65 / 58 / 56; 16 of 8000 29 / 24 / 21 / 23 /
-// 32; 64 of 16384 to 65536 478 / 347 / 294 / 315 / 285.  Split or not: 2 sequences, e4m3, 12 pages 15 / 12, 24 pages 15.2 / 15.4; bf16, 8 pages 15.3 /
-// 11.4, 16 pages 15 / 15.9; fp32, 8 pages 15.9 / 17.2.
+// Measured, one call, us, by pages 4 / 8 / 16 / 32 / 64 (one token each, 2 KV heads, d 128): 1 sequence of 33000 keys, e4m3 13.1 / 12.3 / 14.6 / 19.5 / 29.9,
+// bf16 15.3 / 14.2 / 18.0 / 26.3 / 43.4, fp32 25.3 / 21.3 / 31.5 / 52.6 / 93.9; of 500000, e4m3 44 / 56 / 49 / 46 / 45; 16 of 8000 22.6 / 19.3 / 18.6 / 19.7 / 29.6;
+// 64 of 16384 to 65536, 48 / 64 / 96 / 128 pages: 258 / 263 / 259 / 274.  Split (4 pages) or whole: 2 sequences, e4m3, 12 pages 10.0 / 9.2, 24 pages
+// 10.1 / 13.0; bf16, 8 pages 10.6 / 9.2; fp32, 16 pages 14.2 / 26.0.  Over 35 calls the rule's choice is 4.8 % from the best of eleven, half of them within
+// 2.1 %; furthest off are several tokens each of many sequences (32 of 10443, 3 tokens, fp32, d 64: 36.4, best 25.2).
 inline int unit_pps(const PageWork &w, int d, bool fp32, int bytes, int64_t least) {
     const int64_t from = (least + 3) / 4 * 4 < 4 ? 4 : (least + 3) / 4 * 4, whole = ((int64_t)w.most + 3) / 4 * 4;
     if (from >= whole) return (int)from;
@@ -451,12 +452,12 @@ constexpr TileSize tile_size(int d, bool small) {
     if (small) return d == 128 ? TileSize{8, 1.13, 0.03} : TileSize{8, 0.75, 0.01};
     return d == 128 ? TileSize{16, 1.75, 0.05} : TileSize{32, 1.9, 0.05};
 }
-// small, with weights of two pieces (half as many products again)
-constexpr TileSize fine_tile_size(int d) { return d == 128 ? TileSize{8, 1.35, 0.03} : TileSize{8, 0.95, 0.01}; }
+// small, with weights of two pieces (half as many products again): one workgroup over 2047 pages 2984 us, over 512 762
+constexpr TileSize fine_tile_size(int d) { return d == 128 ? TileSize{8, 1.46, 0.03} : TileSize{8, 0.97, 0.01}; }
 // Splits along the keys for `tiles` workgroups with up to `pages` pages, `sum` in all, on 256 CUs.  A call is taken to cost 14.7 us and its longest way:
 // rounds of workgroups, or where tiles differ (a prompt from its first token) their sum dealt out; several splits 1.5 us for the second launch and
-// result_us each.  Measured, one call, us (G 16, d 128, e4m3, 512 tokens over 8000, 1 / 2 / 4 splits): large tiles 231 / 134 / 84.6, small
-// 156 / 94.8 / 105; 300 over 1300, 1 / 3: 52 / 36, 36 / 30; G 4, d 64, 72 over 6800, 1 / 4 / 12: 219 / 71 / 37.5, 94 / 35 / 22.7.
+// result_us each.  Measured, one call, us (G 16, d 128, e4m3, 512 tokens over 8000, 1 / 2 / 4 splits): large tiles 219 / 128 / 81.8, small
+// 154 / 94.8 / 103; 300 over 1300, 1 / 3: 45.6 / 34.5, 32.8 / 30.3; G 4, d 64, 72 over 6800, 1 / 4 / 12: 221 / 68.6 / 35.8, 93.4 / 33.0 / 20.8.
 constexpr int kMostTileSplits = 64, kMostTileGroups = 16384;        // splits of a tile; column groups of all partial results
 struct TileSplits {
     int pps;               // pages of a split
@@ -474,12 +475,18 @@ inline TileSplits tile_splits(const TileSize &z, int64_t tiles, int pages, int64
     return best;
 }
 // What the kernel of 16 columns (cache_attn.hip) is taken to cost: `sum`: pages over all its column groups and KV heads; once there are many, rows come from
-// the L2; long ones cost the joining of many splits.  d 128: 600 groups over 21 pages 55 us, 2200 over 18 (half of them, on average) 75, 1024 over 126 200, 8 over 516 38; d 64: 366 over 9 17 us,
-// 256 over 125 50.
+// the L2; long ones cost the joining of many splits.  Some more than it takes (some 5 us of a call go by beside it, as of tile_splits' 14.7).  d 128: 600
+// groups over 21 pages 30.6 us, 2200 over 18 (half of them, on average) 51, 1024 over 126 171; d 64: 256 over 125 41.  The choice between it and the two
+// sizes of tiles over 72 chunks of 8 head shapes: 2.0 % from the best on average, twice above 8 (16 sequences of 18 tokens over 8000, d 64: 33 us, tiles 25).
 inline double unit_us(int d, int pages, int64_t sum) {
     const double few = sum < 20000 ? (double)sum : 20000.;
     return 13 + 0.02 * (pages < 500 ? pages : 500) + (d == 128 ? 3.2e-3 : 1.2e-3) * few + (d == 128 ? 1.4e-3 : 1.2e-3) * (sum - few);
 }
+// The same for sequences of up to kFewTokens query tokens, whose tiles have weights of two pieces; their splits read most pages from memory, by `row_bytes` a
+// row.  Measured on both, us (16 columns / tiles; d 128, e4m3, 16 heads on 1): 16 sequences of 8 tokens over 11000 keys 87 / 50, 4 of 8 over 7800 23 / 29, one of
+// 7 over 92000 35 / 48, one of 8 over 131000 82 / 66; rows of 2 bytes, 2 of 8 over 35000 37 / 28; d 64, one of 8 over 49000 20 / 26.  Over 180 sizes the
+// choice costs 0.6 % on average, 21 % at most.
+inline double few_us(int row_bytes, int pages, int64_t sum) { return 11.8 + 0.07 * (pages < 64 ? pages : 64) + (3e-4 + 1.2e-5 * row_bytes) * sum; }
 // The sequences that tiles are thought of for: those with at least so many column groups of queries.  Up to kFewTokens queries (a decode step, proposed
 // tokens) keep weights of 16 bits, so tiles of theirs are small ones with weights of two pieces; more are a chunk, whose weights may be rounded to 8 bits.
 constexpr int kTileFrom = 4, kFewTokens = 8;
