@@ -10,8 +10,9 @@ from test_gpu_cache import _filled, _gen, _params, m  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
-# One token, a few and a chunk of each sequence: the kernel of 16 columns in one launch and in splits, tiles of eight wavefronts
-FORMS = [(1, 1), (1, 300), (1, 9001), (3, 200), (3, 6003), (200, 6001)]
+# One token, a few and a chunk of each sequence: the kernel of 16 columns in one launch and in splits, tiles of eight wavefronts, with weights of two
+# pieces (8 tokens) and of one
+FORMS = [(1, 1), (1, 300), (1, 9001), (3, 200), (3, 6003), (8, 33000), (200, 6001)]
 HEADS = [(32, 2, 128), (8, 2, 64)]
 
 
@@ -130,6 +131,62 @@ def test_sums_of_large_values_stay_finite(m, kv, dtype, hq, hkv, d, n, ctx):  # 
         # a mean of equal values: the weights' rounding (2^-8 each at most, bf16 tiles) and the result's own
         worst = (out[..., ch].double() / x - 1).abs().max()
         assert bool(worst <= (2.0 ** -7 if dtype == "bf16" else 1e-4)), (ch, float(worst))
+
+
+@pytest.mark.parametrize("kv", ["native", "e4m3"])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", *HEADS[0]), ("fp32", 4, 1, 64)])
+@pytest.mark.parametrize("news,topk", [([1, 1], 8), ([1, 1], 40), ([1, 3], 40)])
+def test_sums_of_large_values_over_lists(m, kv, dtype, hq, hkv, d, news, topk):  # noqa: F811
+    """The same where blocks are listed: the pages of a second walk are those of the first."""
+    ctxs = [6001, 700]
+    p = _params(m, dtype, hq, hkv, d, softmax_scale=1.0, topk_total=topk, dense_threshold=0)
+    c, _, _ = _filled(m, p, ctxs, kv, 5)
+    top = 1.75 * 2.0 ** 127 if dtype == "bf16" or kv == "e4m3" else 3.0e38
+    sign = torch.tensor([1.0, -1.0, 0.5, 0.0] * (d // 4), device="cuda")
+    k = torch.zeros((hkv, sum(ctxs), d), device="cuda")
+    k[..., 0] = torch.randn(sum(ctxs), generator=_gen(1), device="cuda") * 0.25
+    v = (sign * top).expand(hkv, sum(ctxs), d).contiguous()
+    m.cache_append(p, c, k.to(p.torch_dtype), v.to(p.torch_dtype), [0, ctxs[0], sum(ctxs)], [0, 0])
+    T, gen = sum(news), torch.Generator().manual_seed(2)
+    blocks = torch.full((T, hkv, topk), -1, dtype=torch.int32)
+    for row, L in enumerate([ctxs[0]] * news[0] + [ctxs[1]] * news[1]):
+        for h in range(hkv):
+            x = torch.randperm((L - 3 + 63) // 64, generator=gen)[:topk]
+            blocks[row, h, torch.randperm(topk, generator=gen)[:len(x)]] = x.to(torch.int32)
+    q = torch.zeros((T, hq, d), device="cuda", dtype=p.torch_dtype)
+    q[..., 0] = 1.0
+    out, lse = m.cache_attn(p, c, q, [0, news[0], T], ctxs, blocks.cuda())
+    want = sign.double() * top
+    assert bool(torch.isfinite(lse).all())
+    # a mean of equal values: the weights' rounding and the result's own
+    assert bool(((out.double() - want).abs() <= (2.0 ** -7 if dtype == "bf16" else 1e-4) * want.abs()).all())
+
+
+@pytest.mark.parametrize("hq,hkv,d,n,ctx", [(32, 2, 128, 3, 200), (8, 2, 64, 60, 700), (32, 2, 128, 8, 33000), (32, 2, 128, 200, 6001), (8, 2, 64, 701, 6000), (32, 2, 128, 1400, 3001)])
+def test_infinities_beside_large_values(m, hq, hkv, d, n, ctx):  # noqa: F811
+    """One channel's sums pass the largest float, another has an infinity that only the last tokens see, a third a NaN that all see: each token and channel has what
+    is its own."""
+    p, c = _large(m, "bf16", "native", hq, hkv, d, ctx)
+    q = torch.zeros((n, hq, d), device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    v = torch.randn((ctx, d), generator=_gen(11), device="cuda")
+    k0 = torch.randn(ctx, generator=_gen(12), device="cuda") * 0.25
+    _write(m, p, c, k0, v)
+    clean, clean_lse = m.cache_attn(p, c, q, [0, n], [ctx])
+    top, late = 1.75 * 2.0 ** 127, ctx - 1 - n // 2
+    v[:, 0], v[:, 9] = top, -top
+    v[late, 5] = float("inf")
+    v[3, 6] = float("nan")
+    _write(m, p, c, k0, v)
+    out, lse = m.cache_attn(p, c, q, [0, n], [ctx])
+    sees = torch.arange(ctx - n, ctx, device="cuda") >= late
+    assert torch.equal(lse, clean_lse)
+    assert bool((out[sees][..., 5] == float("inf")).all()) and torch.equal(out[~sees][..., 5], clean[~sees][..., 5])
+    assert bool(torch.isnan(out[..., 6]).all())
+    for ch, x in ((0, top), (9, -top)):
+        assert bool((out[..., ch].double() / x - 1).abs().max() <= 2.0 ** -7)
+    rest = [x for x in range(d) if x not in (0, 5, 6, 9)]
+    assert torch.equal(out[..., rest], clean[..., rest])
 
 
 @pytest.mark.parametrize("hq,hkv,d,n,ctx", [(32, 2, 128, 200, 6001), (8, 2, 64, 701, 6000), (32, 2, 128, 1400, 3001), (32, 2, 128, 1, 9001), (32, 2, 128, 3, 100)])
