@@ -46,6 +46,7 @@ constexpr int NW = 8;
 constexpr int kThreads = cache_attn::kTileThreads;
 static_assert(kThreads == NW * 64, "eight wavefronts");
 constexpr float kSlack = 64.f;
+constexpr float kTopBf16 = 3.3895314e38f;  // largest bf16 number
 constexpr int kAhead = 4;                  // operands requested in front of their product
 
 // all ones in the elements of w that are infinities or NaN
@@ -451,6 +452,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             const bool seen = used[x] && low <= pos0 + t;
             // (a split without weight is 0 with no weight: others of the column may have some)
             const float inv = seen && (nsplit == 1 || total != 0.f) ? 1.f / total : 0.f;
+            // (weights rounded up may bring a mean of the largest numbers past them)
+            auto mean = [&](float s) { return total > 0.f && finite(s) ? __builtin_amdgcn_fmed3f(s * inv, -kTopBf16, kTopBf16) : s * inv; };
             const uint32_t kept = lift != 0.f ? ~s_bad[x][tid] : 0u;                     // elements that are the first walk's
             if (nsplit == 1) {
                 if (!used[x]) continue;
@@ -459,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                 bf16_t *dst = reinterpret_cast<bf16_t *>(a.out) + (row * a.hq + qh) * D + 4 * g;
 #pragma unroll
                 for (int i = 0; i < DT; ++i) {
-                    float o[4] = {acc[x][i][0] * inv, acc[x][i][1] * inv, acc[x][i][2] * inv, acc[x][i][3] * inv};
+                    float o[4] = {mean(acc[x][i][0]), mean(acc[x][i][1]), mean(acc[x][i][2]), mean(acc[x][i][3])};
                     if (lift != 0.f) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) o[r] = (kept >> (4 * i + r)) & 1u ? Elem<bf16_t>::load(dst + 16 * i + r) : o[r];
@@ -472,7 +475,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                 float *dst = a.part + col * D + 4 * g;
 #pragma unroll
                 for (int i = 0; i < DT; ++i) {
-                    f32x4 o = acc[x][i] * inv;
+                    f32x4 o = {mean(acc[x][i][0]), mean(acc[x][i][1]), mean(acc[x][i][2]), mean(acc[x][i][3])};
                     if (lift != 0.f) {
                         const f32x4 was = *reinterpret_cast<const f32x4 *>(dst + 16 * i);
 #pragma unroll

@@ -133,6 +133,22 @@ def test_sums_of_large_values_stay_finite(m, kv, dtype, hq, hkv, d, n, ctx):  # 
         assert bool(worst <= (2.0 ** -7 if dtype == "bf16" else 1e-4)), (ch, float(worst))
 
 
+@pytest.mark.parametrize("hq,hkv,d,n,ctx", [(32, 2, 128, 1, 9001), (32, 2, 128, 8, 33000), (32, 2, 128, 200, 6001), (8, 2, 64, 701, 6000), (32, 2, 128, 1400, 3001), (8, 2, 64, 2000, 6000)])
+def test_the_largest_value_of_the_type(m, hq, hkv, d, n, ctx):  # noqa: F811
+    """A mean of the largest bf16 number is that number, although a weight of exp(-0.6875), all keys' but one, is rounded up by 0.2 % in eight bits."""
+    p, c = _large(m, "bf16", "native", hq, hkv, d, ctx)
+    q = torch.zeros((n, hq, d), device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = 1.0
+    k0 = torch.full((ctx,), -0.6875, device="cuda")
+    k0[0] = 0.0
+    top = torch.finfo(torch.bfloat16).max
+    v = torch.full((ctx, d), top, device="cuda")
+    v[:, 1::2] = -top
+    _write(m, p, c, k0, v)
+    out, _ = m.cache_attn(p, c, q, [0, n], [ctx])
+    assert bool((out == v[0]).all())
+
+
 @pytest.mark.parametrize("kv", ["native", "e4m3"])
 @pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", *HEADS[0]), ("fp32", 4, 1, 64)])
 @pytest.mark.parametrize("news,topk", [([1, 1], 8), ([1, 1], 40), ([1, 3], 40)])
