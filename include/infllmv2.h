@@ -21,6 +21,12 @@
  *   infllmv2_cache_compress_k   stage 1 for the rows that a growing paged cache has just completed
  *   infllmv2_decode_blocks      stages 2-3 of the decode step: the block lists alone
  *   infllmv2_cache_attn         stage 4 (or dense attention) of the newest tokens over the pages
+ * For drafted tokens (speculative decoding) and for sequences that continue others, come and go:
+ *   infllmv2_tree_masks         ancestors and positions of the tokens of a tree
+ *   infllmv2_cache_tree_attn    attention of a tree's tokens over the pages: the context and each one's ancestors
+ *   infllmv2_cache_accept       the rows of the accepted path brought together
+ *   infllmv2_pages_resize / _fork / _compact   which pages the blocks of a sequence are in
+ *   infllmv2_cache_copy_pages   the copies that follow from the last two
  *
  * General rules
  *   - Every pointer named *_d or documented "device" is GPU memory on the current
@@ -128,7 +134,8 @@ typedef enum infllmv2_op {
     INFLLMV2_OP_SPARSE_ATTN_BWD_MIN = 9,    /* without it */
     INFLLMV2_OP_COMPRESS_K_APPEND = 10,
     INFLLMV2_OP_CACHE_ATTN = 11,            /* total_tokens: query tokens; max_seqlen: longest context */
-    INFLLMV2_OP_DECODE_BLOCKS = 12          /* as INFLLMV2_OP_SPARSE_DECODE */
+    INFLLMV2_OP_DECODE_BLOCKS = 12,         /* as INFLLMV2_OP_SPARSE_DECODE */
+    INFLLMV2_OP_CACHE_TREE_ATTN = 13        /* as INFLLMV2_OP_CACHE_ATTN */
 } infllmv2_op;
 
 /*
@@ -466,6 +473,108 @@ int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cache *c, const
                         const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
                         const int32_t *block_idx_d, void *out_d, float *lse_d, void *workspace_d, size_t workspace_bytes,
                         void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Trees of drafted tokens.  The last n = cu_q[b + 1] - cu_q[b] of the ctx_lens[b] rows that sequence b has in its pages are drafted tokens: row
+ * ctx_lens[b] - n + i holds token i of its tree, the rows in front are the context.  (A step: infllmv2_tree_masks; infllmv2_cache_append of the tree's keys
+ * and values with prev_lens = ctx_lens - n and the tree's positions; infllmv2_cache_tree_attn; the caller's choice of a path; infllmv2_cache_accept.)
+ *
+ * infllmv2_tree_masks: who is whose ancestor, from the tokens' parents.
+ *   parents_d     device int32 [total]: the number, in its tree, of the token that a token continues, in any order; a number outside 0 .. n - 1 is none: the
+ *                 token continues the context.  (Parents that lead back to a token in a circle are no tree: tokens then have everything that can be reached.)
+ *   mask_d        device out uint32 [total, mask_words], 32 mask_words >= the largest n: bit j % 32 of word j / 32 of a token's row: token j is it or an
+ *                 ancestor of it
+ *   pos_d         device out int32 [total] or NULL: the token's position, ctx_lens[b] - n + its ancestors (ctx_lens may be NULL where pos_d is)
+ * Trees of more than INFLLMV2_TREE_MOST tokens are UNSUPPORTED.
+ */
+#define INFLLMV2_TREE_MOST 1024
+int infllmv2_tree_masks(const int32_t *parents_d, const int32_t *cu_q_h, const int32_t *cu_q_d, const int32_t *ctx_lens_h,
+                        const int32_t *ctx_lens_d, int32_t batch, uint32_t *mask_d, int32_t mask_words, int32_t *pos_d, void *stream);
+
+/*
+ * Attention of the drafted tokens of each sequence over its pages: token i attends to the context and to those of the n drafted rows that its row of the mask
+ * names (itself only if it does; any mask is allowed, of any n).
+ *   mask_d         device uint32 [total, mask_words], as infllmv2_tree_masks writes it; 32 mask_words >= the largest n, bits from n on say nothing
+ *   block_idx_d    device int32 [batch, num_kv_heads, topk_total]: the blocks whose context rows the tokens of a sequence attend to, each listed once, in any
+ *                  order (other numbers than those of blocks with context rows are skipped); sequences with ctx_lens[b] < dense_threshold attend to all of
+ *                  the context.  Drafted rows are the mask's, listed or not.  NULL: all sequences attend to all of the context.  infllmv2_decode_blocks makes
+ *                  such lists from a query of the sequence, its newest token's for instance.
+ * Other arguments, rows without a key, rounding and limits as for infllmv2_cache_attn (scratch: INFLLMV2_OP_CACHE_TREE_ATTN).
+ */
+int infllmv2_cache_tree_attn(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h,
+                             const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
+                             const uint32_t *mask_d, int32_t mask_words, const int32_t *block_idx_d, void *out_d, float *lse_d,
+                             void *workspace_d, size_t workspace_bytes, void *stream);
+
+/*
+ * Keeps a path of each sequence's tree: drafted row path[i] becomes drafted row i, keys and values of every head.
+ *   path_d        device int32 [batch, path_stride]: numbers of drafted tokens, rising; the path ends in front of the first entry that is outside 0 .. n - 1
+ *                 or not above the one before it (-1 behind the last), or after path_stride entries
+ *   new_lens_d    device out int32 [batch] or NULL: ctx_lens[b] - n + the path's length
+ * Rows of the context and drafted rows that no row of the path moves to keep their values.  e4m3: a page that rows move to keeps its scale or gets the larger one
+ * that they need, and its other rows are then rounded again, as in infllmv2_cache_append.  A row moves only if its page and the page it moves to are there.
+ * Pages that rows move to must be in no other sequence's table.
+ */
+int infllmv2_cache_accept(const infllmv2_params *p, const infllmv2_cache *c, const int32_t *cu_q_h, const int32_t *cu_q_d,
+                          const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch, const int32_t *path_d,
+                          int32_t path_stride, int32_t *new_lens_d, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Page tables: which pages the blocks of a sequence are in (one table serves the caches of all layers).  refs[g] counts the table entries that name page g; a
+ * page with none is free.  Table and counts are the caller's; a new pool has counts of 0 and entries of -1.  The calls take the lowest free page for
+ * the first entry that wants one, and so on, in order of sequences (or forks) and blocks: the same table and counts give the same result.  Where
+ * pages run out, the last entries get -1 (a page that is not there) and short_d, device int32 [1] or NULL, holds how many.  Calls on one pool follow each
+ * other on a stream or by events.
+ */
+typedef struct infllmv2_pages {
+    int32_t num_pages;            /* >= 1                                                                        */
+    int32_t rows, blocks;         /* of the table: sequences, blocks of a sequence; >= 1                         */
+    int32_t table_stride;         /* >= blocks                                                                   */
+    int32_t *page_table_d;        /* device [rows, table_stride]; as in infllmv2_cache                           */
+    int32_t *refs_d;              /* device [num_pages]                                                          */
+    int32_t reserved;             /* 0                                                                           */
+} infllmv2_pages;
+
+#define INFLLMV2_PAGES_MOST_ROWS 4096   /* sequences or forks of a call (infllmv2_pages_fork: rows of the table too), else UNSUPPORTED */
+
+/*
+ * Sequence b (row b of the table) had room for old_lens[b] tokens and gets room for new_lens[b]: blocks ceil(old / 64) .. ceil(new / 64) - 1 get pages, blocks
+ * ceil(new / 64) .. ceil(old / 64) - 1 lose theirs (entries become -1; pages that no other entry names are free, to sequences of the same call as well).  A
+ * new length of 0 frees a sequence.
+ *   old_lens_h/d, new_lens_h/d   host / device int32 [batch], at most 64 * blocks
+ */
+int infllmv2_pages_resize(const infllmv2_pages *g, const int32_t *old_lens_h, const int32_t *old_lens_d, const int32_t *new_lens_h,
+                          const int32_t *new_lens_d, int32_t batch, int32_t *short_d, void *stream);
+
+/*
+ * Row dst gets the first `tokens` tokens of row src: the pages of whole blocks are shared, a last block that is not whole gets a page of its own, to which
+ * the source's is to be copied (infllmv2_cache_copy_pages of copies_d, for each layer).  What row dst had room for before (old_tokens; 0: nothing) is given back first,
+ * so that a continuation can take another's place.  Several forks may continue one source; a row that is written must not be written twice nor be a source.
+ *   forks_h/d     host / device [count]; forks_d 16-byte aligned
+ *   copies_d      device out int32 [count][2] or NULL: the page to copy from and the page to copy to, or -1, -1
+ */
+typedef struct infllmv2_fork {
+    int32_t src, dst, tokens, old_tokens;
+} infllmv2_fork;
+int infllmv2_pages_fork(const infllmv2_pages *g, const infllmv2_fork *forks_h, const infllmv2_fork *forks_d, int32_t count,
+                        int32_t *copies_d, int32_t *short_d, void *stream);
+
+/*
+ * Brings the pages in use to the front of the pool: with L of them, those numbered L and above move, in order, to the free ones below L, in order.  The table (of
+ * its first `batch` rows blocks 0 .. ceil(lens / 64) - 1, which hold all entries that refs counts; the others become -1) and the counts by the new numbers go to `out`,
+ * which is g, or has table and counts apart from g's.
+ *   moves_d       device out int32 [num_pages / 2][2]: page to copy from and page to copy to (infllmv2_cache_copy_pages), -1, -1 behind the last
+ *   live_d        device out int32 [2]: L and the number of moves
+ */
+int infllmv2_pages_compact(const infllmv2_pages *g, const int32_t *lens_h, const int32_t *lens_d, int32_t batch, const infllmv2_pages *out,
+                           int32_t *moves_d, int32_t *live_d, void *stream);
+
+/*
+ * Copies pages whole: keys, values and scales of every head.
+ *   pairs_d       device int32 [count][2]: page to copy from, page to copy to; pairs with a number outside [0, num_pages) are skipped.  No page that a pair writes may be
+ *                 another pair's.
+ */
+int infllmv2_cache_copy_pages(const infllmv2_params *p, const infllmv2_cache *c, const int32_t *pairs_d, int32_t count, void *stream);
 
 #ifdef __cplusplus
 }

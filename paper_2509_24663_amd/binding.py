@@ -77,7 +77,14 @@ class _CacheC(ctypes.Structure):
                 ("table_stride", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
-_RP, _CP = ctypes.POINTER(_RotaryC), ctypes.POINTER(_CacheC)
+class _PagesC(ctypes.Structure):
+    """Mirror of `infllmv2_pages`."""
+
+    _fields_ = [("num_pages", ctypes.c_int32), ("rows", ctypes.c_int32), ("blocks", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("page_table_d", ctypes.c_void_p), ("refs_d", ctypes.c_void_p), ("reserved", ctypes.c_int32)]
+
+
+_RP, _CP, _GP = ctypes.POINTER(_RotaryC), ctypes.POINTER(_CacheC), ctypes.POINTER(_PagesC)
 
 _SIGNATURES = {
     "infllmv2_num_cmp": (_I32, [_PP, _I32]),
@@ -107,6 +114,13 @@ _SIGNATURES = {
     "infllmv2_cache_compress_k": (ctypes.c_int, [_PP, _CP, _P, _I64, _P, _P, _P, _P, _I32, _P]),
     "infllmv2_decode_blocks": (ctypes.c_int, [_PP, _P, _P, _I64, _P, _P, _I32, _P, _P, _SZ, _P]),
     "infllmv2_cache_attn": (ctypes.c_int, [_PP, _CP, _P, _P, _P, _P, _P, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "infllmv2_tree_masks": (ctypes.c_int, [_P, _P, _P, _P, _P, _I32, _P, _I32, _P, _P]),
+    "infllmv2_cache_tree_attn": (ctypes.c_int, [_PP, _CP, _P, _P, _P, _P, _P, _I32, _P, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "infllmv2_cache_accept": (ctypes.c_int, [_PP, _CP, _P, _P, _P, _P, _I32, _P, _I32, _P, _P]),
+    "infllmv2_pages_resize": (ctypes.c_int, [_GP, _P, _P, _P, _P, _I32, _P, _P]),
+    "infllmv2_pages_fork": (ctypes.c_int, [_GP, _P, _P, _I32, _P, _P, _P]),
+    "infllmv2_pages_compact": (ctypes.c_int, [_GP, _P, _P, _I32, _GP, _P, _P, _P]),
+    "infllmv2_cache_copy_pages": (ctypes.c_int, [_PP, _CP, _P, _I32, _P]),
 }
 
 
@@ -166,7 +180,7 @@ def _stream():
 # `op` of infllmv2_workspace_bytes (enum infllmv2_op)
 OP_COMPRESS_K, OP_BLOCK_SCORES, OP_TOPK_BLOCKS, OP_SPARSE_ATTN_FWD, OP_DENSE_ATTN_FWD, OP_SPARSE_DECODE = range(6)
 OP_BLOCK_SCORES_POOLED, OP_TOPK_POOLED, OP_SPARSE_ATTN_BWD, OP_SPARSE_ATTN_BWD_MIN, OP_COMPRESS_K_APPEND = range(6, 11)
-OP_CACHE_ATTN, OP_DECODE_BLOCKS = 11, 12
+OP_CACHE_ATTN, OP_DECODE_BLOCKS, OP_CACHE_TREE_ATTN = 11, 12, 13
 
 
 def workspace_bytes(op: int, p: Params, batch: int, total_tokens: int, max_seqlen: int) -> int:
@@ -612,3 +626,154 @@ def cache_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q, ctx_
                                    *_ws_args(workspace), _stream())
     _check(st, "infllmv2_cache_attn")
     return out, lse
+
+
+# ---------------------------------------------------------------------------------- trees of drafted tokens
+TREE_MOST = 1024
+
+
+def tree_masks(parents: torch.Tensor, cu_seqlens_q, ctx_lens, mask: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
+    """parents: device int32 [T], packed by cu_seqlens_q: the token of its tree that each drafted token continues, -1: the context.  Sequence b has
+    ctx_lens[b] tokens, the drafted ones with them.  Returns (mask [T, words] int32 bit patterns: a token and its ancestors, positions [T] int32)."""
+    si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
+    assert parents.dtype is torch.int32 and parents.is_contiguous() and parents.shape == (si.total,) and si.batch == cx.batch
+    if mask is None:
+        mask = parents.new_empty((si.total, max(1, (si.max_len + 31) // 32)))
+    if positions is None:
+        positions = torch.empty_like(parents)
+    assert mask.dtype is torch.int32 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == si.total
+    assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (si.total,)
+    st = lib().infllmv2_tree_masks(parents.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch,
+                                   mask.data_ptr(), mask.shape[1], positions.data_ptr(), _stream())
+    _check(st, "infllmv2_tree_masks")
+    return mask, positions
+
+
+def cache_tree_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q, ctx_lens, mask: torch.Tensor,
+                    block_idx: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None):
+    """Attention of drafted tokens over the pages.  q [T, hq, d], packed by cu_seqlens_q; sequence b has ctx_lens[b] cached tokens, its drafted ones the last
+    of them.  A token attends to the context and to the drafted tokens that its row of mask [T, words] (tree_masks) names.  block_idx [B, hkv, topk_total]
+    int32: blocks of the context that a sequence's tokens attend to, or None (all).  Returns (out [T, hq, d], lse [T, hq])."""
+    si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
+    tokens, hq, _ = shape = q.shape
+    assert q.is_contiguous() and q.dtype is p.torch_dtype and shape == (si.total, p.num_q_heads, p.head_dim)
+    assert si.batch == cx.batch <= cache.batch and cache._holds(p, cx.max_ctx)
+    assert mask.dtype is torch.int32 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == tokens
+    if block_idx is not None:
+        assert block_idx.is_contiguous() and block_idx.dtype is torch.int32 and block_idx.shape == (si.batch, p.num_kv_heads, p.topk_total)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        assert out.is_contiguous() and out.shape == shape and out.dtype is q.dtype
+    if lse is None:
+        lse = q.new_empty((tokens, hq), dtype=torch.float32)
+    else:
+        assert lse.is_contiguous() and lse.shape == (tokens, hq) and lse.dtype is torch.float32
+    if workspace is None:
+        need = workspace_bytes(OP_CACHE_TREE_ATTN, p, si.batch, si.total, cx.max_ctx)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    st = lib().infllmv2_cache_tree_attn(ctypes.byref(p), cache.ref, q.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(),
+                                        cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch, mask.data_ptr(), mask.shape[1], _ptr(block_idx),
+                                        out.data_ptr(), lse.data_ptr(), *_ws_args(workspace), _stream())
+    _check(st, "infllmv2_cache_tree_attn")
+    return out, lse
+
+
+def cache_accept(p: Params, cache: PagedCache, cu_seqlens_q, ctx_lens, path: torch.Tensor, new_lens: Optional[torch.Tensor] = None):
+    """Brings the rows of path [B, steps] (device int32: numbers of drafted tokens, rising, -1 behind the last) together behind each sequence's context.
+    Returns the new lengths (device int32 [B])."""
+    si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
+    assert path.dtype is torch.int32 and path.dim() == 2 and path.is_contiguous() and path.shape[0] == si.batch == cx.batch <= cache.batch
+    assert cache._holds(p, cx.max_ctx)
+    if new_lens is None:
+        new_lens = path.new_empty((si.batch,))
+    assert new_lens.dtype is torch.int32 and new_lens.is_contiguous() and new_lens.shape == (si.batch,)
+    st = lib().infllmv2_cache_accept(ctypes.byref(p), cache.ref, si.cu_h.data_ptr(), si.cu_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(),
+                                     si.batch, path.data_ptr(), path.shape[1], new_lens.data_ptr(), _stream())
+    _check(st, "infllmv2_cache_accept")
+    return new_lens
+
+
+# ---------------------------------------------------------------------------------- page tables
+class PagePool:
+    """Which pages are in use: refs [num_pages] (device int32: table entries that name a page; 0: free) and page_table [rows, blocks] (device int32, -1: none)."""
+
+    def __init__(self, refs: torch.Tensor, page_table: torch.Tensor):
+        assert refs.dtype is torch.int32 and refs.dim() == 1 and refs.is_contiguous()
+        assert page_table.dim() == 2 and page_table.dtype is torch.int32 and page_table.stride(1) == 1
+        self.refs, self.page_table = refs, page_table
+        rows, blocks = page_table.shape
+        self.c = _PagesC(refs.numel(), rows, blocks, page_table.stride(0) if rows > 1 else blocks, page_table.data_ptr(), refs.data_ptr(), 0)
+        self.ref = ctypes.byref(self.c)
+
+    @staticmethod
+    def empty(num_pages: int, rows: int, blocks: int, device="cuda") -> "PagePool":
+        """A pool with every page free."""
+        return PagePool(torch.zeros(num_pages, dtype=torch.int32, device=device),
+                        torch.full((rows, blocks), -1, dtype=torch.int32, device=device))
+
+
+class Forks:
+    """Sequences that continue others, as the ABI wants them (host + device copy): row dst[i] gets the first tokens[i] tokens of row src[i]; old_tokens[i]: what
+    row dst[i] holds so far (given back)."""
+
+    def __init__(self, src, dst, tokens, old_tokens=None):
+        cols = [torch.as_tensor(x, dtype=torch.int32, device="cpu") for x in (src, dst, tokens)]
+        cols.append(torch.zeros_like(cols[0]) if old_tokens is None else torch.as_tensor(old_tokens, dtype=torch.int32, device="cpu"))
+        self.h = torch.stack(cols, 1).contiguous()
+        self.d = self.h.cuda()
+        self.count = self.h.shape[0]
+
+
+def _shortage(pool: PagePool, short: Optional[torch.Tensor]):
+    short = pool.refs.new_empty((1,)) if short is None else short
+    assert short.dtype is torch.int32 and short.numel() == 1
+    return short
+
+
+def pages_resize(pool: PagePool, old_lens, new_lens, short: Optional[torch.Tensor] = None):
+    """Sequence b had room for old_lens[b] tokens and gets room for new_lens[b] (0: none).  Returns how many pages were wanting (device int32 [1])."""
+    old, new = _decode_info(old_lens), _decode_info(new_lens)
+    assert old.batch == new.batch
+    short = _shortage(pool, short)
+    st = lib().infllmv2_pages_resize(pool.ref, old.ctx_h.data_ptr(), old.ctx_d.data_ptr(), new.ctx_h.data_ptr(), new.ctx_d.data_ptr(), old.batch,
+                                     short.data_ptr(), _stream())
+    _check(st, "infllmv2_pages_resize")
+    return short
+
+
+def pages_fork(pool: PagePool, forks: Forks, copies: Optional[torch.Tensor] = None, short: Optional[torch.Tensor] = None):
+    """Returns (copies [n, 2]: pages to copy from and to with cache_copy_pages, -1: none; how many pages were wanting), device int32."""
+    if copies is None:
+        copies = pool.refs.new_empty((forks.count, 2))
+    assert copies.dtype is torch.int32 and copies.is_contiguous() and copies.shape == (forks.count, 2)
+    short = _shortage(pool, short)
+    st = lib().infllmv2_pages_fork(pool.ref, forks.h.data_ptr(), forks.d.data_ptr(), forks.count, copies.data_ptr(), short.data_ptr(), _stream())
+    _check(st, "infllmv2_pages_fork")
+    return copies, short
+
+
+def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: Optional[torch.Tensor] = None, live: Optional[torch.Tensor] = None):
+    """Brings the pages in use to the front; sequence b has lens[b] tokens.  out: where the new table and counts go (default: the pool itself).  Returns
+    (moves [num_pages // 2, 2] for cache_copy_pages, live [2]: pages in use and moves), device int32."""
+    info, out = _decode_info(lens), pool if out is None else out
+    half = pool.refs.numel() // 2
+    if moves is None:
+        moves = pool.refs.new_empty((half, 2))
+    if live is None:
+        live = pool.refs.new_empty((2,))
+    assert moves.dtype is torch.int32 and moves.is_contiguous() and moves.shape == (half, 2)
+    assert live.dtype is torch.int32 and live.is_contiguous() and live.shape == (2,)
+    st = lib().infllmv2_pages_compact(pool.ref, info.ctx_h.data_ptr(), info.ctx_d.data_ptr(), info.batch, out.ref, moves.data_ptr(), live.data_ptr(),
+                                      _stream())
+    _check(st, "infllmv2_pages_compact")
+    return moves, live
+
+
+def cache_copy_pages(p: Params, cache: PagedCache, pairs: torch.Tensor):
+    """Copies page pairs[i, 0] to page pairs[i, 1] for each i (device int32 [n, 2]; -1: no copy): keys, values, scales.  Returns the cache."""
+    assert pairs.dtype is torch.int32 and pairs.is_contiguous() and pairs.dim() == 2 and pairs.shape[1] == 2 and cache._holds(p, 0)
+    st = lib().infllmv2_cache_copy_pages(ctypes.byref(p), cache.ref, pairs.data_ptr(), pairs.shape[0], _stream())
+    _check(st, "infllmv2_cache_copy_pages")
+    return cache

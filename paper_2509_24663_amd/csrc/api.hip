@@ -308,6 +308,7 @@ size_t infllmv2_workspace_bytes(int op, const infllmv2_params *p, int32_t batch,
         case INFLLMV2_OP_DENSE_ATTN_FWD: return attn_fwd_ws_bytes(p, t);
         case INFLLMV2_OP_SPARSE_ATTN_BWD: return attn_bwd_ws_bytes(p, t, true);
         case INFLLMV2_OP_SPARSE_ATTN_BWD_MIN: return attn_bwd_ws_bytes(p, t, false);
+        case INFLLMV2_OP_CACHE_TREE_ATTN:
         case INFLLMV2_OP_CACHE_ATTN: return cache_attn_ws_bound(p, batch, total_tokens, max_seqlen);
         default: return 0;      // compress_k, compress_k_append, top-k: no scratch
     }

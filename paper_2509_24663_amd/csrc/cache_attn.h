@@ -1,5 +1,5 @@
-// What the two kernels of infllmv2_cache_attn share: cache_attn.hip (16 columns per workgroup, any data) and cache_attn_tile.hip (chunks of prompts and a few
-// tokens over long contexts, bf16).
+// What the two kernels of infllmv2_cache_attn and infllmv2_cache_tree_attn share: cache_attn.hip (16 columns per workgroup, any data) and cache_attn_tile.hip
+// (chunks of prompts and a few tokens over long contexts, bf16).
 #pragma once
 #include "cache.h"
 #include "gen_unit.h"
@@ -52,7 +52,9 @@ __device__ inline Pieces pieces(float a, float b) {
     return Pieces{gen::upper_halves(u, v), pack(a - __uint_as_float(u & 0xffff0000u), b - __uint_as_float(v & 0xffff0000u))};
 }
 
+// Queries in a row: each is at the place of its key and attends to those up to it.
 struct AttnArgs {
+    static constexpr bool kTree = false;
     cache::Args c;
     const char *q;
     char *out;
@@ -84,11 +86,57 @@ struct AttnArgs {
     }
     __host__ __device__ __attribute__((always_inline)) int splits(int len, int pos_last) const { return (pages(len, pos_last) + pps - 1) / pps; }
     __host__ __device__ __attribute__((always_inline)) int most_splits(int n, int len) const { return n == 0 ? 0 : splits(len, len - 1); }
+    // pages of a tile that begins with token `first` of n, as far as the tile's first token sees them, and in all
+    __host__ int first_pages(int n, int len, int first) const { return (len - n + first) / kBlock + 1; }
+    __host__ int most_pages(int, int len) const { return pages(len, len - 1); }
+};
+
+// A tree of drafted tokens: queries and keys are the last n of a sequence's len rows.  Query i attends to the context (the rows in front of the n; of it, a
+// list picks blocks for the whole sequence) and to those of the n that row i of the mask names.  The entries that a tile goes through are the list's, or all
+// blocks in front of the first drafted row's, and then the blocks of drafted rows: an entry's number is what splits are counted in.
+struct TreeArgs : AttnArgs {
+    static constexpr bool kTree = true;
+    const uint32_t *mask;              // [total][words]
+    int words;
+    __host__ __device__ __attribute__((always_inline)) int tile_tokens(int) const { return group_tokens * tile_groups; }
+    __host__ __device__ __attribute__((always_inline)) int tiles(int n, int) const {
+        if ((tile_groups > 1) != (n >= wide_from)) return 0;
+        const int t = group_tokens * tile_groups;
+        return (n + t - 1) / t;
+    }
+    // entries in front of those of drafted rows: a list may be longer than the blocks that it can name, and holds them anywhere
+    __host__ __device__ __attribute__((always_inline)) int listed_entries(int n, int len) const { return listed(len) ? topk : (len - n) / kBlock; }
+    __host__ __device__ __attribute__((always_inline)) int most_pages(int n, int len) const {
+        const int front = (len - n) / kBlock, last = (len - 1) / kBlock;
+        return (listed(len) && topk < front ? topk : front) + last - front + 1;
+    }
+    __host__ __device__ __attribute__((always_inline)) int most_splits(int n, int len) const { return n == 0 ? 0 : (most_pages(n, len) + pps - 1) / pps; }
+    __host__ int first_pages(int n, int len, int) const { return most_pages(n, len); }
+    // which of the N <= 32 keys from `key` on a query sees by its row of the mask: drafted rows start at row `front`, open: the context's rows in front of it are seen
+    template <int N>
+    __device__ __attribute__((always_inline)) uint32_t seen(const uint32_t *row, int key, int front, int n, bool open) const {
+        const int d = key - front;
+        uint32_t x = 0;
+        if (d < n && d > -N) {
+            const int w = d >> 5;                                   // (-1: in front of the mask)
+            const uint64_t lo = w >= 0 ? row[w] : 0u, hi = 32 * (w + 1) < n ? row[w + 1] : 0u;
+            x = (uint32_t)((lo | hi << 32) >> (d & 31));
+            if (n - d < 32) x &= (1u << (n - d)) - 1u;              // bits behind the tree say nothing
+        }
+        const uint32_t before = d >= 0 ? 0u : d <= -N ? ~0u : (1u << -d) - 1u;
+        return ((x & ~before) | (open ? before : 0u)) & (N == 32 ? ~0u : (1u << (N & 31)) - 1u);
+    }
+    template <int N>                   // the same of N <= 64 keys
+    __device__ __attribute__((always_inline)) uint64_t seen_step(const uint32_t *row, int key, int front, int n, bool open) const {
+        if constexpr (N <= 32) return seen<N>(row, key, front, n, open);
+        else return seen<32>(row, key, front, n, open) | (uint64_t)seen<N - 32>(row, key + 32, front, n, open) << 32;
+    }
 };
 
 // cache_attn_tile.hip
 constexpr int kTileThreads = 512;
-int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream);
+template <class A>
+int launch_tile(const A &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream);
 
 }  // namespace cache_attn
 }  // namespace ifv2

@@ -1,5 +1,6 @@
 // Attention of the newest tokens of each sequence over its paged cache (infllmv2_cache_attn): a decode step, a few proposed tokens, or a chunk of a prompt;
-// over all keys or over the listed blocks; the pages in the data's type or as e4m3 codes.
+// over all keys or over the listed blocks; the pages in the data's type or as e4m3 codes.  And of a tree of drafted tokens (infllmv2_cache_tree_attn): the
+// same kernels over TreeArgs, with rows of a mask for "up to its own".
 //
 // Columns and products as in gen_unit.h: a wavefront works on 16 columns (16 / G consecutive tokens of a KV head with their G heads; with block lists
 // one token) and goes through pages of 64 keys, STEP keys at a time, with a running reference and sum of the softmax.  K rows are operands as
@@ -26,6 +27,7 @@ namespace {
 
 using namespace gen;
 using cache_attn::AttnArgs;
+using cache_attn::TreeArgs;
 using cache_attn::formed;
 using cache_attn::kLift;
 using cache_attn::kLn2;
@@ -218,8 +220,8 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TIL
 
 // ------------------------------------------------------------------------------------------ a split of a tile
 // MULTI: tiles may have several tokens
-template <typename T, int D, bool CODES, int TILES, bool MULTI>
-__global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
+template <typename T, int D, bool CODES, int TILES, bool MULTI, class A>
+__global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
     __shared__ int s_item[6];
     __shared__ float s_m[NW][16], s_l[NW][16];
@@ -262,13 +264,22 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     const bool listed = a.listed(len);
     const int split = rem % per, th = rem / per, h = th % hkv, tile = th / hkv;
     const int T0 = a.tile_tokens(len), first = tile * T0, ntok = min(T0, n - first);       // tokens of this tile
-    const int pos0 = len - n + first, pos_last = pos0 + ntok - 1;
-    const int nsplit = a.splits(len, pos_last);
+    // (a tree: the first key that not every token sees, the last that one may see)
+    const int pos0 = A::kTree ? len - n : len - n + first, pos_last = A::kTree ? len - 1 : pos0 + ntok - 1;
+    int nsplit;
+    if constexpr (A::kTree) nsplit = per;
+    else nsplit = a.splits(len, pos_last);
     if (split >= nsplit) return;
     // the entries of this wavefront: of all pages a run for each split; of a list (which may be longer than the pages there can be, and hold them
     // anywhere) every (NW x nsplit)-th
     const int e_first = listed ? split * NW + w : split * a.pps + w, e_step = listed ? NW * nsplit : NW;
-    const int e_end = listed ? a.topk : min(a.pages(len, pos_last), (split + 1) * a.pps);
+    int e_end, tree_e = 0;                       // tree_e: entries in front of those of drafted rows
+    if constexpr (A::kTree) {
+        tree_e = a.listed_entries(n, len);
+        e_end = listed ? tree_e + pos_last / kBlock - pos0 / kBlock + 1 : min(pos_last / kBlock + 1, (split + 1) * a.pps);
+    } else {
+        e_end = listed ? a.topk : min(a.pages(len, pos_last), (split + 1) * a.pps);
+    }
     const int ti = m / G;                                                                // this lane's column
     const bool used = ti < ntok;
     const int pos = used ? pos0 + ti : -1;
@@ -283,7 +294,17 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     float ref, sum;                              // reference in units of log2; this lane's share of the sum, then the column's
     int low = INT32_MAX;                         // first key of any page that this wavefront went through
 
-    const int32_t *list = a.idx + ((int64_t)(row0 + first) * hkv + h) * a.topk;
+    const int32_t *list = a.idx + ((int64_t)(A::kTree ? seq : row0 + first) * hkv + h) * a.topk;
+    // a tree: whether the context's rows in the block of the first drafted one are listed; this column's row of the mask; whether it saw a key
+    bool open = true, any_key = false;
+    const uint32_t *mask_row = nullptr;
+    if constexpr (A::kTree) {
+        mask_row = a.mask + row * a.words;
+        if (listed && pos0 % kBlock != 0) {
+            open = false;
+            for (int e0 = 0; e0 < a.topk && !open; e0 += 64) open = __any(e0 + lane < a.topk && list[min(e0 + lane, a.topk - 1)] == pos0 / kBlock);
+        }
+    }
     const uint32_t tok = (uint32_t)a.c.tok_stride;
     const uint32_t k_off = m * tok + KeyTile<T, D, CODES>::lane_offset(g), v_off = 4 * g * tok + m * ValueRow<T, D, CODES>::BYTES;
     // (a walk as a loop's body instead of twice in the code keeps some 24 more registers)
@@ -299,8 +320,14 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
             int my_page = -1, my_key0 = 0;
             float my_ks = 1.f, my_vs = 1.f;
             if (e < e_end) {
-                const int j = !listed ? e : nsplit == a.even && e0 == e_first ? early : list[e];
-                if (j >= 0 && j <= pos_last / kBlock) {
+                int j, below = pos_last / kBlock + 1;
+                if constexpr (A::kTree) {
+                    j = listed && e < tree_e ? list[e] : pos0 / kBlock + e - tree_e;
+                    if (e < tree_e) below = pos0 / kBlock;           // (the block of the first drafted row has its own entry)
+                } else {
+                    j = !listed ? e : nsplit == a.even && e0 == e_first ? early : list[e];
+                }
+                if (j >= 0 && j < below) {
                     my_page = a.c.page(seq, j);
                     my_key0 = j * kBlock;
                 }
@@ -350,12 +377,22 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
                         load_k(kb);
                     }
                     __builtin_amdgcn_sched_barrier(0);
-                    const bool edge = key0 + STEP - 1 > pos0;                        // keys behind a token
+                    const bool shut = A::kTree && !open && page_key0 <= pos0 && page_key0 + kBlock > pos0;
+                    const bool edge = A::kTree ? shut || key0 + STEP > pos0 : key0 + STEP - 1 > pos0;          // keys behind a token
+                    if constexpr (A::kTree) any_key |= used && !edge;
                     if (edge) {
+                        uint64_t bits = 0;
+                        if constexpr (A::kTree) {
+                            bits = used ? a.template seen_step<STEP>(mask_row, key0, pos0, n, !shut) >> (4 * g) : 0u;
+                            any_key |= (bits & 0x000f000f000f000full) != 0;
+                        }
 #pragma unroll
                         for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) s[t][r] = key0 + 16 * t + 4 * g + r <= pos ? s[t][r] : -INFINITY;
+                            for (int r = 0; r < 4; ++r) {
+                                const bool in = A::kTree ? (bits >> (16 * t + r) & 1u) != 0u : key0 + 16 * t + 4 * g + r <= pos;
+                                s[t][r] = in ? s[t][r] : -INFINITY;
+                            }
                     }
                     float mx = s[0][0];
 #pragma unroll
@@ -390,12 +427,28 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
                         for (int t = 0; t < TILES; ++t)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                v[4 * t + r].clear_unless(key0 + 16 * t + 4 * g + r <= pos_last);
-                                if (MULTI) odd |= v[4 * t + r].odd();
+                                const int key = key0 + 16 * t + 4 * g + r;
+                                v[4 * t + r].clear_unless(key <= pos_last && (!shut || key >= pos0));
+                                if (MULTI || A::kTree) odd |= v[4 * t + r].odd();
                             }
-                        if (MULTI && __any(odd)) rounds = ntok;
+                        if ((MULTI || A::kTree) && __any(odd)) rounds = A::kTree ? ntok + 1 : ntok;
                     }
-                    if (!MULTI) {
+                    if constexpr (A::kTree) {
+                        // 0 x infinity: where rows are not finite, the sums of each token from the rows that it sees, which are no other's: requested again for each
+                        const bool apart = rounds > 1;
+#pragma unroll 1
+                        for (int i = apart ? ntok - 1 : 0; i >= 0; --i) {
+                            if (apart) {
+                                const uint64_t bits = a.template seen_step<STEP>(a.mask + (int64_t)(row0 + first + i) * a.words, key0, pos0, n, !shut) >> (4 * g);
+                                load_v(vb);
+#pragma unroll
+                                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) v[4 * t + r].clear_unless((bits >> (16 * t + r) & 1u) != 0u);
+                            }
+                            add_values<true, D, TILES, CODES>(acc, wt, v, vs, !apart || ti == i);
+                        }
+                    } else if constexpr (!MULTI) {
                         add_values<false, D, TILES, CODES>(acc, wt, v, vs, true);
                     } else {
                         // 0 x infinity: where rows are not finite, the sums of each token from the rows that it sees, latest token first
@@ -447,7 +500,9 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
     }
 
     // the four wavefronts' results together
-    if (ref == -INFINITY && low <= pos) ref = kLowest;       // only logits of minus infinity (0 / 0 below), not no key at all
+    bool some_key = low <= pos;
+    if constexpr (A::kTree) some_key = (__ballot(any_key) >> m & 0x0001000100010001ull) != 0;
+    if (ref == -INFINITY && some_key) ref = kLowest;         // only logits of minus infinity (0 / 0 below), not no key at all
     if (lane < 16) s_m[w][m] = ref, s_l[w][m] = sum;
     __syncthreads();
     const bool direct = nsplit == 1;
@@ -511,8 +566,8 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(AttnArgs a) {
 // sequence, 33000 keys, 65 splits: 20.7 -> 16.0 us; 130 tokens, 4608 columns, 15 splits: 92.8 -> 112.8).
 constexpr int kAhead = 8;
 
-template <typename T, int D, int SG, int COLS>
-__global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs a) {
+template <typename T, int D, int SG, int COLS, class A>
+__global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(A a) {
     constexpr int kThreads = D / 4 * COLS;               // of a share
     __shared__ int s_item[6];
     __shared__ f32x4 s_o[SG == 1 ? 1 : SG - 1][SG == 1 ? 1 : kThreads];
@@ -549,7 +604,9 @@ __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs
     const int cols = 16 * a.tile_groups;
     if (!a.even) slot += (int64_t)th * a.most_splits(n, len);
     const int h = th % hkv, tile = th / hkv, T0 = a.tile_tokens(len), first = tile * T0, ntok = min(T0, n - first);
-    const int nsplit = a.splits(len, len - n + first + ntok - 1);
+    int nsplit;
+    if constexpr (A::kTree) nsplit = a.most_splits(n, len);
+    else nsplit = a.splits(len, len - n + first + ntok - 1);
     if (nsplit == 1) return;                             // (written by the split itself)
     const int col = blockIdx.y * COLS + tid / (D / 4), c0 = (tid % (D / 4)) * 4, m = col & 15;
     const int in_group = m / G, ti = (col >> 4) * a.group_tokens + in_group;
@@ -625,7 +682,8 @@ __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(AttnArgs
 struct Launches {
     int64_t items = 0, merges = 0, slots = 0;
     int most = 0;
-    void add(const AttnArgs &a, int n, int len) {
+    template <class A>
+    void add(const A &a, int n, int len) {
         const int64_t t = (int64_t)a.tiles(n, len) * a.c.hkv;
         if (t == 0) return;
         const int sp = a.most_splits(n, len);
@@ -635,18 +693,19 @@ struct Launches {
     }
 };
 
-template <typename T, int D>
-void merge(const AttnArgs &a, const Launches &l, hipStream_t stream) {
+template <typename T, int D, class A>
+void merge(const A &a, const Launches &l, hipStream_t stream) {
     if (l.merges == 0) return;
     const unsigned cols = 16 * a.tile_groups;
-    if (l.most <= kAhead || l.merges * cols > 1024) hipLaunchKernelGGL((cache_merge_kernel<T, D, 1, 4>), dim3((unsigned)l.merges, cols / 4), dim3(D), 0, stream, a);
-    else hipLaunchKernelGGL((cache_merge_kernel<T, D, 16, 1>), dim3((unsigned)l.merges, cols), dim3(4 * D), 0, stream, a);
+    if (l.most <= kAhead || l.merges * cols > 1024) hipLaunchKernelGGL((cache_merge_kernel<T, D, 1, 4, A>), dim3((unsigned)l.merges, cols / 4), dim3(D), 0, stream, a);
+    else hipLaunchKernelGGL((cache_merge_kernel<T, D, 16, 1, A>), dim3((unsigned)l.merges, cols), dim3(4 * D), 0, stream, a);
 }
 
-template <typename T, int D, bool CODES, int TILES>
-int launch_t(const AttnArgs &a, const Launches &l, hipStream_t stream) {
-    if (a.multi) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, true>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
-    else hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, false>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
+template <typename T, int D, bool CODES, int TILES, class A>
+int launch_t(const A &a, const Launches &l, hipStream_t stream) {
+    // (a tree's tokens see different rows, so that its kernel has the code for several in any case)
+    if (A::kTree || a.multi) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, true, A>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
+    else if constexpr (!A::kTree) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, false, A>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
     merge<T, D>(a, l, stream);
     return hip_status(hipGetLastError());
 }
@@ -684,32 +743,21 @@ size_t cache_attn_ws_bound(const infllmv2_params *p, int32_t batch, int64_t toke
     return unit_bytes(p, slots) + tile_bytes(p, groups, 1);
 }
 
-}  // namespace ifv2
+namespace {
 
-extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h,
-                                   const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
-                                   const int32_t *block_idx_d, void *out_d, float *lse_d, void *workspace_d, size_t workspace_bytes,
-                                   void *stream) {
-    using namespace ifv2;
-    int st = check_params(p);
-    if (st) return st;
-    int64_t total;
-    int32_t max_new;
-    st = check_cu(cu_q_h, cu_q_d, batch, &total, &max_new);
-    if (st) return st;
-    if (total == 0) return INFLLMV2_OK;
-    if (q_d == nullptr || out_d == nullptr || ctx_lens_h == nullptr || ctx_lens_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
+// a: what the two entry points differ in is set (idx, mask)
+template <class A>
+int attend(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h, const int32_t *cu_q_d, const int32_t *ctx_lens_h,
+           const int32_t *ctx_lens_d, int32_t batch, void *out_d, float *lse_d, void *workspace_d, size_t workspace_bytes, hipStream_t s, A a) {
     const int hkv = p->num_kv_heads;
-    AttnArgs a{};
     a.c.hkv = hkv;
-    a.idx = block_idx_d;
     a.batch = batch;
     a.topk = p->topk_total;
     a.dense_below = p->dense_threshold;
     a.group_tokens = kCols / (p->num_q_heads / hkv);
     a.wide_from = tile_from(p);
     a.tile_groups = 1;
-    AttnArgs wide = a;                         // the tile kernel's launch, with large tiles or small ones
+    A wide = a;                                // the tile kernel's launch, with large tiles or small ones
     const rules::TileSize size[2] = {rules::tile_size(p->head_dim, false), rules::tile_size(p->head_dim, true)};
     int max_ctx = 0;
     rules::PageWork work;                      // of the kernel of 16 columns
@@ -725,19 +773,20 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
         if (len < n || len > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
         if (n == 0) continue;
         if (len > max_ctx) max_ctx = len;
-        const int pages = a.pages(len, len - 1);
+        const int pages = a.most_pages(n, len);
         const int64_t groups = (int64_t)((n + a.tile_tokens(len) - 1) / a.tile_tokens(len)) * hkv;
-        if (a.listed(len) || n < a.wide_from) {
-            work.add(groups, pages, a.listed(len) ? groups * pages : (int64_t)hkv * pages);
+        const bool alone = !A::kTree && a.listed(len);                       // every token has a list of its own
+        if (alone || n < a.wide_from) {
+            work.add(groups, pages, alone ? groups * pages : (int64_t)hkv * pages);
             continue;
         }
         Either &e = n > rules::kFewTokens ? chunks : few;
         e.work.add(groups, pages, (int64_t)hkv * pages);
         if (pages > e.most) e.most = pages;
-        const int first = (len - n) / kBlock + 1;                            // pages that the first token sees
+        const int first = a.first_pages(n, len, 0);                          // pages that the first token sees
         e.unit_pages += groups * (first + pages) / 2;
         for (int i = 0; i < 2; ++i) {
-            const int t0 = a.group_tokens * size[i].groups, t = (n + t0 - 1) / t0, low = t > 1 ? (len - n + t0 - 1) / kBlock + 1 : pages;
+            const int t0 = a.group_tokens * size[i].groups, t = (n + t0 - 1) / t0, low = t > 1 ? a.first_pages(n, len, t0 - 1) : pages;
             e.tiles[i] += (int64_t)t * hkv;
             e.tile_pages[i] += (int64_t)t * hkv * (low + pages) / 2;
         }
@@ -763,7 +812,7 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
         a.multi = n > 1 && a.tiles(n, len) > 0 && a.tile_tokens(len) > 1;
     }
-    st = cache::check(p, c, max_ctx, true);
+    int st = cache::check(p, c, max_ctx, true);
     if (st) return st;
     // (rows of a page are addressed with 32-bit offsets)
     if (c->tok_stride > (1ll << 24)) return INFLLMV2_ERR_UNSUPPORTED;
@@ -781,7 +830,7 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     // as many workgroups for each (sequence, head): nothing has to be looked up.  Where those with nothing to do are few, or a CU each: others are placed
     // beside them, not evenly (16 sequences of 1000 to 33000 keys: 54.5 us, looked up 41.4)
     const int64_t alike = (int64_t)batch * hkv * mine.most;
-    if (single && alike <= 2 * kMostGroups && (alike <= 256 || 10 * alike <= 11 * mine.items)) {
+    if (!A::kTree && single && alike <= 2 * kMostGroups && (alike <= 256 || 10 * alike <= 11 * mine.items)) {
         a.even = mine.most;
         mine.items = alike;
         mine.merges = mine.most > 1 ? (int64_t)batch * hkv : 0;
@@ -791,7 +840,7 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     st = check_ws(workspace_d, workspace_bytes, need + wide_need);
     if (st) return st;
     if (!cache::fits_launch(mine.items, NW * 64) || !cache::fits_launch(other.items, cache_attn::kTileThreads)) return INFLLMV2_ERR_UNSUPPORTED;
-    for (AttnArgs *x : {&a, &wide}) {
+    for (A *x : {&a, &wide}) {
         x->c = cache::args(p, c);
         x->q = (const char *)q_d;
         x->out = (char *)out_d;
@@ -805,7 +854,6 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     a.ml = a.part + mine.slots * 16 * p->head_dim;
     wide.part = (float *)((char *)workspace_d + need);
     wide.ml = wide.part + other.slots * 16 * wide.tile_groups * p->head_dim;
-    const hipStream_t s = (hipStream_t)stream;
     if (other.items > 0) {
         st = cache_attn::launch_tile(wide, p, codes, other.items, s);
         if (st) return st;
@@ -820,4 +868,47 @@ extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cach
     }
     if (p->dtype == INFLLMV2_BF16) return codes ? launch_t<bf16_t, 64, true, 4>(a, mine, s) : launch_t<bf16_t, 64, false, 4>(a, mine, s);
     return codes ? launch_t<float, 64, true, 2>(a, mine, s) : launch_t<float, 64, false, 2>(a, mine, s);
+}
+
+}  // namespace
+
+}  // namespace ifv2
+
+extern "C" int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h,
+                                   const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
+                                   const int32_t *block_idx_d, void *out_d, float *lse_d, void *workspace_d, size_t workspace_bytes,
+                                   void *stream) {
+    using namespace ifv2;
+    int st = check_params(p);
+    if (st) return st;
+    int64_t total;
+    int32_t max_new;
+    st = check_cu(cu_q_h, cu_q_d, batch, &total, &max_new);
+    if (st) return st;
+    if (total == 0) return INFLLMV2_OK;
+    if (q_d == nullptr || out_d == nullptr || ctx_lens_h == nullptr || ctx_lens_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    AttnArgs a{};
+    a.idx = block_idx_d;
+    return attend(p, c, q_d, cu_q_h, cu_q_d, ctx_lens_h, ctx_lens_d, batch, out_d, lse_d, workspace_d, workspace_bytes, (hipStream_t)stream, a);
+}
+
+extern "C" int infllmv2_cache_tree_attn(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h,
+                                        const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
+                                        const uint32_t *mask_d, int32_t mask_words, const int32_t *block_idx_d, void *out_d, float *lse_d,
+                                        void *workspace_d, size_t workspace_bytes, void *stream) {
+    using namespace ifv2;
+    int st = check_params(p);
+    if (st) return st;
+    int64_t total;
+    int32_t max_new;
+    st = check_cu(cu_q_h, cu_q_d, batch, &total, &max_new);
+    if (st) return st;
+    if (total == 0) return INFLLMV2_OK;
+    if (q_d == nullptr || out_d == nullptr || ctx_lens_h == nullptr || ctx_lens_d == nullptr || mask_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if ((int64_t)mask_words * 32 < max_new) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    TreeArgs a{};
+    a.idx = block_idx_d;
+    a.mask = mask_d;
+    a.words = mask_words;
+    return attend(p, c, q_d, cu_q_h, cu_q_d, ctx_lens_h, ctx_lens_d, batch, out_d, lse_d, workspace_d, workspace_bytes, (hipStream_t)stream, a);
 }

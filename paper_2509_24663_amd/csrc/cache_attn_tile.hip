@@ -34,6 +34,7 @@ namespace {
 using namespace gen;
 using attn_unit::lds_read16;
 using cache_attn::AttnArgs;
+using cache_attn::TreeArgs;
 using cache_attn::kLift;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
@@ -74,8 +75,8 @@ struct Page {
 };
 
 // PIECES: bf16 pieces of a weight in the second product
-template <int D, int CG, int W, int PIECES, bool CODES>
-__global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_attn_tile_kernel(AttnArgs a) {
+template <int D, int CG, int W, int PIECES, bool CODES, class A>
+__global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_attn_tile_kernel(A a) {
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int KB = CODES ? 1 : 2;                               // bytes of an element
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // two K pages, three V pages, rows of V as they come
@@ -105,9 +106,29 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     const int split = rem % per, th = rem / per, h = th % hkv, tile = ntiles - 1 - th / hkv;          // (longest first)
     const int64_t slot = slot0 + (int64_t)(tile * hkv + h) * per + split;
     const int T0 = GT * NW * CG, first = tile * T0, ntok = min(T0, n - first);
-    const int pos0 = len - n + first, pos_last = pos0 + ntok - 1;
-    const int nsplit = a.splits(len, pos_last);
+    // (a tree: the first key that not every token sees, the last that one may see)
+    const int pos0 = A::kTree ? len - n : len - n + first, pos_last = A::kTree ? len - 1 : pos0 + ntok - 1;
+    int nsplit;
+    if constexpr (A::kTree) nsplit = per;
+    else nsplit = a.splits(len, pos_last);
     if (split >= nsplit) return;
+    // a tree: entries in front of those of drafted rows (a list, or all blocks); whether the context's rows in the block of the first drafted one are listed
+    const int32_t *list = nullptr;
+    int tree_e = 0;
+    bool open = true;
+    if constexpr (A::kTree) {
+        tree_e = a.listed_entries(n, len);
+        if (a.listed(len)) {
+            list = a.idx + ((int64_t)seq * hkv + h) * a.topk;
+            if (pos0 % kBlock != 0) {
+                open = false;
+                for (int e0 = 0; e0 < a.topk && !open; e0 += 64) open = __any(e0 + lane < a.topk && list[min(e0 + lane, a.topk - 1)] == pos0 / kBlock);
+            }
+        }
+    }
+    // a page whose context rows are not seen; a page (or half of one) of which not all rows are seen by all tokens of the tile from token t on
+    auto shut = [&](int key0) { return A::kTree && !open && key0 / kBlock == pos0 / kBlock; };
+    auto edge = [&](int key0, int keys, int t) { return A::kTree ? key0 + keys > pos0 || shut(key0) : key0 + keys - 1 > pos0 + t; };
 
     int ti[CG];
     bool used[CG];
@@ -195,7 +216,11 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             for (int k = 0; k < VW; ++k) {
                 constexpr int PER = 4 / KB;                         // keys of a word
                 const int seen = pos_last + 1 - (key0 + 8 * w + PER * k);            // .. that some token sees
-                const uint32_t keep = seen >= PER ? ~0u : seen <= 0 ? 0u : (1u << (8 * KB * seen)) - 1u;
+                uint32_t keep = seen >= PER ? ~0u : seen <= 0 ? 0u : (1u << (8 * KB * seen)) - 1u;
+                if (A::kTree && shut(key0)) {
+                    const int front = pos0 - (key0 + 8 * w + PER * k);
+                    keep &= front >= PER ? 0u : front <= 0 ? ~0u : ~((1u << (8 * KB * front)) - 1u);
+                }
                 const uint32_t o = not_finite<CODES>(raw_v[q][k]);
                 odd |= o & keep;
                 raw_v[q][k] &= ~o & keep;
@@ -217,14 +242,34 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     };
 
     // the pages of the split: lane l holds the l-th of the next 64
-    const int e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
+    int e_end, e_by = 1;                                            // of a list every nsplit-th
+    if constexpr (A::kTree) {
+        e_end = list ? tree_e + pos_last / kBlock - pos0 / kBlock + 1 : min(pos_last / kBlock + 1, (split + 1) * a.pps);
+        e_by = list ? nsplit : 1;
+    } else {
+        e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
+    }
+    const int e_first = A::kTree && list ? split : split * a.pps;
     int e0 = 0, list_key0 = 0;
     int64_t list_at = 0;
     float list_ks = 1.f, list_vs = 1.f;
     uint64_t there = 0;
     auto refill = [&]() {
         while (there == 0 && e0 < e_end) {
-            const int j = e0 + lane, page = j < e_end ? a.c.page(seq, j) : -1;
+            int j, page;
+            if constexpr (A::kTree) {
+                const int e = e0 + lane * e_by;
+                int below = pos_last / kBlock + 1;
+                j = pos0 / kBlock + e - tree_e;
+                if (list && e < tree_e) {                           // (the block of the first drafted row has its own entry)
+                    j = list[e];
+                    below = pos0 / kBlock;
+                }
+                page = e < e_end && j >= 0 && j < below ? a.c.page(seq, j) : -1;
+            } else {
+                j = e0 + lane;
+                page = j < e_end ? a.c.page(seq, j) : -1;
+            }
             list_at = a.c.at(page, h);
             list_key0 = j * kBlock;
             if (CODES && page >= 0) {
@@ -232,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                 list_vs = a.c.vs[(int64_t)page * hkv + h];
             }
             there = __ballot(page >= 0);
-            e0 += 64;
+            e0 += A::kTree ? 64 * e_by : 64;
         }
     };
     auto next = [&](Where &p) {                                     // the next page of the list, which is not empty
@@ -246,6 +291,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     if (tid == 0) s_odd = s_again = 0;
 
     // The walk, in steps of half a page k (32 keys): logits of k; then sums of the weights of k - 1 and, between those products, the weights of k.
+    uint32_t saw = 0;                                               // a tree: bit x: this lane's column x saw a key
     constexpr int LOGITS = 8 * CG, KF = 2 * KS;                     // logits of a lane, K operands of a step
     f32x4 s[CG][2];
     uint32_t pb[2][CG][PIECES][4];                                  // by the parity of k
@@ -290,15 +336,27 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             beside(j);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (first_key + 31 > pos0 + wave_first) {                   // keys behind a token
+        if (edge(first_key, 32, wave_first)) {                      // keys behind a token
 #pragma unroll
             for (int x = 0; x < CG; ++x) {
-                const int lim = used[x] ? pos0 + ti[x] - (first_key + 8 * g) : -1;
+                if constexpr (A::kTree) {
+                    const uint32_t *row = a.mask + (int64_t)(row0 + first + (used[x] ? ti[x] : 0)) * a.words;
+                    const uint32_t bits = used[x] ? a.template seen<8>(row, first_key + 8 * g, pos0, n, !shut(first_key)) : 0u;
+                    saw |= bits != 0u ? 1u << x : 0u;
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+                    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[x][kt][r] = 4 * kt + r <= lim ? s[x][kt][r] : -INFINITY;
+                        for (int r = 0; r < 4; ++r) s[x][kt][r] = bits >> (4 * kt + r) & 1u ? s[x][kt][r] : -INFINITY;
+                } else {
+                    const int lim = used[x] ? pos0 + ti[x] - (first_key + 8 * g) : -1;
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[x][kt][r] = 4 * kt + r <= lim ? s[x][kt][r] : -INFINITY;
+                }
             }
+        } else if (A::kTree) {
+            saw = ~0u;
         }
         float part[CG], last = 0.f;
 #pragma unroll
@@ -361,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             for (int i = 0; i < DT; ++i) acc[x][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         Where now{}, then{}, after{};                                   // pages p, p + 1, p + 2 (those that are not there repeat the last)
-        e0 = split * a.pps;
+        e0 = e_first;
         there = 0;
         refill();
         const bool here = there != 0;
@@ -379,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             for (uint32_t at = 16 * tid; at < Page<D>::kBytes; at += 16 * kThreads) lds_write16(lds + 4 * Page<D>::kBytes + at, u32x4{0, 0, 0, 0});
             __syncthreads();                                            // (s_odd)
             collect();
-            if (now.key0 + kBlock - 1 > pos0) clean(now.key0);
+            if (edge(now.key0, kBlock, 0)) clean(now.key0);
 #pragma unroll
             for (int i = 0; i < KP + CV; ++i) write(i, lds, lds + 2 * Page<D>::kBytes, now.ks, now.vs);
 #pragma unroll
@@ -396,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                 const bool most = there != 0;
                 if (most) next(after);
                 const int ahead3 = p3 == 2 ? 0 : p3 + 1;
-                if (then.key0 + kBlock - 1 > pos0) clean(then.key0);
+                if (edge(then.key0, kBlock, 0)) clean(then.key0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (what this wavefront wrote)
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
@@ -449,7 +507,9 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             int t = ti[x];
             asm volatile("" : "+v"(t));                             // (addresses are formed here: kept through the second walk they take registers)
             const float total = rows_add(sum[x]);
-            const bool seen = used[x] && low <= pos0 + t;
+            bool seen;
+            if constexpr (A::kTree) seen = used[x] && (__ballot(saw >> x & 1u) >> m & 0x0001000100010001ull) != 0;
+            else seen = used[x] && low <= pos0 + t;
             // (a split without weight is 0 with no weight: others of the column may have some)
             const float inv = seen && (nsplit == 1 || total != 0.f) ? 1.f / total : 0.f;
             // (weights rounded up may bring a mean of the largest numbers past them)
@@ -495,18 +555,25 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     if (low == INT32_MAX || s_odd == 0) return;
     // Values that are not finite were taken as 0 in pages that some tokens see further than others (0 x infinity): the tokens that do see them get them now.
     __threadfence_block();
-    for (int j = max(pos0 / kBlock, split * a.pps); j <= pos_last / kBlock && j < e_end; ++j) {
+    for (int j = A::kTree ? pos0 / kBlock : max(pos0 / kBlock, split * a.pps); j <= pos_last / kBlock && (A::kTree || j < e_end); ++j) {
+        if constexpr (A::kTree) {                                   // (this split's entries)
+            const int e = tree_e + j - pos0 / kBlock;
+            if (list ? e % nsplit != split : e < e_first || e >= e_end) continue;
+        }
         const int odd_page = __builtin_amdgcn_readfirstlane(a.c.page(seq, j));
         if (odd_page < 0) continue;
         const char *vb = a.c.v + a.c.at(odd_page, h);
         for (int x = 0; x < CG; ++x) {
             const int t = (w * CG + x) * GT + m / G;
             if (m / G >= GT || t >= ntok) continue;
-            const int rows = min(kBlock, pos0 + t + 1 - j * kBlock);
+            const int rows = min(kBlock, (A::kTree ? len : pos0 + t + 1) - j * kBlock);
             for (int i = 0; i < DT; ++i) {
                 float add[4] = {0.f, 0.f, 0.f, 0.f};
                 bool any = false;
                 for (int u = 0; u < rows; ++u) {
+                    if constexpr (A::kTree) {
+                        if (!a.template seen<1>(a.mask + (int64_t)(row0 + first + t) * a.words, j * kBlock + u, pos0, n, !shut(j * kBlock))) continue;
+                    }
                     const char *at = vb + (int64_t)u * tok + (16 * i + 4 * g) * KB;
                     for (int r = 0; r < 4; ++r) {
                         float y;
@@ -530,10 +597,10 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     }
 }
 
-template <int D, int CG, int PIECES, bool CODES>
-int launch_d(const AttnArgs &a, int64_t items, hipStream_t stream) {
+template <int D, int CG, int PIECES, bool CODES, class A>
+int launch_d(const A &a, int64_t items, hipStream_t stream) {
     constexpr int LDS = 5 * Page<D>::kBytes + 64 * D * (CODES ? 1 : 2);
-    const auto kernel = cache_attn_tile_kernel<D, CG, kAhead, PIECES, CODES>;
+    const auto kernel = cache_attn_tile_kernel<D, CG, kAhead, PIECES, CODES, A>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
         return INFLLMV2_ERR_HIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(kThreads), LDS, stream, a);
@@ -544,7 +611,8 @@ int launch_d(const AttnArgs &a, int64_t items, hipStream_t stream) {
 
 namespace cache_attn {
 
-int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream) {
+template <class A>
+int launch_tile(const A &a, const infllmv2_params *p, bool codes, int64_t items, hipStream_t stream) {
     static_assert(rules::tile_size(128, false).groups == 2 * NW && rules::tile_size(64, false).groups == 4 * NW, "the tiles that the rules count with");
     static_assert(rules::tile_size(128, true).groups == NW && rules::tile_size(64, true).groups == NW, "the tiles that the rules count with");
     const auto launch = [&](auto d, auto groups, auto pieces) {
@@ -560,6 +628,8 @@ int launch_tile(const AttnArgs &a, const infllmv2_params *p, bool codes, int64_t
     if (p->head_dim == 128) return !small ? launch(d128, two, one) : a.fine ? launch(d128, one, two) : launch(d128, one, one);
     return !small ? launch(d64, four, one) : a.fine ? launch(d64, one, two) : launch(d64, one, one);
 }
+template int launch_tile(const AttnArgs &, const infllmv2_params *, bool, int64_t, hipStream_t);
+template int launch_tile(const TreeArgs &, const infllmv2_params *, bool, int64_t, hipStream_t);
 
 }  // namespace cache_attn
 }  // namespace ifv2

@@ -1,0 +1,388 @@
+// Which pages a sequence's blocks are in: pages handed out and taken back (infllmv2_pages_resize), a sequence that continues another
+// (infllmv2_pages_fork), the pages in use brought to the front (infllmv2_pages_compact), and the copies that follow from the two
+// (infllmv2_cache_copy_pages).
+//
+// refs[g] counts the table entries that name page g; a page with none is free.  That is all the state there is: pages are taken lowest number first, for
+// sequences and blocks in order, so that what a call does depends on table and refs alone, not on the order in which its threads arrive.
+//
+// Bound: latency.  Entries are given back and shared by as many workgroups as they are worth (counts added with atomics, whose order does not matter);
+// handing out needs every free page's rank, which one workgroup works out, 8192 counts at a time, only as far as pages are wanted.  Copies: HBM.
+#include <algorithm>
+
+#include "cache.h"
+
+namespace ifv2 {
+
+namespace {
+
+typedef uint32_t Piece __attribute__((ext_vector_type(4)));      // 16 bytes of a row
+
+constexpr int kMostRows = INFLLMV2_PAGES_MOST_ROWS;
+constexpr int kTakeThreads = 1024, kTakeWaves = kTakeThreads / 64, kDeep = 8;      // counts of a round: kTakeThreads * kDeep
+constexpr int kChunk = 1024;                                                        // table entries of a workgroup
+
+struct Pool {
+    int32_t *table, *refs;
+    int stride, num_pages;
+    __device__ inline int32_t *row(int r) const { return table + (int64_t)r * stride; }
+    __device__ inline bool is_page(int g) const { return g >= 0 && g < num_pages; }
+};
+Pool pool_of(const infllmv2_pages *g) { return Pool{g->page_table_d, g->refs_d, g->table_stride, g->num_pages}; }
+
+__host__ __device__ inline int blocks_of(int tokens) { return (int)(((int64_t)tokens + kBlock - 1) / kBlock); }
+
+// ------------------------------------------------------------------------------------------ the lowest free pages
+// Workgroup-wide: the sum of x over all threads' (k, wavefront, lane) in that order, exclusive for each; x: one bit (a flag) per k
+struct Ranks {
+    int cell[kDeep * kTakeWaves];          // flags of (k, wavefront), then how many stand in front
+    int total;
+};
+
+// Counts that other workgroups' atomics have changed are read past the first cache by the launch in between, which begins with an empty one.
+// flag(page): whether page is wanted; found(page, rank) for those, in order of their numbers, ranks from `before` on; until `most` or the last page
+template <class Flag, class Found>
+__device__ inline int ranked_pages(int num_pages, int most, Ranks &s, Flag flag, Found found) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    int before = 0;
+    for (int64_t base = 0; base < num_pages && before < most; base += kTakeThreads * kDeep) {
+        bool is[kDeep];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const int64_t g = base + k * kTakeThreads + tid;
+            is[k] = g < num_pages && flag((int)g);
+        }
+        uint64_t hits[kDeep];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            hits[k] = __ballot(is[k]);
+            if (lane == 0) s.cell[k * kTakeWaves + w] = __popcll(hits[k]);
+        }
+        __syncthreads();
+        if (w == 0) {                      // two cells a lane
+            const int x = s.cell[2 * lane], y = s.cell[2 * lane + 1], incl = cache::wave_sums(x + y);
+            s.cell[2 * lane] = incl - x - y;
+            s.cell[2 * lane + 1] = incl - y;
+            if (lane == 63) s.total = incl;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k)
+            if (is[k]) found((int)(base + k * kTakeThreads + tid), before + s.cell[k * kTakeWaves + w] + __popcll(hits[k] & ((1ull << lane) - 1)));
+        before += s.total;
+        __syncthreads();
+    }
+    return before;
+}
+static_assert(kDeep * kTakeWaves == 128, "two cells a lane");
+
+// Sums in front of each of `rows` counts, in LDS; returns the sum of all
+template <class Count>
+__device__ inline int sums_before(int rows, int *s_before, Ranks &s, Count count) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    int before = 0;
+    for (int r0 = 0; r0 < rows; r0 += kTakeThreads) {
+        const int r = r0 + tid, x = r < rows ? count(r) : 0, incl = cache::wave_sums(x);
+        if (lane == 63) s.cell[w] = incl;
+        __syncthreads();
+        int front = before;
+        for (int i = 0; i < w; ++i) front += s.cell[i];
+        if (r < rows) s_before[r] = front + incl - x;
+        for (int i = 0; i < kTakeWaves; ++i) before += s.cell[i];
+        __syncthreads();
+    }
+    return before;
+}
+// the last of `rows` sums that is at most x
+__device__ inline int row_of(int rows, const int *s_before, int x) {
+    int lo = 0, hi = rows - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_before[mid] <= x) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// ------------------------------------------------------------------------------------------ resize
+struct ResizeArgs {
+    Pool g;
+    const int32_t *old_lens, *new_lens;
+    int rows;
+    int32_t *shortage;                     // or nullptr
+};
+
+__global__ void __launch_bounds__(256) pages_release_kernel(ResizeArgs a) {
+    const int r = blockIdx.x, want = blocks_of(a.new_lens[r]), have = blocks_of(a.old_lens[r]);
+    int32_t *row = a.g.row(r);
+    for (int64_t j = (int64_t)want + blockIdx.y * 256 + threadIdx.x; j < have; j += 256 * gridDim.y) {
+        const int page = row[j];
+        if (a.g.is_page(page)) atomicSub(&a.g.refs[page], 1);
+        row[j] = -1;
+    }
+}
+
+__global__ void __launch_bounds__(kTakeThreads) pages_take_kernel(ResizeArgs a) {
+    __shared__ int s_before[kMostRows];
+    __shared__ Ranks s_ranks;
+    const int wanted = sums_before(a.rows, s_before, s_ranks, [&](int r) { return max(blocks_of(a.new_lens[r]) - blocks_of(a.old_lens[r]), 0); });
+    auto entry = [&](int x) {
+        const int r = row_of(a.rows, s_before, x);
+        return a.g.row(r) + blocks_of(a.old_lens[r]) + (x - s_before[r]);
+    };
+    const int found = min(ranked_pages(a.g.num_pages, wanted, s_ranks, [&](int g) { return a.g.refs[g] <= 0; },
+                                       [&](int g, int rank) {
+                                           if (rank >= wanted) return;
+                                           a.g.refs[g] = 1;
+                                           *entry(rank) = g;
+                                       }),
+                          wanted);
+    for (int x = found + threadIdx.x; x < wanted; x += kTakeThreads) *entry(x) = -1;
+    if (threadIdx.x == 0 && a.shortage != nullptr) *a.shortage = wanted - found;
+}
+
+// ------------------------------------------------------------------------------------------ fork
+struct ForkArgs {
+    Pool g;
+    const infllmv2_fork *forks;
+    int count;
+    int32_t *copies, *shortage;            // (each or nullptr)
+};
+
+// whole pages shared, what the row held before given back
+__global__ void __launch_bounds__(256) pages_share_kernel(ForkArgs a) {
+    const infllmv2_fork f = a.forks[blockIdx.x];
+    const int32_t *src = a.g.row(f.src);
+    int32_t *dst = a.g.row(f.dst);
+    const int whole = f.tokens / kBlock, held = blocks_of(f.tokens), had = blocks_of(f.old_tokens);
+    for (int64_t j = blockIdx.y * 256 + threadIdx.x; j < max(held, had); j += 256 * gridDim.y) {
+        const int was = j < had ? dst[j] : -1, page = j < whole ? src[j] : -1;
+        const bool good = a.g.is_page(page);
+        if (a.g.is_page(was)) atomicSub(&a.g.refs[was], 1);
+        if (good) atomicAdd(&a.g.refs[page], 1);
+        dst[j] = good ? page : -1;
+    }
+}
+
+// a page for every last one that is not whole
+__global__ void __launch_bounds__(kTakeThreads) pages_split_kernel(ForkArgs a) {
+    __shared__ int s_before[kMostRows];
+    __shared__ Ranks s_ranks;
+    auto from = [&](int i) {               // the page that is continued, or -1
+        const infllmv2_fork f = a.forks[i];
+        const int page = f.tokens % kBlock != 0 ? a.g.row(f.src)[f.tokens / kBlock] : -1;
+        return a.g.is_page(page) ? page : -1;
+    };
+    const int wanted = sums_before(a.count, s_before, s_ranks, [&](int i) { return from(i) >= 0 ? 1 : 0; });
+    auto set = [&](int x, int page) {
+        const int i = row_of(a.count, s_before, x);
+        const infllmv2_fork f = a.forks[i];
+        a.g.row(f.dst)[f.tokens / kBlock] = page;
+        if (a.copies != nullptr && page >= 0) {
+            a.copies[2 * i] = from(i);
+            a.copies[2 * i + 1] = page;
+        }
+    };
+    if (a.copies != nullptr) {
+        for (int i = threadIdx.x; i < 2 * a.count; i += kTakeThreads) a.copies[i] = -1;
+        __threadfence();
+        __syncthreads();
+    }
+    const int found = min(ranked_pages(a.g.num_pages, wanted, s_ranks, [&](int g) { return a.g.refs[g] <= 0; },
+                                       [&](int g, int rank) {
+                                           if (rank >= wanted) return;
+                                           a.g.refs[g] = 1;
+                                           set(rank, g);
+                                       }),
+                          wanted);
+    for (int x = found + threadIdx.x; x < wanted; x += kTakeThreads) set(x, -1);
+    if (threadIdx.x == 0 && a.shortage != nullptr) *a.shortage = wanted - found;
+}
+
+// ------------------------------------------------------------------------------------------ compact
+struct CompactArgs {
+    Pool g, out;
+    const int32_t *lens;
+    int rows, blocks, out_blocks;
+    int32_t *moves, *live;                 // [num_pages / 2][2], [2]: pages in use, moves
+};
+
+// Of the pages in use those from number `used` on move, in order, to the free ones below it, in order: there are as many of either.
+__global__ void __launch_bounds__(kTakeThreads) pages_moves_kernel(CompactArgs a) {
+    __shared__ Ranks s_ranks;
+    const int used = ranked_pages(a.g.num_pages, INT32_MAX, s_ranks, [&](int g) { return a.g.refs[g] > 0; }, [](int, int) {});
+    const int n = ranked_pages(used, INT32_MAX, s_ranks, [&](int g) { return a.g.refs[g] <= 0; }, [&](int g, int rank) { a.moves[2 * rank + 1] = g; });
+    ranked_pages(a.g.num_pages - used, INT32_MAX, s_ranks, [&](int g) { return a.g.refs[used + g] > 0; }, [&](int g, int rank) { a.moves[2 * rank] = used + g; });
+    for (int i = 2 * n + threadIdx.x; i < a.g.num_pages / 2 * 2; i += kTakeThreads) a.moves[i] = -1;
+    if (threadIdx.x == 0) a.live[0] = used, a.live[1] = n;
+}
+
+// The tables and counts by the new numbers; in may be out: an entry, and the two counts of a move, are one thread's.
+__global__ void __launch_bounds__(256) pages_renumber_kernel(CompactArgs a) {
+    const int used = a.live[0], n = a.live[1];
+    if (blockIdx.y == 0) {
+        for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < a.g.num_pages; g += gridDim.x * 256) {
+            // (counts of moved pages are the move's: of one of those, read while it changes, the same comes out either way)
+            const int x = a.g.refs[g];
+            if (g < used ? x > 0 : x <= 0) a.out.refs[g] = g < used ? x : 0;
+            if (g < n) {
+                const int from = a.moves[2 * g], to = a.moves[2 * g + 1], y = a.g.refs[from];
+                a.out.refs[to] = y;
+                a.out.refs[from] = 0;
+            }
+        }
+        return;
+    }
+    const int64_t entries = (int64_t)a.rows * a.out_blocks;
+    for (int64_t i = ((int64_t)(blockIdx.y - 1) * gridDim.x + blockIdx.x) * 256 + threadIdx.x; i < entries; i += (int64_t)(gridDim.y - 1) * gridDim.x * 256) {
+        const int r = (int)(i / a.out_blocks), j = (int)(i - (int64_t)r * a.out_blocks);
+        int page = j < min(blocks_of(a.lens[r]), a.blocks) ? a.g.row(r)[j] : -1;
+        if (!a.g.is_page(page)) page = -1;
+        if (page >= used) {                // (pages to move are in order)
+            int lo = 0, hi = n;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (a.moves[2 * mid] < page) lo = mid + 1;
+                else hi = mid;
+            }
+            page = lo < n && a.moves[2 * lo] == page ? a.moves[2 * lo + 1] : -1;
+        }
+        a.out.row(r)[j] = page;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ copies
+struct CopyArgs {
+    cache::Args c;
+    const int32_t *pairs;
+    int vecs, vecs_log2;                   // 16-byte pieces of a row
+};
+
+// a workgroup: K or V of one head of a page; PER pieces a thread
+template <int PER>
+__global__ void __launch_bounds__(256) cache_copy_kernel(CopyArgs a) {
+    const int from = a.pairs[2 * (int64_t)blockIdx.x], to = a.pairs[2 * (int64_t)blockIdx.x + 1], h = blockIdx.y;
+    if (from < 0 || from >= a.c.num_pages || to < 0 || to >= a.c.num_pages || from == to) return;
+    char *pool = blockIdx.z != 0 ? a.c.v : a.c.k;
+    float *scales = blockIdx.z != 0 ? a.c.vs : a.c.ks;
+    const char *src = pool + a.c.at(from, h);
+    char *dst = pool + a.c.at(to, h);
+    Piece x[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int v = threadIdx.x + e * 256;
+        x[e] = *reinterpret_cast<const Piece *>(src + (v >> a.vecs_log2) * a.c.tok_stride + (v & (a.vecs - 1)) * 16);
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int v = threadIdx.x + e * 256;
+        *reinterpret_cast<Piece *>(dst + (v >> a.vecs_log2) * a.c.tok_stride + (v & (a.vecs - 1)) * 16) = x[e];
+    }
+    if (threadIdx.x == 0 && scales != nullptr) scales[(int64_t)to * a.c.hkv + h] = scales[(int64_t)from * a.c.hkv + h];
+}
+
+int check_pages(const infllmv2_pages *g) {
+    if (g == nullptr || g->num_pages < 1 || g->rows < 1 || g->blocks < 1 || g->table_stride < g->blocks || g->reserved != 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (g->page_table_d == nullptr || g->refs_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    return INFLLMV2_OK;
+}
+bool fits(const infllmv2_pages *g, int tokens) { return tokens >= 0 && blocks_of(tokens) <= g->blocks; }
+unsigned chunks(int64_t entries, int per) { return (unsigned)std::max<int64_t>(std::min<int64_t>((entries + per - 1) / per, 64), 1); }
+
+}  // namespace
+
+}  // namespace ifv2
+
+extern "C" int infllmv2_pages_resize(const infllmv2_pages *g, const int32_t *old_lens_h, const int32_t *old_lens_d, const int32_t *new_lens_h,
+                                     const int32_t *new_lens_d, int32_t batch, int32_t *short_d, void *stream) {
+    using namespace ifv2;
+    const int st = check_pages(g);
+    if (st) return st;
+    if (batch < 0 || batch > g->rows) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (batch == 0) return INFLLMV2_OK;
+    if (old_lens_h == nullptr || old_lens_d == nullptr || new_lens_h == nullptr || new_lens_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    int64_t more = 0;
+    int less = 0;                                                    // the most blocks that a sequence gives back
+    for (int b = 0; b < batch; ++b) {
+        if (!fits(g, old_lens_h[b]) || !fits(g, new_lens_h[b])) return INFLLMV2_ERR_INVALID_ARGUMENT;
+        const int change = blocks_of(new_lens_h[b]) - blocks_of(old_lens_h[b]);
+        if (change > 0) more += change;
+        less = std::max(less, -change);
+    }
+    if (batch > kMostRows || more > INT32_MAX) return INFLLMV2_ERR_UNSUPPORTED;
+    if (less == 0 && more == 0 && short_d == nullptr) return INFLLMV2_OK;
+    const ResizeArgs a{pool_of(g), old_lens_d, new_lens_d, batch, short_d};
+    if (less > 0) hipLaunchKernelGGL(pages_release_kernel, dim3(batch, chunks(less, 256)), dim3(256), 0, (hipStream_t)stream, a);
+    if (more > 0 || short_d != nullptr) hipLaunchKernelGGL(pages_take_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
+    return hip_status(hipGetLastError());
+}
+
+extern "C" int infllmv2_pages_fork(const infllmv2_pages *g, const infllmv2_fork *forks_h, const infllmv2_fork *forks_d, int32_t count,
+                                   int32_t *copies_d, int32_t *short_d, void *stream) {
+    using namespace ifv2;
+    const int st = check_pages(g);
+    if (st) return st;
+    if (count < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (count == 0) return INFLLMV2_OK;
+    if (forks_h == nullptr || forks_d == nullptr || ((uintptr_t)forks_d & 15) != 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (g->rows > kMostRows || count > kMostRows) return INFLLMV2_ERR_UNSUPPORTED;
+    uint64_t to[kMostRows / 64] = {};                                // rows that are written
+    int most = 0;
+    bool part = false;
+    for (int i = 0; i < count; ++i) {
+        const infllmv2_fork &f = forks_h[i];
+        if (f.src < 0 || f.src >= g->rows || f.dst < 0 || f.dst >= g->rows || !fits(g, f.tokens) || !fits(g, f.old_tokens)) return INFLLMV2_ERR_INVALID_ARGUMENT;
+        if (to[f.dst / 64] >> (f.dst % 64) & 1) return INFLLMV2_ERR_INVALID_ARGUMENT;
+        to[f.dst / 64] |= 1ull << (f.dst % 64);
+        most = std::max(most, blocks_of(std::max(f.tokens, f.old_tokens)));
+        part = part || f.tokens % kBlock != 0;
+    }
+    for (int i = 0; i < count; ++i)
+        if (to[forks_h[i].src / 64] >> (forks_h[i].src % 64) & 1) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (most == 0 && copies_d == nullptr && short_d == nullptr) return INFLLMV2_OK;
+    const ForkArgs a{pool_of(g), forks_d, count, copies_d, short_d};
+    if (most > 0) hipLaunchKernelGGL(pages_share_kernel, dim3(count, chunks(most, 256)), dim3(256), 0, (hipStream_t)stream, a);
+    if (part || copies_d != nullptr || short_d != nullptr) hipLaunchKernelGGL(pages_split_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
+    return hip_status(hipGetLastError());
+}
+
+extern "C" int infllmv2_pages_compact(const infllmv2_pages *g, const int32_t *lens_h, const int32_t *lens_d, int32_t batch,
+                                      const infllmv2_pages *out, int32_t *moves_d, int32_t *live_d, void *stream) {
+    using namespace ifv2;
+    int st = check_pages(g);
+    if (!st) st = check_pages(out);
+    if (st) return st;
+    if (batch < 0 || batch > g->rows || batch > out->rows || out->num_pages != g->num_pages) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if ((batch > 0 && (lens_h == nullptr || lens_d == nullptr)) || (moves_d == nullptr && g->num_pages > 1) || live_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    // in place, or apart
+    if ((out->page_table_d == g->page_table_d && out->table_stride != g->table_stride)) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    for (int b = 0; b < batch; ++b)
+        if (!fits(g, lens_h[b]) || !fits(out, lens_h[b])) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    const CompactArgs a{pool_of(g), pool_of(out), lens_d, batch, g->blocks, out->blocks, moves_d, live_d};
+    hipLaunchKernelGGL(pages_moves_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
+    const int64_t entries = (int64_t)batch * out->blocks;
+    const unsigned x = chunks(g->num_pages, 256), y = 1 + chunks(entries, 256 * (int)x);
+    hipLaunchKernelGGL(pages_renumber_kernel, dim3(x, y), dim3(256), 0, (hipStream_t)stream, a);
+    return hip_status(hipGetLastError());
+}
+
+extern "C" int infllmv2_cache_copy_pages(const infllmv2_params *p, const infllmv2_cache *c, const int32_t *pairs_d, int32_t count, void *stream) {
+    using namespace ifv2;
+    int st = check_params(p);
+    if (st) return st;
+    if (count < 0) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    if (count == 0) return INFLLMV2_OK;
+    if (pairs_d == nullptr) return INFLLMV2_ERR_INVALID_ARGUMENT;
+    st = cache::check(p, c, 0, true);
+    if (st) return st;
+    if (p->num_kv_heads > 65535 || !cache::fits_launch((int64_t)count * p->num_kv_heads * 2, 256)) return INFLLMV2_ERR_UNSUPPORTED;
+    const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3;
+    const int vecs = p->head_dim * (codes ? 1 : p->dtype == INFLLMV2_BF16 ? 2 : 4) / 16;
+    CopyArgs a{cache::args(p, c), pairs_d, vecs, __builtin_ctz(vecs)};
+    if (!codes) a.c.ks = a.c.vs = nullptr;
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(count, p->num_kv_heads, 2), dim3(256), 0, (hipStream_t)stream, a); };
+    if (vecs == 32) launch(cache_copy_kernel<8>);
+    else if (vecs == 16) launch(cache_copy_kernel<4>);
+    else if (vecs == 8) launch(cache_copy_kernel<2>);
+    else launch(cache_copy_kernel<1>);
+    return hip_status(hipGetLastError());
+}
