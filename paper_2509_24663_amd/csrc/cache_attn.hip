@@ -767,6 +767,7 @@ int attend(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, c
         rules::PageWork work;
         int most = 0;
         int64_t tiles[2] = {0, 0}, tile_pages[2] = {0, 0}, unit_pages = 0;
+        rules::PageWork tree[2];
     } chunks, few;
     for (int b = 0; b < batch; ++b) {
         const int n = cu_q_h[b + 1] - cu_q_h[b], len = ctx_lens_h[b];
@@ -789,12 +790,15 @@ int attend(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, c
             const int t0 = a.group_tokens * size[i].groups, t = (n + t0 - 1) / t0, low = t > 1 ? a.first_pages(n, len, t0 - 1) : pages;
             e.tiles[i] += (int64_t)t * hkv;
             e.tile_pages[i] += (int64_t)t * hkv * (low + pages) / 2;
+            if (A::kTree) e.tree[i].add((int64_t)t * hkv, pages, 0);
         }
     }
     wide.fine = chunks.tiles[0] == 0;
     const Either &tiled = wide.fine ? few : chunks;
-    const rules::TileSplits large = rules::tile_splits(size[0], tiled.tiles[0], tiled.most, tiled.tile_pages[0]);
-    const rules::TileSplits small = rules::tile_splits(wide.fine ? rules::fine_tile_size(p->head_dim) : size[1], tiled.tiles[1], tiled.most, tiled.tile_pages[1]);
+    const auto splits = [&](const rules::TileSize &z, int i) {
+        return A::kTree ? rules::tree_splits(z, tiled.tree[i]) : rules::tile_splits(z, tiled.tiles[i], tiled.most, tiled.tile_pages[i]);
+    };
+    const rules::TileSplits large = splits(size[0], 0), small = splits(wide.fine ? rules::fine_tile_size(p->head_dim) : size[1], 1);
     const bool use_small = wide.fine || small.us < large.us;
     wide.tile_groups = size[use_small].groups;
     wide.pps = use_small ? small.pps : large.pps;

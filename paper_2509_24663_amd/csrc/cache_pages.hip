@@ -32,31 +32,38 @@ Pool pool_of(const infllmv2_pages *g) { return Pool{g->page_table_d, g->refs_d, 
 __host__ __device__ inline int blocks_of(int tokens) { return (int)(((int64_t)tokens + kBlock - 1) / kBlock); }
 
 // ------------------------------------------------------------------------------------------ the lowest free pages
-// Workgroup-wide: the sum of x over all threads' (k, wavefront, lane) in that order, exclusive for each; x: one bit (a flag) per k
 struct Ranks {
     int cell[kDeep * kTakeWaves];          // flags of (k, wavefront), then how many stand in front
     int total;
 };
+// a thread's counts of a round: those of pages base + k * kTakeThreads + its number
+struct Counts {
+    int x[kDeep];
+    __device__ inline void load(const int32_t *refs, int64_t base, int num_pages) {
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            const int64_t g = base + k * kTakeThreads + threadIdx.x;
+            x[k] = refs[g < num_pages ? g : num_pages - 1];
+        }
+    }
+};
 
-// Counts that other workgroups' atomics have changed are read past the first cache by the launch in between, which begins with an empty one.
-// flag(page): whether page is wanted; found(page, rank) for those, in order of their numbers, ranks from `before` on; until `most` or the last page
-template <class Flag, class Found>
-__device__ inline int ranked_pages(int num_pages, int most, Ranks &s, Flag flag, Found found) {
+// Workgroup-wide: found(page, rank) for the pages of refs[0 .. num_pages) whose count is wanted, in order of their numbers, until there are `most` or none are
+// left; returns how many there were.  c: the first round's counts (each round's are requested a round ahead).
+template <class Wanted, class Found>
+__device__ inline int ranked_pages(const int32_t *refs, int num_pages, int most, Counts c, Ranks &s, Wanted wanted, Found found) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     int before = 0;
     for (int64_t base = 0; base < num_pages && before < most; base += kTakeThreads * kDeep) {
         bool is[kDeep];
-#pragma unroll
-        for (int k = 0; k < kDeep; ++k) {
-            const int64_t g = base + k * kTakeThreads + tid;
-            is[k] = g < num_pages && flag((int)g);
-        }
         uint64_t hits[kDeep];
 #pragma unroll
         for (int k = 0; k < kDeep; ++k) {
+            is[k] = base + k * kTakeThreads + tid < num_pages && wanted(c.x[k]);
             hits[k] = __ballot(is[k]);
             if (lane == 0) s.cell[k * kTakeWaves + w] = __popcll(hits[k]);
         }
+        if (base + kTakeThreads * kDeep < num_pages) c.load(refs, base + kTakeThreads * kDeep, num_pages);
         __syncthreads();
         if (w == 0) {                      // two cells a lane
             const int x = s.cell[2 * lane], y = s.cell[2 * lane + 1], incl = cache::wave_sums(x + y);
@@ -103,41 +110,71 @@ __device__ inline int row_of(int rows, const int *s_before, int x) {
     return lo;
 }
 
+// Hands out the `wanted` lowest free pages: set(x, page) for the x-th, -1 where there is none
+template <class Set>
+__device__ inline void hand_out(const Pool &g, int wanted, const Counts &c, Ranks &s, int32_t *shortage, Set set) {
+    const int all = ranked_pages(g.refs, g.num_pages, wanted, c, s, [](int x) { return x <= 0; },
+                                 [&](int page, int rank) {
+                                     if (rank >= wanted) return;
+                                     g.refs[page] = 1;
+                                     set(rank, page);
+                                 });
+    const int found = min(all, wanted);
+    for (int x = found + threadIdx.x; x < wanted; x += kTakeThreads) set(x, -1);
+    if (threadIdx.x == 0 && shortage != nullptr) *shortage = wanted - found;
+}
+
 // ------------------------------------------------------------------------------------------ resize
 struct ResizeArgs {
     Pool g;
     const int32_t *old_lens, *new_lens;
     int rows;
+    int pitch_log2;                        // >= 0: entries are given back by the workgroup that hands out, 2^pitch_log2 >= those of any row
     int32_t *shortage;                     // or nullptr
 };
+
+__device__ inline void release(const Pool &g, int32_t *entry, int page) {
+    if (g.is_page(page)) atomicSub(&g.refs[page], 1);
+    *entry = -1;
+}
 
 __global__ void __launch_bounds__(256) pages_release_kernel(ResizeArgs a) {
     const int r = blockIdx.x, want = blocks_of(a.new_lens[r]), have = blocks_of(a.old_lens[r]);
     int32_t *row = a.g.row(r);
-    for (int64_t j = (int64_t)want + blockIdx.y * 256 + threadIdx.x; j < have; j += 256 * gridDim.y) {
-        const int page = row[j];
-        if (a.g.is_page(page)) atomicSub(&a.g.refs[page], 1);
-        row[j] = -1;
-    }
+    if (r == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.shortage != nullptr) *a.shortage = 0;
+    for (int64_t j = (int64_t)want + blockIdx.y * 256 + threadIdx.x; j < have; j += 256 * gridDim.y) release(a.g, row + j, row[j]);
 }
 
 __global__ void __launch_bounds__(kTakeThreads) pages_take_kernel(ResizeArgs a) {
     __shared__ int s_before[kMostRows];
     __shared__ Ranks s_ranks;
+    Counts c;
+    if (a.pitch_log2 >= 0) {
+        const int items = a.rows << a.pitch_log2;
+        for (int i0 = threadIdx.x; i0 < items; i0 += 4 * kTakeThreads) {
+            int32_t *entry[4];
+            int page[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + k * kTakeThreads, r = min(i >> a.pitch_log2, a.rows - 1), j = i & ((1 << a.pitch_log2) - 1);
+                const int want = blocks_of(a.new_lens[r]), have = blocks_of(a.old_lens[r]);
+                entry[k] = i < items && j < have - want ? a.g.row(r) + want + j : nullptr;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) page[k] = entry[k] ? *entry[k] : -1;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (entry[k]) release(a.g, entry[k], page[k]);
+        }
+        __threadfence();                   // (the counts below are read as the atomics left them)
+        __syncthreads();
+    }
+    c.load(a.g.refs, 0, a.g.num_pages);
     const int wanted = sums_before(a.rows, s_before, s_ranks, [&](int r) { return max(blocks_of(a.new_lens[r]) - blocks_of(a.old_lens[r]), 0); });
-    auto entry = [&](int x) {
+    hand_out(a.g, wanted, c, s_ranks, a.shortage, [&](int x, int page) {
         const int r = row_of(a.rows, s_before, x);
-        return a.g.row(r) + blocks_of(a.old_lens[r]) + (x - s_before[r]);
-    };
-    const int found = min(ranked_pages(a.g.num_pages, wanted, s_ranks, [&](int g) { return a.g.refs[g] <= 0; },
-                                       [&](int g, int rank) {
-                                           if (rank >= wanted) return;
-                                           a.g.refs[g] = 1;
-                                           *entry(rank) = g;
-                                       }),
-                          wanted);
-    for (int x = found + threadIdx.x; x < wanted; x += kTakeThreads) *entry(x) = -1;
-    if (threadIdx.x == 0 && a.shortage != nullptr) *a.shortage = wanted - found;
+        a.g.row(r)[blocks_of(a.old_lens[r]) + (x - s_before[r])] = page;
+    });
 }
 
 // ------------------------------------------------------------------------------------------ fork
@@ -145,21 +182,63 @@ struct ForkArgs {
     Pool g;
     const infllmv2_fork *forks;
     int count;
+    int pitch_log2;                        // >= 0: pages are shared by the workgroup that hands out, 2^pitch_log2 >= the blocks of any fork
     int32_t *copies, *shortage;            // (each or nullptr)
 };
 
-// whole pages shared, what the row held before given back
+// A count that a thread changes for several forks in turn, added up as long as they name the same page: forks of one source share its pages, and the
+// rows they take the place of mostly did
+struct Change {
+    int page = -1, by = 0;
+    __device__ inline void add(const Pool &g, int to, int d) {
+        if (to != page) {
+            flush(g);
+            page = to;
+            by = 0;
+        }
+        by += d;
+    }
+    __device__ inline void flush(const Pool &g) {
+        if (by != 0 && g.is_page(page)) atomicAdd(&g.refs[page], by);
+    }
+};
+// block j of a fork: what the row holds, what it gets (a page that stays needs no change)
+struct Shared {
+    int was, page;
+    __device__ inline void load(const Pool &g, const infllmv2_fork &f, int64_t j) {
+        was = j < blocks_of(f.old_tokens) ? g.row(f.dst)[j] : -1;
+        page = j < f.tokens / kBlock ? g.row(f.src)[j] : -1;
+        if (!g.is_page(page)) page = -1;
+    }
+    __device__ inline void apply(const Pool &g, const infllmv2_fork &f, int64_t j, Change &gained, Change &lost) const {
+        if (j >= max(blocks_of(f.tokens), blocks_of(f.old_tokens))) return;
+        if (was != page) {
+            gained.add(g, page, 1);
+            lost.add(g, was, -1);
+        }
+        if (was != page || page < 0) g.row(f.dst)[j] = page;
+    }
+};
+
+// whole pages shared, what the row held before given back: a workgroup goes through kForks forks
+constexpr int kForks = 16;
 __global__ void __launch_bounds__(256) pages_share_kernel(ForkArgs a) {
-    const infllmv2_fork f = a.forks[blockIdx.x];
-    const int32_t *src = a.g.row(f.src);
-    int32_t *dst = a.g.row(f.dst);
-    const int whole = f.tokens / kBlock, held = blocks_of(f.tokens), had = blocks_of(f.old_tokens);
-    for (int64_t j = blockIdx.y * 256 + threadIdx.x; j < max(held, had); j += 256 * gridDim.y) {
-        const int was = j < had ? dst[j] : -1, page = j < whole ? src[j] : -1;
-        const bool good = a.g.is_page(page);
-        if (a.g.is_page(was)) atomicSub(&a.g.refs[was], 1);
-        if (good) atomicAdd(&a.g.refs[page], 1);
-        dst[j] = good ? page : -1;
+    const int first = blockIdx.x * kForks, end = min(first + kForks, a.count);
+    int most = 0;
+    for (int i = first; i < end; ++i) most = max(most, max(blocks_of(a.forks[i].tokens), blocks_of(a.forks[i].old_tokens)));
+    for (int64_t j = blockIdx.y * 256 + threadIdx.x; j < most; j += 256 * gridDim.y) {
+        Change gained, lost;
+        for (int i0 = first; i0 < end; i0 += 8) {
+            Shared s[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + k < end) s[k].load(a.g, a.forks[i0 + k], j);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + k < end) s[k].apply(a.g, a.forks[i0 + k], j, gained, lost);
+        }
+        gained.flush(a.g);
+        lost.flush(a.g);
     }
 }
 
@@ -167,13 +246,38 @@ __global__ void __launch_bounds__(256) pages_share_kernel(ForkArgs a) {
 __global__ void __launch_bounds__(kTakeThreads) pages_split_kernel(ForkArgs a) {
     __shared__ int s_before[kMostRows];
     __shared__ Ranks s_ranks;
+    Counts c;
+    if (a.pitch_log2 >= 0) {
+        const int items = a.count << a.pitch_log2;
+        for (int i0 = threadIdx.x; i0 < items; i0 += 4 * kTakeThreads) {
+            Shared s[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + k * kTakeThreads;
+                if (i < items) s[k].load(a.g, a.forks[i >> a.pitch_log2], i & ((1 << a.pitch_log2) - 1));
+            }
+            Change gained, lost;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + k * kTakeThreads;
+                if (i < items) s[k].apply(a.g, a.forks[i >> a.pitch_log2], i & ((1 << a.pitch_log2) - 1), gained, lost);
+            }
+            gained.flush(a.g);
+            lost.flush(a.g);
+        }
+    }
+    if (a.copies != nullptr)
+        for (int i = threadIdx.x; i < 2 * a.count; i += kTakeThreads) a.copies[i] = -1;
+    __threadfence();                       // (the counts below are read as the atomics left them; table and copies are written again behind these)
+    __syncthreads();
+    c.load(a.g.refs, 0, a.g.num_pages);
     auto from = [&](int i) {               // the page that is continued, or -1
         const infllmv2_fork f = a.forks[i];
         const int page = f.tokens % kBlock != 0 ? a.g.row(f.src)[f.tokens / kBlock] : -1;
         return a.g.is_page(page) ? page : -1;
     };
     const int wanted = sums_before(a.count, s_before, s_ranks, [&](int i) { return from(i) >= 0 ? 1 : 0; });
-    auto set = [&](int x, int page) {
+    hand_out(a.g, wanted, c, s_ranks, a.shortage, [&](int x, int page) {
         const int i = row_of(a.count, s_before, x);
         const infllmv2_fork f = a.forks[i];
         a.g.row(f.dst)[f.tokens / kBlock] = page;
@@ -181,21 +285,7 @@ __global__ void __launch_bounds__(kTakeThreads) pages_split_kernel(ForkArgs a) {
             a.copies[2 * i] = from(i);
             a.copies[2 * i + 1] = page;
         }
-    };
-    if (a.copies != nullptr) {
-        for (int i = threadIdx.x; i < 2 * a.count; i += kTakeThreads) a.copies[i] = -1;
-        __threadfence();
-        __syncthreads();
-    }
-    const int found = min(ranked_pages(a.g.num_pages, wanted, s_ranks, [&](int g) { return a.g.refs[g] <= 0; },
-                                       [&](int g, int rank) {
-                                           if (rank >= wanted) return;
-                                           a.g.refs[g] = 1;
-                                           set(rank, g);
-                                       }),
-                          wanted);
-    for (int x = found + threadIdx.x; x < wanted; x += kTakeThreads) set(x, -1);
-    if (threadIdx.x == 0 && a.shortage != nullptr) *a.shortage = wanted - found;
+    });
 }
 
 // ------------------------------------------------------------------------------------------ compact
@@ -209,9 +299,15 @@ struct CompactArgs {
 // Of the pages in use those from number `used` on move, in order, to the free ones below it, in order: there are as many of either.
 __global__ void __launch_bounds__(kTakeThreads) pages_moves_kernel(CompactArgs a) {
     __shared__ Ranks s_ranks;
-    const int used = ranked_pages(a.g.num_pages, INT32_MAX, s_ranks, [&](int g) { return a.g.refs[g] > 0; }, [](int, int) {});
-    const int n = ranked_pages(used, INT32_MAX, s_ranks, [&](int g) { return a.g.refs[g] <= 0; }, [&](int g, int rank) { a.moves[2 * rank + 1] = g; });
-    ranked_pages(a.g.num_pages - used, INT32_MAX, s_ranks, [&](int g) { return a.g.refs[used + g] > 0; }, [&](int g, int rank) { a.moves[2 * rank] = used + g; });
+    const auto in_use = [](int x) { return x > 0; };
+    Counts c;
+    c.load(a.g.refs, 0, a.g.num_pages);
+    const int used = ranked_pages(a.g.refs, a.g.num_pages, INT32_MAX, c, s_ranks, in_use, [](int, int) {});
+    const int n = ranked_pages(a.g.refs, used, INT32_MAX, c, s_ranks, [](int x) { return x <= 0; }, [&](int g, int rank) { a.moves[2 * rank + 1] = g; });
+    if (n > 0) {
+        c.load(a.g.refs + used, 0, a.g.num_pages - used);
+        ranked_pages(a.g.refs + used, a.g.num_pages - used, INT32_MAX, c, s_ranks, in_use, [&](int g, int rank) { a.moves[2 * rank] = used + g; });
+    }
     for (int i = 2 * n + threadIdx.x; i < a.g.num_pages / 2 * 2; i += kTakeThreads) a.moves[i] = -1;
     if (threadIdx.x == 0) a.live[0] = used, a.live[1] = n;
 }
@@ -286,6 +382,13 @@ int check_pages(const infllmv2_pages *g) {
     return INFLLMV2_OK;
 }
 bool fits(const infllmv2_pages *g, int tokens) { return tokens >= 0 && blocks_of(tokens) <= g->blocks; }
+int pitch_log2(int x) {                    // least power of two that is at least x
+    int p = 0;
+    while ((1ll << p) < x) ++p;
+    return p;
+}
+// Entries, with those that a row does not have, up to which one workgroup gives back or shares them and hands out pages after it: one launch for two.
+constexpr int64_t kTogether = 16384;
 unsigned chunks(int64_t entries, int per) { return (unsigned)std::max<int64_t>(std::min<int64_t>((entries + per - 1) / per, 64), 1); }
 
 }  // namespace
@@ -310,9 +413,11 @@ extern "C" int infllmv2_pages_resize(const infllmv2_pages *g, const int32_t *old
     }
     if (batch > kMostRows || more > INT32_MAX) return INFLLMV2_ERR_UNSUPPORTED;
     if (less == 0 && more == 0 && short_d == nullptr) return INFLLMV2_OK;
-    const ResizeArgs a{pool_of(g), old_lens_d, new_lens_d, batch, short_d};
-    if (less > 0) hipLaunchKernelGGL(pages_release_kernel, dim3(batch, chunks(less, 256)), dim3(256), 0, (hipStream_t)stream, a);
-    if (more > 0 || short_d != nullptr) hipLaunchKernelGGL(pages_take_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
+    const int pitch = pitch_log2(less);
+    const bool together = less > 0 && more > 0 && (int64_t)batch << pitch <= kTogether;
+    const ResizeArgs a{pool_of(g), old_lens_d, new_lens_d, batch, together ? pitch : -1, short_d};
+    if (less > 0 && !together) hipLaunchKernelGGL(pages_release_kernel, dim3(batch, chunks(less, 256)), dim3(256), 0, (hipStream_t)stream, a);
+    if (more > 0 || less == 0) hipLaunchKernelGGL(pages_take_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());
 }
 
@@ -339,9 +444,11 @@ extern "C" int infllmv2_pages_fork(const infllmv2_pages *g, const infllmv2_fork 
     for (int i = 0; i < count; ++i)
         if (to[forks_h[i].src / 64] >> (forks_h[i].src % 64) & 1) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (most == 0 && copies_d == nullptr && short_d == nullptr) return INFLLMV2_OK;
-    const ForkArgs a{pool_of(g), forks_d, count, copies_d, short_d};
-    if (most > 0) hipLaunchKernelGGL(pages_share_kernel, dim3(count, chunks(most, 256)), dim3(256), 0, (hipStream_t)stream, a);
-    if (part || copies_d != nullptr || short_d != nullptr) hipLaunchKernelGGL(pages_split_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
+    const int pitch = pitch_log2(most);
+    const bool together = most > 0 && (int64_t)count << pitch <= kTogether;
+    const ForkArgs a{pool_of(g), forks_d, count, together ? pitch : -1, copies_d, short_d};
+    if (most > 0 && !together) hipLaunchKernelGGL(pages_share_kernel, dim3((count + kForks - 1) / kForks, chunks(most, 256)), dim3(256), 0, (hipStream_t)stream, a);
+    if (part || together || copies_d != nullptr || short_d != nullptr) hipLaunchKernelGGL(pages_split_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());
 }
 

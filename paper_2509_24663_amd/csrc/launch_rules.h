@@ -474,6 +474,20 @@ inline TileSplits tile_splits(const TileSize &z, int64_t tiles, int pages, int64
     }
     return best;
 }
+// The same for trees of drafted tokens, whose tiles all go through all pages of their sequence: work has the tiles by their pages, so that the workgroups of a
+// choice are counted, not taken to be alike.
+inline TileSplits tree_splits(const TileSize &z, const PageWork &work) {
+    TileSplits best{work.most, 0};
+    for (int s = 1; s <= kMostTileSplits && s <= work.most; s += s < 8 ? 1 : s / 8) {
+        const int per = (work.most + s - 1) / s;
+        const int64_t n = work.groups(per), rounds = (n + 255) / 256;
+        if (s > 1 && (work.sum / per + work.all) * z.groups > kMostTileGroups) break;
+        const double dealt = (double)work.sum / 256 + per / 2., way = rounds > 1 && dealt < (double)rounds * per ? dealt : (double)rounds * per;
+        const double us = 14.7 + z.page_us * way + 3. * (rounds - 1) + (s > 1 ? 1.5 + z.result_us * n : 0);
+        if (s == 1 || us < best.us) best = {per, us};
+    }
+    return best;
+}
 // What the kernel of 16 columns (cache_attn.hip) is taken to cost: `sum`: pages over all its column groups and KV heads; once there are many, rows come from
 // the L2; long ones cost the joining of many splits.  Some more than it takes (some 5 us of a call go by beside it, as of tile_splits' 14.7).  d 128: 600
 // groups over 21 pages 30.6 us, 2200 over 18 (half of them, on average) 51, 1024 over 126 171; d 64: 256 over 125 41.  The choice between it and the two

@@ -18,50 +18,46 @@ struct MaskArgs {
     const int32_t *parents, *cu, *ctx;
     uint32_t *mask;
     int32_t *pos;                          // or nullptr
-    int words;                             // of a row
+    int words, words_log2;                 // of a row; threads of one
 };
 
+// Threads of a row stand side by side, 2^words_log2 of them (a power of two: a division for every word would be most of the kernel).
 __global__ void tree_masks_kernel(MaskArgs a) {
     extern __shared__ int32_t s_tree[];                       // jumps [2][n], rows [n][W]
     const int row0 = a.cu[blockIdx.x], n = a.cu[blockIdx.x + 1] - row0, W = (n + 31) / 32;
     if (n == 0) return;
-    int32_t *jump = s_tree;
+    int32_t *jump = s_tree, *next = s_tree + n;
     uint32_t *rows = (uint32_t *)(s_tree + 2 * n);
+    const int w = threadIdx.x & ((1 << a.words_log2) - 1), r0 = threadIdx.x >> a.words_log2, by = blockDim.x >> a.words_log2;
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
         const int p = a.parents[row0 + i];
         jump[i] = p >= 0 && p < n ? p : -1;
     }
-    for (int i = threadIdx.x; i < n * W; i += blockDim.x) {
-        const int r = i / W, w = i - r * W;
-        rows[i] = r / 32 == w ? 1u << (r % 32) : 0u;
-    }
+    for (int r = r0; w < W && r < n; r += by) rows[r * W + w] = r / 32 == w ? 1u << (r % 32) : 0u;
     __syncthreads();
     for (int far = 1; far < n; far *= 2) {
-        for (int i = threadIdx.x; i < n * W; i += blockDim.x) {
-            const int r = i / W, j = jump[r];
-            if (j >= 0) rows[i] |= rows[j * W + i - r * W];
+        for (int r = r0; w < W && r < n; r += by) {
+            const int j = jump[r];
+            if (j >= 0) rows[r * W + w] |= rows[j * W + w];
         }
         int more = 0;
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
             const int j = jump[i], to = j >= 0 ? jump[j] : -1;
-            jump[n + i] = to;
+            next[i] = to;
             more |= to >= 0;
         }
-        more = __syncthreads_or(more);
-        if (!more) break;
-        for (int i = threadIdx.x; i < n; i += blockDim.x) jump[i] = jump[n + i];
-        __syncthreads();
+        if (!__syncthreads_or(more)) break;
+        int32_t *was = jump;
+        jump = next;
+        next = was;
     }
-    for (int64_t i = threadIdx.x; i < (int64_t)n * a.words; i += blockDim.x) {
-        const int r = (int)(i / a.words), w = (int)(i - (int64_t)r * a.words);
-        a.mask[(int64_t)row0 * a.words + i] = w < W ? rows[r * W + w] : 0u;
-    }
-    if (a.pos == nullptr) return;
-    const int front = a.ctx[blockIdx.x] - n;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        int depth = -1;
-        for (int w = 0; w < W; ++w) depth += __popc(rows[i * W + w]);
-        a.pos[row0 + i] = front + depth;
+    const int front = a.pos != nullptr ? a.ctx[blockIdx.x] - n : 0;
+    for (int r = r0; r < n; r += by) {
+        const uint32_t bits = w < W ? rows[r * W + w] : 0u;
+        for (int x = w; x < a.words; x += 1 << a.words_log2) a.mask[(int64_t)(row0 + r) * a.words + x] = x < W ? bits : 0u;
+        int count = __popc(bits);
+        for (int o = 1 << a.words_log2 >> 1; o > 0; o >>= 1) count += __shfl_xor(count, o);
+        if (a.pos != nullptr && w == 0) a.pos[row0 + r] = front + count - 1;
     }
 }
 
@@ -83,11 +79,12 @@ extern "C" int infllmv2_tree_masks(const int32_t *parents_d, const int32_t *cu_q
     for (int b = 0; pos_d != nullptr && b < batch; ++b)
         if (ctx_lens_h[b] < cu_q_h[b + 1] - cu_q_h[b] || ctx_lens_h[b] > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (most > kMost) return INFLLMV2_ERR_UNSUPPORTED;
-    const int words = (most + 31) / 32, lds = (2 + words) * most * (int)sizeof(int32_t), threads = most * words > 1024 ? 1024 : (most * words + 63) / 64 * 64;
+    const int words = (most + 31) / 32, words_log2 = words > 16 ? 5 : words > 8 ? 4 : words > 4 ? 3 : words > 2 ? 2 : words - 1;
+    const int lds = (2 + words) * most * (int)sizeof(int32_t), items = most << words_log2, threads = items > 1024 ? 1024 : (items + 63) / 64 * 64;
     if (lds > 64 * 1024 &&
         hipFuncSetAttribute(reinterpret_cast<const void *>(tree_masks_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (2 + kMost / 32) * kMost * (int)sizeof(int32_t)) != hipSuccess)
         return INFLLMV2_ERR_HIP;
-    const MaskArgs a{parents_d, cu_q_d, ctx_lens_d, mask_d, pos_d, mask_words};
+    const MaskArgs a{parents_d, cu_q_d, ctx_lens_d, mask_d, pos_d, mask_words, words_log2};
     hipLaunchKernelGGL(tree_masks_kernel, dim3(batch), dim3(threads), lds, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());
 }
