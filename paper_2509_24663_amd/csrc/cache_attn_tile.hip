@@ -128,7 +128,30 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     }
     // a page whose context rows are not seen; a page (or half of one) of which not all rows are seen by all tokens of the tile from token t on
     auto shut = [&](int key0) { return A::kTree && !open && key0 / kBlock == pos0 / kBlock; };
-    auto edge = [&](int key0, int keys, int t) { return A::kTree ? key0 + keys > pos0 || shut(key0) : key0 + keys - 1 > pos0 + t; };
+    const int edge_from = A::kTree && !open ? pos0 / kBlock * kBlock : pos0;
+    auto edge = [&](int key0, int keys, int t) { return A::kTree ? key0 + keys > edge_from : key0 + keys - 1 > pos0 + t; };
+
+    int e_end, e_by = 1;                                            // entries of this split; of a list every nsplit-th
+    const int e_first = A::kTree && list ? split : split * a.pps;
+    int tree_j = 0, tree_page = -1;
+    // a tree: the block of this lane's entry from e0 on, and its page
+    auto look_up = [&](int e0) __attribute__((always_inline)) {
+        const int e = e0 + lane * e_by;
+        int below = pos_last / kBlock + 1;
+        tree_j = pos0 / kBlock + e - tree_e;
+        if (list && e < tree_e) {                                   // (the block of the first drafted row has its own entry)
+            tree_j = list[e];
+            below = pos0 / kBlock;
+        }
+        tree_page = e < e_end && tree_j >= 0 && tree_j < below ? a.c.page(seq, tree_j) : -1;
+    };
+    if constexpr (A::kTree) {
+        e_end = list ? tree_e + pos_last / kBlock - pos0 / kBlock + 1 : min(pos_last / kBlock + 1, (split + 1) * a.pps);
+        e_by = list ? nsplit : 1;
+        look_up(e_first);                                           // (beside the queries, not behind them)
+    } else {
+        e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
+    }
 
     int ti[CG];
     bool used[CG];
@@ -242,15 +265,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     };
 
     // the pages of the split: lane l holds the l-th of the next 64
-    int e_end, e_by = 1;                                            // of a list every nsplit-th
-    if constexpr (A::kTree) {
-        e_end = list ? tree_e + pos_last / kBlock - pos0 / kBlock + 1 : min(pos_last / kBlock + 1, (split + 1) * a.pps);
-        e_by = list ? nsplit : 1;
-    } else {
-        e_end = min(a.pages(len, pos_last), (split + 1) * a.pps);
-    }
-    const int e_first = A::kTree && list ? split : split * a.pps;
-    int e0 = 0, list_key0 = 0;
+    int e0 = 0, e_now = e_first, list_key0 = 0;
     int64_t list_at = 0;
     float list_ks = 1.f, list_vs = 1.f;
     uint64_t there = 0;
@@ -258,14 +273,10 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
         while (there == 0 && e0 < e_end) {
             int j, page;
             if constexpr (A::kTree) {
-                const int e = e0 + lane * e_by;
-                int below = pos_last / kBlock + 1;
-                j = pos0 / kBlock + e - tree_e;
-                if (list && e < tree_e) {                           // (the block of the first drafted row has its own entry)
-                    j = list[e];
-                    below = pos0 / kBlock;
-                }
-                page = e < e_end && j >= 0 && j < below ? a.c.page(seq, j) : -1;
+                if (e0 != e_now) look_up(e0);
+                e_now = e0;
+                j = tree_j;
+                page = tree_page;
             } else {
                 j = e0 + lane;
                 page = j < e_end ? a.c.page(seq, j) : -1;
@@ -291,7 +302,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     if (tid == 0) s_odd = s_again = 0;
 
     // The walk, in steps of half a page k (32 keys): logits of k; then sums of the weights of k - 1 and, between those products, the weights of k.
-    uint32_t saw = 0;                                               // a tree: bit x: this lane's column x saw a key
+    uint32_t saw = 0;                                               // a tree: bit x: this lane's column x saw a key ..
+    bool saw_all = false;                                           // .. all columns did
     constexpr int LOGITS = 8 * CG, KF = 2 * KS;                     // logits of a lane, K operands of a step
     f32x4 s[CG][2];
     uint32_t pb[2][CG][PIECES][4];                                  // by the parity of k
@@ -355,8 +367,6 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                         for (int r = 0; r < 4; ++r) s[x][kt][r] = 4 * kt + r <= lim ? s[x][kt][r] : -INFINITY;
                 }
             }
-        } else if (A::kTree) {
-            saw = ~0u;
         }
         float part[CG], last = 0.f;
 #pragma unroll
@@ -454,6 +464,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
                 const bool most = there != 0;
                 if (most) next(after);
                 const int ahead3 = p3 == 2 ? 0 : p3 + 1;
+                if (A::kTree) saw_all |= !edge(now.key0, 32, 0);
                 if (edge(then.key0, kBlock, 0)) clean(then.key0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (what this wavefront wrote)
                 __builtin_amdgcn_s_barrier();
@@ -508,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             asm volatile("" : "+v"(t));                             // (addresses are formed here: kept through the second walk they take registers)
             const float total = rows_add(sum[x]);
             bool seen;
-            if constexpr (A::kTree) seen = used[x] && (__ballot(saw >> x & 1u) >> m & 0x0001000100010001ull) != 0;
+            if constexpr (A::kTree) seen = used[x] && (saw_all || (__ballot(saw >> x & 1u) >> m & 0x0001000100010001ull) != 0);
             else seen = used[x] && low <= pos0 + t;
             // (a split without weight is 0 with no weight: others of the column may have some)
             const float inv = seen && (nsplit == 1 || total != 0.f) ? 1.f / total : 0.f;

@@ -388,7 +388,7 @@ int pitch_log2(int x) {                    // least power of two that is at leas
     return p;
 }
 // Entries, with those that a row does not have, up to which one workgroup gives back or shares them and hands out pages after it: one launch for two.
-constexpr int64_t kTogether = 16384;
+constexpr int64_t kTogether = 4096;
 unsigned chunks(int64_t entries, int per) { return (unsigned)std::max<int64_t>(std::min<int64_t>((entries + per - 1) / per, 64), 1); }
 
 }  // namespace

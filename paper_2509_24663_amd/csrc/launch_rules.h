@@ -478,13 +478,26 @@ inline TileSplits tile_splits(const TileSize &z, int64_t tiles, int pages, int64
 // choice are counted, not taken to be alike.
 inline TileSplits tree_splits(const TileSize &z, const PageWork &work) {
     TileSplits best{work.most, 0};
-    for (int s = 1; s <= kMostTileSplits && s <= work.most; s += s < 8 ? 1 : s / 8) {
-        const int per = (work.most + s - 1) / s;
+    const int least = (work.most + kMostTileSplits - 1) / kMostTileSplits;
+    auto consider = [&](int per) {
+        const bool split = per < work.most;
+        if (split && (per < least || (work.sum / per + work.all) * z.groups > kMostTileGroups)) return;
         const int64_t n = work.groups(per), rounds = (n + 255) / 256;
-        if (s > 1 && (work.sum / per + work.all) * z.groups > kMostTileGroups) break;
         const double dealt = (double)work.sum / 256 + per / 2., way = rounds > 1 && dealt < (double)rounds * per ? dealt : (double)rounds * per;
-        const double us = 14.7 + z.page_us * way + 3. * (rounds - 1) + (s > 1 ? 1.5 + z.result_us * n : 0);
-        if (s == 1 || us < best.us) best = {per, us};
+        const double us = 14.7 + z.page_us * way + 3. * (rounds - 1) + (split ? 1.5 + z.result_us * n : 0);
+        if (best.us == 0 || us < best.us) best = {per, us};
+    };
+    consider(work.most);
+    // the fewest pages of a workgroup with which there are no more of them than run in one, two or three rounds
+    const int64_t whole = (work.groups(work.most) + 255) / 256;
+    for (int64_t r = whole; r < whole + 3; ++r) {
+        int lo = 1, hi = work.most;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (work.groups(mid) <= 256 * r) hi = mid;
+            else lo = mid + 1;
+        }
+        consider(lo > least ? lo : least);
     }
     return best;
 }
