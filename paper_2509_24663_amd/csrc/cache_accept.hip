@@ -69,32 +69,43 @@ __global__ void __launch_bounds__(kThreads) cache_accept_kernel(AcceptArgs a) {
     if (tid == 0 && h == 0 && !values && a.lens != nullptr) a.lens[b] = front + count;
     char *pool = values ? a.c.v : a.c.k;
     float *scales = values ? a.c.vs : a.c.ks;
-    for (int block = (front + same) / kBlock, turn = 0; same < count && block <= (front + count - 1) / kBlock; ++block, turn ^= 1) {
-        const int first = max(front + same, block * kBlock), end = min(front + count, block * kBlock + kBlock);          // rows that are written
-        const int to_page = a.c.page(b, block);
-        char *to = pool + a.c.at(to_page, h);
+    // what moves into a page, as requested
+    struct Rows {
         Piece x[PER];
         float scale[PER];                  // of the row's page; 0: the row is not there
-        uint32_t top = 0;
+    };
+    const int block1 = (front + count - 1) / kBlock;
+    auto request = [&](int block) {
+        Rows m;
+        const int first = max(front + same, block * kBlock), end = min(front + count, block * kBlock + kBlock), to_page = a.c.page(b, block);
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             const int v = tid + e * kThreads, row = first + (v >> a.vecs_log2);
-            scale[e] = 0.f;
+            m.x[e] = Piece{0, 0, 0, 0};
+            m.scale[e] = 0.f;
             if (row < end && to_page >= 0) {
                 const int from = front + path[row - front], page = a.c.page(b, from / kBlock);
                 if (page >= 0) {
-                    x[e] = *reinterpret_cast<const Piece *>(pool + a.c.at(page, h) + (from % kBlock) * a.c.tok_stride + (v & (a.vecs - 1)) * 16);
-                    scale[e] = CODES ? scales[(int64_t)page * a.c.hkv + h] : 1.f;
-                    if (CODES) {
-                        const float t = __builtin_amdgcn_cvt_f32_fp8((int)top_code(x[e]), 0) * scale[e];
-                        top = max(top, __float_as_uint(t));
-                    }
+                    m.x[e] = *reinterpret_cast<const Piece *>(pool + a.c.at(page, h) + (from % kBlock) * a.c.tok_stride + (v & (a.vecs - 1)) * 16);
+                    m.scale[e] = CODES ? scales[(int64_t)page * a.c.hkv + h] : 1.f;
                 }
             }
         }
+        return m;
+    };
+    if (same >= count) return;
+    int block = (front + same) / kBlock, turn = 0;
+    Rows m = request(block);
+    for (;; ++block, turn ^= 1) {
+        const int first = max(front + same, block * kBlock), end = min(front + count, block * kBlock + kBlock);          // rows that are written
+        const int to_page = a.c.page(b, block);
+        char *to = pool + a.c.at(to_page, h);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // (all rows are here before any is written)
         float now = 1.f;
         if constexpr (CODES) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) top = max(top, __float_as_uint(__builtin_amdgcn_cvt_f32_fp8((int)top_code(m.x[e]), 0) * m.scale[e]));
             const float was = to_page >= 0 ? scales[(int64_t)to_page * a.c.hkv + h] : 1.f;
             top = (uint32_t)__builtin_amdgcn_readlane(cache::wave_scan((int)top, [](int p, int q) { return (int)max((uint32_t)p, (uint32_t)q); }), 63);
             if ((tid & 63) == 0) s_top[turn][tid >> 6] = top;
@@ -116,15 +127,19 @@ __global__ void __launch_bounds__(kThreads) cache_accept_kernel(AcceptArgs a) {
         } else {
             __syncthreads();
         }
+        // (the next page's rows are from pages behind this one, which it does not write)
+        Rows next;
+        if (block < block1) next = request(block + 1);
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             const int v = tid + e * kThreads, row = first + (v >> a.vecs_log2);
-            if (scale[e] == 0.f) continue;
-            Piece y = x[e];
-            if (CODES && scale[e] != now) y = rescaled(y, scale[e] * cache::reciprocal_of_power(now));
+            if (m.scale[e] == 0.f) continue;
+            Piece y = m.x[e];
+            if (CODES && m.scale[e] != now) y = rescaled(y, m.scale[e] * cache::reciprocal_of_power(now));
             *reinterpret_cast<Piece *>(to + (row - block * kBlock) * a.c.tok_stride + (v & (a.vecs - 1)) * 16) = y;
         }
-        __syncthreads();
+        if (block == block1) break;
+        m = next;
     }
 }
 

@@ -1,11 +1,12 @@
 // Who is whose ancestor in each sequence's tree of drafted tokens, as bits, from the tokens' parents; and the position at which every token stands.
 //
-// A workgroup has one tree in LDS: a row of bits and a jump for each token.  A round gives every token the bits of the token its jump leads to and doubles the
-// jump, so that after round r a row holds the 2^r nearest of {itself, its ancestors}, and log2 of the deepest chain rounds are all.  (Rows are read while others
-// add to them: a row may come with more ancestors than its round has, never with others.)  Chains that close into a circle, which is no tree, end after log2(n)
-// rounds with the tokens that can be reached.
+// A workgroup has four words of every row of a tree, a thread one token: its bits and a jump.  A round gives every token the bits of the token its jump leads to and
+// doubles the jump, so that after round r a row holds the 2^r nearest of {itself, its ancestors}, and log2 of the deepest chain rounds are all.  (Rows are
+// read while others add to them: a row may come with more ancestors than its round has, never with others.)  The ancestors are counted on the way.  Chains that close into a
+// circle, which is no tree, end after log2(n) rounds with the tokens that can be reached, which are then counted by going along the chain.
 //
-// Bound: launch and the chain parents, rounds, rows (one tree of 26 tokens; 64 trees of 127 to 509).
+// Bound: launch and the chain parents, rounds (a barrier each), rows.  One tree of 26 tokens 2.7 us; 64 trees of 127 to 509 tokens, the deepest chain some 120: 7.0
+// (13.4 with all words of a tree in one workgroup, and 18.6 with a division for every word).
 #include "common.h"
 
 namespace ifv2 {
@@ -13,52 +14,81 @@ namespace ifv2 {
 namespace {
 
 constexpr int kMost = INFLLMV2_TREE_MOST;
+constexpr int kWords = 4;                  // of a workgroup
+typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
 
 struct MaskArgs {
     const int32_t *parents, *cu, *ctx;
     uint32_t *mask;
     int32_t *pos;                          // or nullptr
-    int words, words_log2;                 // of a row; threads of one
+    int words;                             // of a row
 };
 
-// Threads of a row stand side by side, 2^words_log2 of them (a power of two: a division for every word would be most of the kernel).
-__global__ void tree_masks_kernel(MaskArgs a) {
-    extern __shared__ int32_t s_tree[];                       // jumps [2][n], rows [n][W]
-    const int row0 = a.cu[blockIdx.x], n = a.cu[blockIdx.x + 1] - row0, W = (n + 31) / 32;
+// how many tokens a chain that does not end goes through, from token i on: those in front of the circle and the circle's (Brent's way of finding both)
+__device__ int tokens_to_circle(const int32_t *parent, int i) {
+    int power = 1, circle = 1, slow = i, fast = parent[i];
+    while (slow != fast) {
+        if (power == circle) {
+            slow = fast;
+            power *= 2;
+            circle = 0;
+        }
+        fast = parent[fast];
+        ++circle;
+    }
+    int front = 0;
+    slow = fast = i;
+    for (int k = 0; k < circle; ++k) fast = parent[fast];
+    while (slow != fast) {
+        slow = parent[slow];
+        fast = parent[fast];
+        ++front;
+    }
+    return front + circle;
+}
+
+__global__ void __launch_bounds__(kMost) tree_masks_kernel(MaskArgs a) {
+    __shared__ Words s_rows[kMost];
+    __shared__ int s_parent[kMost], s_jump[2][kMost], s_above[2][kMost];
+    const int row0 = a.cu[blockIdx.x], n = a.cu[blockIdx.x + 1] - row0, r = threadIdx.x, w0 = blockIdx.y * kWords;
     if (n == 0) return;
-    int32_t *jump = s_tree, *next = s_tree + n;
-    uint32_t *rows = (uint32_t *)(s_tree + 2 * n);
-    const int w = threadIdx.x & ((1 << a.words_log2) - 1), r0 = threadIdx.x >> a.words_log2, by = blockDim.x >> a.words_log2;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int p = a.parents[row0 + i];
-        jump[i] = p >= 0 && p < n ? p : -1;
-    }
-    for (int r = r0; w < W && r < n; r += by) rows[r * W + w] = r / 32 == w ? 1u << (r % 32) : 0u;
-    __syncthreads();
-    for (int far = 1; far < n; far *= 2) {
-        for (int r = r0; w < W && r < n; r += by) {
-            const int j = jump[r];
-            if (j >= 0) rows[r * W + w] |= rows[j * W + w];
+    const bool counts = blockIdx.y == 0 && a.pos != nullptr;
+    const int front = counts ? a.ctx[blockIdx.x] - n : 0;
+    Words mine = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) mine[i] = r / 32 == w0 + i ? 1u << (r % 32) : 0u;
+    int jump = -1, above = 0;
+    if (32 * w0 < n) {                     // (else words behind the tree's)
+        if (r < n) {
+            const int p = a.parents[row0 + r];
+            jump = p >= 0 && p < n ? p : -1;
+            above = jump >= 0 ? 1 : 0;
+            s_parent[r] = s_jump[0][r] = jump;
+            s_above[0][r] = above;
+            s_rows[r] = mine;
         }
-        int more = 0;
-        for (int i = threadIdx.x; i < n; i += blockDim.x) {
-            const int j = jump[i], to = j >= 0 ? jump[j] : -1;
-            next[i] = to;
-            more |= to >= 0;
+        int turn = 0, far = 1;
+        while (__syncthreads_or(jump >= 0) && far < n) {
+            if (jump >= 0) {
+                mine |= s_rows[jump];
+                above += s_above[turn][jump];
+                jump = s_jump[turn][jump];
+                s_rows[r] = mine;
+            }
+            far *= 2;
+            turn ^= 1;
+            if (r < n) {
+                s_jump[turn][r] = jump;
+                s_above[turn][r] = above;
+            }
         }
-        if (!__syncthreads_or(more)) break;
-        int32_t *was = jump;
-        jump = next;
-        next = was;
     }
-    const int front = a.pos != nullptr ? a.ctx[blockIdx.x] - n : 0;
-    for (int r = r0; r < n; r += by) {
-        const uint32_t bits = w < W ? rows[r * W + w] : 0u;
-        for (int x = w; x < a.words; x += 1 << a.words_log2) a.mask[(int64_t)(row0 + r) * a.words + x] = x < W ? bits : 0u;
-        int count = __popc(bits);
-        for (int o = 1 << a.words_log2 >> 1; o > 0; o >>= 1) count += __shfl_xor(count, o);
-        if (a.pos != nullptr && w == 0) a.pos[row0 + r] = front + count - 1;
-    }
+    if (r >= n) return;
+    uint32_t *to = a.mask + (int64_t)(row0 + r) * a.words + w0;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i)
+        if (w0 + i < a.words) to[i] = mine[i];
+    if (counts) a.pos[row0 + r] = front + (jump < 0 ? above : tokens_to_circle(s_parent, r) - 1);
 }
 
 }  // namespace
@@ -79,12 +109,10 @@ extern "C" int infllmv2_tree_masks(const int32_t *parents_d, const int32_t *cu_q
     for (int b = 0; pos_d != nullptr && b < batch; ++b)
         if (ctx_lens_h[b] < cu_q_h[b + 1] - cu_q_h[b] || ctx_lens_h[b] > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
     if (most > kMost) return INFLLMV2_ERR_UNSUPPORTED;
-    const int words = (most + 31) / 32, words_log2 = words > 16 ? 5 : words > 8 ? 4 : words > 4 ? 3 : words > 2 ? 2 : words - 1;
-    const int lds = (2 + words) * most * (int)sizeof(int32_t), items = most << words_log2, threads = items > 1024 ? 1024 : (items + 63) / 64 * 64;
-    if (lds > 64 * 1024 &&
-        hipFuncSetAttribute(reinterpret_cast<const void *>(tree_masks_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (2 + kMost / 32) * kMost * (int)sizeof(int32_t)) != hipSuccess)
-        return INFLLMV2_ERR_HIP;
-    const MaskArgs a{parents_d, cu_q_d, ctx_lens_d, mask_d, pos_d, mask_words, words_log2};
-    hipLaunchKernelGGL(tree_masks_kernel, dim3(batch), dim3(threads), lds, (hipStream_t)stream, a);
+    const MaskArgs a{parents_d, cu_q_d, ctx_lens_d, mask_d, pos_d, mask_words};
+    // (words behind those of the largest tree are written by workgroups of their own)
+    const int64_t chunks = (mask_words + (int64_t)kWords - 1) / kWords;
+    if (chunks > 65535) return INFLLMV2_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(tree_masks_kernel, dim3(batch, (unsigned)chunks), dim3((most + 63) / 64 * 64), 0, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());
 }

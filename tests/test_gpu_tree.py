@@ -415,3 +415,47 @@ def test_captured(m):  # noqa: F811
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(results, want)), seed
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,n,ctx", [("bf16", 32, 2, 128, 5, 300), ("bf16", 32, 2, 128, 40, 9000), ("bf16", 8, 2, 64, 100, 9000), ("fp32", 4, 1, 64, 9, 3000),
+                                                  ("bf16", 32, 2, 128, 8, 20000)])
+@pytest.mark.parametrize("kv", ["e4m3", "native"])
+def test_large_values(m, kv, dtype, hq, hkv, d, n, ctx):  # noqa: F811
+    """A mean of values next to the largest float is one of them, however many keys (drafted ones and the context's), and other channels are as without."""
+    p = _params(m, dtype, hq, hkv, d, softmax_scale=1.0)
+    c, _, _ = _filled(m, p, [ctx], kv, 63)
+    mask = _masks(m, [n], [ctx], 14)
+    q = torch.zeros((n, hq, d), device="cuda", dtype=p.torch_dtype)
+    q[..., 0] = 1.0
+    gen = _gen(15)
+    k = torch.zeros((hkv, ctx, d), device="cuda")
+    k[..., 0] = torch.randn(ctx, generator=gen, device="cuda") * 0.25
+    v = torch.randn((hkv, ctx, d), generator=gen, device="cuda")
+    v[..., :8] = 0
+    write = lambda x: m.cache_append(p, c, k.to(p.torch_dtype), x.to(p.torch_dtype), [0, ctx], [0])  # noqa: E731
+    write(v)
+    clean, clean_lse = m.cache_tree_attn(p, c, q, [0, n], [ctx], mask)
+    big = 3.3895313892515355e38 if dtype == "bf16" else 3.4028234663852886e38
+    if kv == "e4m3":
+        big = 448 * 2.0 ** 119
+    large = v.clone()
+    large[..., 0], large[..., 1] = big, -big
+    write(large)
+    got, lse = m.cache_tree_attn(p, c, q, [0, n], [ctx], mask)
+    assert torch.equal(lse, clean_lse)
+    # sums of up to 9000 weights in 32 bits, each rounded; 2^-8 for bf16 outputs and weights
+    tol = 2.0 ** -7 if dtype == "bf16" else 1e-4
+    near = lambda x, to: (x.double() / to - 1).abs() <= tol  # noqa: E731
+    up, down = near(got[..., 0], big), near(got[..., 1], -big)
+    if dtype == "fp32" and kv == "native":
+        # A mean of N values that are the largest float, N products and sums in 32 bits: off by up to (N + 3) 2^-24 of it, and what is above the largest float
+        # by half a step is infinity.  At 3e38, 12 % below it, there is room for that.
+        up, down = up | (got[..., 0] == float("inf")), down | (got[..., 1] == -float("inf"))
+        lower = large.clone()
+        lower[..., :2] *= 3.0e38 / big
+        write(lower)
+        less, _ = m.cache_tree_attn(p, c, q, [0, n], [ctx], mask)
+        assert bool(near(less[..., 0], 3.0e38).all()) and bool(near(less[..., 1], -3.0e38).all())
+    assert bool(up.all()) and bool(down.all())
+    if kv == "native":                      # (a page's scale serves all its channels)
+        assert torch.equal(got[..., 8:], clean[..., 8:])
