@@ -7,7 +7,7 @@
 //
 // Bound: launch and the chain parents, rounds (a barrier each), rows.  One tree of 26 tokens 2.7 us; 64 trees of 127 to 509 tokens, the deepest chain some 120: 7.0
 // (13.4 with all words of a tree in one workgroup, and 18.6 with a division for every word).
-#include "common.h"
+#include "cache.h"
 
 namespace ifv2 {
 
@@ -112,7 +112,7 @@ extern "C" int infllmv2_tree_masks(const int32_t *parents_d, const int32_t *cu_q
     const MaskArgs a{parents_d, cu_q_d, ctx_lens_d, mask_d, pos_d, mask_words};
     // (words behind those of the largest tree are written by workgroups of their own)
     const int64_t chunks = (mask_words + (int64_t)kWords - 1) / kWords;
-    if (chunks > 65535) return INFLLMV2_ERR_UNSUPPORTED;
+    if (chunks > 65535 || !cache::fits_launch(batch * chunks, kMost)) return INFLLMV2_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(tree_masks_kernel, dim3(batch, (unsigned)chunks), dim3((most + 63) / 64 * 64), 0, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());
 }

@@ -459,3 +459,14 @@ def test_large_values(m, kv, dtype, hq, hkv, d, n, ctx):  # noqa: F811
     assert bool(up.all()) and bool(down.all())
     if kv == "native":                      # (a page's scale serves all its channels)
         assert torch.equal(got[..., 8:], clean[..., 8:])
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", 32, 2, 128), ("fp32", 4, 1, 64), ("bf16", 8, 2, 64)])
+def test_masks_of_many_tokens(m, dtype, hq, hkv, d):  # noqa: F811
+    """More drafted tokens than infllmv2_tree_masks takes, by a mask of the caller's own that is wider than they need: a window of 300 tokens and every 97th."""
+    p = _params(m, dtype, hq, hkv, d)
+    news, ctxs = [1500, 3], [1711, 70]
+    c, _, _ = _filled(m, p, ctxs, "native", 64)
+    sets = [{j for j in range(i + 1) if i - j < 300 or j % 97 == 5} for i in range(1500)] + [{0}, {0, 1}, {2}]
+    mask = trees.to_words(sets, 50).cuda()
+    _check(m, p, c, _q(p, news, 16), news, ctxs, mask)

@@ -33,6 +33,7 @@ def test_mask_refusals(m):  # noqa: F811
                dict(ctx=()), dict(words=1), dict(words=-1), dict(words=0), dict(ctx=(39,)), dict(ctx=(2 ** 31 - 1,))):
         assert call(**kw) == INVALID, kw
     assert call(cu=(0, 1025), ctx=(2000,), words=33) == UNSUPPORTED
+    assert call(words=4 * 65536) == UNSUPPORTED
     assert call(cu=(0, 0), parents=None, mask=None) == 0 and call(cu=(0,), batch=0) == 0
 
 
