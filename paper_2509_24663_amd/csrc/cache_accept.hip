@@ -6,7 +6,8 @@
 // pages that are not written yet.  e4m3 pages: the scale grows to hold the rows that come in, as in an append; they are rounded to it, and so are the
 // page's other rows if it grew.
 //
-// Bound: latency: lengths, path, page numbers, rows, one after the other.
+// Bound: latency: lengths, path, page numbers, rows, one after the other.  16 trees of 26 tokens, up to 6 kept, e4m3: 4.1 us; 5 of 301, up to 99 kept, fp32, d 64: 7.6 (a
+// page's rows requested while the page before is written).
 #include "cache.h"
 
 namespace ifv2 {

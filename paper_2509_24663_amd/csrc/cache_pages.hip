@@ -6,7 +6,10 @@
 // sequences and blocks in order, so that what a call does depends on table and refs alone, not on the order in which its threads arrive.
 //
 // Bound: latency.  Entries are given back and shared by as many workgroups as they are worth (counts added with atomics, whose order does not matter);
-// handing out needs every free page's rank, which one workgroup works out, 8192 counts at a time, only as far as pages are wanted.  Copies: HBM.
+// handing out needs every free page's rank, which one workgroup works out, 8192 counts at a time, only as far as pages are wanted.  64 rows that give 3000 pages
+// back and get 3200 of a pool of 12288: 2.5 and 6.2 us.  32 forks of up to 47 blocks 9.4; 240 forks of 512 blocks of one row 3.5 (an atomic for each entry: 58)
+// and 4.0 for their last pages.  8192 pages, 6126 of them in use: 5.4 to find the 1529 that move, 5.4 to renumber 12288 entries.  Copies: HBM, those 1529
+// pages of 32 KB 17.5 us, 5.7 TB/s read and written.
 #include <algorithm>
 
 #include "cache.h"
@@ -19,7 +22,6 @@ typedef uint32_t Piece __attribute__((ext_vector_type(4)));      // 16 bytes of 
 
 constexpr int kMostRows = INFLLMV2_PAGES_MOST_ROWS;
 constexpr int kTakeThreads = 1024, kTakeWaves = kTakeThreads / 64, kDeep = 8;      // counts of a round: kTakeThreads * kDeep
-constexpr int kChunk = 1024;                                                        // table entries of a workgroup
 
 struct Pool {
     int32_t *table, *refs;
@@ -129,46 +131,24 @@ struct ResizeArgs {
     Pool g;
     const int32_t *old_lens, *new_lens;
     int rows;
-    int pitch_log2;                        // >= 0: entries are given back by the workgroup that hands out, 2^pitch_log2 >= those of any row
     int32_t *shortage;                     // or nullptr
 };
-
-__device__ inline void release(const Pool &g, int32_t *entry, int page) {
-    if (g.is_page(page)) atomicSub(&g.refs[page], 1);
-    *entry = -1;
-}
 
 __global__ void __launch_bounds__(256) pages_release_kernel(ResizeArgs a) {
     const int r = blockIdx.x, want = blocks_of(a.new_lens[r]), have = blocks_of(a.old_lens[r]);
     int32_t *row = a.g.row(r);
     if (r == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.shortage != nullptr) *a.shortage = 0;
-    for (int64_t j = (int64_t)want + blockIdx.y * 256 + threadIdx.x; j < have; j += 256 * gridDim.y) release(a.g, row + j, row[j]);
+    for (int64_t j = (int64_t)want + blockIdx.y * 256 + threadIdx.x; j < have; j += 256 * gridDim.y) {
+        const int page = row[j];
+        if (a.g.is_page(page)) atomicSub(&a.g.refs[page], 1);
+        row[j] = -1;
+    }
 }
 
 __global__ void __launch_bounds__(kTakeThreads) pages_take_kernel(ResizeArgs a) {
     __shared__ int s_before[kMostRows];
     __shared__ Ranks s_ranks;
     Counts c;
-    if (a.pitch_log2 >= 0) {
-        const int items = a.rows << a.pitch_log2;
-        for (int i0 = threadIdx.x; i0 < items; i0 += 4 * kTakeThreads) {
-            int32_t *entry[4];
-            int page[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = i0 + k * kTakeThreads, r = min(i >> a.pitch_log2, a.rows - 1), j = i & ((1 << a.pitch_log2) - 1);
-                const int want = blocks_of(a.new_lens[r]), have = blocks_of(a.old_lens[r]);
-                entry[k] = i < items && j < have - want ? a.g.row(r) + want + j : nullptr;
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) page[k] = entry[k] ? *entry[k] : -1;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (entry[k]) release(a.g, entry[k], page[k]);
-        }
-        __threadfence();                   // (the counts below are read as the atomics left them)
-        __syncthreads();
-    }
     c.load(a.g.refs, 0, a.g.num_pages);
     const int wanted = sums_before(a.rows, s_before, s_ranks, [&](int r) { return max(blocks_of(a.new_lens[r]) - blocks_of(a.old_lens[r]), 0); });
     hand_out(a.g, wanted, c, s_ranks, a.shortage, [&](int x, int page) {
@@ -389,7 +369,9 @@ int pitch_log2(int x) {                    // least power of two that is at leas
     while ((1ll << p) < x) ++p;
     return p;
 }
-// Entries, with those that a row does not have, up to which one workgroup gives back or shares them and hands out pages after it: one launch for two.
+// Blocks of forks, with those that a fork does not have, up to which one workgroup shares them and hands out pages after it, one launch for two: 4 forks of 500 tokens
+// and their copies 14.0 -> 11.2 us, 32 of 3000 14.8 -> 12.2, 64 of 4000 14.9 -> 14.4.  (Entries that are given back by the workgroup that hands out: 64 rows with
+// 3000 of them 8.7 -> 14.7 us of kernels, with 30 to 400 no gain.)
 constexpr int64_t kTogether = 4096;
 unsigned chunks(int64_t entries, int per) { return (unsigned)std::max<int64_t>(std::min<int64_t>((entries + per - 1) / per, 64), 1); }
 
@@ -415,10 +397,8 @@ extern "C" int infllmv2_pages_resize(const infllmv2_pages *g, const int32_t *old
     }
     if (batch > kMostRows || more > INT32_MAX) return INFLLMV2_ERR_UNSUPPORTED;
     if (less == 0 && more == 0 && short_d == nullptr) return INFLLMV2_OK;
-    const int pitch = pitch_log2(less);
-    const bool together = less > 0 && more > 0 && (int64_t)batch << pitch <= kTogether;
-    const ResizeArgs a{pool_of(g), old_lens_d, new_lens_d, batch, together ? pitch : -1, short_d};
-    if (less > 0 && !together) hipLaunchKernelGGL(pages_release_kernel, dim3(batch, chunks(less, 256)), dim3(256), 0, (hipStream_t)stream, a);
+    const ResizeArgs a{pool_of(g), old_lens_d, new_lens_d, batch, short_d};
+    if (less > 0) hipLaunchKernelGGL(pages_release_kernel, dim3(batch, chunks(less, 256)), dim3(256), 0, (hipStream_t)stream, a);
     if (more > 0 || less == 0) hipLaunchKernelGGL(pages_take_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());
 }
