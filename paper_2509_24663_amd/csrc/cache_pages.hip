@@ -7,8 +7,8 @@
 //
 // Bound: latency.  Entries are given back and shared by as many workgroups as they are worth (counts added with atomics, whose order does not matter);
 // handing out needs every free page's rank, which one workgroup works out, 8192 counts at a time, only as far as pages are wanted.  64 rows that give 3000 pages
-// back and get 3200 of a pool of 12288: 2.5 and 6.2 us.  32 forks of up to 47 blocks 9.4; 240 forks of 512 blocks of one row 3.5 (an atomic for each entry: 58)
-// and 4.0 for their last pages.  8192 pages, 6126 of them in use: 5.4 to find the 1529 that move, 5.4 to renumber 12288 entries.  Copies: HBM, those 1529
+// back and get 3200 of a pool of 12288: 2.5 and 6.2 us.  32 forks of up to 47 blocks 9.4; 240 forks of 512 blocks of one row 3.5 where they had its pages before (with
+// an add and a subtract for each entry: 58; where they had others a call takes 10.9 for 8.2) and 4.0 for their last pages.  8192 pages, 6126 of them in use: 5.4 to find the 1529 that move, 5.4 to renumber 12288 entries.  Copies: HBM, those 1529
 // pages of 32 KB 17.5 us, 5.7 TB/s read and written.
 #include <algorithm>
 
@@ -428,7 +428,8 @@ extern "C" int infllmv2_pages_fork(const infllmv2_pages *g, const infllmv2_fork 
     if (most == 0 && copies_d == nullptr && short_d == nullptr) return INFLLMV2_OK;
     const int pitch = pitch_log2(most);
     const bool together = most > 0 && (int64_t)count << pitch <= kTogether;
-    // (forks of a workgroup: more add up more of their counts, as long as there is one for each CU)
+    // Forks of a workgroup: more add up more of their counts, as long as there is a workgroup for each CU.  A call, us, all pages others than before, by 1 / 2 / 4 / 8 / 16 forks:
+    // 240 of 512 blocks 10.9 / 9.2 / 9.7 / 11.6 / 18.3 (1 here), 1000 of 100 14.8 / 11.2 / 10.6 / 12.2 / 17.7 (3), 3000 of 64 65 / 37 / 25 / 21 / 23 (11).
     const int per = (int)std::max<int64_t>(std::min<int64_t>((int64_t)count * chunks(most, 256) / 256, 16), 1);
     const ForkArgs a{pool_of(g), forks_d, count, together ? pitch : -1, per, copies_d, short_d};
     if (most > 0 && !together) hipLaunchKernelGGL(pages_share_kernel, dim3((count + per - 1) / per, chunks(most, 256)), dim3(256), 0, (hipStream_t)stream, a);
