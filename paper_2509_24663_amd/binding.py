@@ -726,17 +726,17 @@ class Forks:
         self.count = self.h.shape[0]
 
 
-def _shortage(pool: PagePool, short: Optional[torch.Tensor]):
+def _shortage(pool: PagePool, short: Optional[torch.Tensor], calls: int):
     short = pool.refs.new_empty((1,)) if short is None else short
     assert short.dtype is torch.int32 and short.numel() == 1
-    return short
+    return short if calls else short.zero_()         # (the library writes nothing where there is nothing to do)
 
 
 def pages_resize(pool: PagePool, old_lens, new_lens, short: Optional[torch.Tensor] = None):
     """Sequence b had room for old_lens[b] tokens and gets room for new_lens[b] (0: none).  Returns how many pages were wanting (device int32 [1])."""
     old, new = _decode_info(old_lens), _decode_info(new_lens)
     assert old.batch == new.batch
-    short = _shortage(pool, short)
+    short = _shortage(pool, short, old.batch)
     st = lib().infllmv2_pages_resize(pool.ref, old.ctx_h.data_ptr(), old.ctx_d.data_ptr(), new.ctx_h.data_ptr(), new.ctx_d.data_ptr(), old.batch,
                                      short.data_ptr(), _stream())
     _check(st, "infllmv2_pages_resize")
@@ -748,7 +748,7 @@ def pages_fork(pool: PagePool, forks: Forks, copies: Optional[torch.Tensor] = No
     if copies is None:
         copies = pool.refs.new_empty((forks.count, 2))
     assert copies.dtype is torch.int32 and copies.is_contiguous() and copies.shape == (forks.count, 2)
-    short = _shortage(pool, short)
+    short = _shortage(pool, short, forks.count)
     st = lib().infllmv2_pages_fork(pool.ref, forks.h.data_ptr(), forks.d.data_ptr(), forks.count, copies.data_ptr(), short.data_ptr(), _stream())
     _check(st, "infllmv2_pages_fork")
     return copies, short

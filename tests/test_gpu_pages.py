@@ -89,6 +89,18 @@ def test_fork(m, pages, rows, blocks):  # noqa: F811
     assert _same_pool(pool, want)
 
 
+def test_nothing_to_do(m):  # noqa: F811
+    """No sequences, no forks, lengths that stay, prefixes of no tokens: nothing changes, nothing is wanting."""
+    pool = _pool(m, [1, 0, 1], [[0, 2], [-1, -1]])
+    assert int(m.pages_resize(pool, [], [])) == 0 and int(m.pages_resize(pool, [100, 0], [128, 0])) == 0
+    copies, short = m.pages_fork(pool, m.Forks([], [], [], []))
+    assert copies.shape == (0, 2) and int(short) == 0
+    copies, short = m.pages_fork(pool, m.Forks([0], [1], [0]))
+    assert copies.tolist() == [[-1, -1]] and int(short) == 0
+    moves, live = m.pages_compact(pool, [128, 0])
+    assert pool.refs.tolist() == [1, 1, 0] and pool.page_table.tolist() == [[0, 1], [-1, -1]] and moves.tolist() == [[2, 1]] and live.tolist() == [2, 1]
+
+
 @pytest.mark.parametrize("apart", [False, True])
 @pytest.mark.parametrize("pages,rows,blocks", [(1, 1, 1), (2, 1, 2), (9, 3, 4), (1000, 30, 40), (50000, 40, 1500)])
 def test_compact(m, pages, rows, blocks, apart):  # noqa: F811
