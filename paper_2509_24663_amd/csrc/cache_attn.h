@@ -41,6 +41,12 @@ __device__ inline uint32_t pack(float a, float b) {          // nearest even
     const bf16x2 x = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, x);
 }
+// all ones in the elements of w (e4m3 codes, bf16) that are infinities or NaN
+template <bool CODES>
+__device__ inline uint32_t not_finite(uint32_t w) {
+    if (CODES) return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+    return ((((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
+}
 // Two weights as two bf16 pieces each, the upper 16 bits and the rest rounded to nearest: off by at most 2^-16 of the weight, either way.  The first piece is
 // that of the next smaller float: below the weight, also where 16 bits hold it, so that the second is above 0 and both products with an infinite value are
 // that infinity (0 x infinity is not a number).
@@ -98,6 +104,7 @@ struct TreeArgs : AttnArgs {
     static constexpr bool kTree = true;
     const uint32_t *mask;              // [total][words]
     int words;
+    int even_n, even_tiles;            // even > 0: as many drafted tokens for each sequence, so many tiles
     __host__ __device__ __attribute__((always_inline)) int tile_tokens(int) const { return group_tokens * tile_groups; }
     __host__ __device__ __attribute__((always_inline)) int tiles(int n, int) const {
         if ((tile_groups > 1) != (n >= wide_from)) return 0;
@@ -130,6 +137,21 @@ struct TreeArgs : AttnArgs {
     __device__ __attribute__((always_inline)) uint64_t seen_step(const uint32_t *row, int key, int front, int n, bool open) const {
         if constexpr (N <= 32) return seen<N>(row, key, front, n, open);
         else return seen<32>(row, key, front, n, open) | (uint64_t)seen<N - 32>(row, key + 32, front, n, open) << 32;
+    }
+    // Trees of up to 64 tokens: a row of the mask is requested with the query and kept (at the edge it would be one more trip to memory, in tiles behind the
+    // pages that are on their way)
+    __device__ __attribute__((always_inline)) uint64_t kept_row(const uint32_t *row, int n) const {
+        if (n > 64) return 0;
+        const uint64_t x = row[0] | (n > 32 ? (uint64_t)row[1] << 32 : 0u);
+        return n == 64 ? x : x & ((1ull << n) - 1);
+    }
+    template <int N>
+    __device__ __attribute__((always_inline)) uint64_t seen_kept(uint64_t kept, const uint32_t *row, int key, int front, int n, bool open) const {
+        if (n > 64) return seen_step<N>(row, key, front, n, open);
+        const int d = key - front;
+        const uint64_t x = d >= 64 || d <= -64 ? 0 : d >= 0 ? kept >> d : kept << -d;
+        const uint64_t before = d >= 0 ? 0 : d <= -64 ? ~0ull : (1ull << -d) - 1;
+        return (x | (open ? before : 0)) & (N == 64 ? ~0ull : (1ull << (N & 63)) - 1);          // (x has nothing in front of the drafted rows)
     }
 };
 

@@ -109,6 +109,20 @@ struct ValueRow {
 #pragma unroll
         for (int i = 0; i < W; ++i) raw[i] = keep ? raw[i] : 0u;
     }
+    __device__ inline bool clear_odd() {                     // infinities and NaN become 0: whether there were any
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const uint32_t w = raw[i];
+            uint32_t o;
+            if constexpr (CODES) o = cache_attn::not_finite<true>(w);
+            else if constexpr (sizeof(T) == 2) o = cache_attn::not_finite<false>(w);
+            else o = (w & 0x7fffffffu) >= 0x7f800000u ? ~0u : 0u;
+            raw[i] = w & ~o;
+            any |= o;
+        }
+        return any != 0u;
+    }
     __device__ inline bool odd() const {                     // holds an infinity or a NaN
         bool any = false;
 #pragma unroll
@@ -225,6 +239,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
     __shared__ int s_item[6];
     __shared__ float s_m[NW][16], s_l[NW][16];
+    __shared__ int s_odd[A::kTree ? NW : 1];
     __shared__ __attribute__((aligned(16))) float s_o[NW][16][D + 4];          // (rows four banks apart)
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv;
@@ -232,7 +247,16 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     // the item: sequence, tile, KV head, split; slot: where a partial result goes
     int seq, rem, row0, n, len, early = -1;
     int64_t slot = blockIdx.x;
-    if (a.even) {
+    if (A::kTree && a.even) {
+        if constexpr (A::kTree) {
+            const unsigned each = (unsigned)(hkv * a.even_tiles * a.even);
+            seq = (int)(blockIdx.x / each);
+            rem = (int)(blockIdx.x - (unsigned)seq * each);
+            n = a.even_n;
+            row0 = seq * n;
+            len = a.ctx[seq];
+        }
+    } else if (a.even) {
         seq = (int)(blockIdx.x / (unsigned)(hkv * a.even));
         rem = (int)(blockIdx.x - (unsigned)seq * (unsigned)(hkv * a.even));
         row0 = seq;
@@ -267,7 +291,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     // (a tree: the first key that not every token sees, the last that one may see)
     const int pos0 = A::kTree ? len - n : len - n + first, pos_last = A::kTree ? len - 1 : pos0 + ntok - 1;
     int nsplit;
-    if constexpr (A::kTree) nsplit = per;
+    if constexpr (A::kTree) nsplit = a.most_splits(n, len);
     else nsplit = a.splits(len, pos_last);
     if (split >= nsplit) return;
     // the entries of this wavefront: of all pages a run for each split; of a list (which may be longer than the pages there can be, and hold them
@@ -295,11 +319,14 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     int low = INT32_MAX;                         // first key of any page that this wavefront went through
 
     const int32_t *list = a.idx + ((int64_t)(A::kTree ? seq : row0 + first) * hkv + h) * a.topk;
-    // a tree: whether the context's rows in the block of the first drafted one are listed; this column's row of the mask; whether it saw a key
-    bool open = true, any_key = false;
+    // a tree: whether the context's rows in the block of the first drafted one are listed; this column's row of the mask; whether it saw a key; whether a value of
+    // a page of drafted rows is not finite
+    bool open = true, any_key = false, odd_edge = false;
     const uint32_t *mask_row = nullptr;
+    uint64_t kept = 0;
     if constexpr (A::kTree) {
         mask_row = a.mask + row * a.words;
+        kept = a.kept_row(mask_row, n);
         if (listed && pos0 % kBlock != 0) {
             open = false;
             for (int e0 = 0; e0 < a.topk && !open; e0 += 64) open = __any(e0 + lane < a.topk && list[min(e0 + lane, a.topk - 1)] == pos0 / kBlock);
@@ -383,7 +410,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
                     if (edge) {
                         uint64_t bits = 0;
                         if constexpr (A::kTree) {
-                            bits = used ? a.template seen_step<STEP>(mask_row, key0, pos0, n, !shut) >> (4 * g) : 0u;
+                            bits = used ? a.template seen_kept<STEP>(kept, mask_row, key0, pos0, n, !shut) >> (4 * g) : 0u;
                             any_key |= (bits & 0x000f000f000f000full) != 0;
                         }
 #pragma unroll
@@ -429,26 +456,12 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
                             for (int r = 0; r < 4; ++r) {
                                 const int key = key0 + 16 * t + 4 * g + r;
                                 v[4 * t + r].clear_unless(key <= pos_last && (!shut || key >= pos0));
-                                if (MULTI || A::kTree) odd |= v[4 * t + r].odd();
+                                if (A::kTree) odd_edge |= v[4 * t + r].clear_odd();      // (0 x infinity; those that see them get them behind the sums)
+                                else if (MULTI) odd |= v[4 * t + r].odd();
                             }
-                        if ((MULTI || A::kTree) && __any(odd)) rounds = A::kTree ? ntok + 1 : ntok;
+                        if (!A::kTree && MULTI && __any(odd)) rounds = ntok;
                     }
-                    if constexpr (A::kTree) {
-                        // 0 x infinity: where rows are not finite, the sums of each token from the rows that it sees, which are no other's: requested again for each
-                        const bool apart = rounds > 1;
-#pragma unroll 1
-                        for (int i = apart ? ntok - 1 : 0; i >= 0; --i) {
-                            if (apart) {
-                                const uint64_t bits = a.template seen_step<STEP>(a.mask + (int64_t)(row0 + first + i) * a.words, key0, pos0, n, !shut) >> (4 * g);
-                                load_v(vb);
-#pragma unroll
-                                for (int t = 0; t < TILES; ++t)
-#pragma unroll
-                                    for (int r = 0; r < 4; ++r) v[4 * t + r].clear_unless((bits >> (16 * t + r) & 1u) != 0u);
-                            }
-                            add_values<true, D, TILES, CODES>(acc, wt, v, vs, !apart || ti == i);
-                        }
-                    } else if constexpr (!MULTI) {
+                    if constexpr (A::kTree || !MULTI) {
                         add_values<false, D, TILES, CODES>(acc, wt, v, vs, true);
                     } else {
                         // 0 x infinity: where rows are not finite, the sums of each token from the rows that it sees, latest token first
@@ -504,6 +517,8 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     if constexpr (A::kTree) some_key = (__ballot(any_key) >> m & 0x0001000100010001ull) != 0;
     if (ref == -INFINITY && some_key) ref = kLowest;         // only logits of minus infinity (0 / 0 below), not no key at all
     if (lane < 16) s_m[w][m] = ref, s_l[w][m] = sum;
+    if (A::kTree && lane == 0) s_odd[w] = 0;
+    if (A::kTree && odd_edge) s_odd[w] = 1;                  // (behind that write: one wavefront's)
     __syncthreads();
     const bool direct = nsplit == 1;
     float top = s_m[0][m];
@@ -558,6 +573,37 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
             a.ml[(slot * 16 + m) * 2 + 1] = total;
         }
     }
+    if constexpr (A::kTree) {
+        int any = 0;
+#pragma unroll
+        for (int x = 0; x < NW; ++x) any |= s_odd[x];
+        if (any == 0 || ci >= ntok) return;
+        // Values that are not finite were taken as 0 in the pages of drafted rows: the tokens that see them get them now (this thread's channels of its column).
+        const uint32_t *token_row = a.mask + (int64_t)(row0 + first + ci) * a.words;
+        T *dst = reinterpret_cast<T *>(a.out) + (((int64_t)row0 + first + ci) * a.hq + h * G + col - ci * G) * D + ch;
+        float *part = a.part + (slot * 16 + col) * D + ch;
+        for (int j = pos0 / kBlock; j <= pos_last / kBlock; ++j) {
+            const int e = tree_e + j - pos0 / kBlock;
+            if (listed ? e % (NW * nsplit) / NW != split : e < split * a.pps || e >= e_end) continue;      // (another split's)
+            const int page = a.c.page(seq, j);
+            if (page < 0) continue;
+            const bool shut = !open && j == pos0 / kBlock;
+            const char *rows = a.c.v + a.c.at(page, h);
+            for (int u = 0; u < kBlock && j * kBlock + u <= pos_last; ++u) {
+                if (a.template seen<1>(token_row, j * kBlock + u, pos0, n, !shut) == 0u) continue;
+                const char *at = rows + (int64_t)u * tok + ch * (CODES ? 1 : (int)sizeof(T));
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    float y;
+                    if constexpr (CODES) y = ((uint8_t)at[i] & 0x7f) == 0x7f ? NAN : 0.f;
+                    else y = Elem<T>::load(reinterpret_cast<const T *>(at) + i);
+                    if (finite(y)) continue;
+                    if (direct) Elem<T>::store(dst + i, Elem<T>::load(dst + i) + y);
+                    else part[i] += y;
+                }
+            }
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------ joining the splits of a tile
@@ -576,7 +622,16 @@ __global__ void __launch_bounds__(D / 4 * COLS * SG) cache_merge_kernel(A a) {
     const int tid = threadIdx.x % kThreads, sg = threadIdx.x / kThreads, hkv = a.c.hkv, G = a.hq / hkv;
     int th, seq, row0, n, len;
     int64_t slot;
-    if (a.even) {
+    if (A::kTree && a.even) {
+        if constexpr (A::kTree) {
+            seq = (int)(blockIdx.x / (unsigned)(hkv * a.even_tiles));
+            th = (int)(blockIdx.x - (unsigned)seq * (unsigned)(hkv * a.even_tiles));
+            slot = (int64_t)blockIdx.x * a.even;
+            n = a.even_n;
+            row0 = seq * n;
+            len = a.ctx[seq];
+        }
+    } else if (a.even) {
         seq = (int)(blockIdx.x / (unsigned)hkv);
         th = (int)(blockIdx.x - (unsigned)seq * (unsigned)hkv);
         slot = (int64_t)blockIdx.x * a.even;
@@ -846,6 +901,23 @@ int attend(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, c
         mine.items = alike;
         mine.merges = mine.most > 1 ? (int64_t)batch * hkv : 0;
         mine.slots = mine.most > 1 ? mine.items : 0;
+    }
+    if constexpr (A::kTree) {                  // trees of one size: the same, in either kernel
+        bool alike_n = true;
+        for (int b = 1; b < batch; ++b) alike_n = alike_n && cu_q_h[b + 1] - cu_q_h[b] == cu_q_h[1];
+        const auto look_up_nothing = [&](A &x, Launches &l, int64_t most_slots) {
+            const int tiles = batch > 0 ? x.tiles(cu_q_h[1], 0) : 0;
+            const int64_t same = (int64_t)batch * hkv * tiles * l.most;
+            if (!alike_n || tiles == 0 || same > most_slots || (same > 256 && 10 * same > 11 * l.items)) return;
+            x.even = l.most;
+            x.even_n = cu_q_h[1];
+            x.even_tiles = tiles;
+            l.items = same;
+            l.merges = l.most > 1 ? (int64_t)batch * hkv * tiles : 0;
+            l.slots = l.most > 1 ? same : 0;
+        };
+        look_up_nothing(a, mine, 2 * kMostGroups);
+        look_up_nothing(wide, other, rules::kMostTileGroups / wide.tile_groups);
     }
     const size_t need = unit_bytes(p, mine.slots), wide_need = tile_bytes(p, other.slots, wide.tile_groups);
     st = check_ws(workspace_d, workspace_bytes, need + wide_need);

@@ -44,6 +44,7 @@ using cache_attn::TreeArgs;
 using cache_attn::kLift;
 using cache_attn::kLn2;
 using cache_attn::kLowest;
+using cache_attn::not_finite;
 using cache_attn::pack;
 using cache_attn::rows_add;
 using cache_attn::rows_max;
@@ -56,12 +57,6 @@ constexpr float kSlack = 64.f;
 constexpr float kTopBf16 = 3.3895314e38f;  // largest bf16 number
 constexpr int kAhead = 4;                  // operands requested in front of their product
 
-// all ones in the elements of w that are infinities or NaN
-template <bool CODES>
-__device__ inline uint32_t not_finite(uint32_t w) {
-    if (CODES) return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
-    return ((((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu;
-}
 __device__ inline void lds_write16(uint32_t at, u32x4 x) {
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
     *(lds_u32x4 *)(uintptr_t)at = x;
@@ -93,29 +88,45 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, hkv = a.c.hkv, G = a.hq / hkv, GT = a.group_tokens;
 
-    int rem;
-    int slot0;
-    cache::Facts facts;
-    const int seq = cache::find_item(a.batch, (int)blockIdx.x, rem, slot0, facts, s_item,
-        [&](int s) {
-            const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
-            return a.tiles(n, len) * hkv * a.most_splits(n, len);
-        },
-        [&](int s) {
-            const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
-            return sp > 1 ? a.tiles(n, len) * hkv * sp : 0;
-        },
-        [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
-    if (seq >= a.batch) return;
-    const int row0 = facts.x[0], n = facts.x[1] - row0, len = facts.x[2];
-    const int per = a.most_splits(n, len), ntiles = a.tiles(n, len);
+    int rem, seq, row0, n, len;
+    int64_t slot0;
+    if (A::kTree && a.even) {
+        if constexpr (A::kTree) {
+            const unsigned each = (unsigned)(hkv * a.even_tiles * a.even);
+            seq = (int)(blockIdx.x / each);
+            rem = (int)(blockIdx.x - (unsigned)seq * each);
+            slot0 = (int64_t)seq * each;
+            n = a.even_n;
+            row0 = seq * n;
+            len = a.ctx[seq];
+        }
+    } else {
+        int before;
+        cache::Facts facts;
+        seq = cache::find_item(a.batch, (int)blockIdx.x, rem, before, facts, s_item,
+            [&](int s) {
+                const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s];
+                return a.tiles(n, len) * hkv * a.most_splits(n, len);
+            },
+            [&](int s) {
+                const int n = a.cu[s + 1] - a.cu[s], len = a.ctx[s], sp = a.most_splits(n, len);
+                return sp > 1 ? a.tiles(n, len) * hkv * sp : 0;
+            },
+            [&](int s, int i) { return i < 2 ? a.cu[s + i] : a.ctx[s]; });
+        if (seq >= a.batch) return;
+        slot0 = before;
+        row0 = facts.x[0];
+        n = facts.x[1] - row0;
+        len = facts.x[2];
+    }
+    const int per = A::kTree && a.even ? a.even : a.most_splits(n, len), ntiles = a.tiles(n, len);
     const int split = rem % per, th = rem / per, h = th % hkv, tile = ntiles - 1 - th / hkv;          // (longest first)
     const int64_t slot = slot0 + (int64_t)(tile * hkv + h) * per + split;
     const int T0 = GT * NW * CG, first = tile * T0, ntok = min(T0, n - first);
     // (a tree: the first key that not every token sees, the last that one may see)
     const int pos0 = A::kTree ? len - n : len - n + first, pos_last = A::kTree ? len - 1 : pos0 + ntok - 1;
     int nsplit;
-    if constexpr (A::kTree) nsplit = per;
+    if constexpr (A::kTree) nsplit = a.most_splits(n, len);
     else nsplit = a.splits(len, pos_last);
     if (split >= nsplit) return;
     // a tree: entries in front of those of drafted rows (a list, or all blocks); whether the context's rows in the block of the first drafted one are listed
@@ -162,12 +173,14 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
     int ti[CG];
     bool used[CG];
     bf16x8 qf[CG][KS];
+    uint64_t kept[CG];                                              // a tree: the column's row of the mask (TreeArgs::kept_row)
 #pragma unroll
     for (int x = 0; x < CG; ++x) {
         ti[x] = (w * CG + x) * GT + m / G;
         used[x] = m / G < GT && ti[x] < ntok;
         const int64_t row = row0 + first + (used[x] ? ti[x] : 0);
         const int qh = h * G + (used[x] ? m % G : 0);
+        if constexpr (A::kTree) kept[x] = a.kept_row(a.mask + row * a.words, n);
         const uint16_t *q = reinterpret_cast<const uint16_t *>(a.q) + (row * a.hq + qh) * D;
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8_u *>(q + 32 * s + 8 * g));
@@ -359,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 && CG == 1 ? 4 : 2) cache_at
             for (int x = 0; x < CG; ++x) {
                 if constexpr (A::kTree) {
                     const uint32_t *row = a.mask + (int64_t)(row0 + first + (used[x] ? ti[x] : 0)) * a.words;
-                    const uint32_t bits = used[x] ? a.template seen<8>(row, first_key + 8 * g, pos0, n, !shut(first_key)) : 0u;
+                    const uint32_t bits = used[x] ? (uint32_t)a.template seen_kept<8>(kept[x], row, first_key + 8 * g, pos0, n, !shut(first_key)) : 0u;
                     saw |= bits != 0u ? 1u << x : 0u;
 #pragma unroll
                     for (int kt = 0; kt < 2; ++kt)

@@ -214,6 +214,37 @@ def test_rows_that_are_not_finite(m, kv, dtype, hq, hkv, d, n, ctx):  # noqa: F8
     assert torch.equal(got[~sees], clean[~sees])
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,d,n,ctx", [("bf16", 32, 2, 128, 3, 300), ("bf16", 32, 2, 128, 2, 9001), ("bf16", 8, 2, 64, 6, 9001), ("fp32", 4, 1, 64, 9, 9001), ("fp32", 6, 2, 128, 70, 330),
+                                                  ("bf16", 32, 2, 128, 40, 9001), ("bf16", 8, 2, 64, 70, 3001), ("bf16", 12, 4, 128, 8, 30001)])
+@pytest.mark.parametrize("kv", ["e4m3", "native"])
+def test_rows_beside_the_tree_that_are_not_finite(m, kv, dtype, hq, hkv, d, n, ctx):  # noqa: F811
+    """An infinite (e4m3: NaN) value in a row of the context, in the block that drafted rows begin in, of a drafted row, and behind the sequence: each token gets those
+    that it sees, in calls of one and of several splits, with the block listed and not."""
+    p = _params(m, dtype, hq, hkv, d, topk_total=70, dense_threshold=0)
+    c, _, _ = _filled(m, p, [ctx], kv, 65)
+    q, mask = _q(p, [n], 17), _masks(m, [n], [ctx], 18)
+    front = (ctx - n) // PAGE
+    assert (ctx - n) % PAGE > 0 and ctx % PAGE > 0
+    clean = {}
+    blocks = {"all": None, "listed": [front, 0, 1], "not listed": [0, 1]}
+    give = lambda x: None if x is None else torch.tensor([[x + [-1] * (70 - len(x))] * hkv], dtype=torch.int32, device="cuda")  # noqa: E731
+    for name, x in blocks.items():
+        clean[name] = m.cache_tree_attn(p, c, q, [0, n], [ctx], mask, give(x))[0]
+    raw = c.v.view(torch.uint8) if kv == "e4m3" else c.v
+    bad = 0x7f if kv == "e4m3" else float("inf")
+    sees = torch.tensor([n - 1 in s for s in trees.to_sets(mask.cpu(), n)], device="cuda")
+    rows = [(ctx - n - 1, 5, None), (ctx - 1, 6, sees)] + [(t, 7, torch.zeros(n, dtype=torch.bool, device="cuda")) for t in range(ctx, front * PAGE + PAGE)]
+    for t, ch, _ in rows:
+        raw[int(c.page_table[0, t // PAGE]), :, t % PAGE, ch] = bad
+    for name, x in blocks.items():
+        got = m.cache_tree_attn(p, c, q, [0, n], [ctx], mask, give(x))[0]
+        want = clean[name].clone()
+        for t, ch, who in rows:
+            who = torch.full((n,), name != "not listed", device="cuda") if who is None else who
+            want[who, :, ch] = float("nan") if kv == "e4m3" else bad
+        assert bool(((got == want) | (got.isnan() & want.isnan())).all()), name
+
+
 def test_context_rows_that_are_not_listed(m):  # noqa: F811
     """The block that drafted rows begin in, not listed: its context rows are as if they were not there, whatever they hold."""
     for n, ctx, hq, hkv, d in ((5, 300, 32, 2, 128), (40, 2020, 32, 2, 128), (40, 2020, 8, 2, 64)):

@@ -73,7 +73,11 @@ def test_scratch_that_was_asked_for_is_enough(m):  # noqa: F811
         p = m.Params.make(dtype, hq, hkv, d, topk_total=rng.choice([4, 64, 1024]), n_init=1, n_local=1, dense_threshold=rng.choice([0, 4000, 1 << 30]))
         batch, far = rng.choice([1, 2, 7, 64, 700]), rng.choice([100, 5000, 200000, 100000000])
         news = [rng.choice([0, 1, 3, 8, 9, 26, 64, 300]) for _ in range(batch)]
+        if i % 2:                                        # trees of one size
+            news = [rng.choice([1, 5, 8, 9, 26, 64, 300])] * batch
         ctx = [max(n, int(far ** rng.random())) for n in news]
+        if i % 4 == 1:
+            ctx = [max(ctx)] * batch
         cu = np.concatenate([[0], np.cumsum(news)]).tolist()
         if cu[-1] == 0:
             continue
