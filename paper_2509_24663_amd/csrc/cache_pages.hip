@@ -94,9 +94,13 @@ __device__ inline int sums_before(int rows, int *s_before, Ranks &s, Count count
         if (lane == 63) s.cell[w] = incl;
         __syncthreads();
         int front = before;
-        for (int i = 0; i < w; ++i) front += s.cell[i];
+#pragma unroll
+        for (int i = 0; i < kTakeWaves; ++i) {
+            const int y = s.cell[i];
+            front += i < w ? y : 0;
+            before += y;
+        }
         if (r < rows) s_before[r] = front + incl - x;
-        for (int i = 0; i < kTakeWaves; ++i) before += s.cell[i];
         __syncthreads();
     }
     return before;
@@ -146,14 +150,18 @@ __global__ void __launch_bounds__(256) pages_release_kernel(ResizeArgs a) {
 }
 
 __global__ void __launch_bounds__(kTakeThreads) pages_take_kernel(ResizeArgs a) {
-    __shared__ int s_before[kMostRows];
+    __shared__ int s_before[kMostRows], s_have[kMostRows];
     __shared__ Ranks s_ranks;
     Counts c;
     c.load(a.g.refs, 0, a.g.num_pages);
-    const int wanted = sums_before(a.rows, s_before, s_ranks, [&](int r) { return max(blocks_of(a.new_lens[r]) - blocks_of(a.old_lens[r]), 0); });
+    const int wanted = sums_before(a.rows, s_before, s_ranks, [&](int r) {
+        const int have = blocks_of(a.old_lens[r]);
+        s_have[r] = have;
+        return max(blocks_of(a.new_lens[r]) - have, 0);
+    });
     hand_out(a.g, wanted, c, s_ranks, a.shortage, [&](int x, int page) {
         const int r = row_of(a.rows, s_before, x);
-        a.g.row(r)[blocks_of(a.old_lens[r]) + (x - s_before[r])] = page;
+        a.g.row(r)[s_have[r] + (x - s_before[r])] = page;
     });
 }
 
