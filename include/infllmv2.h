@@ -485,7 +485,7 @@ int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cache *c, const
  *   mask_d        device out uint32 [total, mask_words], 32 mask_words >= the largest n: bit j % 32 of word j / 32 of a token's row: token j is it or an
  *                 ancestor of it
  *   pos_d         device out int32 [total] or NULL: the token's position, ctx_lens[b] - n + its ancestors (ctx_lens may be NULL where pos_d is)
- * Trees of more than INFLLMV2_TREE_MOST tokens are UNSUPPORTED.
+ * Trees of more than INFLLMV2_TREE_MOST tokens are UNSUPPORTED.  The outputs are in no memory of the inputs (pos_d: checked).
  */
 #define INFLLMV2_TREE_MOST 1024
 int infllmv2_tree_masks(const int32_t *parents_d, const int32_t *cu_q_h, const int32_t *cu_q_d, const int32_t *ctx_lens_h,
@@ -510,7 +510,8 @@ int infllmv2_cache_tree_attn(const infllmv2_params *p, const infllmv2_cache *c, 
  * Keeps a path of each sequence's tree: drafted row path[i] becomes drafted row i, keys and values of every head.
  *   path_d        device int32 [batch, path_stride]: numbers of drafted tokens, rising; the path ends in front of the first entry that is outside 0 .. n - 1
  *                 or not above the one before it (-1 behind the last), or after path_stride entries
- *   new_lens_d    device out int32 [batch] or NULL: ctx_lens[b] - n + the path's length
+ *   new_lens_d    device out int32 [batch] or NULL: ctx_lens[b] - n + the path's length; apart from the inputs, ctx_lens_d too (written also where no
+ *                 sequence has drafted tokens)
  * Rows of the context and drafted rows that no row of the path moves to keep their values.  e4m3: a page that rows move to keeps its scale or gets the larger one
  * that they need, and its other rows are then rounded again, as in infllmv2_cache_append.  A row moves only if its page and the page it moves to are there.
  * Pages that rows move to must be in no other sequence's table.
@@ -540,7 +541,8 @@ typedef struct infllmv2_pages {
 /*
  * Sequence b (row b of the table) had room for old_lens[b] tokens and gets room for new_lens[b]: blocks ceil(old / 64) .. ceil(new / 64) - 1 get pages, blocks
  * ceil(new / 64) .. ceil(old / 64) - 1 lose theirs (entries become -1; pages that no other entry names are free, to sequences of the same call as well).  A
- * new length of 0 frees a sequence.
+ * new length of 0 frees a sequence.  (A sequence that is cut back into a page that others name as well must not write there: infllmv2_pages_fork continues it in
+ * another row, with a page of its own.)
  *   old_lens_h/d, new_lens_h/d   host / device int32 [batch], at most 64 * blocks
  */
 int infllmv2_pages_resize(const infllmv2_pages *g, const int32_t *old_lens_h, const int32_t *old_lens_d, const int32_t *new_lens_h,

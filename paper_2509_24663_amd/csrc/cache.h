@@ -22,6 +22,11 @@ struct Args {
 int check(const infllmv2_params *p, const infllmv2_cache *c, int max_ctx, bool values);
 // a launch's threads are counted in 32 bits
 inline bool fits_launch(int64_t workgroups, int threads) { return workgroups < (1ll << 32) / threads; }
+// whether two arrays of 32-bit numbers have memory in common
+inline bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
+    const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+    return p < q + 4 * (uintptr_t)nb && q < p + 4 * (uintptr_t)na;
+}
 Args args(const infllmv2_params *p, const infllmv2_cache *c);
 
 constexpr float kTop = 448.f;                          // largest e4m3 magnitude

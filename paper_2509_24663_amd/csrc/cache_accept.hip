@@ -158,13 +158,17 @@ extern "C" int infllmv2_cache_accept(const infllmv2_params *p, const infllmv2_ca
     int32_t max_new;
     st = check_cu(cu_q_h, cu_q_d, batch, &total, &max_new);
     if (st) return st;
-    if (batch == 0) return INFLLMV2_OK;
+    if (batch == 0 || (total == 0 && new_lens_d == nullptr)) return INFLLMV2_OK;
     if (ctx_lens_h == nullptr || ctx_lens_d == nullptr || path_d == nullptr || path_stride < 1) return INFLLMV2_ERR_INVALID_ARGUMENT;
     int max_ctx = 0;
     for (int b = 0; b < batch; ++b) {
         if (ctx_lens_h[b] < cu_q_h[b + 1] - cu_q_h[b] || ctx_lens_h[b] > INT32_MAX - kBlock) return INFLLMV2_ERR_INVALID_ARGUMENT;
         if (cu_q_h[b + 1] > cu_q_h[b] && ctx_lens_h[b] > max_ctx) max_ctx = ctx_lens_h[b];
     }
+    // (every workgroup of a sequence reads its lengths and path, one writes the new length)
+    if (new_lens_d != nullptr && (cache::overlap(new_lens_d, batch, ctx_lens_d, batch) || cache::overlap(new_lens_d, batch, cu_q_d, batch + 1ll) ||
+                                  cache::overlap(new_lens_d, batch, path_d, (int64_t)batch * path_stride)))
+        return INFLLMV2_ERR_INVALID_ARGUMENT;
     st = cache::check(p, c, max_ctx, true);
     if (st) return st;
     if (p->num_kv_heads > 65535 || !cache::fits_launch((int64_t)batch * p->num_kv_heads * 2, kThreads)) return INFLLMV2_ERR_UNSUPPORTED;

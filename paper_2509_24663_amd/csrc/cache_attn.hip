@@ -765,7 +765,7 @@ void merge(const A &a, const Launches &l, hipStream_t stream) {
 
 template <typename T, int D, bool CODES, int TILES, class A>
 int launch_t(const A &a, const Launches &l, hipStream_t stream) {
-    // (a tree's tokens see different rows, so that its kernel has the code for several in any case)
+    // (MULTI decides how values that are not finite are taken, which trees add behind the sums: one kernel for them)
     if (A::kTree || a.multi) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, true, A>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
     else if constexpr (!A::kTree) hipLaunchKernelGGL((cache_attn_kernel<T, D, CODES, TILES, false, A>), dim3((unsigned)l.items), dim3(NW * 64), 0, stream, a);
     merge<T, D>(a, l, stream);

@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kTakeThreads) pages_moves_kernel(CompactArgs a
         c.load(a.g.refs + used, 0, a.g.num_pages - used);
         ranked_pages(a.g.refs + used, a.g.num_pages - used, INT32_MAX, c, s_ranks, in_use, [&](int g, int rank) { a.moves[2 * rank] = used + g; });
     }
-    for (int i = 2 * n + threadIdx.x; i < a.g.num_pages / 2 * 2; i += kTakeThreads) a.moves[i] = -1;
+    for (int64_t i = 2 * (int64_t)n + threadIdx.x; i < a.g.num_pages / 2 * 2; i += kTakeThreads) a.moves[i] = -1;
     if (threadIdx.x == 0) a.live[0] = used, a.live[1] = n;
 }
 

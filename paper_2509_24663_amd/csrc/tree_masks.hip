@@ -113,6 +113,10 @@ extern "C" int infllmv2_tree_masks(const int32_t *parents_d, const int32_t *cu_q
     // (words behind those of the largest tree are written by workgroups of their own)
     const int64_t chunks = (mask_words + (int64_t)kWords - 1) / kWords;
     if (chunks > 65535 || !cache::fits_launch(batch * chunks, kMost)) return INFLLMV2_ERR_UNSUPPORTED;
+    // (every workgroup of a tree reads its parents, one writes the positions)
+    if (pos_d != nullptr && (cache::overlap(pos_d, total, parents_d, total) || cache::overlap(pos_d, total, ctx_lens_d, batch) ||
+                             cache::overlap(pos_d, total, cu_q_d, batch + 1ll)))
+        return INFLLMV2_ERR_INVALID_ARGUMENT;
     hipLaunchKernelGGL(tree_masks_kernel, dim3(batch, (unsigned)chunks), dim3((most + 63) / 64 * 64), 0, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());
 }

@@ -209,3 +209,14 @@ def test_long_paths(m, dtype, hkv, d, layout, kv):  # noqa: F811
     assert got.tolist() == want
     assert _same(c.k, k) and _same(c.v, v)
     assert ks is None or (torch.equal(c.k_scale, ks) and torch.equal(c.v_scale, vs))
+
+
+def test_paths_of_sequences_without_drafted_tokens(m):  # noqa: F811
+    """Lengths stay as they are, and so does the cache."""
+    p = m.Params.make("bf16", 8, 2, 64)
+    ctxs = [100, 0, 64]
+    c = _random_cache(m, p, ctxs, "e4m3", 5)
+    k, v, ks, vs = _state(c)
+    path = torch.zeros((3, 4), dtype=torch.int32, device="cuda")
+    assert m.cache_accept(p, c, [0, 0, 0, 0], ctxs, path).tolist() == ctxs
+    assert _same(c.k, k) and _same(c.v, v) and torch.equal(c.k_scale, ks) and torch.equal(c.v_scale, vs)

@@ -37,6 +37,33 @@ def test_mask_refusals(m):  # noqa: F811
     assert call(cu=(0, 0), parents=None, mask=None) == 0 and call(cu=(0,), batch=0) == 0
 
 
+def test_outputs_over_inputs(m):  # noqa: F811
+    """Lengths that a call reads are not where it writes the new ones, in whole or in part."""
+    p, c = m.Params.make("bf16", 8, 2, 64), _cache(m)
+    (_a, cu), (_b, cx) = _ints([0, 5, 9]), _ints([200, 100])
+    apart = dict(cu=4096, ctx=8192, other=12288)          # (addresses of nothing: a refused call reads none)
+
+    def accept(new):
+        return m.lib().infllmv2_cache_accept(ctypes.byref(p), ctypes.byref(c), cu, apart["cu"], cx, apart["ctx"], 2, apart["other"], 4, new, None)
+
+    def masks(pos):
+        return m.lib().infllmv2_tree_masks(apart["other"], cu, apart["cu"], cx, apart["ctx"], 2, one, 1, pos, None)
+
+    for call, others, mine in ((accept, 4 * 2 * 4, 4 * 2), (masks, 4 * 9, 4 * 9)):
+        for name, size in (("cu", 4 * 3), ("ctx", 4 * 2), ("other", others)):
+            for at in (apart[name], apart[name] + size - 4, apart[name] - mine + 4):
+                assert call(at) == INVALID, (call.__name__, name, at)
+            if not torch.cuda.is_available():
+                for at in (apart[name] + size, apart[name] - mine):
+                    assert call(at) == HIP, (call.__name__, name, at)
+
+
+def test_accept_with_nothing_to_do(m):  # noqa: F811
+    p, c = m.Params.make("bf16", 8, 2, 64), _cache(m)
+    (_a, cu), (_b, cx) = _ints([0, 0]), _ints([200])
+    assert m.lib().infllmv2_cache_accept(ctypes.byref(p), ctypes.byref(c), cu, one, cx, one, 1, None, 0, None, None) == 0
+
+
 @no_gpu
 def test_masks_without_positions_need_no_lengths(m):  # noqa: F811
     (_a, cu) = _ints([0, 40])
