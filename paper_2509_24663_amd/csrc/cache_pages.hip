@@ -7,8 +7,8 @@
 //
 // Bound: latency.  Entries are given back and shared by as many workgroups as they are worth (counts added with atomics, whose order does not matter);
 // handing out needs every free page's rank, which one workgroup works out, 8192 counts at a time, only as far as pages are wanted.  64 rows that give 3000 pages
-// back and get 3200 of a pool of 12288: 2.5 and 6.2 us.  32 forks of up to 47 blocks 9.4; 240 forks of 512 blocks of one row 3.5 where they had its pages before (with
-// an add and a subtract for each entry: 58; where they had others a call takes 10.9 for 8.2) and 4.0 for their last pages.  8192 pages, 6126 of them in use: 5.4 to find the 1529 that move, 5.4 to renumber 12288 entries.  Copies: HBM, those 1529
+// back and get 3200 of a pool of 12288: 2.6 and 5.6 us.  32 forks of up to 47 blocks 9.4; 240 forks of 512 blocks of one row 3.5 where they had its pages before (with
+// an add and a subtract for each entry: 58; where they had others a call takes 10.9 for 8.2) and 3.7 for their last pages.  8192 pages, 6126 of them in use: 5.4 to find the 1529 that move, 5.4 to renumber 12288 entries.  Copies: HBM, those 1529
 // pages of 32 KB 17.5 us, 5.7 TB/s read and written.
 #include <algorithm>
 
