@@ -93,6 +93,54 @@ template <int D> struct KeyTile<float, D, true> {
     }
 };
 
+// fp32 data over codes: a code is a bf16 value as it is and a fp32 number three of them, exactly, so that queries (and weights) as three pieces take three
+// bf16 products, 48 clocks for 32 channels of which fp32 products take 256 (and those leave the vector unit idle for no other wavefront).  Off by what
+// the sums round; a query that is not finite is in the first piece alone.
+struct Thirds;
+template <int D> struct Row3 { RowFrag<bf16_t, D> p[3]; };
+// two numbers as pieces, the first of each in x[0]
+__device__ inline void thirds(float a, float b, uint32_t (&x)[3]) {
+    const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+    x[0] = upper_halves(u, v);
+    const float a1 = a - __uint_as_float(u & 0xffff0000u), b1 = b - __uint_as_float(v & 0xffff0000u);
+    const uint32_t u1 = __float_as_uint(a1), v1 = __float_as_uint(b1);
+    x[1] = upper_halves(u1, v1);
+    x[2] = cache_attn::pack(a1 - __uint_as_float(u1 & 0xffff0000u), b1 - __uint_as_float(v1 & 0xffff0000u));
+}
+template <int D> struct KeyTile<Thirds, D, true> : KeyTile<bf16_t, D, true> {
+    static __device__ inline void load_query(Row3<D> &q, const float *row, int g) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            u32x4 x[3];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const f32x4 y = __builtin_bit_cast(f32x4, *reinterpret_cast<const f32x4_u *>(row + 64 * (s / 2) + 16 * g + 8 * (s & 1) + 4 * i));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const bool odd0 = !finite(y[2 * j]), odd1 = !finite(y[2 * j + 1]);
+                    uint32_t three[3];
+                    thirds(odd0 ? 0.f : y[2 * j], odd1 ? 0.f : y[2 * j + 1], three);
+                    const uint32_t odd = cache_attn::pack(odd0 ? y[2 * j] : 0.f, odd1 ? y[2 * j + 1] : 0.f);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) x[k][2 * i + j] = three[k] | (k == 0 ? odd : 0u);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) q.p[k].x[s] = __builtin_bit_cast(bf16x8, x[k]);
+        }
+    }
+};
+using gen::row_product;
+template <int D>
+__device__ inline f32x4 row_product(const RowFrag<bf16_t, D> &a, const Row3<D> &b) {
+    f32x4 rest = {0.f, 0.f, 0.f, 0.f};       // (apart from the first piece's sums, which round to 2^8 times as much)
+#pragma unroll
+    for (int k = 2; k > 0; --k)
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) rest = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x[s], b.p[k].x[s], rest, 0, 0, 0);
+    return row_product<D>(a, b.p[0]) + rest;
+}
+
 // Values: D / 16 channels of one row per lane, in 32-bit words as stored
 template <typename T, int D, bool CODES>
 struct ValueRow {
@@ -136,6 +184,8 @@ struct ValueRow {
     }
 };
 
+template <int D> struct ValueRow<Thirds, D, true> : ValueRow<bf16_t, D, true> {};
+
 // Weights of a step as operands: bf16 data as two bf16 pieces, so that an output is off by little more than its own rounding; fp32 data as they are.
 template <typename T, int TILES> struct Weights;
 template <int TILES> struct Weights<bf16_t, TILES> {
@@ -164,19 +214,42 @@ template <int TILES> struct Weights<float, TILES> {
     }
 };
 
+template <int TILES> struct Weights<Thirds, TILES> {
+    bf16x8 hi[TILES / 2], lo[TILES / 2], least[TILES / 2];
+    __device__ inline void set(const f32x4 (&p)[TILES], float) {
+#pragma unroll
+        for (int t = 0; t < TILES / 2; ++t) {
+            u32x4 x[3];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 y = p[2 * t + i / 2];
+                uint32_t three[3];
+                thirds(y[2 * (i & 1)], y[2 * (i & 1) + 1], three);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) x[k][i] = three[k];
+            }
+            hi[t] = __builtin_bit_cast(bf16x8, x[0]);
+            lo[t] = __builtin_bit_cast(bf16x8, x[1]);
+            least[t] = __builtin_bit_cast(bf16x8, x[2]);
+        }
+    }
+};
+
 // acc[j] += (rows' channel N (4 g + r) + j) x (weights of column m); rows v[4 t + r]: key 16 t + 4 g + r of the step
 // SOLO: only into the columns (lanes) that take
-template <bool SOLO, int D, int TILES, bool CODES>
-__device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<bf16_t, TILES> &w, const ValueRow<bf16_t, D, CODES> (&v)[4 * TILES], float scale, bool take) {
+template <bool SOLO, int D, int TILES, bool CODES, class E>
+__device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<E, TILES> &w, const ValueRow<E, D, CODES> (&v)[4 * TILES], float scale, bool take) {
     auto add = [&](f32x4 &to, bf16x8 row, int t) {
-        f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.lo[t], to, 0, 0, 0);
+        f32x4 x = to;
+        if constexpr (std::is_same_v<E, Thirds>) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.least[t], x, 0, 0, 0);
+        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.lo[t], x, 0, 0, 0);
         x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(row, w.hi[t], x, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r) to[r] = !SOLO || take ? x[r] : to[r];
     };
 #pragma unroll
     for (int t = 0; t < TILES / 2; ++t) {
-        const ValueRow<bf16_t, D, CODES> *a = &v[8 * t];
+        const ValueRow<E, D, CODES> *a = &v[8 * t];
         if constexpr (CODES) {
 #pragma unroll
             for (int i = 0; i < D / 64; ++i) {
@@ -233,10 +306,14 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TIL
 }
 
 // ------------------------------------------------------------------------------------------ a split of a tile
+// Parts of a page that are dealt out to wavefronts: steps of fp32 data over trees, a page of which takes a wavefront 2.6 or 5.2 us
+template <typename T, int TILES, class A>
+constexpr int parts_of() { return A::kTree && sizeof(T) == 4 ? kBlock / (16 * TILES) : 1; }
 // MULTI: tiles may have several tokens
 template <typename T, int D, bool CODES, int TILES, bool MULTI, class A>
 __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
-    constexpr int STEP = 16 * TILES, STEPS = kBlock / STEP, N = D / 16;
+    constexpr int STEP = 16 * TILES, N = D / 16;
+    constexpr int PARTS = parts_of<T, TILES, A>(), STEPS = kBlock / PARTS / STEP;
     __shared__ int s_item[6];
     __shared__ float s_m[NW][16], s_l[NW][16];
     __shared__ int s_odd[A::kTree ? NW : 1];
@@ -294,9 +371,9 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     if constexpr (A::kTree) nsplit = a.most_splits(n, len);
     else nsplit = a.splits(len, pos_last);
     if (split >= nsplit) return;
-    // the entries of this wavefront: of all pages a run for each split; of a list (which may be longer than the pages there can be, and hold them
-    // anywhere) every (NW x nsplit)-th
-    const int e_first = listed ? split * NW + w : split * a.pps + w, e_step = listed ? NW * nsplit : NW;
+    // the entries (or parts of them) of this wavefront: of all pages a run for each split; of a list (which may be longer than the pages there can be, and
+    // hold them anywhere) every (NW x nsplit)-th
+    const int e_first = listed ? split * NW + w : split * a.pps * PARTS + w, e_step = listed ? NW * nsplit : NW;
     int e_end, tree_e = 0;                       // tree_e: entries in front of those of drafted rows
     if constexpr (A::kTree) {
         tree_e = a.listed_entries(n, len);
@@ -310,8 +387,9 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     const int64_t row = row0 + first + (used ? ti : 0);
     const int qh = h * G + (used ? m - ti * G : 0);
 
-    RowFrag<T, D> qf;
-    KeyTile<T, D, CODES>::load_query(qf, reinterpret_cast<const T *>(a.q) + (row * a.hq + qh) * D, g);
+    using E = std::conditional_t<A::kTree && CODES && sizeof(T) == 4, Thirds, T>;
+    std::conditional_t<std::is_same_v<E, T>, RowFrag<T, D>, Row3<D>> qf;
+    KeyTile<E, D, CODES>::load_query(qf, reinterpret_cast<const T *>(a.q) + (row * a.hq + qh) * D, g);
     const float c = a.scale * kLog2e;
 
     f32x4 acc[N];
@@ -333,7 +411,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
         }
     }
     const uint32_t tok = (uint32_t)a.c.tok_stride;
-    const uint32_t k_off = m * tok + KeyTile<T, D, CODES>::lane_offset(g), v_off = 4 * g * tok + m * ValueRow<T, D, CODES>::BYTES;
+    const uint32_t k_off = m * tok + KeyTile<E, D, CODES>::lane_offset(g), v_off = 4 * g * tok + m * ValueRow<E, D, CODES>::BYTES;
     // (a walk as a loop's body instead of twice in the code keeps some 24 more registers)
     auto walk = [&](auto second) {
         constexpr float lift = decltype(second)::value ? kLift : 0.f;
@@ -342,8 +420,8 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         // lane l holds the l-th of the next 64 pages: where it is, its first key, its scales
-        for (int e0 = e_first; e0 < e_end; e0 += 64 * e_step) {
-            const int e = e0 + lane * e_step;
+        for (int e0 = e_first; e0 < e_end * PARTS; e0 += 64 * e_step) {
+            const int e = (e0 + lane * e_step) / PARTS;
             int my_page = -1, my_key0 = 0;
             float my_ks = 1.f, my_vs = 1.f;
             if (e < e_end) {
@@ -356,7 +434,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
                 }
                 if (j >= 0 && j < below) {
                     my_page = a.c.page(seq, j);
-                    my_key0 = j * kBlock;
+                    my_key0 = j * kBlock + (e0 + lane * e_step) % PARTS * (kBlock / PARTS);
                 }
             }
             uint64_t there = __ballot(my_page >= 0);
@@ -365,9 +443,11 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
                 my_ks = a.c.ks[(int64_t)my_page * hkv + h];
                 my_vs = a.c.vs[(int64_t)my_page * hkv + h];
             }
-            KeyTile<T, D, CODES> k[TILES];
-            ValueRow<T, D, CODES> v[4 * TILES];
-            auto base_of = [&](const char *p, int l) { return p + a.c.at(__builtin_amdgcn_readlane(my_page, l), h); };
+            KeyTile<E, D, CODES> k[TILES];
+            ValueRow<E, D, CODES> v[4 * TILES];
+            auto base_of = [&](const char *p, int l) {
+                return p + a.c.at(__builtin_amdgcn_readlane(my_page, l), h) + (PARTS > 1 ? (int64_t)(__builtin_amdgcn_readlane(my_key0, l) % kBlock) * tok : 0);
+            };
             auto load_k = [&](const char *base) {
 #pragma unroll
                 for (int t = 0; t < TILES; ++t) k[t].load(base + (int64_t)(16 * t) * tok, k_off);
@@ -404,7 +484,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
                         load_k(kb);
                     }
                     __builtin_amdgcn_sched_barrier(0);
-                    const bool shut = A::kTree && !open && page_key0 <= pos0 && page_key0 + kBlock > pos0;
+                    const bool shut = A::kTree && !open && page_key0 / kBlock == pos0 / kBlock;
                     const bool edge = A::kTree ? shut || key0 + STEP > pos0 : key0 + STEP - 1 > pos0;          // keys behind a token
                     if constexpr (A::kTree) any_key |= used && !edge;
                     if (edge) {
@@ -445,7 +525,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
                             part_sum += s[t][r];
                         }
                     sum += part_sum;
-                    Weights<T, TILES> wt;
+                    Weights<E, TILES> wt;
                     wt.set(s, vs);
                     int rounds = 1;
                     if (edge) {                                                      // rows that no token of the tile sees, and those that only some see
@@ -584,7 +664,7 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
         float *part = a.part + (slot * 16 + col) * D + ch;
         for (int j = pos0 / kBlock; j <= pos_last / kBlock; ++j) {
             const int e = tree_e + j - pos0 / kBlock;
-            if (listed ? e % (NW * nsplit) / NW != split : e < split * a.pps || e >= e_end) continue;      // (another split's)
+            if (listed ? e * PARTS % (NW * nsplit) / NW != split : e < split * a.pps || e >= e_end) continue;      // (another split's)
             const int page = a.c.page(seq, j);
             if (page < 0) continue;
             const bool shut = !open && j == pos0 / kBlock;
