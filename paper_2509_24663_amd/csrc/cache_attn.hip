@@ -14,7 +14,8 @@
 // Bound: HBM where the pages are many (64 sequences of 16384 to 65536 keys, 16 heads on 1, e4m3: 258 + 8 us for 1.37 GB, 5.2 TB/s, the matrix cores busy for 10 % of
 // it; one of 500000: 54 us for 256 MB), else a chain of trips to memory: length, page number, rows, partial results, joined results (16 sequences, 64 listed
 // blocks each: 11.0 + 4.0 us traced, of which some 0.5 to the length, 1.4 to the page, 1.7 to its first logits, 2.8 for the rest of two pages, 0.5 in LDS; 5
-// sequences of 300 to 2011 keys with 4 tokens each, fp32: 10.6 + 3.9).  fp32 data: the products, 2.6 us for a page of 64 channels and wavefront.  Measured and
+// sequences of 300 to 2011 keys with 4 tokens each, fp32: 10.6 + 3.9).  fp32 data: the products, 2.6 us for a page of 64 channels and wavefront, and what else the vector unit has to do, which none of them leave
+// it time for (fp32 pages of 60 tokens over 15000 keys: products 42 % of the clocks, the loads' return path 63 %); trees over codes: Thirds.  Measured and
 // not taken: a word of each line of the page after the next requested ahead, for the L2 (16 sequences of 33000 keys: 56 -> 64 us).
 #include <type_traits>
 
@@ -306,7 +307,8 @@ __device__ inline void add_values(f32x4 (&acc)[D / 16], const Weights<float, TIL
 }
 
 // ------------------------------------------------------------------------------------------ a split of a tile
-// Parts of a page that are dealt out to wavefronts: steps of fp32 data over trees, a page of which takes a wavefront 2.6 or 5.2 us
+// Parts of a page that are dealt out to wavefronts: trees over fp32 data a step each, since a page of them takes a wavefront long (fp32 pages 2.6 or 5.4 us by the head
+// dim, codes 1.2 or 1.9; 8 trees of 8 tokens over 500 fp32 keys, 8 heads on 2, d 128: 17.8 -> 12.2 us, rules::tree_unit_pps with it)
 template <typename T, int TILES, class A>
 constexpr int parts_of() { return A::kTree && sizeof(T) == 4 ? kBlock / (16 * TILES) : 1; }
 // MULTI: tiles may have several tokens
@@ -853,7 +855,7 @@ int launch_t(const A &a, const Launches &l, hipStream_t stream) {
 }
 
 constexpr int kMostGroups = 2048;          // a workgroup has at least all pages / kMostGroups (64 sequences of 16384 to 65536 keys: 480 313 us, 2048 272)
-constexpr int kLeastPages = NW;            // .. and a page for each wavefront
+constexpr int kLeastPages = NW;            // .. and a page for each wavefront (trees over fp32 data: a page)
 constexpr int kMostPages = 1 << 25;        // of a context: with so many to a split there is one split
 // Bytes of a partial result.  A sequence with more than one split has at most twice pages / pps of them; cache_attn.hip has pps >= all pages /
 // kMostGroups, so at most 2 kMostGroups partial results.
@@ -867,8 +869,8 @@ size_t tile_bytes(const infllmv2_params *p, int64_t slots, int groups) { return 
 
 }  // namespace
 
-size_t cache_attn_ws_bound(const infllmv2_params *p, int32_t batch, int64_t tokens, int32_t max_ctx) {
-    const int64_t most = (max_ctx + (int64_t)kBlock - 1) / kBlock, per = (most + kLeastPages - 1) / kLeastPages;
+size_t cache_attn_ws_bound(const infllmv2_params *p, int32_t batch, int64_t tokens, int32_t max_ctx, bool tree) {
+    const int64_t most = (max_ctx + (int64_t)kBlock - 1) / kBlock, least = tree && p->dtype == INFLLMV2_FP32 ? 1 : kLeastPages, per = (most + least - 1) / least;
     const int64_t units = tokens * p->num_kv_heads;
     const int64_t slots = per <= 1 ? 0 : units < 2 * kMostGroups && units * per < 2 * kMostGroups ? units * per : 2 * kMostGroups;
     // the tile kernel: at most tokens / (tokens of a tile) tiles and one more for each sequence
@@ -964,7 +966,9 @@ int attend(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, c
     if (c->tok_stride > (1ll << 24)) return INFLLMV2_ERR_UNSUPPORTED;
     const bool codes = c->kv_type == INFLLMV2_CACHE_E4M3, fp32 = p->dtype == INFLLMV2_FP32;
     const int64_t share = (work.sum + kMostGroups - 1) / kMostGroups;
-    a.pps = share >= kMostPages ? kMostPages : rules::unit_pps(work, p->head_dim, fp32, codes ? 1 : fp32 ? 4 : 2, share);
+    if (share >= kMostPages) a.pps = kMostPages;
+    else if (A::kTree && fp32) a.pps = rules::tree_unit_pps(work, p->head_dim, codes, p->head_dim == 128 && !codes ? parts_of<float, 1, A>() : parts_of<float, 2, A>(), share);
+    else a.pps = rules::unit_pps(work, p->head_dim, fp32, codes ? 1 : fp32 ? 4 : 2, share);
     Launches mine, other;
     bool single = true;                        // one query token for each sequence
     for (int b = 0; b < batch; ++b) {

@@ -441,6 +441,30 @@ inline int unit_pps(const PageWork &w, int d, bool fp32, int bytes, int64_t leas
     }
     return (int)best;
 }
+// The same for trees of drafted tokens over fp32 data, whose pages are dealt out to the four wavefronts in `parts` parts: any number of pages is a workgroup's.
+// Workgroups that share a CU take turns at its matrix cores: what counts past 256 of them is the work dealt out and, in part, the longest workgroup.
+// Measured, one call, us, by pages 1 / 2 / 4 / 8 / 16 / 32 (e4m3): one token over 4132 keys (32 heads on 2, d 128) 11.8 / 11.6 / 12.3 / 14.5 / 18.0 / 25.4, 58
+// over 3268 102 / 52 / 34.8 / 28.8 / 23.8 / 26.3, 12 trees of 25 over lists of 64 (12 on 4) 222 / 129 / 84.5 / 61.0 / 52.4 / 47.8, by 48 41.4; fp32 pages, 8 trees of 8
+// tokens over 500 (8 on 2, d 128) 12.0 / 12.7 / 15.1 / 17.7, 60 over 15000 (32 on 2) 547 / 353 / 272 / 202 / 207 / 209.  Over 81 calls
+// of 8 head shapes the choice is 0.7 % from the best of some ten on average, 16 % at most (that 41.4: 48.1).
+inline int tree_unit_pps(const PageWork &w, int d, bool codes, int parts, int64_t least) {
+    const int64_t from = least < 1 ? 1 : least;
+    if (from >= w.most) return (int)from;
+    const double part_us = (codes ? 0.6 + 0.6 * d / 64 : 2.6 * d / 64) / parts;
+    int64_t best = from;
+    double best_us = 0;
+    for (int64_t pps = from;; pps += pps < 4 ? 1 : pps < 12 ? 2 : pps < 24 ? 4 : pps < 32 ? 8 : pps / 2) {
+        if (pps > w.most) pps = w.most;
+        const int64_t n = w.groups((int)pps);
+        const double longest = (double)((pps * parts + 3) / 4), mean = (double)w.sum * parts / 4 / n + 0.4;
+        const double dealt = (codes ? 0.8 : 0.9) / 256 * n * (mean < longest ? mean : longest) + 0.6 * longest;
+        const double way = n <= 256 || dealt < longest ? longest : dealt;
+        const double us = part_us * way + (codes ? 0.007 : 0.01) * n + (pps < w.most ? 4 : 0) + (w.most > 8 * pps ? 1 : 0);
+        if (pps == from || us < best_us) best = pps, best_us = us;
+        if (pps == w.most) break;
+    }
+    return (int)best;
+}
 
 // Paged cache, chunks of prompts: cache_attn_tile.hip takes a sequence's queries in tiles of `groups` column groups (16 columns each), a workgroup over the
 // pages of one.  Two sizes: large tiles read the least of LDS for a product, small ones fill the chip where there are few of them.

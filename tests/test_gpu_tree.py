@@ -1,4 +1,6 @@
 """Trees of drafted tokens over the paged cache: ancestors and positions, attention against a plain form in 64 bits, a step from the draft to the accepted path."""
+import math
+
 import pytest
 import torch
 
@@ -501,3 +503,62 @@ def test_masks_of_many_tokens(m, dtype, hq, hkv, d):  # noqa: F811
     sets = [{j for j in range(i + 1) if i - j < 300 or j % 97 == 5} for i in range(1500)] + [{0}, {0, 1}, {2}]
     mask = trees.to_words(sets, 50).cuda()
     _check(m, p, c, _q(p, news, 16), news, ctxs, mask)
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "native"])
+@pytest.mark.parametrize("hq,hkv,d", [(32, 2, 128), (4, 1, 64), (5, 5, 64)])
+def test_all_bits_of_fp32_queries_and_weights(m, kv, hq, hkv, d):  # noqa: F811
+    """Results that are what the last bits of a query or of a weight leave: where those are dropped, nothing or something else is left."""
+    p = _params(m, "fp32", hq, hkv, d, softmax_scale=1.0)
+    B = 40
+    gen = _gen(91)
+    # one key (1, 1, 0, ..): a logit of x - y, y being x without its last 8 bits
+    x = torch.randn((B, hq), generator=gen, device="cuda") * 4
+    y = (x.view(torch.int32) & ~0xff).view(torch.float32)
+    c, _, _ = _filled(m, p, [1] * B, kv, 5)
+    k = torch.zeros((hkv, B, d), device="cuda")
+    k[..., 0] = k[..., d - 1] = 1.0
+    m.cache_append(p, c, k, k, list(range(B + 1)), [0] * B)
+    q = torch.zeros((B, hq, d), device="cuda")
+    q[..., 0], q[..., d - 1] = x, -y
+    mask = torch.ones((B, 1), dtype=torch.int32, device="cuda")
+    _, lse = m.cache_tree_attn(p, c, q, list(range(B + 1)), [1] * B, mask)
+    # (the sum is exact; times log2 e, by ln 2 back, each rounded: four roundings of 2^-24)
+    want = x.double() - y.double()
+    assert bool(((lse.double() - want).abs() <= 2.0 ** -21 * want.abs()).all())
+    # two keys, the second's weight w = exp(-q) close to 1 / 8, their values 1 and -8: (1 - 8 w) / (1 + w)
+    c, _, _ = _filled(m, p, [2] * B, kv, 6)
+    k, v = (torch.zeros((hkv, 2 * B, d), device="cuda") for _ in range(2))
+    k[:, 0::2, 0] = 1.0
+    v[:, 0::2], v[:, 1::2] = 1.0, -8.0
+    m.cache_append(p, c, k, v, list(range(0, 2 * B + 1, 2)), [0] * B)
+    q = torch.zeros((B, hq, d), device="cuda")
+    q[..., 0] = math.log(8) + 2.0 ** -10 * torch.rand((B, hq), generator=gen, device="cuda")
+    got, _ = m.cache_tree_attn(p, c, q, list(range(B + 1)), [2] * B, mask)
+    w = torch.exp(-q[..., 0].double())
+    # 8 w = 1 + less than 2^-9: a logit of 3 in units of log2, rounded three times (3 x 3 x 2^-24 ln 2), its power by 2 steps (2^-22), three sums and a
+    # quotient; a weight without its last 8 bits would be off by up to 2^-17
+    assert bool(((got.double() - ((1 - 8 * w) / (1 + w))[..., None]).abs() <= 2.0 ** -20).all())
+
+
+@pytest.mark.parametrize("kv", ["e4m3", "native"])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("fp32", 8, 2, 128), ("fp32", 4, 1, 64), ("bf16", 32, 2, 128)])
+def test_queries_that_are_not_finite(m, kv, dtype, hq, hkv, d):  # noqa: F811
+    """They give NaN (of keys seen) and leave other rows and heads as they are."""
+    p = _params(m, dtype, hq, hkv, d)
+    n, ctx = 12, 700
+    c, _, _ = _filled(m, p, [ctx], kv, 7)
+    mask, q = _masks(m, [n], [ctx], 15), _q(p, [n], 16)
+    want, want_lse = m.cache_tree_attn(p, c, q, [0, n], [ctx], mask)
+    odd = q.clone()
+    bad = torch.zeros((n, hq), dtype=torch.bool)
+    for t, h, ch, x in ((0, 1, 3, float("inf")), (4, 0, d - 1, -float("inf")), (5, hq - 1, 17, float("nan")), (11, 2, 40, float("inf"))):
+        odd[t, h, ch] = x
+        bad[t, h] = True
+    if dtype == "fp32":
+        odd.view(torch.int32)[7, 3, 9] = 0x7f800001          # a NaN of low bits only
+        bad[7, 3] = True
+    got, lse = m.cache_tree_attn(p, c, odd, [0, n], [ctx], mask)
+    bad = bad.cuda()
+    assert bool(got[bad].isnan().all())
+    assert torch.equal(got[~bad], want[~bad]) and torch.equal(lse[~bad], want_lse[~bad])
