@@ -286,40 +286,25 @@ struct CompactArgs {
     int32_t *moves, *live;                 // [num_pages / 2][2], [2]: pages in use, moves
 };
 
-// Of the pages in use those from number `used` on move, in order, to the free ones below it, in order: there are as many of either.
-__global__ void __launch_bounds__(kTakeThreads) pages_moves_kernel(CompactArgs a) {
-    __shared__ Ranks s_ranks;
-    const auto in_use = [](int x) { return x > 0; };
-    Counts c;
-    c.load(a.g.refs, 0, a.g.num_pages);
-    const int used = ranked_pages(a.g.refs, a.g.num_pages, INT32_MAX, c, s_ranks, in_use, [](int, int) {});
-    const int n = ranked_pages(a.g.refs, used, INT32_MAX, c, s_ranks, [](int x) { return x <= 0; }, [&](int g, int rank) { a.moves[2 * rank + 1] = g; });
-    if (n > 0) {
-        c.load(a.g.refs + used, 0, a.g.num_pages - used);
-        ranked_pages(a.g.refs + used, a.g.num_pages - used, INT32_MAX, c, s_ranks, in_use, [&](int g, int rank) { a.moves[2 * rank] = used + g; });
-    }
-    for (int64_t i = 2 * (int64_t)n + threadIdx.x; i < a.g.num_pages / 2 * 2; i += kTakeThreads) a.moves[i] = -1;
-    if (threadIdx.x == 0) a.live[0] = used, a.live[1] = n;
-}
-
-// The tables and counts by the new numbers; in may be out: an entry, and the two counts of a move, are one thread's.
-__global__ void __launch_bounds__(256) pages_renumber_kernel(CompactArgs a) {
-    const int used = a.live[0], n = a.live[1];
-    if (blockIdx.y == 0) {
-        for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < a.g.num_pages; g += gridDim.x * 256) {
-            // (counts of moved pages are the move's: of one of those, read while it changes, the same comes out either way)
-            const int x = a.g.refs[g];
-            if (g < used ? x > 0 : x <= 0) a.out.refs[g] = g < used ? x : 0;
-            if (g < n) {
-                const int from = a.moves[2 * g], to = a.moves[2 * g + 1], y = a.g.refs[from];
-                a.out.refs[to] = y;
-                a.out.refs[from] = 0;
-            }
+// The counts by the new numbers, and the entries of the table; move(i): the i-th move.  In may be out: an entry, and the two counts of a move, are one thread's.
+template <class Move>
+__device__ inline void renumber_counts(const CompactArgs &a, int used, int n, int64_t first, int64_t step, Move move) {
+    for (int64_t g = first; g < a.g.num_pages; g += step) {
+        // (counts of moved pages are the move's: of one of those, read while it changes, the same comes out either way)
+        const int x = a.g.refs[g];
+        if (g < used ? x > 0 : x <= 0) a.out.refs[g] = g < used ? x : 0;
+        if (g < n) {
+            const int2 m = move((int)g);
+            const int y = a.g.refs[m.x];
+            a.out.refs[m.y] = y;
+            a.out.refs[m.x] = 0;
         }
-        return;
     }
+}
+template <class Move>
+__device__ inline void renumber_entries(const CompactArgs &a, int used, int n, int64_t first, int64_t step, Move move) {
     const int64_t entries = (int64_t)a.rows * a.out_blocks;
-    for (int64_t i = ((int64_t)(blockIdx.y - 1) * gridDim.x + blockIdx.x) * 256 + threadIdx.x; i < entries; i += (int64_t)(gridDim.y - 1) * gridDim.x * 256) {
+    for (int64_t i = first; i < entries; i += step) {
         const int r = (int)(i / a.out_blocks), j = (int)(i - (int64_t)r * a.out_blocks);
         int page = a.g.row(r)[min(j, a.blocks - 1)];                  // (beside the length, not behind it)
         if (j >= min(blocks_of(a.lens[r]), a.blocks) || !a.g.is_page(page)) page = -1;
@@ -327,13 +312,55 @@ __global__ void __launch_bounds__(256) pages_renumber_kernel(CompactArgs a) {
             int lo = 0, hi = n;
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
-                if (a.moves[2 * (int64_t)mid] < page) lo = mid + 1;
+                if (move(mid).x < page) lo = mid + 1;
                 else hi = mid;
             }
-            page = lo < n && a.moves[2 * (int64_t)lo] == page ? a.moves[2 * (int64_t)lo + 1] : -1;
+            const int2 m = lo < n ? move(lo) : int2{-1, -1};
+            page = m.x == page ? m.y : -1;
         }
         a.out.row(r)[j] = page;
     }
+}
+
+// Pages (whose moves are kept in LDS) and entries up to which the workgroup that finds the moves renumbers as well, one launch for two: with the copies, 331 pages and
+// 299 entries 14.0 -> 11.8 us, 1300 and 940 13.6 -> 11.5, 2600 and 1890 14.1 -> 13.0, 4000 and 2840 18.7 -> 19.2.
+constexpr int kSmallPages = 4096, kSmallEntries = 2048;
+
+// Of the pages in use those from number `used` on move, in order, to the free ones below it, in order: there are as many of either.
+template <bool SMALL>
+__global__ void __launch_bounds__(kTakeThreads) pages_moves_kernel(CompactArgs a) {
+    __shared__ Ranks s_ranks;
+    __shared__ int2 s_moves[SMALL ? kSmallPages / 2 : 1];
+    const auto in_use = [](int x) { return x > 0; };
+    Counts c;
+    c.load(a.g.refs, 0, a.g.num_pages);
+    const int used = ranked_pages(a.g.refs, a.g.num_pages, INT32_MAX, c, s_ranks, in_use, [](int, int) {});
+    const int n = ranked_pages(a.g.refs, used, INT32_MAX, c, s_ranks, [](int x) { return x <= 0; }, [&](int g, int rank) {
+        a.moves[2 * rank + 1] = g;
+        if (SMALL) s_moves[rank].y = g;
+    });
+    if (n > 0) {
+        c.load(a.g.refs + used, 0, a.g.num_pages - used);
+        ranked_pages(a.g.refs + used, a.g.num_pages - used, INT32_MAX, c, s_ranks, in_use, [&](int g, int rank) {
+            a.moves[2 * rank] = used + g;
+            if (SMALL) s_moves[rank].x = used + g;
+        });
+    }
+    for (int64_t i = 2 * (int64_t)n + threadIdx.x; i < a.g.num_pages / 2 * 2; i += kTakeThreads) a.moves[i] = -1;
+    if (threadIdx.x == 0) a.live[0] = used, a.live[1] = n;
+    if constexpr (SMALL) {                 // (every count has been read: ranked_pages ends with a barrier)
+        const auto move = [&](int i) { return s_moves[i]; };
+        renumber_entries(a, used, n, threadIdx.x, kTakeThreads, move);
+        renumber_counts(a, used, n, threadIdx.x, kTakeThreads, move);
+    }
+}
+
+__global__ void __launch_bounds__(256) pages_renumber_kernel(CompactArgs a) {
+    const int used = a.live[0], n = a.live[1];
+    const auto move = [&](int i) { return int2{a.moves[2 * (int64_t)i], a.moves[2 * (int64_t)i + 1]}; };
+    const int64_t step = (int64_t)gridDim.x * 256;
+    if (blockIdx.y == 0) renumber_counts(a, used, n, (int64_t)blockIdx.x * 256 + threadIdx.x, step, move);
+    else renumber_entries(a, used, n, ((int64_t)(blockIdx.y - 1) * gridDim.x + blockIdx.x) * 256 + threadIdx.x, (gridDim.y - 1) * step, move);
 }
 
 // ------------------------------------------------------------------------------------------ copies
@@ -458,8 +485,12 @@ extern "C" int infllmv2_pages_compact(const infllmv2_pages *g, const int32_t *le
     for (int b = 0; b < batch; ++b)
         if (!fits(g, lens_h[b]) || !fits(out, lens_h[b])) return INFLLMV2_ERR_INVALID_ARGUMENT;
     const CompactArgs a{pool_of(g), pool_of(out), lens_d, batch, g->blocks, out->blocks, moves_d, live_d};
-    hipLaunchKernelGGL(pages_moves_kernel, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
     const int64_t entries = (int64_t)batch * out->blocks;
+    if (g->num_pages <= kSmallPages && entries <= kSmallEntries) {
+        hipLaunchKernelGGL(pages_moves_kernel<true>, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
+        return hip_status(hipGetLastError());
+    }
+    hipLaunchKernelGGL(pages_moves_kernel<false>, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
     const unsigned x = chunks(g->num_pages, 256), y = 1 + chunks(entries, 256 * (int)x);
     hipLaunchKernelGGL(pages_renumber_kernel, dim3(x, y), dim3(256), 0, (hipStream_t)stream, a);
     return hip_status(hipGetLastError());

@@ -102,7 +102,7 @@ def test_nothing_to_do(m):  # noqa: F811
 
 
 @pytest.mark.parametrize("apart", [False, True])
-@pytest.mark.parametrize("pages,rows,blocks", [(1, 1, 1), (2, 1, 2), (9, 3, 4), (1000, 30, 40), (50000, 40, 1500)])
+@pytest.mark.parametrize("pages,rows,blocks", [(1, 1, 1), (2, 1, 2), (9, 3, 4), (1000, 30, 40), (4096, 16, 128), (4097, 16, 128), (4096, 683, 3), (50000, 40, 1500)])
 def test_compact(m, pages, rows, blocks, apart):  # noqa: F811
     rng = random.Random(pages + 1)
     for fill in (0.0, 0.4, 0.9, 1.0):
