@@ -638,13 +638,17 @@ def tree_masks(parents: torch.Tensor, cu_seqlens_q, ctx_lens, mask: Optional[tor
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     assert parents.dtype is torch.int32 and parents.is_contiguous() and parents.shape == (si.total,) and si.batch == cx.batch
     if mask is None:
-        mask = parents.new_empty((si.total, max(1, (si.max_len + 31) // 32)))
+        words = (si.max_len + 31) // 32 or 1
+        mask = parents.new_empty(si.total, words)
+    else:
+        assert mask.dtype is torch.int32 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == si.total
+        words = mask.shape[1]
     if positions is None:
         positions = torch.empty_like(parents)
-    assert mask.dtype is torch.int32 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == si.total
-    assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (si.total,)
+    else:
+        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (si.total,)
     st = lib().infllmv2_tree_masks(parents.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch,
-                                   mask.data_ptr(), mask.shape[1], positions.data_ptr(), _stream())
+                                   mask.data_ptr(), words, positions.data_ptr(), _stream())
     _check(st, "infllmv2_tree_masks")
     return mask, positions
 
@@ -659,7 +663,8 @@ def cache_tree_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q,
     tokens, hq, _ = shape = q.shape
     assert q.is_contiguous() and q.dtype is p.torch_dtype and shape == (si.total, p.num_q_heads, p.head_dim)
     assert si.batch == cx.batch <= cache.batch and cache._holds(p, cx.max_ctx)
-    assert mask.dtype is torch.int32 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == tokens
+    rows, words = mask.shape
+    assert mask.dtype is torch.int32 and mask.is_contiguous() and rows == tokens
     if block_idx is not None:
         assert block_idx.is_contiguous() and block_idx.dtype is torch.int32 and block_idx.shape == (si.batch, p.num_kv_heads, p.topk_total)
     if out is None:
@@ -667,14 +672,14 @@ def cache_tree_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q,
     else:
         assert out.is_contiguous() and out.shape == shape and out.dtype is q.dtype
     if lse is None:
-        lse = q.new_empty((tokens, hq), dtype=torch.float32)
+        lse = torch.empty_strided((tokens, hq), (hq, 1), dtype=torch.float32, device=q.device)          # (the quickest of torch's ways)
     else:
         assert lse.is_contiguous() and lse.shape == (tokens, hq) and lse.dtype is torch.float32
     if workspace is None:
         need = workspace_bytes(OP_CACHE_TREE_ATTN, p, si.batch, si.total, cx.max_ctx)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     st = lib().infllmv2_cache_tree_attn(ctypes.byref(p), cache.ref, q.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(),
-                                        cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch, mask.data_ptr(), mask.shape[1], _ptr(block_idx),
+                                        cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch, mask.data_ptr(), words, _ptr(block_idx),
                                         out.data_ptr(), lse.data_ptr(), *_ws_args(workspace), _stream())
     _check(st, "infllmv2_cache_tree_attn")
     return out, lse
@@ -684,13 +689,15 @@ def cache_accept(p: Params, cache: PagedCache, cu_seqlens_q, ctx_lens, path: tor
     """Brings the rows of path [B, steps] (device int32: numbers of drafted tokens, rising, -1 behind the last) together behind each sequence's context.
     Returns the new lengths (device int32 [B])."""
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
-    assert path.dtype is torch.int32 and path.dim() == 2 and path.is_contiguous() and path.shape[0] == si.batch == cx.batch <= cache.batch
+    rows, steps = path.shape
+    assert path.dtype is torch.int32 and path.is_contiguous() and rows == si.batch == cx.batch <= cache.batch
     assert cache._holds(p, cx.max_ctx)
     if new_lens is None:
-        new_lens = path.new_empty((si.batch,))
-    assert new_lens.dtype is torch.int32 and new_lens.is_contiguous() and new_lens.shape == (si.batch,)
+        new_lens = path.new_empty(rows)
+    else:
+        assert new_lens.dtype is torch.int32 and new_lens.is_contiguous() and new_lens.shape == (rows,)
     st = lib().infllmv2_cache_accept(ctypes.byref(p), cache.ref, si.cu_h.data_ptr(), si.cu_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(),
-                                     si.batch, path.data_ptr(), path.shape[1], new_lens.data_ptr(), _stream())
+                                     rows, path.data_ptr(), steps, new_lens.data_ptr(), _stream())
     _check(st, "infllmv2_cache_accept")
     return new_lens
 
@@ -727,8 +734,10 @@ class Forks:
 
 
 def _shortage(pool: PagePool, short: Optional[torch.Tensor], calls: int):
-    short = pool.refs.new_empty((1,)) if short is None else short
-    assert short.dtype is torch.int32 and short.numel() == 1
+    if short is None:
+        short = pool.refs.new_empty(1)
+    else:
+        assert short.dtype is torch.int32 and short.numel() == 1
     return short if calls else short.zero_()         # (the library writes nothing where there is nothing to do)
 
 
@@ -746,8 +755,9 @@ def pages_resize(pool: PagePool, old_lens, new_lens, short: Optional[torch.Tenso
 def pages_fork(pool: PagePool, forks: Forks, copies: Optional[torch.Tensor] = None, short: Optional[torch.Tensor] = None):
     """Returns (copies [n, 2]: pages to copy from and to with cache_copy_pages, -1: none; how many pages were wanting), device int32."""
     if copies is None:
-        copies = pool.refs.new_empty((forks.count, 2))
-    assert copies.dtype is torch.int32 and copies.is_contiguous() and copies.shape == (forks.count, 2)
+        copies = pool.refs.new_empty(forks.count, 2)
+    else:
+        assert copies.dtype is torch.int32 and copies.is_contiguous() and copies.shape == (forks.count, 2)
     short = _shortage(pool, short, forks.count)
     st = lib().infllmv2_pages_fork(pool.ref, forks.h.data_ptr(), forks.d.data_ptr(), forks.count, copies.data_ptr(), short.data_ptr(), _stream())
     _check(st, "infllmv2_pages_fork")
@@ -757,14 +767,15 @@ def pages_fork(pool: PagePool, forks: Forks, copies: Optional[torch.Tensor] = No
 def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: Optional[torch.Tensor] = None, live: Optional[torch.Tensor] = None):
     """Brings the pages in use to the front; sequence b has lens[b] tokens.  out: where the new table and counts go (default: the pool itself).  Returns
     (moves [num_pages // 2, 2] for cache_copy_pages, live [2]: pages in use and moves), device int32."""
-    info, out = _decode_info(lens), pool if out is None else out
-    half = pool.refs.numel() // 2
+    info, out, half = _decode_info(lens), pool if out is None else out, pool.c.num_pages // 2
     if moves is None:
-        moves = pool.refs.new_empty((half, 2))
+        moves = pool.refs.new_empty(half, 2)
+    else:
+        assert moves.dtype is torch.int32 and moves.is_contiguous() and moves.shape == (half, 2)
     if live is None:
-        live = pool.refs.new_empty((2,))
-    assert moves.dtype is torch.int32 and moves.is_contiguous() and moves.shape == (half, 2)
-    assert live.dtype is torch.int32 and live.is_contiguous() and live.shape == (2,)
+        live = pool.refs.new_empty(2)
+    else:
+        assert live.dtype is torch.int32 and live.is_contiguous() and live.shape == (2,)
     st = lib().infllmv2_pages_compact(pool.ref, info.ctx_h.data_ptr(), info.ctx_d.data_ptr(), info.batch, out.ref, moves.data_ptr(), live.data_ptr(),
                                       _stream())
     _check(st, "infllmv2_pages_compact")
@@ -773,7 +784,8 @@ def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: O
 
 def cache_copy_pages(p: Params, cache: PagedCache, pairs: torch.Tensor):
     """Copies page pairs[i, 0] to page pairs[i, 1] for each i (device int32 [n, 2]; -1: no copy): keys, values, scales.  Returns the cache."""
-    assert pairs.dtype is torch.int32 and pairs.is_contiguous() and pairs.dim() == 2 and pairs.shape[1] == 2 and cache._holds(p, 0)
-    st = lib().infllmv2_cache_copy_pages(ctypes.byref(p), cache.ref, pairs.data_ptr(), pairs.shape[0], _stream())
+    count, two = pairs.shape
+    assert pairs.dtype is torch.int32 and pairs.is_contiguous() and two == 2 and cache._holds(p, 0)
+    st = lib().infllmv2_cache_copy_pages(ctypes.byref(p), cache.ref, pairs.data_ptr(), count, _stream())
     _check(st, "infllmv2_cache_copy_pages")
     return cache
