@@ -16,7 +16,10 @@
 // blocks each: 11.0 + 4.0 us traced, of which some 0.5 to the length, 1.4 to the page, 1.7 to its first logits, 2.8 for the rest of two pages, 0.5 in LDS; 5
 // sequences of 300 to 2011 keys with 4 tokens each, fp32: 10.6 + 3.9).  fp32 data: the products, 2.6 us for a page of 64 channels and wavefront, and what else the vector unit has to do, which none of them leave
 // it time for (fp32 pages of 60 tokens over 15000 keys: products 42 % of the clocks, the loads' return path 63 %); trees over codes: Thirds.  Measured and
-// not taken: a word of each line of the page after the next requested ahead, for the L2 (16 sequences of 33000 keys: 56 -> 64 us).
+// not taken: a word of each line of the page after the next requested ahead, for the L2 (16 sequences of 33000 keys: 56 -> 64 us); trees over fp32 pages with K and V in
+// three pieces too, six products (60 tokens over 15000 keys, 32 heads on 2, d 128: 210 -> 188, 4 trees of 3 over 2673 to 10694 31 -> 36, 60 over 15000, 8 on 2, d 64
+// 32 -> 37).  Key rows requested so that neighbouring lanes read one row would save at most 6 % of the 210 and 11 % with bf16 pages, before what it takes to bring
+// them into the operands' order.
 #include <type_traits>
 
 #include "cache_attn.h"
