@@ -136,7 +136,9 @@ __global__ void __launch_bounds__(kThreads) cache_accept_kernel(AcceptArgs a) {
             const int v = tid + e * kThreads, row = first + (v >> a.vecs_log2);
             if (m.scale[e] == 0.f) continue;
             Piece y = m.x[e];
-            if (CODES && m.scale[e] != now) y = rescaled(y, m.scale[e] * cache::reciprocal_of_power(now));
+            // (a code that is not 0 is at least 2^-9, and the largest 448, so the new scale is at least 2^-17 of its own: no such row needs more than 2^17.  A row of
+            // zeros may come from any scale to the least one, 2^219 times as small: a factor of infinity would make NaN of it.)
+            if (CODES && m.scale[e] != now) y = rescaled(y, fminf(m.scale[e] * cache::reciprocal_of_power(now), 0x1p17f));
             *reinterpret_cast<Piece *>(to + (row - block * kBlock) * a.c.tok_stride + (v & (a.vecs - 1)) * 16) = y;
         }
         if (block == block1) break;
