@@ -563,8 +563,8 @@ int infllmv2_pages_fork(const infllmv2_pages *g, const infllmv2_fork *forks_h, c
 
 /*
  * Brings the pages in use to the front of the pool: with L of them, those numbered L and above move, in order, to the free ones below L, in order.  The table (of
- * its first `batch` rows blocks 0 .. ceil(lens / 64) - 1, which hold all entries that refs counts; the others become -1) and the counts by the new numbers go to `out`,
- * which is g, or has table and counts apart from g's.
+ * its first `batch` rows blocks 0 .. ceil(lens / 64) - 1, which hold all entries that refs counts; all others of out's rows and blocks become -1, those of rows from
+ * `batch` on too) and the counts by the new numbers go to `out`, which is g, or has table and counts apart from g's.
  *   moves_d       device out int32 [num_pages / 2][2]: page to copy from and page to copy to (infllmv2_cache_copy_pages), -1, -1 behind the last
  *   live_d        device out int32 [2]: L and the number of moves
  */

@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kTakeThreads) pages_split_kernel(ForkArgs a) {
 struct CompactArgs {
     Pool g, out;
     const int32_t *lens;
-    int rows, blocks, out_blocks;
+    int rows, blocks, out_rows, out_blocks;        // rows: with lengths; those of `out` behind them get no pages
     int32_t *moves, *live;                 // [num_pages / 2][2], [2]: pages in use, moves
 };
 
@@ -303,9 +303,13 @@ __device__ inline void renumber_counts(const CompactArgs &a, int used, int n, in
 }
 template <class Move>
 __device__ inline void renumber_entries(const CompactArgs &a, int used, int n, int64_t first, int64_t step, Move move) {
-    const int64_t entries = (int64_t)a.rows * a.out_blocks;
+    const int64_t entries = (int64_t)a.out_rows * a.out_blocks;
     for (int64_t i = first; i < entries; i += step) {
         const int r = (int)(i / a.out_blocks), j = (int)(i - (int64_t)r * a.out_blocks);
+        if (r >= a.rows) {
+            a.out.row(r)[j] = -1;
+            continue;
+        }
         int page = a.g.row(r)[min(j, a.blocks - 1)];                  // (beside the length, not behind it)
         if (j >= min(blocks_of(a.lens[r]), a.blocks) || !a.g.is_page(page)) page = -1;
         if (page >= used) {                // (pages to move are in order; seven looked at together take longer: 9.1 us of the kernel, not 5.2)
@@ -484,8 +488,8 @@ extern "C" int infllmv2_pages_compact(const infllmv2_pages *g, const int32_t *le
     if ((out->page_table_d == g->page_table_d && out->table_stride != g->table_stride)) return INFLLMV2_ERR_INVALID_ARGUMENT;
     for (int b = 0; b < batch; ++b)
         if (!fits(g, lens_h[b]) || !fits(out, lens_h[b])) return INFLLMV2_ERR_INVALID_ARGUMENT;
-    const CompactArgs a{pool_of(g), pool_of(out), lens_d, batch, g->blocks, out->blocks, moves_d, live_d};
-    const int64_t entries = (int64_t)batch * out->blocks;
+    const CompactArgs a{pool_of(g), pool_of(out), lens_d, batch, g->blocks, out->rows, out->blocks, moves_d, live_d};
+    const int64_t entries = (int64_t)out->rows * out->blocks;
     if (g->num_pages <= kSmallPages && entries <= kSmallEntries) {
         hipLaunchKernelGGL(pages_moves_kernel<true>, dim3(1), dim3(kTakeThreads), 0, (hipStream_t)stream, a);
         return hip_status(hipGetLastError());
