@@ -602,8 +602,10 @@ __global__ void __launch_bounds__(NW * 64, 2) cache_attn_kernel(A a) {
     if constexpr (A::kTree) some_key = (__ballot(any_key) >> m & 0x0001000100010001ull) != 0;
     if (ref == -INFINITY && some_key) ref = kLowest;         // only logits of minus infinity (0 / 0 below), not no key at all
     if (lane < 16) s_m[w][m] = ref, s_l[w][m] = sum;
-    if (A::kTree && lane == 0) s_odd[w] = 0;
-    if (A::kTree && odd_edge) s_odd[w] = 1;                  // (behind that write: one wavefront's)
+    if constexpr (A::kTree) {
+        const bool odd = __any(odd_edge);
+        if (lane == 0) s_odd[w] = odd;
+    }
     __syncthreads();
     const bool direct = nsplit == 1;
     float top = s_m[0][m];
