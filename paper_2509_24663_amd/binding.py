@@ -177,6 +177,21 @@ def _stream():
     return _raw_stream(_device())
 
 
+def _current_device() -> int:
+    return torch.cuda.current_device() if _device is None else _device()
+
+
+def _here(first: torch.Tensor, *others: Optional[torch.Tensor]) -> bool:
+    """Whether tensors (None: not given) are on the current device: an address of the host's or of another device's would go to a kernel as it is."""
+    at = first.get_device()                 # (-1: the host; 0.05 us)
+    if at < 0 or at != _current_device():
+        return False
+    for t in others:
+        if t is not None and t.get_device() != at:
+            return False
+    return True
+
+
 # `op` of infllmv2_workspace_bytes (enum infllmv2_op)
 OP_COMPRESS_K, OP_BLOCK_SCORES, OP_TOPK_BLOCKS, OP_SPARSE_ATTN_FWD, OP_DENSE_ATTN_FWD, OP_SPARSE_DECODE = range(6)
 OP_BLOCK_SCORES_POOLED, OP_TOPK_POOLED, OP_SPARSE_ATTN_BWD, OP_SPARSE_ATTN_BWD_MIN, OP_COMPRESS_K_APPEND = range(6, 11)
@@ -522,7 +537,8 @@ class PagedCache:
         assert k.shape[1:] == (p.num_kv_heads, p.block_size, p.head_dim) and (coded or k.dtype == p.torch_dtype)
         assert page_table.dim() == 2 and page_table.dtype == torch.int32 and page_table.stride(1) == 1
         for s in (k_scale, v_scale) if coded else ():
-            assert s.dtype == torch.float32 and s.is_contiguous() and s.shape == k.shape[:2]
+            assert s.dtype == torch.float32 and s.is_contiguous() and s.shape == k.shape[:2] and s.get_device() == k.get_device()
+        assert k.get_device() == v.get_device() == page_table.get_device()
         self.k, self.v, self.page_table, self.k_scale, self.v_scale = k, v, page_table, k_scale, v_scale
         self.batch, blocks = page_table.shape
         self.rows = (p.num_kv_heads, p.head_dim, p.dtype)
@@ -637,6 +653,7 @@ def tree_masks(parents: torch.Tensor, cu_seqlens_q, ctx_lens, mask: Optional[tor
     ctx_lens[b] tokens, the drafted ones with them.  Returns (mask [T, words] int32 bit patterns: a token and its ancestors, positions [T] int32)."""
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     assert parents.dtype is torch.int32 and parents.is_contiguous() and parents.shape == (si.total,) and si.batch == cx.batch
+    assert _here(parents, mask, positions, si.cu_d, cx.ctx_d)
     if mask is None:
         words = (si.max_len + 31) // 32 or 1
         mask = parents.new_empty(si.total, words)
@@ -665,6 +682,7 @@ def cache_tree_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q,
     assert si.batch == cx.batch <= cache.batch and cache._holds(p, cx.max_ctx)
     rows, words = mask.shape
     assert mask.dtype is torch.int32 and mask.is_contiguous() and rows == tokens
+    assert _here(q, mask, cache.k, block_idx, out, lse, workspace, si.cu_d, cx.ctx_d)
     if block_idx is not None:
         assert block_idx.is_contiguous() and block_idx.dtype is torch.int32 and block_idx.shape == (si.batch, p.num_kv_heads, p.topk_total)
     if out is None:
@@ -691,7 +709,7 @@ def cache_accept(p: Params, cache: PagedCache, cu_seqlens_q, ctx_lens, path: tor
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     rows, steps = path.shape
     assert path.dtype is torch.int32 and path.is_contiguous() and rows == si.batch == cx.batch <= cache.batch
-    assert cache._holds(p, cx.max_ctx)
+    assert cache._holds(p, cx.max_ctx) and _here(path, cache.k, new_lens, si.cu_d, cx.ctx_d)
     if new_lens is None:
         new_lens = path.new_empty(rows)
     else:
@@ -709,6 +727,7 @@ class PagePool:
     def __init__(self, refs: torch.Tensor, page_table: torch.Tensor):
         assert refs.dtype is torch.int32 and refs.dim() == 1 and refs.is_contiguous()
         assert page_table.dim() == 2 and page_table.dtype is torch.int32 and page_table.stride(1) == 1
+        assert refs.get_device() == page_table.get_device() >= 0
         self.refs, self.page_table = refs, page_table
         rows, blocks = page_table.shape
         self.c = _PagesC(refs.numel(), rows, blocks, page_table.stride(0) if rows > 1 else blocks, page_table.data_ptr(), refs.data_ptr(), 0)
@@ -744,7 +763,7 @@ def _shortage(pool: PagePool, short: Optional[torch.Tensor], calls: int):
 def pages_resize(pool: PagePool, old_lens, new_lens, short: Optional[torch.Tensor] = None):
     """Sequence b had room for old_lens[b] tokens and gets room for new_lens[b] (0: none).  Returns how many pages were wanting (device int32 [1])."""
     old, new = _decode_info(old_lens), _decode_info(new_lens)
-    assert old.batch == new.batch
+    assert old.batch == new.batch and _here(pool.refs, short, old.ctx_d, new.ctx_d)
     short = _shortage(pool, short, old.batch)
     st = lib().infllmv2_pages_resize(pool.ref, old.ctx_h.data_ptr(), old.ctx_d.data_ptr(), new.ctx_h.data_ptr(), new.ctx_d.data_ptr(), old.batch,
                                      short.data_ptr(), _stream())
@@ -754,6 +773,7 @@ def pages_resize(pool: PagePool, old_lens, new_lens, short: Optional[torch.Tenso
 
 def pages_fork(pool: PagePool, forks: Forks, copies: Optional[torch.Tensor] = None, short: Optional[torch.Tensor] = None):
     """Returns (copies [n, 2]: pages to copy from and to with cache_copy_pages, -1: none; how many pages were wanting), device int32."""
+    assert _here(pool.refs, copies, short, forks.d)
     if copies is None:
         copies = pool.refs.new_empty(forks.count, 2)
     else:
@@ -768,6 +788,7 @@ def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: O
     """Brings the pages in use to the front; sequence b has lens[b] tokens.  out: where the new table and counts go (default: the pool itself).  Returns
     (moves [num_pages // 2, 2] for cache_copy_pages, live [2]: pages in use and moves), device int32."""
     info, out, half = _decode_info(lens), pool if out is None else out, pool.c.num_pages // 2
+    assert _here(pool.refs, out.refs, moves, live, info.ctx_d)
     if moves is None:
         moves = pool.refs.new_empty(half, 2)
     else:
@@ -785,7 +806,7 @@ def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: O
 def cache_copy_pages(p: Params, cache: PagedCache, pairs: torch.Tensor):
     """Copies page pairs[i, 0] to page pairs[i, 1] for each i (device int32 [n, 2]; -1: no copy): keys, values, scales.  Returns the cache."""
     count, two = pairs.shape
-    assert pairs.dtype is torch.int32 and pairs.is_contiguous() and two == 2 and cache._holds(p, 0)
+    assert pairs.dtype is torch.int32 and pairs.is_contiguous() and two == 2 and cache._holds(p, 0) and _here(pairs, cache.k)
     st = lib().infllmv2_cache_copy_pages(ctypes.byref(p), cache.ref, pairs.data_ptr(), count, _stream())
     _check(st, "infllmv2_cache_copy_pages")
     return cache
