@@ -177,19 +177,7 @@ def _stream():
     return _raw_stream(_device())
 
 
-def _current_device() -> int:
-    return torch.cuda.current_device() if _device is None else _device()
-
-
-def _here(first: torch.Tensor, *others: Optional[torch.Tensor]) -> bool:
-    """Whether tensors (None: not given) are on the current device: an address of the host's or of another device's would go to a kernel as it is."""
-    at = first.get_device()                 # (-1: the host; 0.05 us)
-    if at < 0 or at != _current_device():
-        return False
-    for t in others:
-        if t is not None and t.get_device() != at:
-            return False
-    return True
+_current_device = torch.cuda.current_device if _device is None else _device
 
 
 # `op` of infllmv2_workspace_bytes (enum infllmv2_op)
@@ -653,17 +641,18 @@ def tree_masks(parents: torch.Tensor, cu_seqlens_q, ctx_lens, mask: Optional[tor
     ctx_lens[b] tokens, the drafted ones with them.  Returns (mask [T, words] int32 bit patterns: a token and its ancestors, positions [T] int32)."""
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     assert parents.dtype is torch.int32 and parents.is_contiguous() and parents.shape == (si.total,) and si.batch == cx.batch
-    assert _here(parents, mask, positions, si.cu_d, cx.ctx_d)
+    at = parents.get_device()               # (-1: the host, whose addresses would go to a kernel as they are)
+    assert at >= 0 and at == _current_device()
     if mask is None:
         words = (si.max_len + 31) // 32 or 1
         mask = parents.new_empty(si.total, words)
     else:
-        assert mask.dtype is torch.int32 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == si.total
+        assert mask.dtype is torch.int32 and mask.is_contiguous() and mask.dim() == 2 and mask.shape[0] == si.total and mask.get_device() == at
         words = mask.shape[1]
     if positions is None:
         positions = torch.empty_like(parents)
     else:
-        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (si.total,)
+        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == (si.total,) and positions.get_device() == at
     st = lib().infllmv2_tree_masks(parents.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch,
                                    mask.data_ptr(), words, positions.data_ptr(), _stream())
     _check(st, "infllmv2_tree_masks")
@@ -682,20 +671,24 @@ def cache_tree_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q,
     assert si.batch == cx.batch <= cache.batch and cache._holds(p, cx.max_ctx)
     rows, words = mask.shape
     assert mask.dtype is torch.int32 and mask.is_contiguous() and rows == tokens
-    assert _here(q, mask, cache.k, block_idx, out, lse, workspace, si.cu_d, cx.ctx_d)
+    at = q.get_device()
+    assert at >= 0 and at == _current_device() and mask.get_device() == at and cache.k.get_device() == at
     if block_idx is not None:
         assert block_idx.is_contiguous() and block_idx.dtype is torch.int32 and block_idx.shape == (si.batch, p.num_kv_heads, p.topk_total)
+        assert block_idx.get_device() == at
     if out is None:
         out = torch.empty_like(q)
     else:
-        assert out.is_contiguous() and out.shape == shape and out.dtype is q.dtype
+        assert out.is_contiguous() and out.shape == shape and out.dtype is q.dtype and out.get_device() == at
     if lse is None:
         lse = torch.empty_strided((tokens, hq), (hq, 1), dtype=torch.float32, device=q.device)          # (the quickest of torch's ways)
     else:
-        assert lse.is_contiguous() and lse.shape == (tokens, hq) and lse.dtype is torch.float32
+        assert lse.is_contiguous() and lse.shape == (tokens, hq) and lse.dtype is torch.float32 and lse.get_device() == at
     if workspace is None:
         need = workspace_bytes(OP_CACHE_TREE_ATTN, p, si.batch, si.total, cx.max_ctx)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    else:
+        assert workspace.get_device() == at
     st = lib().infllmv2_cache_tree_attn(ctypes.byref(p), cache.ref, q.data_ptr(), si.cu_h.data_ptr(), si.cu_d.data_ptr(),
                                         cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(), si.batch, mask.data_ptr(), words, _ptr(block_idx),
                                         out.data_ptr(), lse.data_ptr(), *_ws_args(workspace), _stream())
@@ -709,11 +702,12 @@ def cache_accept(p: Params, cache: PagedCache, cu_seqlens_q, ctx_lens, path: tor
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     rows, steps = path.shape
     assert path.dtype is torch.int32 and path.is_contiguous() and rows == si.batch == cx.batch <= cache.batch
-    assert cache._holds(p, cx.max_ctx) and _here(path, cache.k, new_lens, si.cu_d, cx.ctx_d)
+    at = path.get_device()
+    assert cache._holds(p, cx.max_ctx) and at >= 0 and at == _current_device() and cache.k.get_device() == at
     if new_lens is None:
         new_lens = path.new_empty(rows)
     else:
-        assert new_lens.dtype is torch.int32 and new_lens.is_contiguous() and new_lens.shape == (rows,)
+        assert new_lens.dtype is torch.int32 and new_lens.is_contiguous() and new_lens.shape == (rows,) and new_lens.get_device() == at
     st = lib().infllmv2_cache_accept(ctypes.byref(p), cache.ref, si.cu_h.data_ptr(), si.cu_d.data_ptr(), cx.ctx_h.data_ptr(), cx.ctx_d.data_ptr(),
                                      rows, path.data_ptr(), steps, new_lens.data_ptr(), _stream())
     _check(st, "infllmv2_cache_accept")
@@ -727,7 +721,8 @@ class PagePool:
     def __init__(self, refs: torch.Tensor, page_table: torch.Tensor):
         assert refs.dtype is torch.int32 and refs.dim() == 1 and refs.is_contiguous()
         assert page_table.dim() == 2 and page_table.dtype is torch.int32 and page_table.stride(1) == 1
-        assert refs.get_device() == page_table.get_device() >= 0
+        self.device = refs.get_device()
+        assert self.device == page_table.get_device() >= 0
         self.refs, self.page_table = refs, page_table
         rows, blocks = page_table.shape
         self.c = _PagesC(refs.numel(), rows, blocks, page_table.stride(0) if rows > 1 else blocks, page_table.data_ptr(), refs.data_ptr(), 0)
@@ -756,14 +751,14 @@ def _shortage(pool: PagePool, short: Optional[torch.Tensor], calls: int):
     if short is None:
         short = pool.refs.new_empty(1)
     else:
-        assert short.dtype is torch.int32 and short.numel() == 1
+        assert short.dtype is torch.int32 and short.numel() == 1 and short.get_device() == pool.device
     return short if calls else short.zero_()         # (the library writes nothing where there is nothing to do)
 
 
 def pages_resize(pool: PagePool, old_lens, new_lens, short: Optional[torch.Tensor] = None):
     """Sequence b had room for old_lens[b] tokens and gets room for new_lens[b] (0: none).  Returns how many pages were wanting (device int32 [1])."""
     old, new = _decode_info(old_lens), _decode_info(new_lens)
-    assert old.batch == new.batch and _here(pool.refs, short, old.ctx_d, new.ctx_d)
+    assert old.batch == new.batch and pool.device == _current_device()
     short = _shortage(pool, short, old.batch)
     st = lib().infllmv2_pages_resize(pool.ref, old.ctx_h.data_ptr(), old.ctx_d.data_ptr(), new.ctx_h.data_ptr(), new.ctx_d.data_ptr(), old.batch,
                                      short.data_ptr(), _stream())
@@ -773,11 +768,11 @@ def pages_resize(pool: PagePool, old_lens, new_lens, short: Optional[torch.Tenso
 
 def pages_fork(pool: PagePool, forks: Forks, copies: Optional[torch.Tensor] = None, short: Optional[torch.Tensor] = None):
     """Returns (copies [n, 2]: pages to copy from and to with cache_copy_pages, -1: none; how many pages were wanting), device int32."""
-    assert _here(pool.refs, copies, short, forks.d)
+    assert pool.device == _current_device()
     if copies is None:
         copies = pool.refs.new_empty(forks.count, 2)
     else:
-        assert copies.dtype is torch.int32 and copies.is_contiguous() and copies.shape == (forks.count, 2)
+        assert copies.dtype is torch.int32 and copies.is_contiguous() and copies.shape == (forks.count, 2) and copies.get_device() == pool.device
     short = _shortage(pool, short, forks.count)
     st = lib().infllmv2_pages_fork(pool.ref, forks.h.data_ptr(), forks.d.data_ptr(), forks.count, copies.data_ptr(), short.data_ptr(), _stream())
     _check(st, "infllmv2_pages_fork")
@@ -788,15 +783,15 @@ def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: O
     """Brings the pages in use to the front; sequence b has lens[b] tokens.  out: where the new table and counts go (default: the pool itself).  Returns
     (moves [num_pages // 2, 2] for cache_copy_pages, live [2]: pages in use and moves), device int32."""
     info, out, half = _decode_info(lens), pool if out is None else out, pool.c.num_pages // 2
-    assert _here(pool.refs, out.refs, moves, live, info.ctx_d)
+    assert pool.device == out.device == _current_device()
     if moves is None:
         moves = pool.refs.new_empty(half, 2)
     else:
-        assert moves.dtype is torch.int32 and moves.is_contiguous() and moves.shape == (half, 2)
+        assert moves.dtype is torch.int32 and moves.is_contiguous() and moves.shape == (half, 2) and moves.get_device() == pool.device
     if live is None:
         live = pool.refs.new_empty(2)
     else:
-        assert live.dtype is torch.int32 and live.is_contiguous() and live.shape == (2,)
+        assert live.dtype is torch.int32 and live.is_contiguous() and live.shape == (2,) and live.get_device() == pool.device
     st = lib().infllmv2_pages_compact(pool.ref, info.ctx_h.data_ptr(), info.ctx_d.data_ptr(), info.batch, out.ref, moves.data_ptr(), live.data_ptr(),
                                       _stream())
     _check(st, "infllmv2_pages_compact")
@@ -806,7 +801,9 @@ def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: O
 def cache_copy_pages(p: Params, cache: PagedCache, pairs: torch.Tensor):
     """Copies page pairs[i, 0] to page pairs[i, 1] for each i (device int32 [n, 2]; -1: no copy): keys, values, scales.  Returns the cache."""
     count, two = pairs.shape
-    assert pairs.dtype is torch.int32 and pairs.is_contiguous() and two == 2 and cache._holds(p, 0) and _here(pairs, cache.k)
+    assert pairs.dtype is torch.int32 and pairs.is_contiguous() and two == 2 and cache._holds(p, 0)
+    at = pairs.get_device()
+    assert at >= 0 and at == _current_device() and cache.k.get_device() == at
     st = lib().infllmv2_cache_copy_pages(ctypes.byref(p), cache.ref, pairs.data_ptr(), count, _stream())
     _check(st, "infllmv2_cache_copy_pages")
     return cache
