@@ -482,6 +482,8 @@ int infllmv2_cache_attn(const infllmv2_params *p, const infllmv2_cache *c, const
  * infllmv2_tree_masks: who is whose ancestor, from the tokens' parents.
  *   parents_d     device int32 [total]: the number, in its tree, of the token that a token continues, in any order; a number outside 0 .. n - 1 is none: the
  *                 token continues the context.  (Parents that lead back to a token in a circle are no tree: tokens then have everything that can be reached.)
+ *                 infllmv2_cache_accept keeps paths whose numbers rise: a tree of which a path is to be kept has its tokens behind their parents, as depth by
+ *                 depth or branch by branch.
  *   mask_d        device out uint32 [total, mask_words], 32 mask_words >= the largest n: bit j % 32 of word j / 32 of a token's row: token j is it or an
  *                 ancestor of it
  *   pos_d         device out int32 [total] or NULL: the token's position, ctx_lens[b] - n + its ancestors (ctx_lens may be NULL where pos_d is)
@@ -499,7 +501,10 @@ int infllmv2_tree_masks(const int32_t *parents_d, const int32_t *cu_q_h, const i
  *                  order (other numbers than those of blocks with context rows are skipped); sequences with ctx_lens[b] < dense_threshold attend to all of
  *                  the context.  Drafted rows are the mask's, listed or not.  NULL: all sequences attend to all of the context.  infllmv2_decode_blocks makes
  *                  such lists from a query of the sequence, its newest token's for instance.
- * Other arguments, rows without a key, rounding and limits as for infllmv2_cache_attn (scratch: INFLLMV2_OP_CACHE_TREE_ATTN).
+ * Other arguments, rows without a key and limits as for infllmv2_cache_attn (scratch: INFLLMV2_OP_CACHE_TREE_ATTN).
+ * Rounding, bf16 data: the weights p of trees of up to 8 tokens are taken to 2^-16, those of larger ones may be taken to 2^-8 (with lists too).  Whether they are,
+ * and how the keys are split, depends on the whole batch: the last bits of a tree's outputs may be others beside other trees than alone.  The same batch gives
+ * the same bits.
  */
 int infllmv2_cache_tree_attn(const infllmv2_params *p, const infllmv2_cache *c, const void *q_d, const int32_t *cu_q_h,
                              const int32_t *cu_q_d, const int32_t *ctx_lens_h, const int32_t *ctx_lens_d, int32_t batch,
@@ -509,7 +514,8 @@ int infllmv2_cache_tree_attn(const infllmv2_params *p, const infllmv2_cache *c, 
 /*
  * Keeps a path of each sequence's tree: drafted row path[i] becomes drafted row i, keys and values of every head.
  *   path_d        device int32 [batch, path_stride]: numbers of drafted tokens, rising; the path ends in front of the first entry that is outside 0 .. n - 1
- *                 or not above the one before it (-1 behind the last), or after path_stride entries
+ *                 or not above the one before it (-1 behind the last), or after path_stride entries.  A path through a tree whose tokens stand in front
+ *                 of their parents falls somewhere, and ends there
  *   new_lens_d    device out int32 [batch] or NULL: ctx_lens[b] - n + the path's length; apart from the inputs, ctx_lens_d too (written also where no
  *                 sequence has drafted tokens)
  * Rows of the context and drafted rows that no row of the path moves to keep their values.  e4m3: a page that rows move to keeps its scale or gets the larger one
@@ -524,8 +530,8 @@ int infllmv2_cache_accept(const infllmv2_params *p, const infllmv2_cache *c, con
  * Page tables: which pages the blocks of a sequence are in (one table serves the caches of all layers).  refs[g] counts the table entries that name page g; a
  * page with none is free.  Table and counts are the caller's; a new pool has counts of 0 and entries of -1.  The calls take the lowest free page for
  * the first entry that wants one, and so on, in order of sequences (or forks) and blocks: the same table and counts give the same result.  Where
- * pages run out, the last entries get -1 (a page that is not there) and short_d, device int32 [1] or NULL, holds how many.  Calls on one pool follow each
- * other on a stream or by events.
+ * pages run out, the last entries get -1 (a page that is not there) and short_d, device int32 [1] or NULL, holds how many (a resize of no sequences and a call
+ * of no forks do not write it).  Calls on one pool follow each other on a stream or by events.
  */
 typedef struct infllmv2_pages {
     int32_t num_pages;            /* >= 1                                                                        */

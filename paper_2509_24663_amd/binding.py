@@ -637,8 +637,8 @@ TREE_MOST = 1024
 
 
 def tree_masks(parents: torch.Tensor, cu_seqlens_q, ctx_lens, mask: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
-    """parents: device int32 [T], packed by cu_seqlens_q: the token of its tree that each drafted token continues, -1: the context.  Sequence b has
-    ctx_lens[b] tokens, the drafted ones with them.  Returns (mask [T, words] int32 bit patterns: a token and its ancestors, positions [T] int32)."""
+    """parents: device int32 [T], packed by cu_seqlens_q: the token of its tree that each drafted token continues, -1: the context (in any order, but
+    cache_accept keeps paths that rise only).  Sequence b has ctx_lens[b] tokens, the drafted ones with them.  Returns (mask [T, words] int32 bit patterns: a token and its ancestors, positions [T] int32)."""
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     assert parents.dtype is torch.int32 and parents.is_contiguous() and parents.shape == (si.total,) and si.batch == cx.batch
     at = parents.get_device()               # (-1: the host, whose addresses would go to a kernel as they are)
@@ -698,7 +698,7 @@ def cache_tree_attn(p: Params, cache: PagedCache, q: torch.Tensor, cu_seqlens_q,
 
 def cache_accept(p: Params, cache: PagedCache, cu_seqlens_q, ctx_lens, path: torch.Tensor, new_lens: Optional[torch.Tensor] = None):
     """Brings the rows of path [B, steps] (device int32: numbers of drafted tokens, rising, -1 behind the last) together behind each sequence's context.
-    Returns the new lengths (device int32 [B])."""
+    A path ends in front of a number that does not rise.  Returns the new lengths (device int32 [B]; the next calls want them on the host as well)."""
     si, cx = _seq_info(cu_seqlens_q), _decode_info(ctx_lens)
     rows, steps = path.shape
     assert path.dtype is torch.int32 and path.is_contiguous() and rows == si.batch == cx.batch <= cache.batch
@@ -780,7 +780,7 @@ def pages_fork(pool: PagePool, forks: Forks, copies: Optional[torch.Tensor] = No
 
 
 def pages_compact(pool: PagePool, lens, out: Optional[PagePool] = None, moves: Optional[torch.Tensor] = None, live: Optional[torch.Tensor] = None):
-    """Brings the pages in use to the front; sequence b has lens[b] tokens.  out: where the new table and counts go (default: the pool itself).  Returns
+    """Brings the pages in use to the front; sequence b has lens[b] tokens (rows behind the last are cleared).  out: where the new table and counts go (default: the pool itself).  Returns
     (moves [num_pages // 2, 2] for cache_copy_pages, live [2]: pages in use and moves), device int32."""
     info, out, half = _decode_info(lens), pool if out is None else out, pool.c.num_pages // 2
     assert pool.device == out.device == _current_device()

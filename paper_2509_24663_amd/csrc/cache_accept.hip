@@ -6,7 +6,8 @@
 // pages that are not written yet.  e4m3 pages: the scale grows to hold the rows that come in, as in an append; they are rounded to it, and so are the
 // page's other rows if it grew.
 //
-// Bound: latency: lengths, path, page numbers, rows, one after the other.  16 trees of 26 tokens, up to 6 kept, e4m3: 4.1 us; 5 of 301, up to 99 kept, fp32, d 64: 7.6 (a
+// Bound: latency: lengths, path, page numbers, rows, one after the other.  16 trees of 26 tokens, up to 6 kept, e4m3: 4.2 us, 7.2 where
+// scales grow and the other rows of their pages are rounded again; 5 of 301, up to 99 kept, fp32, d 64: 7.8, rows that another kernel has just written 9.0 (a
 // page's rows requested while the page before is written).
 #include "cache.h"
 

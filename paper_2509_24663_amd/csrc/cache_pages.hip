@@ -7,8 +7,10 @@
 //
 // Bound: latency.  Entries are given back and shared by as many workgroups as they are worth (counts added with atomics, whose order does not matter);
 // handing out needs every free page's rank, which one workgroup works out, 8192 counts at a time, only as far as pages are wanted.  64 rows that give 3000 pages
-// back and get 3200 of a pool of 12288: 2.6 and 5.6 us.  32 forks of up to 47 blocks 9.4; 240 forks of 512 blocks of one row 3.5 where they had its pages before (with
-// an add and a subtract for each entry: 58; where they had others a call takes 10.9 for 8.2) and 3.7 for their last pages.  8192 pages, 6126 of them in use: 5.4 to find the 1529 that move, 5.4 to renumber 12288 entries.  Copies: HBM, those 1529
+// back and get 3200 of a pool of 12288: 2.6 and 5.6 us.  32 forks of up to 47 blocks 9.1 (rows that
+// held other pages: 11.2).  240 forks of 512 blocks of one row, the kernel that shares: 3.5 where they had its pages before, so that no count and no entry changes (with
+// an add and a subtract for each entry: 58); into rows that hold nothing 35 where the pages are anywhere in the pool and 7.5 where they are in order, so that a
+// wavefront's adds meet in few lines; in the place of others 39.6.  Their last pages: 3.7 to 5.  8192 pages, 6126 of them in use: 5.4 to find the 1529 that move, 5.4 to renumber 12288 entries.  Copies: HBM, those 1529
 // pages of 32 KB 17.5 us, 5.7 TB/s read and written.
 #include <algorithm>
 
@@ -467,7 +469,7 @@ extern "C" int infllmv2_pages_fork(const infllmv2_pages *g, const infllmv2_fork 
     if (most == 0 && copies_d == nullptr && short_d == nullptr) return INFLLMV2_OK;
     const int pitch = pitch_log2(most);
     const bool together = most > 0 && (int64_t)count << pitch <= kTogether;
-    // Forks of a workgroup: more add up more of their counts, as long as there is a workgroup for each CU.  A call, us, all pages others than before, by 1 / 2 / 4 / 8 / 16 forks:
+    // Forks of a workgroup: more add up more of their counts, as long as there is a workgroup for each CU.  A call, us, all pages others than before, in order in the pool, by 1 / 2 / 4 / 8 / 16 forks:
     // 240 of 512 blocks 10.9 / 9.2 / 9.7 / 11.6 / 18.3 (1 here), 1000 of 100 14.8 / 11.2 / 10.6 / 12.2 / 17.7 (3), 3000 of 64 65 / 37 / 25 / 21 / 23 (11).
     const int per = (int)std::max<int64_t>(std::min<int64_t>((int64_t)count * chunks(most, 256) / 256, 16), 1);
     const ForkArgs a{pool_of(g), forks_d, count, together ? pitch : -1, per, copies_d, short_d};
